@@ -75,8 +75,13 @@ typedef enum {
 typedef enum {
     GEMM2M_OP_GAUSSIAN_INT = 0, GEMM2M_OP_ZGEMM = 1, GEMM2M_OP_CGEMM = 2, GEMM2M_OP_ZHERK = 3,
     GEMM2M_OP_ZHER2K = 4, GEMM2M_OP_DSYRK = 5, GEMM2M_OP_DSYR2K = 6, GEMM2M_OP_DGEMM_OZAKI2 = 7,
-    GEMM2M_OP_ZGEMM_EISENSTEIN = 8, GEMM2M_OP_ZGEMM_HOST = 9
+    GEMM2M_OP_ZGEMM_EISENSTEIN = 8, GEMM2M_OP_ZGEMM_HOST = 9,
+    GEMM2M_OP_FP8_GEMM = 10, GEMM2M_OP_NEWTON_SCHULZ = 11       /* layer operators, below; k = batch for the latter, nmod is ignored */
 } gemm2m_op;
+
+/* Element types of the layer operators.  E4M3 and E5M2 are the 8-bit formats with 4 / 5 exponent bits and largest finite
+ * values 448 and 57344. */
+typedef enum { GEMM2M_F32 = 0, GEMM2M_F16 = 1, GEMM2M_BF16 = 2, GEMM2M_E4M3 = 3, GEMM2M_E5M2 = 4 } gemm2m_type;
 
 /* Human-readable name of a status code (static string). */
 const char* gemm2m_status_string(int status);
@@ -228,6 +233,53 @@ int dsyr2k2m(int64_t n, int64_t k, const double* A, int64_t lda, const double* B
  *   - gemm2m_last_cuda_error is not updated by this entry point. */
 #define GEMM2M_STATIC_MAX_ROWS 65536
 int gemm2m_zscale_exponents_static(int64_t m, int64_t k, const double* A, int64_t lda, int nmod, int32_t* e, void* stream);
+
+/* ---- layer operators: quantise to 8-bit floating point, multiply, orthogonalise ----
+ *
+ * What one training step of a linear layer runs next to each other: activations and output gradients are quantised and
+ * multiplied (forward, input gradient, weight gradient), the weight gradient is orthogonalised, and the updated weights are
+ * quantised again; serving runs the first two.  The conventions above hold, with one exception: matrices of these operators
+ * are ROW-major (k contiguous, the order the 8-bit tensor cores read), ld = elements from one row to the next.  Scale matrices
+ * are column-major like everything else: one column of scales per 128 entries of k.
+ *
+ * 8-bit matrices start on 16-byte boundaries and have leading dimensions that are multiples of 16; what lies between the end
+ * of a row and the next one is neither read as data nor written. */
+
+/* X (rows x cols, type F32 / F16 / BF16, any alignment) to 8-bit floating point (fmt E4M3 / E5M2) with one scale per block of
+ * block_rows x 128 entries, block_rows = 1 or 128.  Per block u = max(max |x|, 2^-100), scale s = u / MAX, q = rn(x (MAX / u)),
+ * MAX = 448 or 57344: x is about q s.  Two forms, either may be left out (both pointers NULL), both from one read of X:
+ *   Q  (rows x cols, ldq), S  (column-major, ceil(rows / block_rows) x ceil(cols / 128), lds): blocks along the rows of X;
+ *   Qt (cols x rows, ldqt), St (column-major, ceil(cols / block_rows) x ceil(rows / 128), ldst): the transpose, with blocks along
+ *      the columns of X (its own scales for block_rows = 1; the transposed scales for block_rows = 128).
+ * A ragged last block counts the entries it has.  A block with an Inf or NaN gets the scale NaN (its 8-bit values are then
+ * unspecified).  Needs no workspace. */
+int gemm2m_fp8_quantise(int64_t rows, int64_t cols, const void* X, int type, int64_t ldx, int fmt, int block_rows, void* Q, int64_t ldq,
+                        float* S, int64_t lds, void* Qt, int64_t ldqt, float* St, int64_t ldst, void* stream);
+
+/* D = C + A B^T of block-scaled 8-bit matrices A (m x k) and B (n x k), as the quantiser writes them:
+ *   D[i, j] = C[i, j] + sum_b SA[i / a_block, b] SB[j / b_block, b] sum_{p in block b} A[i, p] B[j, p],  b = p / 128.
+ * a_block, b_block = 1 (a scale per row and block) or 128 (per 128 x 128 block); the formats may differ.  C and D are m x n of
+ * the same type (F32, F16, BF16), row-major; C may be NULL (nothing is added) or D itself (then ldc = ldd), not otherwise overlap D.  Block sums and
+ * their total are held in 32 bits, and rounded once.  m = 1 (one token) is an ordinary size.  k = 0 gives D = C, or zero.
+ * A NaN scale makes the rows (columns) of D that it belongs to NaN.
+ * Forward: X quantised with 1-row blocks, W (out x in) with 128: Y = X W^T.  Input gradient: dY with 1-row blocks, Qt of W.
+ * Weight gradient: dW = Qt of dY times Qt of X, block 1 on both sides, C = D = the 32-bit sum over micro-batches.
+ * Workspace: GEMM2M_OP_FP8_GEMM. */
+int gemm2m_fp8_gemm(int64_t m, int64_t n, int64_t k, const void* A, int a_fmt, int64_t lda, const float* SA, int64_t ldsa, int a_block,
+                    const void* B, int b_fmt, int64_t ldb, const float* SB, int64_t ldsb, int b_block, const void* C, int64_t ldc, void* D,
+                    int type, int64_t ldd, void* stream);
+
+/* O = orthogonalised G by `steps` (1 .. 64) Newton-Schulz steps, for `batch` (<= 65535) matrices of m x n (sides <= 2^20),
+ * stride_g / stride_o elements apart: X_0 = G / (|G|_F + eps), then X <- a X + (b A + c A^2) X with A = X X^T (m <= n; the same
+ * polynomial with X^T X from the right for m > n), O = X rounded to bf16.  G: F32 / F16 / BF16, any alignment; O: BF16, may be G.
+ * coeffs: host pointer to (a, b, c) of each step, or NULL for (3.4445, -4.7750, 2.0315) in every step, which drives the singular
+ * values towards 1 (into about [0.7, 1.2]).  The coefficients must keep the singular values below about 100.  Products run on
+ * 16-bit operands with 32-bit sums; before its rounding O is within about 2e-3 (relative, Frobenius norm;
+ * 4e-3 for sides below 20) of the exact iteration.
+ * A zero matrix gives zero (for eps > 0 or = 0), a matrix with an Inf or NaN gives NaN throughout.  Results do not depend on the
+ * batch a matrix is in.  Workspace: GEMM2M_OP_NEWTON_SCHULZ with (m, n, batch). */
+int gemm2m_newton_schulz(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* O, int64_t ldo,
+                         int64_t stride_o, int steps, const float* coeffs, float eps, void* stream);
 
 /* Waits for `stream` and returns GEMM2M_ERR_DEVICE_TIMEOUT if a kernel of an earlier call on the registered
  * workspace gave up a bounded wait (its results are then invalid), GEMM2M_ERR_CUDA on a CUDA error, else OK. */

@@ -13,6 +13,8 @@ import os
 OP_GAUSSIAN_INT, OP_ZGEMM, OP_CGEMM, OP_ZHERK, OP_ZHER2K, OP_DSYRK, OP_DSYR2K, OP_DGEMM_OZAKI2 = 0, 1, 2, 3, 4, 5, 6, 7
 OP_ZGEMM_EISENSTEIN = 8
 OP_ZGEMM_HOST = 9
+OP_FP8_GEMM, OP_NEWTON_SCHULZ = 10, 11
+F32, F16, BF16, E4M3, E5M2 = 0, 1, 2, 3, 4              # gemm2m_type
 OK = 0
 ERR_ARG, ERR_NMOD, ERR_WORKSPACE, ERR_CUDA, ERR_ARCH, ERR_DEVICE_TIMEOUT = 1, 2, 3, 4, 5, 6     # gemm2m_status
 
@@ -85,6 +87,9 @@ def lib():
     L.gemm2m_debug_tables.argtypes = [i32, i64, i32, vp, vp, vp, vp, vp, vp]
     L.gemm2m_debug_residue_reduction.argtypes = [i32, vp, vp, vp, vp, vp]
     L.gemm2m_debug_post_operands.argtypes = [i32, i32, vp, vp, vp]
+    L.gemm2m_fp8_quantise.argtypes = [i64, i64, vp, i32, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
+    L.gemm2m_fp8_gemm.argtypes = [i64, i64, i64] + [vp, i32, i64, vp, i64, i32] * 2 + [vp, i64, vp, i32, i64, vp]
+    L.gemm2m_newton_schulz.argtypes = [i64, i64, i64, vp, i32, i64, i64, vp, i64, i64, i32, vp, ctypes.c_float, vp]
     _lib = L
     return L
 
@@ -316,6 +321,128 @@ def dsyrk2m(A, C, nmod=16, stream=None):
 
 def dsyr2k2m(A, B, C, nmod=16, stream=None):
     _rank(lib().dsyr2k2m, "dsyr2k2m", A, B, C, nmod, stream)
+
+
+# ---- layer operators: row-major matrices (torch's default order), column-major scales ----
+
+def _types():
+    import torch
+    return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
+
+
+_type_codes = None
+
+
+def _type_of(t, name, allowed):
+    global _type_codes
+    if _type_codes is None:
+        _type_codes = _types()
+    code = _type_codes.get(t.dtype, -1)
+    if code not in allowed:
+        raise ValueError(f"{name}: unsupported type {t.dtype}")
+    return code
+
+
+def _rowmajor(t, name, allowed):
+    """(pointer, type code, rows, cols, leading dimension) of a 2-D CUDA tensor with contiguous rows."""
+    if t.dim() != 2 or not t.is_cuda:
+        raise ValueError(f"{name}: need a 2-D CUDA tensor")
+    code = _type_of(t, name, allowed)
+    rows, cols = t.shape
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError(f"{name}: need row-major storage (stride 1 along dim 1)")
+    ld = t.stride(0) if rows > 1 else -(-max(cols, 1) // 16) * 16
+    return t.data_ptr(), code, rows, cols, max(ld, 1)
+
+
+def _scales(t, name, rows, cols):
+    """(pointer, leading dimension) of a column-major float32 scale matrix of the given shape."""
+    if not t.is_cuda or tuple(t.shape) != (rows, cols):
+        raise ValueError(f"{name}: need a CUDA tensor of shape {(rows, cols)}")
+    _type_of(t, name, (F32,))
+    if rows > 1 and t.stride(0) != 1:
+        raise ValueError(f"{name}: need column-major storage (stride 1 along dim 0), e.g. torch.empty(cols, rows).t()")
+    return t.data_ptr(), max(t.stride(1) if cols > 1 else rows, 1)
+
+
+_FP8 = (E4M3, E5M2)
+_FLOATS = (F32, F16, BF16)
+
+
+def fp8_empty(rows, cols, fmt=E4M3, block_rows=1, device="cuda"):
+    """Uninitialised (values, scales) for a rows x cols matrix, laid out as fp8_quantise and fp8_gemm take them."""
+    import torch
+    dtype = {E4M3: torch.float8_e4m3fn, E5M2: torch.float8_e5m2}[fmt]
+    q = torch.empty((rows, -(-cols // 16) * 16), dtype=dtype, device=device)[:, :cols]
+    return q, torch.empty((-(-cols // 128), -(-rows // block_rows)), dtype=torch.float32, device=device).t()
+
+
+def fp8_quantise(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None):
+    """X (row-major, float32 / float16 / bfloat16) to 8-bit values Q with scales S, and / or its transpose Qt with scales St."""
+    px, tx, rows, cols, ldx = _rowmajor(X, "X", _FLOATS)
+    if block_rows not in (1, 128):
+        raise ValueError("block_rows: need 1 or 128")
+    blocks = lambda v, b: -(-v // b)
+    fits = lambda width: -(-max(width, 1) // 16) * 16
+    big = max(rows, cols, 1)
+    fmt, form, form_t = None, (None, fits(cols), None, big), (None, fits(rows), None, big)
+    if Q is not None:
+        pq, fmt, r, c, ldq = _rowmajor(Q, "Q", _FP8)
+        if (r, c) != (rows, cols) or S is None:
+            raise ValueError("Q, S: shape mismatch")
+        form = (pq, ldq) + _scales(S, "S", blocks(rows, block_rows), blocks(cols, 128))
+    if Qt is not None:
+        pq, fmt_t, r, c, ldq = _rowmajor(Qt, "Qt", _FP8)
+        if (r, c) != (cols, rows) or St is None or fmt not in (None, fmt_t):
+            raise ValueError("Qt, St: shape or type mismatch")
+        fmt = fmt_t
+        form_t = (pq, ldq) + _scales(St, "St", blocks(cols, block_rows), blocks(rows, 128))
+    if fmt is None:
+        raise ValueError("need Q and S, or Qt and St")
+    _check(lib().gemm2m_fp8_quantise(rows, cols, px, tx, ldx, fmt, block_rows, *form, *form_t, _stream_ptr(stream)), "gemm2m_fp8_quantise")
+
+
+def fp8_gemm(A, SA, B, SB, D, C=None, a_block=1, b_block=128, stream=None):
+    """D = C + A B^T with A (m x k), B (n x k) in 8 bits and their scales; D, C float32 / float16 / bfloat16 (C may be D)."""
+    pa, fa, m, k, lda = _rowmajor(A, "A", _FP8)
+    pb, fb, n, k2, ldb = _rowmajor(B, "B", _FP8)
+    pd, td, md, nd, ldd = _rowmajor(D, "D", _FLOATS)
+    if k != k2 or (md, nd) != (m, n):
+        raise ValueError("shape mismatch")
+    if a_block not in (1, 128) or b_block not in (1, 128):
+        raise ValueError("a_block, b_block: need 1 or 128")
+    kb = -(-k // 128)
+    sa, ldsa = _scales(SA, "SA", -(-m // a_block), kb)
+    sb, ldsb = _scales(SB, "SB", -(-n // b_block), kb)
+    pc, ldc = None, ldd
+    if C is not None:
+        pc, tc, mc, nc, ldc = _rowmajor(C, "C", _FLOATS)
+        if (mc, nc) != (m, n) or tc != td:
+            raise ValueError("C: need the shape and type of D")
+    _check(lib().gemm2m_fp8_gemm(m, n, k, pa, fa, lda, sa, ldsa, a_block, pb, fb, ldb, sb, ldsb, b_block, pc, ldc, pd, td, ldd,
+                                 _stream_ptr(stream)), "gemm2m_fp8_gemm")
+
+
+def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
+    """O (bfloat16) = G orthogonalised by Newton-Schulz steps; 2-D, or 3-D for a batch.  coeffs: (a, b, c), or one such per step."""
+    if G.dim() not in (2, 3) or not G.is_cuda or not O.is_cuda or O.shape != G.shape:
+        raise ValueError("G, O: need CUDA tensors of the same 2-D or 3-D shape")
+    tg = _type_of(G, "G", _FLOATS)
+    _type_of(O, "O", (BF16,))
+    batch = G.shape[0] if G.dim() == 3 else 1
+    m, n = G.shape[-2:]
+    if n > 1 and (G.stride(-1) != 1 or O.stride(-1) != 1):
+        raise ValueError("G, O: need row-major storage (stride 1 along the last dim)")
+    ld = lambda t: t.stride(-2) if m > 1 else max(n, 1)
+    stride = lambda t: t.stride(0) if batch > 1 and t.dim() == 3 else m * max(n, 1)
+    co = None
+    if coeffs is not None:
+        rows = [coeffs] * steps if not hasattr(coeffs[0], "__len__") else list(coeffs)
+        if len(rows) != steps or any(len(r) != 3 for r in rows):
+            raise ValueError("coeffs: need (a, b, c), or one such per step")
+        co = ctypes.cast((ctypes.c_float * (3 * steps))(*[float(v) for r in rows for v in r]), ctypes.c_void_p)
+    _check(lib().gemm2m_newton_schulz(batch, m, n, G.data_ptr(), tg, ld(G), stride(G), O.data_ptr(), ld(O), stride(O), steps, co, eps,
+                                      _stream_ptr(stream)), "gemm2m_newton_schulz")
 
 
 def device_status(stream=None):

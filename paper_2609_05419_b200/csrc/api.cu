@@ -3,6 +3,7 @@
 #include "../../include/gemm2m.h"
 
 #include "common.cuh"
+#include "layer_ops.cuh"
 
 #include <cstdio>
 #include <cstring>
@@ -182,6 +183,17 @@ int ensure_copy_streams() {
     for (auto& e : D().g_ready) CK(make(e));
     for (auto& e : D().c_ready) CK(make(e));
     return GEMM2M_OK;
+}
+
+// Layer operators: their part of the workspace lies behind the status word and the post-processing operand, which they leave alone.
+constexpr int64_t kLayerOpsOffset = 256 + 4 * kPostFragWords;
+constexpr int64_t kMaxCoord = INT32_MAX - 1024;      // row and column indexes of the layer operators fit 32 bits, tile overhang included
+bool fp8_sizes_ok(int64_t m, int64_t n, int64_t k) {
+    return m >= 0 && n >= 0 && k >= 0 && m <= kMaxCoord && n <= kMaxCoord && k <= kMaxCoord;
+}
+constexpr int64_t kMaxNsSide = 1 << 20;              // sides of a Newton-Schulz matrix
+bool newton_schulz_sizes_ok(int64_t batch, int64_t m, int64_t n) {
+    return batch >= 0 && batch <= 65535 && m >= 0 && n >= 0 && m <= kMaxNsSide && n <= kMaxNsSide;
 }
 
 constexpr int64_t kMaxRows = 65535LL * 32;   // grid.y limit of the residue kernels
@@ -542,6 +554,8 @@ int gemm2m_modulus(int j, int* m, int* s) {
 }
 
 size_t gemm2m_workspace_bytes(int op, int64_t m, int64_t n, int64_t k, int nmod) {
+    if (op == GEMM2M_OP_FP8_GEMM) return fp8_sizes_ok(m, n, k) ? (size_t)kLayerOpsOffset : 0;
+    if (op == GEMM2M_OP_NEWTON_SCHULZ) return newton_schulz_sizes_ok(k, m, n) ? (size_t)newton_schulz_layout(k, m, n, kLayerOpsOffset).total : 0;
     Carve c;
     if (op == GEMM2M_OP_GAUSSIAN_INT && nmod > 8) return 0;
     if (!carve(op, m, n, k, nmod, &c)) return 0;
@@ -860,6 +874,101 @@ int dsyrk2m(int64_t n, int64_t k, const double* A, int64_t lda, double* C, int64
 int dsyr2k2m(int64_t n, int64_t k, const double* A, int64_t lda, const double* B, int64_t ldb, double* C, int64_t ldc, int nmod,
              void* stream) {
     return rank_update(GEMM2M_OP_DSYR2K, n, k, A, lda, B, ldb, C, ldc, nmod, stream);
+}
+
+int gemm2m_fp8_quantise(int64_t rows, int64_t cols, const void* X, int type, int64_t ldx, int fmt, int block_rows, void* Q, int64_t ldq,
+                        float* S, int64_t lds, void* Qt, int64_t ldqt, float* St, int64_t ldst, void* stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    if (!fp8_sizes_ok(rows, cols, 0) || ldx < (cols > 1 ? cols : 1)) return GEMM2M_ERR_ARG;
+    if (type < GEMM2M_F32 || type > GEMM2M_BF16 || (fmt != GEMM2M_E4M3 && fmt != GEMM2M_E5M2)) return GEMM2M_ERR_ARG;
+    if (block_rows != 1 && block_rows != kScaleBlock) return GEMM2M_ERR_ARG;
+    if ((Q == nullptr) != (S == nullptr) || (Qt == nullptr) != (St == nullptr)) return GEMM2M_ERR_ARG;
+    const int64_t rb = block_rows == 1 ? rows : (rows + kScaleBlock - 1) / kScaleBlock;      // rows of scales of either form
+    const int64_t cb = block_rows == 1 ? cols : (cols + kScaleBlock - 1) / kScaleBlock;
+    auto bytes_ok = [](const void* p, int64_t ld, int64_t width) { return ld >= (width > 1 ? width : 1) && ld % 16 == 0 && ((uintptr_t)p & 15) == 0; };
+    if (Q && (!bytes_ok(Q, ldq, cols) || lds < (rb > 1 ? rb : 1))) return GEMM2M_ERR_ARG;
+    if (Qt && (!bytes_ok(Qt, ldqt, rows) || ldst < (cb > 1 ? cb : 1))) return GEMM2M_ERR_ARG;
+    if (rows == 0 || cols == 0) return GEMM2M_OK;
+    if (!X || (!Q && !Qt)) return GEMM2M_ERR_ARG;
+    if (((rows + 127) / 128) * ((cols + 127) / 128) > INT32_MAX) return GEMM2M_ERR_ARG;
+    if (int s = check_device()) return s;
+    cudaStream_t st = (cudaStream_t)stream;
+    Phases ph;
+    if (int s = begin_call(&ph)) return s;
+    const QuantiseArgs a = {rows, cols, X, type, ldx, fmt, block_rows, (uint8_t*)Q, ldq, S, lds, (uint8_t*)Qt, ldqt, St, ldst};
+    CK(ph.begin(1, st));
+    CK(launch_fp8_quantise(a, st, &g.launches[1]));
+    CK(ph.end(st));
+    ph.done();
+    return GEMM2M_OK;
+}
+
+int gemm2m_fp8_gemm(int64_t m, int64_t n, int64_t k, const void* A, int a_fmt, int64_t lda, const float* SA, int64_t ldsa, int a_block,
+                    const void* B, int b_fmt, int64_t ldb, const float* SB, int64_t ldsb, int b_block, const void* C, int64_t ldc, void* D,
+                    int type, int64_t ldd, void* stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    if (!fp8_sizes_ok(m, n, k)) return GEMM2M_ERR_ARG;
+    auto operand_ok = [k](const void* Q, int fmt, int64_t ld, const float* S, int64_t lds, int block, int64_t rows) {
+        if ((fmt != GEMM2M_E4M3 && fmt != GEMM2M_E5M2) || (block != 1 && block != kScaleBlock)) return false;
+        const int64_t rb = block == 1 ? rows : (rows + kScaleBlock - 1) / kScaleBlock;
+        if (ld < (k > 1 ? k : 1) || ld % 16 != 0 || ((uintptr_t)Q & 15) != 0 || lds < (rb > 1 ? rb : 1)) return false;
+        return rows == 0 || k == 0 || (Q && S);
+    };
+    if (!operand_ok(A, a_fmt, lda, SA, ldsa, a_block, m) || !operand_ok(B, b_fmt, ldb, SB, ldsb, b_block, n)) return GEMM2M_ERR_ARG;
+    if (type < GEMM2M_F32 || type > GEMM2M_BF16) return GEMM2M_ERR_ARG;
+    const int64_t width = n > 1 ? n : 1;
+    if (ldd < width || (C && ldc < width) || (C == D && C && ldc != ldd)) return GEMM2M_ERR_ARG;
+    if (m == 0 || n == 0) return GEMM2M_OK;
+    if (!D) return GEMM2M_ERR_ARG;
+    if (int s = check_device()) return s;
+    cudaStream_t st = (cudaStream_t)stream;
+    const size_t es = type == GEMM2M_F32 ? 4 : 2;
+    Phases ph;
+    if (k == 0) {                        // nothing to multiply: D = C, or zero
+        std::memset(g.launches, 0, sizeof(g.launches));
+        if (!C) CK(cudaMemset2DAsync(D, (size_t)ldd * es, 0, (size_t)n * es, (size_t)m, st));
+        else if (C != D) CK(cudaMemcpy2DAsync(D, (size_t)ldd * es, C, (size_t)ldc * es, (size_t)n * es, (size_t)m, cudaMemcpyDeviceToDevice, st));
+        return GEMM2M_OK;
+    }
+    DevState& dev = g.dev[g.cur];
+    if (!dev.ws || dev.ws_bytes < (size_t)kLayerOpsOffset) return GEMM2M_ERR_WORKSPACE;
+    if (int s = begin_call(&ph)) return s;
+    const Fp8GemmArgs a = {m, n, k, {(const uint8_t*)A, a_fmt, lda, SA, ldsa, a_block}, {(const uint8_t*)B, b_fmt, ldb, SB, ldsb, b_block},
+                           C, ldc, D, type, ldd, (int*)dev.ws};
+    CK(ph.begin(2, st));
+    CK(launch_fp8_gemm(a, dev.sm_count, st, &g.launches[2]));
+    CK(ph.end(st));
+    ph.done();
+    return GEMM2M_OK;
+}
+
+int gemm2m_newton_schulz(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* O, int64_t ldo,
+                         int64_t stride_o, int steps, const float* coeffs, float eps, void* stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    constexpr int kMaxSteps = 64;
+    if (!newton_schulz_sizes_ok(batch, m, n) || ldg < (n > 1 ? n : 1) || ldo < (n > 1 ? n : 1)) return GEMM2M_ERR_ARG;
+    if (type < GEMM2M_F32 || type > GEMM2M_BF16 || steps < 1 || steps > kMaxSteps || !(eps >= 0.f)) return GEMM2M_ERR_ARG;
+    if (batch > 1 && (stride_g < 0 || stride_o < (m > 0 ? (m - 1) * ldo + n : 0))) return GEMM2M_ERR_ARG;    // matrices of O do not overlap
+    if (batch == 0 || m == 0 || n == 0) return GEMM2M_OK;
+    if (!G || !O) return GEMM2M_ERR_ARG;
+    if (int s = check_device()) return s;
+    cudaStream_t st = (cudaStream_t)stream;
+    const NewtonSchulzLayout lay = newton_schulz_layout(batch, m, n, kLayerOpsOffset);
+    if (!D().ws || D().ws_bytes < (size_t)lay.total) return GEMM2M_ERR_WORKSPACE;
+    static const float kMuon[3] = {3.4445f, -4.7750f, 2.0315f};
+    float co[3 * kMaxSteps];
+    for (int i = 0; i < 3 * steps; ++i) co[i] = coeffs ? coeffs[i] : kMuon[i % 3];
+    Phases ph;
+    if (int s = begin_call(&ph)) return s;
+    const NewtonSchulzArgs a = {batch, m, n, G, type, ldg, stride_g, O, ldo, stride_o, steps, co, eps, (char*)D().ws, lay, (int*)D().ws};
+    int launches[2] = {0, 0};
+    CK(ph.begin(2, st));
+    CK(launch_newton_schulz(a, D().sm_count, st, launches));
+    CK(ph.end(st));
+    g.launches[1] = launches[0];
+    g.launches[2] = launches[1];
+    ph.done();
+    return GEMM2M_OK;
 }
 
 int gemm2m_device_status(void* stream) {

@@ -1,0 +1,53 @@
+// Operators of a layer's training step next to the products of common.cuh: quantisation to 8-bit floating point with block
+// scales (fp8_quantise.cu), the product of two such matrices (fp8_gemm.cu) and Newton-Schulz orthogonalisation
+// (newton_schulz.cu).  Matrices are row-major here: rows contiguous, leading dimension = elements between rows.
+#pragma once
+#include "common.cuh"
+
+namespace gemm2m {
+
+constexpr int kScaleBlock = 128;          // entries along k that share a scale
+constexpr float kLeastMax = 0x1p-100f;    // smallest block maximum: keeps MAX / maximum finite, and gives a block of zeros a scale
+
+// Element types, numbered as in gemm2m_type.
+enum ElemType { kF32 = 0, kF16 = 1, kBF16 = 2, kE4M3 = 3, kE5M2 = 4 };
+
+struct QuantiseArgs {
+    int64_t rows, cols;
+    const void* X; int type; int64_t ldx;
+    int fmt, block_rows;                  // kE4M3 / kE5M2; 1 or 128 rows per scale
+    uint8_t* Q; int64_t ldq; float* S; int64_t lds;
+    uint8_t* Qt; int64_t ldqt; float* St; int64_t ldst;      // transposed form, or null
+};
+cudaError_t launch_fp8_quantise(const QuantiseArgs& a, cudaStream_t st, int* launches);
+
+// One operand of the scaled product: rows x k bytes, k contiguous; scale of (row r, block b) at S[b lds + r / block].
+struct Fp8Operand { const uint8_t* Q; int fmt; int64_t ld; const float* S; int64_t lds; int block; };
+struct Fp8GemmArgs {
+    int64_t m, n, k;
+    Fp8Operand A, B;
+    const void* C; int64_t ldc;           // added to the product, or null; same type as D
+    void* D; int type; int64_t ldd;
+    int* dev_status;
+};
+cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches);
+
+// Newton-Schulz iteration on `batch` matrices (see newton_schulz.cu for the arithmetic and the workspace).
+struct NewtonSchulzLayout {
+    int64_t ldx, lds;                     // leading dimensions of the iterate and of the short-side squares, in elements
+    int64_t off_norm, off_trace[2], off_hi[2], off_lo[2], off_gram, off_poly, total;      // bytes from the start of the workspace
+    int norm_parts, trace_parts;          // partial sums per matrix
+};
+NewtonSchulzLayout newton_schulz_layout(int64_t batch, int64_t m, int64_t n, int64_t offset);
+struct NewtonSchulzArgs {
+    int64_t batch, m, n;
+    const void* G; int type; int64_t ldg, stride_g;
+    void* O; int64_t ldo, stride_o;       // bf16
+    int steps; const float* coeffs;       // host, (a, b, c) per step
+    float eps;
+    char* ws; NewtonSchulzLayout lay;
+    int* dev_status;
+};
+cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaStream_t st, int launches[2]);
+
+}  // namespace gemm2m
