@@ -35,13 +35,13 @@ template <int BN, bool COLS>
 struct Cfg {
     static constexpr int kHalfRows = BN / 2;                          // rows of B per CTA
     static constexpr int kStageBytes = (kBM + kHalfRows) * kGemmBK;
-    static constexpr int kStages = BN == 256 ? 6 : 8;
+    static constexpr int kStages = 5;
     static constexpr int kCols = BN / 2;                              // columns per epilogue warp: totals per thread
     static constexpr uint32_t kTmemCols = 2 * BN;
     static constexpr int kSlotFloats = kBM + (COLS ? BN : 2);         // scales of one block: 128 rows, and the columns or their two halves
     static constexpr int kSlotBytes = (kSlotFloats * 4 + 15) / 16 * 16;
     static constexpr size_t kScaleBytes = (size_t)kSlots * kSlotBytes;
-    static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + kScaleBytes + PairPipe<kStages>::kBytes;
+    static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + kScaleBytes + PairPipe<kStages>::kBytes + 16 + kEpilogueWarps * 4096;
 };
 
 struct Fp8GemmParams {
@@ -52,7 +52,7 @@ struct Fp8GemmParams {
     uint32_t idesc;
     const void* C; int64_t ldc;
     void* D; int64_t ldd;
-    int type;
+    int vec;                             // rows of C and D allow stores of four entries
     int* dev_status;
     unsigned long long wait_ns;
 };
@@ -89,24 +89,46 @@ template <> __device__ __forceinline__ float to_type<float>(float v) { return v;
 template <> __device__ __forceinline__ __half to_type<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 to_type<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
 
-// NT totals of one row, columns [col, col + NT) of which those below n exist, to D (plus C).  Whole 16-byte pieces where the
-// row's address allows it.
-template <typename T, int NT>
-__device__ __forceinline__ void store_row(const float* v, const T* crow, T* drow, int col, int n) {
-    constexpr int V = 16 / (int)sizeof(T);
-    const bool vec = ((reinterpret_cast<uintptr_t>(drow + col) | (crow ? reinterpret_cast<uintptr_t>(crow + col) : 0)) & 15) == 0;
+// NC columns of 32 rows, one row per lane, to rows [row0, row0 + 32) and columns [col0, col0 + NC) of D (plus C), of which those
+// below m and n exist.  Through `turn`, 4 KB of shared memory per warp, 32 columns at a time: a lane writes its row's 128 bytes,
+// 16-byte pieces XORed with the row, and then eight lanes store one row's 32 columns side by side (whole 32-byte
+// sectors; a lane storing along its own row would leave half-written sectors of 32 rows per instruction).
+template <typename T, int NC>
+__device__ __forceinline__ void store_rows(const float (&v)[NC], uint32_t turn, const T* C, int64_t ldc, T* D, int64_t ldd, int row0, int col0, int m, int n, bool vec) {
+    const int lane = threadIdx.x & 31, piece = lane & 7;
+    struct alignas(4 * sizeof(T)) Four { T t[4]; };
 #pragma unroll
-    for (int i = 0; i < NT; i += V) {
-        if (vec && col + i + V <= n) {
-            T out[V], in[V];
-            if (crow) *reinterpret_cast<uint4*>(in) = *reinterpret_cast<const uint4*>(crow + col + i);
+    for (int c = 0; c < NC; c += 32) {
+        __syncwarp();                                     // the previous columns have been read
 #pragma unroll
-            for (int j = 0; j < V; ++j) out[j] = to_type<T>(v[i + j] + (crow ? from_type<T>(in[j]) : 0.f));
-            *reinterpret_cast<uint4*>(drow + col + i) = *reinterpret_cast<const uint4*>(out);
-        } else {
+        for (int q = 0; q < 8; ++q)
+            asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (uint32_t)(lane * 128 + ((q ^ (lane & 7)) << 4))), "f"(v[c + 4 * q]),
+                         "f"(v[c + 4 * q + 1]), "f"(v[c + 4 * q + 2]), "f"(v[c + 4 * q + 3]) : "memory");
+        __syncwarp();
+        const int col = col0 + c + piece * 4;
+        const int rows = col < n ? min(32, m - row0) : 0;
+#pragma unroll 2
+        for (int r = lane >> 3; r < rows; r += 4) {       // (kept short: this code is fetched anew for every tile)
+            float x[4];
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
+                         : "r"(turn + (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4))) : "memory");
+            T* d = D + (int64_t)(row0 + r) * ldd + col;
+            const T* s = C ? C + (int64_t)(row0 + r) * ldc + col : nullptr;
+            if (vec && col + 4 <= n) {
+                Four f;
+                if (s) {
+                    f = *reinterpret_cast<const Four*>(s);
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (col + i + j < n) drow[col + i + j] = to_type<T>(v[i + j] + (crow ? from_type<T>(crow[col + i + j]) : 0.f));
+                    for (int j = 0; j < 4; ++j) x[j] += from_type<T>(f.t[j]);
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f.t[j] = to_type<T>(x[j]);
+                *reinterpret_cast<Four*>(d) = f;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (col + j < n) d[j] = to_type<T>(x[j] + (s ? from_type<T>(s[j]) : 0.f));
+            }
         }
     }
 }
@@ -120,8 +142,8 @@ __device__ __forceinline__ float lds(uint32_t addr) {
     return v;
 }
 
-// COLS: B has a scale per row (of B; column of D) and block, otherwise one per 128 rows.
-template <int BN, bool COLS>
+// T: type of C and D.  COLS: B has a scale per row (of B; column of D) and block, otherwise one per 128 rows.
+template <typename T, int BN, bool COLS>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Fp8GemmParams p) {
     using cfg = Cfg<BN, COLS>;
@@ -232,17 +254,18 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         const uint32_t row_slot = scale_ring + (uint32_t)(quarter * 32 + lane) * 4;
         const uint32_t col_slot = scale_ring + (uint32_t)(kBM + (COLS ? half * NC : half)) * 4;
         const uint32_t taddr = pipe.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * NC);
+        const uint32_t turn = smem_u32(behind) + (uint32_t)(cfg::kScaleBytes + PairPipe<STAGES>::kBytes + 15) / 16 * 16 + (uint32_t)(warp - kFirstEpilogueWarp) * 4096;
         const uint32_t leader_tempty = map_to_cta(pipe.tempty, 0);
         uint32_t it = 0;
         bool ok = true;
         for (int tile = pair; ok && tile < total_tiles; tile += npairs) {
             int tr, tc;
             tile_at(p, tile, &tr, &tc);
-            const int row = tr * (2 * kBM) + (int)pipe.rank * kBM + quarter * 32 + lane;
+            const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM + quarter * 32;
             const int col0 = tc * BN + half * NC;
-            uint64_t acc[NC / 2];
+            float acc[NC];
 #pragma unroll
-            for (int i = 0; i < NC / 2; ++i) acc[i] = 0;
+            for (int i = 0; i < NC; ++i) acc[i] = 0.f;
             for (int kb = p.kblocks; kb > 0; --kb, ++it) {
                 const uint32_t buf = it & 1u;
                 // (a wait that gives up is acted on at the end of the tile: every later one then returns at once)
@@ -263,27 +286,21 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
                     else pipe.release_at(leader_tempty + 8 * buf);
 #pragma unroll
                     for (int i = 0; i < 32; i += 4) {
-                        uint64_t x = s2, y = s2;
+                        float s[4] = {scale, scale, scale, scale};
                         if (COLS) {
                             uint64_t f, g;
                             asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f), "=l"(g) : "r"(col_scale + (c + i) * 4));
-                            x = mul2(s2, f);
-                            y = mul2(s2, g);
+                            unpack2(mul2(s2, f), &s[0], &s[1]);
+                            unpack2(mul2(s2, g), &s[2], &s[3]);
                         }
-                        fma2(acc[(c + i) / 2], pack2(__uint_as_float(w[i]), __uint_as_float(w[i + 1])), x);
-                        fma2(acc[(c + i) / 2 + 1], pack2(__uint_as_float(w[i + 2]), __uint_as_float(w[i + 3])), y);
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) fma1(acc[c + i + j], __uint_as_float(w[i + j]), s[j]);
                     }
                 }
             }
             ok = __all_sync(0xffffffffu, ok);
-            if (ok && row < p.m && col0 < p.n) {
-                float t[NC];
-#pragma unroll
-                for (int i = 0; i < NC / 2; ++i) unpack2(acc[i], &t[2 * i], &t[2 * i + 1]);
-                const int64_t dr = (int64_t)row * p.ldd, cr = (int64_t)row * p.ldc;
-                if (p.type == kF32) store_row<float, NC>(t, p.C ? (const float*)p.C + cr : nullptr, (float*)p.D + dr, col0, p.n);
-                else if (p.type == kF16) store_row<__half, NC>(t, p.C ? (const __half*)p.C + cr : nullptr, (__half*)p.D + dr, col0, p.n);
-                else store_row<__nv_bfloat16, NC>(t, p.C ? (const __nv_bfloat16*)p.C + cr : nullptr, (__nv_bfloat16*)p.D + dr, col0, p.n);
+            if (ok && row0 < p.m && col0 < p.n) {
+                store_rows<T, NC>(acc, turn, (const T*)p.C, p.ldc, (T*)p.D, p.ldd, row0, col0, p.m, p.n, p.vec != 0);
             }
         }
         if (!ok && lane == 0) pipe.tell_peer();
@@ -303,13 +320,13 @@ bool make_byte_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN, bool COLS>
+template <typename T, int BN, bool COLS>
 cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
     static int pairs_dev[kMaxDevices] = {};
     int& max_pairs = pairs_dev[current_device_slot()];
     if (!max_pairs) {
         int pairs = 0;
-        cudaError_t err = resident_pairs(fp8_gemm_pair_kernel<BN, COLS>, kThreads, Cfg<BN, COLS>::kSmem, sm_count, &pairs);
+        cudaError_t err = resident_pairs(fp8_gemm_pair_kernel<T, BN, COLS>, kThreads, Cfg<BN, COLS>::kSmem, sm_count, &pairs);
         if (err != cudaSuccess) return err;
         max_pairs = pairs;
     }
@@ -325,19 +342,28 @@ cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int
     p.SA = a.A.S; p.SB = a.B.S; p.ldsa = a.A.lds; p.ldsb = a.B.lds;
     p.shift_a = a.A.block == 1 ? 0 : 7; p.shift_b = a.B.block == 1 ? 0 : 7;
     p.idesc = make_idesc_f8(a.A.fmt, a.B.fmt, 2 * kBM, BN);
-    p.C = a.C; p.ldc = a.ldc; p.D = a.D; p.ldd = a.ldd; p.type = a.type;
+    p.C = a.C; p.ldc = a.ldc; p.D = a.D; p.ldd = a.ldd; 
+    const uintptr_t es = sizeof(T), at = (uintptr_t)a.D | (uintptr_t)a.C, ld = (uintptr_t)a.ldd | (a.C ? (uintptr_t)a.ldc : 0);
+    p.vec = at % (4 * es) == 0 && ld % 4 == 0;
     p.dev_status = a.dev_status;
     p.wait_ns = kWaitLimitNs;
     const int pairs = (int)(tr * tc < max_pairs ? tr * tc : max_pairs);
-    cudaError_t err = launch_chained(fp8_gemm_pair_kernel<BN, COLS>, dim3(2 * pairs), dim3(kThreads), Cfg<BN, COLS>::kSmem, st, map_a, map_b, p);
+    cudaError_t err = launch_chained(fp8_gemm_pair_kernel<T, BN, COLS>, dim3(2 * pairs), dim3(kThreads), Cfg<BN, COLS>::kSmem, st, map_a, map_b, p);
     if (err == cudaSuccess) ++*launches;
     return err;
+}
+
+template <typename T>
+cudaError_t launch_typed(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
+    return a.B.block == 1 ? launch_pair<T, 256, true>(a, sm_count, st, launches) : launch_pair<T, 256, false>(a, sm_count, st, launches);
 }
 
 }  // namespace
 
 cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
-    return a.B.block == 1 ? launch_pair<256, true>(a, sm_count, st, launches) : launch_pair<256, false>(a, sm_count, st, launches);
+    if (a.type == kF32) return launch_typed<float>(a, sm_count, st, launches);
+    if (a.type == kF16) return launch_typed<__half>(a, sm_count, st, launches);
+    return launch_typed<__nv_bfloat16>(a, sm_count, st, launches);
 }
 
 }  // namespace gemm2m

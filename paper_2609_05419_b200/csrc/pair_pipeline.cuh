@@ -133,8 +133,8 @@ __device__ __forceinline__ uint64_t pack2(float a, float b) {
     return r;
 }
 __device__ __forceinline__ void unpack2(uint64_t v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
-// (volatile: stays behind the wait for the TMEM load that fills the operands)
-__device__ __forceinline__ void fma2(uint64_t& acc, uint64_t x, uint64_t y) { asm volatile("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc) : "l"(x), "l"(y)); }
+// (volatile: stays behind the wait for the TMEM load that fills its operand)
+__device__ __forceinline__ void fma1(float& acc, float x, float y) { asm volatile("fma.rn.f32 %0, %1, %2, %0;" : "+f"(acc) : "f"(x), "f"(y)); }
 __device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
     uint64_t r;
     asm volatile("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
