@@ -146,6 +146,25 @@ inline cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, s
     c.numAttrs = chained_launch_enabled() ? 1 : 0;
     return cudaLaunchKernelEx(&c, kernel, P(args)...);
 }
+// The same in clusters of `cluster` blocks along x.
+template <typename... P, typename... A>
+inline cudaError_t launch_chained_cluster(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, int cluster, cudaStream_t st, A&&... args) {
+    cudaLaunchConfig_t c = {};
+    c.gridDim = grid;
+    c.blockDim = block;
+    c.dynamicSmemBytes = smem;
+    c.stream = st;
+    cudaLaunchAttribute at[2];
+    at[0].id = cudaLaunchAttributeClusterDimension;
+    at[0].val.clusterDim.x = (unsigned)cluster;
+    at[0].val.clusterDim.y = 1;
+    at[0].val.clusterDim.z = 1;
+    at[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    at[1].val.programmaticStreamSerializationAllowed = 1;
+    c.attrs = at;
+    c.numAttrs = chained_launch_enabled() ? 2 : 1;
+    return cudaLaunchKernelEx(&c, kernel, P(args)...);
+}
 #endif
 
 inline int current_device_slot() {

@@ -353,9 +353,310 @@ cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int
     return err;
 }
 
+// ---- thin products -------------------------------------------------------------------------------------------------
+// Few rows on one side (a token, a decoding batch), or too few 256 x 256 tiles to fill the GPU: one CTA per tile of 128 rows of
+// the lane operand (the weights, for tokens) x N rows of the column operand, N = 16, 32, 64 or 128, and the blocks of k split over a cluster
+// of S CTAs, whose totals are added through distributed shared memory in the order of the ranks.  The lane operand is
+// what such a product has to read; all stages of the ring are requested at once, so that every SM has 130 to 190 KB on its way.
+
+constexpr int kThinBuffers = 4;                  // accumulators of N columns
+constexpr int kThinSlots = 16, kThinAhead = 6;   // scales turn to block g after tfull of g - 4, so every warp is through with g - 9; slot of g + 6 - 16
+constexpr int kThinThreads = 256;                // copies, MMAs, two scale warps, four epilogue warps
+constexpr int kMostSplit = 8;
+
+template <int N>
+struct ThinCfg {
+    static constexpr int kStageBytes = (kBM + N) * kGemmBK;
+    static constexpr int kStages = N == 128 ? 6 : 8;
+    static constexpr int kSlotBytes = (kBM + N) * 4;
+    static constexpr size_t kBarBytes = 8 * (2 * kStages + 2 * kThinBuffers + 1) + 16;
+    static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + (size_t)kThinSlots * kSlotBytes + kBarBytes;
+    static constexpr uint32_t kTmemCols = N * kThinBuffers < 32 ? 32 : N * kThinBuffers;
+    static_assert((size_t)kStages * kStageBytes >= (size_t)N * kBM * 4, "the totals of a split product pass through the stages");
+};
+
+struct ThinParams {
+    int lanes, cols, kblocks, lane_tiles;        // rows of the lane and of the column operand, blocks of k, tiles of the lane operand
+    const float *SL, *SC;
+    int64_t ldsl, ldsc;
+    int shift_l, shift_c;
+    uint32_t idesc;
+    const void* C; int64_t c_lane, c_col;        // element strides of C and D along the two operands' rows
+    void* D; int64_t d_lane, d_col;
+    int* dev_status;
+    unsigned long long wait_ns;
+};
+
+__device__ __forceinline__ void umma_f8(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d_tmem), "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
+        : "memory");
+}
+__device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y) {
+    asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4}], [%2];"
+                 ::"r"(dst), "l"(map), "r"(bar), "r"(x), "r"(y) : "memory");
+}
+__device__ __forceinline__ uint32_t cluster_size() {
+    uint32_t r;
+    asm volatile("mov.u32 %0, %%cluster_nctarank;" : "=r"(r));
+    return r;
+}
+
+template <typename T, int N>
+__global__ void __launch_bounds__(kThinThreads, 1)
+fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const __grid_constant__ ThinParams p) {
+    using cfg = ThinCfg<N>;
+    constexpr int STAGES = cfg::kStages;
+    extern __shared__ unsigned char smem_raw[];
+    const uint32_t raw = smem_u32(smem_raw);
+    const uint32_t tiles_base = (raw + 1023u) & ~1023u;
+    unsigned char* behind = smem_raw + (tiles_base - raw) + (size_t)STAGES * cfg::kStageBytes;
+    const uint32_t scale_ring = smem_u32(behind);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(behind + kThinSlots * cfg::kSlotBytes);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, tfull = empty + 8 * STAGES, tempty = tfull + 8 * kThinBuffers;
+    const uint32_t drain = tempty + 8 * kThinBuffers;
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 2 * kThinBuffers + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    volatile uint32_t* fills_issued = reinterpret_cast<volatile uint32_t*>(tmem_slot + 2);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int S = (int)cluster_size(), rank = (int)cluster_ctarank();
+    const int tile = blockIdx.x / S;
+    const int l0 = tile % p.lane_tiles * kBM, c0 = tile / p.lane_tiles * N;
+    const int kb0 = (int)((int64_t)p.kblocks * rank / S), blocks = (int)((int64_t)p.kblocks * (rank + 1) / S) - kb0;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
+        for (int a = 0; a < kThinBuffers; ++a) { mbar_init(tfull + 8 * a, 1 + kScaleWarps); mbar_init(tempty + 8 * a, 4); }
+        mbar_init(drain, 1);
+        *abort_flag = 0;
+        *fills_issued = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(cfg::kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    tcgen05_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    wait_for_prior_kernels();
+    auto wait = [&](uint32_t bar, uint32_t parity, int code) { return mbar_wait(bar, parity, abort_flag, p.dev_status, code, p.wait_ns); };
+
+    float acc[N];
+    if (warp == 0) {
+        if (lane == 0) {
+            RingPos<STAGES> at;
+            int kb = 0;
+            for (; kb < blocks; ++kb) {
+                if (!wait(empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer)) break;
+                const uint32_t dst = tiles_base + at.stage * cfg::kStageBytes, bar = full + 8 * at.stage;
+                mbar_arrive_expect_tx(bar, cfg::kStageBytes);
+                tma_load_2d(dst, &map_l, bar, (kb0 + kb) * kGemmBK, l0);
+                tma_load_2d(dst + kBM * kGemmBK, &map_c, bar, (kb0 + kb) * kGemmBK, c0);
+                at.next();
+            }
+            *fills_issued = (uint32_t)kb;
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            RingPos<STAGES> at;
+            for (int kb = 0; kb < blocks; ++kb) {
+                const uint32_t buf = kb % kThinBuffers, use = kb / kThinBuffers;
+                if (!wait(tempty + 8 * buf, (use & 1u) ^ 1u, kDevTimeoutMma) || !wait(full + 8 * at.stage, at.phase, kDevTimeoutMma)) break;
+                tcgen05_fence_after();
+                const uint32_t a_addr = tiles_base + at.stage * cfg::kStageBytes;
+                const uint64_t adesc = make_smem_desc(a_addr), bdesc = make_smem_desc(a_addr + kBM * kGemmBK);
+#pragma unroll
+                for (int k4 = 0; k4 < 4; ++k4)
+                    umma_f8(tmem + buf * N, adesc + (uint64_t)(k4 * 2), bdesc + (uint64_t)(k4 * 2), p.idesc, (uint32_t)(k4 != 0));
+                umma_commit(empty + 8 * at.stage);
+                umma_commit(tfull + 8 * buf);
+                at.next();
+            }
+        }
+    } else if (warp < 4) {                       // scales: asynchronous 4-byte copies, one group per block
+        const int t = threadIdx.x - 64;
+        int fetched = 0;
+        auto fetch = [&]() {
+            if (fetched < blocks) {
+                const uint32_t slot = scale_ring + (uint32_t)(fetched % kThinSlots) * cfg::kSlotBytes;
+                const float* sl = p.SL + (int64_t)(kb0 + fetched) * p.ldsl;
+                const float* sc = p.SC + (int64_t)(kb0 + fetched) * p.ldsc;
+#pragma unroll
+                for (int i = 0; i < kBM; i += 64) cp_async4(slot + (i + t) * 4, sl + (min(l0 + i + t, p.lanes - 1) >> p.shift_l));
+#pragma unroll
+                for (int i = 0; i < N; i += 64)
+                    if (i + t < N) cp_async4(slot + (kBM + i + t) * 4, sc + (min(c0 + i + t, p.cols - 1) >> p.shift_c));
+                ++fetched;
+            }
+            asm volatile("cp.async.commit_group;" ::: "memory");
+        };
+        for (int i = 0; i < kThinAhead; ++i) fetch();
+        for (int g = 0; g < blocks; ++g) {
+            const uint32_t bar = tfull + 8 * (g % kThinBuffers);
+            if (g >= kThinBuffers && !__all_sync(0xffffffffu, wait(bar, ((g / kThinBuffers) & 1u) ^ 1u, kDevTimeoutProducer))) break;
+            fetch();
+            asm volatile("cp.async.wait_group %0;" ::"n"(kThinAhead) : "memory");
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else {                                     // epilogue: lane = row of the lane operand
+        const int quarter = warp & 3;
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
+#pragma unroll
+        for (int j = 0; j < N; ++j) acc[j] = 0.f;
+        bool ok = true;
+        for (int kb = 0; kb < blocks; ++kb) {
+            const uint32_t buf = kb % kThinBuffers, slot = scale_ring + (uint32_t)(kb % kThinSlots) * cfg::kSlotBytes;
+            ok &= wait(tfull + 8 * buf, (kb / kThinBuffers) & 1u, kDevTimeoutEpilogue);
+            tcgen05_fence_after();
+            const float scale = lds(slot + (quarter * 32 + lane) * 4);
+            const uint64_t s2 = pack2(scale, scale);
+            constexpr int P = N < 32 ? N : 32;
+#pragma unroll
+            for (int c = 0; c < N; c += P) {
+                uint32_t v[P];
+                if constexpr (P == 32) tmem_ld32(taddr + buf * N + c, v);
+                else tmem_ld16(taddr + buf * N + c, v);
+                tmem_ld_wait();
+                if (c + P == N) {
+                    tcgen05_fence_before();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(tempty + 8 * buf);
+                }
+#pragma unroll
+                for (int i = 0; i < P; i += 4) {
+                    uint64_t f, g;
+                    float s[4];
+                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f), "=l"(g) : "r"(slot + (kBM + c + i) * 4));
+                    unpack2(mul2(s2, f), &s[0], &s[1]);
+                    unpack2(mul2(s2, g), &s[2], &s[3]);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) fma1(acc[c + i + j], __uint_as_float(v[i + j]), s[j]);
+                }
+            }
+        }
+        if (S > 1) {                             // totals to shared memory, [column][lane]; the stages are free: all MMAs have completed
+            float* totals = reinterpret_cast<float*>(smem_raw + (tiles_base - raw));
+            if (ok)
+#pragma unroll
+                for (int j = 0; j < N; ++j) totals[j * kBM + quarter * 32 + lane] = acc[j];
+        } else if (ok) {
+            const int l = l0 + quarter * 32 + lane;
+            if (l < p.lanes) {
+                const T* cp = (const T*)p.C + (int64_t)l * p.c_lane;
+                T* dp = (T*)p.D + (int64_t)l * p.d_lane;
+#pragma unroll
+                for (int j = 0; j < N; ++j)
+                    if (c0 + j < p.cols) dp[(int64_t)(c0 + j) * p.d_col] = to_type<T>(acc[j] + (p.C ? from_type<T>(cp[(int64_t)(c0 + j) * p.c_col]) : 0.f));
+            }
+        }
+    }
+    tcgen05_fence_before();
+    __syncthreads();
+    if (*abort_flag) {                           // nothing may be in flight when shared memory and TMEM go away; both waits are bounded
+        if (warp == 1 && lane == 0) {
+            umma_commit(drain);
+            mbar_wait_quiet(drain, 0, kDrainLimitNs);
+        }
+        if (warp == 0 && lane == 0) {
+            const uint32_t fills = *fills_issued;
+            for (uint32_t s = 0; s < (uint32_t)STAGES && s < fills; ++s) {
+                const uint32_t last = s + STAGES * ((fills - 1 - s) / STAGES);
+                mbar_wait_quiet(full + 8 * s, (last / STAGES) & 1u, kDrainLimitNs);
+            }
+        }
+        __syncthreads();
+    }
+    if (S > 1) {
+        cluster_sync_all();                      // every rank's totals are there
+        if (warp >= 4) {                         // this rank's share of the columns, added in the order of the ranks
+            const int row = (int)threadIdx.x - 128, l = l0 + row;
+            const int from = N * rank / S, to = N * (rank + 1) / S;
+            if (l < p.lanes)
+                for (int j = from; j < to && c0 + j < p.cols; ++j) {
+                    float s = 0.f;
+                    for (int q = 0; q < S; ++q)
+                        s += __uint_as_float(ld_cluster_u32(map_to_cta(tiles_base + (uint32_t)(j * kBM + row) * 4, (uint32_t)q)));
+                    const int64_t dj = (int64_t)l * p.d_lane + (int64_t)(c0 + j) * p.d_col, cj = (int64_t)l * p.c_lane + (int64_t)(c0 + j) * p.c_col;
+                    ((T*)p.D)[dj] = to_type<T>(s + (p.C ? from_type<T>(((const T*)p.C)[cj]) : 0.f));
+                }
+        }
+        cluster_sync_all();                      // nobody leaves while its totals are being read
+    }
+    if (warp == 1) {
+        tcgen05_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cfg::kTmemCols) : "memory");
+    }
+}
+
+// Whether the 256 x 256 tiles of CTA pairs are used.
+bool takes_pair(const Fp8GemmArgs& a, int sm_count) {
+    const int64_t tiles = ((a.m + 255) / 256) * ((a.n + 255) / 256);
+    return a.m > 64 && a.n > 64 && tiles >= sm_count / 2;
+}
+
+// How often the blocks of k are split: the least number of rounds of CTAs, each weighed by its length, over the SMs; at least two blocks each.
+int thin_split(int64_t tiles, int64_t kblocks, int sm_count) {
+    int best = 1;
+    double best_cost = 1e30;
+    for (int S = 1; S <= kMostSplit; S *= 2) {
+        if (S > 1 && kblocks < 2 * S) break;
+        const int64_t rounds = (tiles * S + sm_count - 1) / sm_count;
+        const double cost = (double)rounds * ((double)((kblocks + S - 1) / S) + 6.0);      // a round's fixed part is about six blocks
+        if (cost < best_cost * 0.999) { best = S; best_cost = cost; }
+    }
+    return best;
+}
+
+template <typename T, int N>
+cudaError_t launch_thin(const Fp8GemmArgs& a, bool swapped, int sm_count, cudaStream_t st, int* launches) {
+    using cfg = ThinCfg<N>;
+    static bool ready_dev[kMaxDevices] = {};
+    bool& ready = ready_dev[current_device_slot()];
+    if (!ready) {
+        cudaError_t err = cudaFuncSetAttribute(fp8_gemm_thin_kernel<T, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg::kSmem);
+        if (err != cudaSuccess) return err;
+        ready = true;
+    }
+    const Fp8Operand &L = swapped ? a.B : a.A, &R = swapped ? a.A : a.B;
+    ThinParams p = {};
+    p.lanes = (int)(swapped ? a.n : a.m);
+    p.cols = (int)(swapped ? a.m : a.n);
+    CUtensorMap map_l, map_c;
+    if (!make_byte_map(&map_l, L.Q, p.lanes, a.k, L.ld, kBM) || !make_byte_map(&map_c, R.Q, p.cols, a.k, R.ld, N)) return cudaErrorInvalidValue;
+    p.kblocks = (int)((a.k + kScaleBlock - 1) / kScaleBlock);
+    p.lane_tiles = (p.lanes + kBM - 1) / kBM;
+    p.SL = L.S; p.SC = R.S; p.ldsl = L.lds; p.ldsc = R.lds;
+    p.shift_l = L.block == 1 ? 0 : 7; p.shift_c = R.block == 1 ? 0 : 7;
+    p.idesc = make_idesc_f8(L.fmt, R.fmt, kBM, N);
+    p.C = a.C; p.c_lane = swapped ? 1 : a.ldc; p.c_col = swapped ? a.ldc : 1;
+    p.D = a.D; p.d_lane = swapped ? 1 : a.ldd; p.d_col = swapped ? a.ldd : 1;
+    p.dev_status = a.dev_status;
+    p.wait_ns = kWaitLimitNs;
+    const int64_t tiles = (int64_t)p.lane_tiles * ((p.cols + N - 1) / N);
+    const int S = thin_split(tiles, p.kblocks, sm_count);
+    if (tiles * S > INT32_MAX) return cudaErrorInvalidValue;
+    cudaError_t err = launch_chained_cluster(fp8_gemm_thin_kernel<T, N>, dim3((unsigned)(tiles * S)), dim3(kThinThreads), cfg::kSmem, S, st, map_l, map_c, p);
+    if (err == cudaSuccess) ++*launches;
+    return err;
+}
+
 template <typename T>
 cudaError_t launch_typed(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
-    return a.B.block == 1 ? launch_pair<T, 256, true>(a, sm_count, st, launches) : launch_pair<T, 256, false>(a, sm_count, st, launches);
+    if (takes_pair(a, sm_count)) return a.B.block == 1 ? launch_pair<T, 256, true>(a, sm_count, st, launches) : launch_pair<T, 256, false>(a, sm_count, st, launches);
+    const bool swapped = !(a.n <= 64 && a.m > a.n);        // lanes run along the rows of B, so that stores run along rows of D, unless B has few
+    const int64_t cols = swapped ? a.m : a.n;
+    if (cols <= 16) return launch_thin<T, 16>(a, swapped, sm_count, st, launches);
+    if (cols <= 32) return launch_thin<T, 32>(a, swapped, sm_count, st, launches);
+    if (cols <= 64) return launch_thin<T, 64>(a, swapped, sm_count, st, launches);
+    return launch_thin<T, 128>(a, swapped, sm_count, st, launches);
 }
 
 }  // namespace
