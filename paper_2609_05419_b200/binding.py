@@ -99,10 +99,25 @@ def _check(status, where):
         raise Gemm2mError(status, where)
 
 
+_raw_stream = None
+
+
+def _current_stream():
+    """Handle of torch's current stream.  torch's own look-up by device index takes 0.1 us, a Stream object 3 us."""
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+        if raw and device and torch.cuda.is_initialized():
+            _raw_stream = lambda: raw(device())
+        else:
+            return torch.cuda.current_stream().cuda_stream
+    return _raw_stream()
+
+
 def _stream_ptr(stream):
     if stream is None:
-        import torch
-        return ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+        return ctypes.c_void_p(_current_stream())
     if isinstance(stream, int):
         return ctypes.c_void_p(stream)
     return ctypes.c_void_p(stream.cuda_stream)
@@ -325,18 +340,13 @@ def dsyr2k2m(A, B, C, nmod=16, stream=None):
 
 # ---- layer operators: row-major matrices (torch's default order), column-major scales ----
 
-def _types():
-    import torch
-    return {torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2}
-
-
-_type_codes = None
+_type_codes = {}
 
 
 def _type_of(t, name, allowed):
-    global _type_codes
-    if _type_codes is None:
-        _type_codes = _types()
+    if not _type_codes:
+        import torch
+        _type_codes.update({torch.float32: F32, torch.float16: F16, torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3, torch.float8_e5m2: E5M2})
     code = _type_codes.get(t.dtype, -1)
     if code not in allowed:
         raise ValueError(f"{name}: unsupported type {t.dtype}")
@@ -345,24 +355,31 @@ def _type_of(t, name, allowed):
 
 def _rowmajor(t, name, allowed):
     """(pointer, type code, rows, cols, leading dimension) of a 2-D CUDA tensor with contiguous rows."""
-    if t.dim() != 2 or not t.is_cuda:
+    shape = t.shape
+    if len(shape) != 2 or not t.is_cuda:
         raise ValueError(f"{name}: need a 2-D CUDA tensor")
-    code = _type_of(t, name, allowed)
-    rows, cols = t.shape
-    if cols > 1 and t.stride(1) != 1:
+    rows, cols = shape
+    ld, step = t.stride()
+    if cols > 1 and step != 1:
         raise ValueError(f"{name}: need row-major storage (stride 1 along dim 1)")
-    ld = t.stride(0) if rows > 1 else -(-max(cols, 1) // 16) * 16
-    return t.data_ptr(), code, rows, cols, max(ld, 1)
+    if rows <= 1:                                   # the stride of a single row says nothing
+        ld = (max(cols, 1) + 15) // 16 * 16
+    return t.data_ptr(), _type_of(t, name, allowed), rows, cols, ld
 
 
 def _scales(t, name, rows, cols):
     """(pointer, leading dimension) of a column-major float32 scale matrix of the given shape."""
-    if not t.is_cuda or tuple(t.shape) != (rows, cols):
+    if t.shape != (rows, cols) or not t.is_cuda:
         raise ValueError(f"{name}: need a CUDA tensor of shape {(rows, cols)}")
     _type_of(t, name, (F32,))
-    if rows > 1 and t.stride(0) != 1:
+    step, ld = t.stride()
+    if rows > 1 and step != 1:
         raise ValueError(f"{name}: need column-major storage (stride 1 along dim 0), e.g. torch.empty(cols, rows).t()")
-    return t.data_ptr(), max(t.stride(1) if cols > 1 else rows, 1)
+    return t.data_ptr(), ld if cols > 1 and ld > 0 else max(rows, 1)
+
+
+def _stream_of(stream):
+    return _current_stream() if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
 
 
 _FP8 = (E4M3, E5M2)
@@ -399,7 +416,7 @@ def fp8_quantise(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None)
         form_t = (pq, ldq) + _scales(St, "St", blocks(cols, block_rows), blocks(rows, 128))
     if fmt is None:
         raise ValueError("need Q and S, or Qt and St")
-    _check(lib().gemm2m_fp8_quantise(rows, cols, px, tx, ldx, fmt, block_rows, *form, *form_t, _stream_ptr(stream)), "gemm2m_fp8_quantise")
+    _check(lib().gemm2m_fp8_quantise(rows, cols, px, tx, ldx, fmt, block_rows, *form, *form_t, _stream_of(stream)), "gemm2m_fp8_quantise")
 
 
 def fp8_gemm(A, SA, B, SB, D, C=None, a_block=1, b_block=128, stream=None):
@@ -420,7 +437,7 @@ def fp8_gemm(A, SA, B, SB, D, C=None, a_block=1, b_block=128, stream=None):
         if (mc, nc) != (m, n) or tc != td:
             raise ValueError("C: need the shape and type of D")
     _check(lib().gemm2m_fp8_gemm(m, n, k, pa, fa, lda, sa, ldsa, a_block, pb, fb, ldb, sb, ldsb, b_block, pc, ldc, pd, td, ldd,
-                                 _stream_ptr(stream)), "gemm2m_fp8_gemm")
+                                 _stream_of(stream)), "gemm2m_fp8_gemm")
 
 
 def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
@@ -442,7 +459,7 @@ def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
             raise ValueError("coeffs: need (a, b, c), or one such per step")
         co = ctypes.cast((ctypes.c_float * (3 * steps))(*[float(v) for r in rows for v in r]), ctypes.c_void_p)
     _check(lib().gemm2m_newton_schulz(batch, m, n, G.data_ptr(), tg, ld(G), stride(G), O.data_ptr(), ld(O), stride(O), steps, co, eps,
-                                      _stream_ptr(stream)), "gemm2m_newton_schulz")
+                                      _stream_of(stream)), "gemm2m_newton_schulz")
 
 
 def device_status(stream=None):

@@ -175,7 +175,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
                 for (int kb = 0; kb < p.kblocks; ++kb) {
                     if (!(ok = pipe.wait(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
                     const uint32_t dst = tiles_base + at.stage * cfg::kStageBytes;
-                    if (pipe.rank == 0) mbar_arrive_expect_tx(pipe.full + 8 * at.stage, 2 * cfg::kStageBytes);
+                    pipe.announce(at.stage, cfg::kStageBytes);
                     tma_load_2d_pair(dst, &map_a, leader_full + 8 * at.stage, kb * kGemmBK, row0);
                     tma_load_2d_pair(dst + kBM * kGemmBK, &map_b, leader_full + 8 * at.stage, kb * kGemmBK, col0);
                     ++fills;
@@ -305,7 +305,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         }
         if (!ok && lane == 0) pipe.tell_peer();
     }
-    pipe.close(cfg::kTmemCols, cfg::kStageBytes);
+    pipe.close(cfg::kTmemCols);
 }
 
 // rows x k bytes with leading dimension ld; box = 128 bytes of k x box_rows; what lies outside reads as zero.

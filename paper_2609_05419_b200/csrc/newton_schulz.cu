@@ -67,7 +67,7 @@ __global__ void __launch_bounds__(kRowThreads) norm_kernel(const T* G, int64_t m
 // X_0 in two planes.  The first block of each matrix also leaves |X_0|_F^2, the trace of the first step.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t m, int64_t n, int64_t ldg, int64_t stride_g, const double* parts,
-                                                            int nparts, float eps, __half* hi, __half* lo, int64_t ldx, float* trace) {
+                                                            int nparts, float eps, __half* hi, __half* lo, int64_t ldx, float* trace, uint32_t* phase_count) {
     __shared__ double scratch[kRowThreads / 32];
     wait_for_prior_kernels();
     const int64_t b = blockIdx.y;
@@ -76,8 +76,10 @@ __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t 
     sq = block_sum(sq, scratch);
     const double norm = sqrt(sq) + (double)eps;
     const double inv = norm > 0.0 ? (double)(1 << kXExp) / norm : 0.0;       // in 64 bits: 1 / norm of a tiny matrix overflows 32
-    if (blockIdx.x == 0)
-        if (threadIdx.x == 0) trace[b] = norm > 0.0 ? (float)(sq / (norm * norm)) : 0.f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        if (b == 0) *phase_count = 0;
+        trace[b] = norm > 0.0 ? (float)(sq / (norm * norm)) : 0.f;
+    }
     const T* g = G + b * stride_g;
     for (int64_t r = blockIdx.x; r < m; r += gridDim.x)
         for (int64_t c = threadIdx.x; c < n; c += kRowThreads) {
@@ -88,39 +90,59 @@ __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t 
         }
 }
 
-enum Mode { kGram, kPoly, kUpdate, kLast };
-
 constexpr int kBM = 128;                  // rows of the first operand per CTA
 constexpr int kBK = 64;                   // 16-bit entries of the inner dimension per stage: one 128-byte swizzle row
+constexpr int kStages = 6;
+constexpr int kBoxBytes = 64 * 128;       // a copy: 64 rows x 64 inner entries, in either order
+constexpr int kStageBytes = 4 * kBoxBytes;
 constexpr int kEpilogueWarps = 8;
 constexpr int kGemmThreads = 64 + 32 * kEpilogueWarps;
+constexpr int kMaxSteps = 64;
+constexpr size_t kPipeBytes = (PairPipe<kStages>::kBytes + 15) / 16 * 16;
+constexpr size_t kGemmSmem = (size_t)kStages * kStageBytes + 1024 + kPipeBytes + kEpilogueWarps * 4096;
 
-template <int BN>
-struct Cfg {
-    static constexpr int kHalfRows = BN / 2;              // rows of the second operand per CTA
-    static constexpr int kStageBytes = (kBM + kHalfRows) * 128;
-    static constexpr int kStages = BN == 256 ? 6 : 8;
-    static constexpr int kCols = BN / 2;                  // columns per epilogue warp
-    static constexpr uint32_t kTmemCols = 2 * BN;
-    static constexpr size_t kPipeBytes = (PairPipe<kStages>::kBytes + 15) / 16 * 16;
-    static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + kPipeBytes + kEpilogueWarps * 4096;
-};
+enum Mode { kGram, kPoly, kUpdate, kLast };
 
-struct NsGemm {
-    int mode;
-    int M, N, kblocks, batch;
-    int tiles_r, tiles_c, tiles;                          // row and column tiles of a matrix, and how many of them are computed
-    float a, b, c, short_side;
-    const float* trace; int64_t trace_parts;              // kGram: partial sums of |X|_F^2, or null for g = 0
-    float* shift;                                         // g of every matrix: written by kGram, read by the others
-    __half* out; int64_t ldo, stride_o;                   // kGram, kPoly: symmetric square, times 2^kSExp
-    const __half* gram;                                   // kPoly: A', laid out as out
-    const __half *hi, *lo; __half *hi_out, *lo_out; float* trace_out; int64_t ldx, stride_x;      // kUpdate, kLast
-    __nv_bfloat16* last; int64_t ld_last, stride_last; int last_vec;                              // kLast
-    uint32_t idesc;
+struct NsParams {
+    CUtensorMap x[2], gram_map, poly_map;                 // the iterate's hi planes, A' and the polynomial
+    int m, n, s, batch, steps;
+    int wide_square, wide_update;                         // tiles of 256 columns, otherwise of 128
+    float coeffs[3 * kMaxSteps];
+    float* trace[2]; int64_t trace_parts;           // partial sums of |X|_F^2 (one in front of the first step)
+    float* shift;                                         // g of every matrix: written with A', read by the rest of the step
+    __half *gram, *poly; int64_t lds;                     // s x s, times 2^kSExp
+    __half *hi[2], *lo[2]; int64_t ldx;                   // m x n
+    __nv_bfloat16* out; int64_t ld_out, stride_out; int out_vec;
+    uint32_t* phase_count;                                // CTAs that have finished a phase, over all phases so far
     int* dev_status;
     unsigned long long wait_ns;
 };
+
+// One product of a step: kind 0 A' = X X^T - g I, 1 P = (b + 2 c g) A' + c A'^2, 2 X <- (a + b g + c g^2) X + P X.
+struct Phase {
+    int mode, M, N, kblocks, bn, tiles_r, tiles_c, tiles;
+    bool turned_a, turned_b;
+    const CUtensorMap *map_a, *map_b;
+};
+__host__ __device__ inline int square_tiles(int tiles_r, int tiles_c, int per) { return per * tiles_r * (tiles_r - 1) / 2 + tiles_c; }
+__device__ __forceinline__ Phase phase_at(const NsParams& p, int step, int kind) {
+    Phase q;
+    const bool tall = p.m > p.n;
+    q.mode = kind == 0 ? kGram : kind == 1 ? kPoly : step + 1 == p.steps ? kLast : kUpdate;
+    q.bn = (kind == 2 ? p.wide_update : p.wide_square) ? 256 : 128;
+    q.M = kind == 2 ? p.m : p.s;
+    q.N = kind == 2 ? p.n : p.s;
+    q.kblocks = ((kind == 0 ? (tall ? p.m : p.n) : p.s) + kBK - 1) / kBK;
+    q.tiles_r = (q.M + 2 * kBM - 1) / (2 * kBM);
+    q.tiles_c = (q.N + q.bn - 1) / q.bn;
+    q.tiles = kind == 2 ? q.tiles_r * q.tiles_c : square_tiles(q.tiles_r, q.tiles_c, 2 * kBM / q.bn);
+    q.turned_a = kind == 0 && tall;                       // X^T X contracts along the rows of X
+    q.turned_b = (kind == 0 && tall) || (kind == 2 && !tall);
+    const CUtensorMap* x = &p.x[step & 1];
+    q.map_a = kind == 0 ? x : kind == 1 ? &p.gram_map : tall ? x : &p.poly_map;
+    q.map_b = kind == 0 ? x : kind == 1 ? &p.gram_map : tall ? &p.poly_map : x;
+    return q;
+}
 
 __device__ __forceinline__ void umma_f16_pair(uint32_t d_tmem, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
     asm volatile(
@@ -131,7 +153,7 @@ __device__ __forceinline__ void umma_f16_pair(uint32_t d_tmem, uint64_t adesc, u
         : "memory");
 }
 // Instruction descriptor of kind::f16: half-precision operands, 32-bit accumulator; turned = the operand's rows are contiguous.
-uint32_t make_idesc_f16(bool turned_a, bool turned_b, int M, int N) {
+__device__ __forceinline__ uint32_t make_idesc_f16(bool turned_a, bool turned_b, int M, int N) {
     return (1u << 4) | ((uint32_t)turned_a << 15) | ((uint32_t)turned_b << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
 // Shared-memory descriptor of an operand whose rows are contiguous (128-byte swizzle): pieces of 64 rows x 8 inner entries are
@@ -145,162 +167,214 @@ __device__ __forceinline__ uint64_t make_smem_desc_turned(uint32_t addr) {
     d |= (uint64_t)2 << 61;
     return d;
 }
-// This CTA's `rows` rows from row0 and one stage of the inner dimension.
-template <bool TURNED>
-__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* map, uint32_t bar, int kb, int row0, int rows, int b) {
-    if (!TURNED) {
-        tma_load_3d_pair(dst, map, bar, kb * kBK, row0, b);
-    } else {
-        for (int r = 0; r < rows; r += 64) tma_load_3d_pair(dst + r * 128, map, bar, row0 + r, kb * kBK, b);
+// `rows` rows from row0 and one stage of the inner dimension, 64 rows per copy.
+__device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* map, uint32_t bar, bool turned, int kb, int row0, int rows, int b) {
+    for (int r = 0; r < rows; r += 64, dst += kBoxBytes) {
+        if (turned) tma_load_3d_pair(dst, map, bar, row0 + r, kb * kBK, b);
+        else tma_load_3d_pair(dst, map, bar, kb * kBK, row0 + r, b);
     }
 }
 
-// Tile `t` of a launch: matrix, row tile, column tile.  A symmetric square has the tiles up to and including the diagonal block's:
-// row tile r has q (r + 1) of them, q = column tiles per row tile.
-template <int BN>
-__device__ __forceinline__ void tile_at(const NsGemm& p, int t, int* b, int* tr, int* tc) {
-    constexpr int q = 2 * kBM / BN;
-    *b = t / p.tiles;
-    const int i = t - *b * p.tiles;
-    if (p.mode == kGram || p.mode == kPoly) {
-        int r = (int)((sqrtf(8.f * (float)(i / q) + 1.f) - 1.f) * 0.5f);
-        while (q * r * (r + 1) / 2 > i) --r;              // (rounding of the root)
-        while (q * (r + 1) * (r + 2) / 2 <= i) ++r;
+// Tile `t` of a phase: matrix, row tile, column tile.  A symmetric square has the tiles up to and including the diagonal block's:
+// row tile r has per (r + 1) of them, per = column tiles per row tile.
+__device__ __forceinline__ void tile_at(const Phase& q, int t, int* b, int* tr, int* tc) {
+    *b = t / q.tiles;
+    const int i = t - *b * q.tiles;
+    if (q.mode == kGram || q.mode == kPoly) {
+        const int per = 2 * kBM / q.bn;
+        int r = (int)((sqrtf(8.f * (float)(i / per) + 1.f) - 1.f) * 0.5f);
+        while (per * r * (r + 1) / 2 > i) --r;            // (rounding of the root)
+        while (per * (r + 1) * (r + 2) / 2 <= i) ++r;
         *tr = r;
-        *tc = i - q * r * (r + 1) / 2;
+        *tc = i - per * r * (r + 1) / 2;
     } else {                                              // bands of 8 row tiles, column by column: operands are shared through L2
-        const int band = i / (8 * p.tiles_c), in_band = i - band * 8 * p.tiles_c, rows = min(8, p.tiles_r - 8 * band);
+        const int band = i / (8 * q.tiles_c), in_band = i - band * 8 * q.tiles_c, rows = min(8, q.tiles_r - 8 * band);
         *tc = in_band / rows;
         *tr = 8 * band + in_band - *tc * rows;
     }
 }
 
+// Waits (bounded) until `target` CTAs in all have finished their phases, and sees what they wrote.
+__device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t target, volatile int* abort_flag) {
+    const unsigned long long t0 = global_timer_ns();
+    for (uint32_t spins = 1;; ++spins) {
+        uint32_t seen;
+        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(p.phase_count) : "memory");
+        if (seen >= target) break;
+        if ((spins & 63u) == 0) {
+            if (*abort_flag) return false;
+            if (global_timer_ns() - t0 > p.wait_ns) {
+                *abort_flag = 1;
+                atomicCAS(p.dev_status, kDevOk, kDevTimeoutProducer);
+                return false;
+            }
+        }
+    }
+    return true;
+}
+
 struct alignas(8) Half4 { __half h[4]; };
 struct alignas(8) Bf4 { __nv_bfloat16 h[4]; };
 
-// 32 columns of 32 rows (v: this lane's row), at (row0, col0) of matrix b.  The values turn in shared memory (16-byte pieces XORed
-// with the row) so that eight lanes have four columns each of one row, and what is read and written beside them is whole
-// sectors.  Planes have padded rows, so that four columns can always be touched; what lies in the padding is not used.
-__device__ __forceinline__ float finish_block(const NsGemm& p, const uint32_t (&v)[32], uint32_t turn, int b, int row0, int col0, bool mirror, float g) {
-    const int lane = threadIdx.x & 31, piece = lane & 7;
-    __syncwarp();
-#pragma unroll
-    for (int q = 0; q < 8; ++q)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (uint32_t)(lane * 128 + ((q ^ (lane & 7)) << 4))), "r"(v[4 * q]), "r"(v[4 * q + 1]),
-                     "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
-    __syncwarp();
+// 32 columns of 32 rows (v: this lane's row) of a phase's accumulator, at (row0, col0) of matrix b.  The values turn in shared memory
+// (`turn`, 4 KB per warp; 16-byte pieces XORed with the row), so that eight lanes have four columns each of one row and what is
+// read and written beside them is whole sectors.  What is read is asked for first, all at once: the stores might alias it, so
+// that nothing would move ahead of them by itself, and a round trip per row costs ten times the arithmetic.  Planes have
+// padded rows, so that four columns can always be touched; what lies in the padding is not used.
+__device__ __forceinline__ float finish_block(const NsParams& p, const Phase& q, int step, const uint32_t (&v)[32], uint32_t turn, int b, int row0, int col0, bool mirror, float g) {
+    const int lane = threadIdx.x & 31, piece = lane & 7, r0 = lane >> 3;
     const int col = col0 + piece * 4;
-    const int rows = col < p.N ? min(32, p.M - row0) : 0;
-    const float gram_scale = exp2f(kSExp - 2 * kXExp), g_scaled = g * exp2f(kSExp);
-    const float poly_lin = p.b + 2.f * p.c * g, poly_sq = p.c * exp2f(-kSExp);
-    const float x_lin = p.a + g * (p.b + p.c * g);
-    float sum = 0.f;
-#pragma unroll 2
-    for (int r = lane >> 3; r < rows; r += 4) {
-        float x[4];
-        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
+    const int rows = col < q.N ? min(32, q.M - row0) : 0;
+    const bool square = q.mode == kGram || q.mode == kPoly;
+    const int64_t ld = square ? p.lds : p.ldx;
+    const int64_t at0 = (int64_t)b * (square ? (int64_t)p.s * p.lds : (int64_t)p.m * p.ldx) + (int64_t)(row0 + r0) * ld + col;
+    Half4 in[8], in_lo[8];
+    if (q.mode != kGram) {
+        const __half* src = q.mode == kPoly ? p.gram : p.hi[step & 1];
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r0 + 4 * i < rows) in[i] = *reinterpret_cast<const Half4*>(src + at0 + 4 * i * ld);
+    }
+    if (!square) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r0 + 4 * i < rows) in_lo[i] = *reinterpret_cast<const Half4*>(p.lo[step & 1] + at0 + 4 * i * ld);
+    }
+    __syncwarp();                                         // the previous block has been read
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) << 4))), "r"(v[4 * i]), "r"(v[4 * i + 1]),
+                     "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
+    __syncwarp();
+    float x[8][4];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = r0 + 4 * i;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[i][0]), "=f"(x[i][1]), "=f"(x[i][2]), "=f"(x[i][3])
                      : "r"(turn + (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4))) : "memory");
-        const int row = row0 + r;
-        if (p.mode == kGram || p.mode == kPoly) {
-            const int64_t at = (int64_t)b * p.stride_o + (int64_t)row * p.ldo + col;
+    }
+    const float ca = p.coeffs[3 * step], cb = p.coeffs[3 * step + 1], cc = p.coeffs[3 * step + 2];
+    float sum = 0.f;
+    if (square) {
+        __half* out = q.mode == kGram ? p.gram : p.poly;
+        const float lin = cb + 2.f * cc * g, sq = q.mode == kGram ? (float)(1.0 / (1 << (2 * kXExp - kSExp))) : cc * (float)(1.0 / (1 << kSExp));
+        const float diagonal = g * (float)(1 << kSExp);
+        __syncwarp();                                     // x has been read: the block's results take its place, 72 bytes per row
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + 4 * i;
             Half4 o;
-            if (p.mode == kGram) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o.h[j] = __float2half_rn(x[j] * gram_scale - (row == col + j ? g_scaled : 0.f));
-            } else {
-                const Half4 s = *reinterpret_cast<const Half4*>(p.gram + at);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) o.h[j] = __float2half_rn(poly_lin * __half2float(s.h[j]) + poly_sq * x[j]);
+            for (int j = 0; j < 4; ++j)
+                o.h[j] = __float2half_rn(q.mode == kGram ? x[i][j] * sq - (row0 + r == col + j ? diagonal : 0.f) : lin * __half2float(in[i].h[j]) + sq * x[i][j]);
+            if (r < rows) *reinterpret_cast<Half4*>(out + at0 + 4 * i * ld) = o;
+            if (mirror) {
+                const uint2 w = *reinterpret_cast<const uint2*>(&o);
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(turn + (uint32_t)(r * 72 + piece * 8)), "r"(w.x), "r"(w.y) : "memory");
             }
-            *reinterpret_cast<Half4*>(p.out + at) = o;
-        } else {
-            const int64_t at = (int64_t)b * p.stride_x + (int64_t)row * p.ldx + col;
-            const Half4 h = *reinterpret_cast<const Half4*>(p.hi + at), l = *reinterpret_cast<const Half4*>(p.lo + at);
+        }
+        if (mirror) {                                     // the same numbers at (column, row): two rows per lane, 16 lanes along a column
+            __syncwarp();
+            const int r = (lane & 15) * 2;
+            __half* to = out + (int64_t)b * p.s * p.lds + row0 + r;
+            const int have = q.M - row0 - r;              // (the second row may lie in the padding)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int c = 2 * i + (lane >> 4);
+                uint16_t lo, hi;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(lo) : "r"(turn + (uint32_t)(r * 72 + c * 2)) : "memory");
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(hi) : "r"(turn + (uint32_t)(r * 72 + 72 + c * 2)) : "memory");
+                if (have > 0 && col0 + c < q.N) *reinterpret_cast<uint32_t*>(to + (int64_t)(col0 + c) * p.lds) = (uint32_t)lo | ((uint32_t)hi << 16);
+            }
+        }
+    } else {
+        const float lin = ca + g * (cb + cc * g);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + 4 * i;
+            if (r >= rows) continue;
             float w[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = x_lin * (__half2float(h.h[j]) + __half2float(l.h[j]) * exp2f(-kLoExp)) + x[j] * exp2f(-kSExp);
-            if (p.mode == kUpdate) {
+            for (int j = 0; j < 4; ++j)
+                w[j] = lin * (__half2float(in[i].h[j]) + __half2float(in_lo[i].h[j]) * (float)(1.0 / (1 << kLoExp))) + x[i][j] * (float)(1.0 / (1 << kSExp));
+            if (q.mode == kUpdate) {
                 Half4 ho, lo;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     ho.h[j] = __float2half_rn(w[j]);
-                    lo.h[j] = __float2half_rn((w[j] - __half2float(ho.h[j])) * exp2f(kLoExp));
-                    if (col + j < p.N) sum += w[j] * w[j];
+                    lo.h[j] = __float2half_rn((w[j] - __half2float(ho.h[j])) * (float)(1 << kLoExp));
+                    if (col + j < q.N) sum += w[j] * w[j];
                 }
-                *reinterpret_cast<Half4*>(p.hi_out + at) = ho;
-                *reinterpret_cast<Half4*>(p.lo_out + at) = lo;
+                *reinterpret_cast<Half4*>(p.hi[(step + 1) & 1] + at0 + 4 * i * ld) = ho;
+                *reinterpret_cast<Half4*>(p.lo[(step + 1) & 1] + at0 + 4 * i * ld) = lo;
             } else {
-                __nv_bfloat16* d = p.last + (int64_t)b * p.stride_last + (int64_t)row * p.ld_last + col;
+                __nv_bfloat16* d = p.out + (int64_t)b * p.stride_out + (int64_t)(row0 + r) * p.ld_out + col;
                 Bf4 o;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o.h[j] = __float2bfloat16_rn(w[j] * exp2f(-kXExp));
-                if (p.last_vec && col + 4 <= p.N) *reinterpret_cast<Bf4*>(d) = o;
+                for (int j = 0; j < 4; ++j) o.h[j] = __float2bfloat16_rn(w[j] * (float)(1.0 / (1 << kXExp)));
+                if (p.out_vec && col + 4 <= q.N) *reinterpret_cast<Bf4*>(d) = o;
                 else
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (col + j < p.N) d[j] = o.h[j];
+                        if (col + j < q.N) d[j] = o.h[j];
             }
-        }
-    }
-    if (mirror && row0 + lane < p.M) {                    // the same numbers at (column, row): 32 lanes are 32 neighbours there
-        const int64_t base = (int64_t)b * p.stride_o + row0 + lane;
-#pragma unroll
-        for (int c = 0; c < 32; ++c) {
-            if (col0 + c >= p.N) break;
-            const int64_t at = base + (int64_t)(col0 + c) * p.ldo;
-            const float x = __uint_as_float(v[c]);
-            p.out[at] = __float2half_rn(p.mode == kGram ? x * gram_scale : poly_lin * __half2float(p.gram[at]) + poly_sq * x);
         }
     }
     return sum;
 }
 
-// g = trace(A) / s of matrix b, by one warp, from the partial sums in their order.
-__device__ __forceinline__ float shift_of(const NsGemm& p, int b) {
-    if (p.mode != kGram) return p.shift[b];
-    if (!p.trace) return 0.f;
+// g of matrix b, by one warp: with A', trace(A) / s from the partial sums in their order (in the last two steps), or zero.
+__device__ __forceinline__ float shift_of(const NsParams& p, int step, int mode, int b) {
+    if (mode != kGram) return p.shift[b];
+    if (step + 2 < p.steps) return 0.f;
+    const int64_t parts = step == 0 ? 1 : p.trace_parts;
     double t = 0.0;
-    for (int64_t i = threadIdx.x & 31; i < p.trace_parts; i += 32) t += (double)p.trace[(int64_t)b * p.trace_parts + i];
+    for (int64_t i = threadIdx.x & 31; i < parts; i += 32) t += (double)p.trace[step & 1][b * parts + i];
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-    return (float)(t / (double)p.short_side);
+    return (float)(t / (double)p.s);
 }
 
-template <int BN, bool TURNED_A, bool TURNED_B>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1)
-ns_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ NsGemm p) {
-    using cfg = Cfg<BN>;
-    constexpr int STAGES = cfg::kStages;
+// All steps in one launch.  The CTA pairs share a phase's tiles; a phase begins when every CTA has finished the one before (a counter
+// in the workspace, which every CTA adds to; the launch is cooperative).  Without launches in between, what is left between
+// two phases is the counter's round trip and the filling of the pipeline.
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_steps_kernel(const __grid_constant__ NsParams p) {
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
     const uint32_t tiles_base = (raw + 1023u) & ~1023u;
-    unsigned char* behind = smem_raw + (tiles_base - raw) + (size_t)STAGES * cfg::kStageBytes;
-    PairPipe<STAGES> pipe;
-    pipe.open(behind, kEpilogueWarps, 1, cfg::kTmemCols, p.dev_status, p.wait_ns);
-    wait_for_prior_kernels();
+    unsigned char* behind = smem_raw + (tiles_base - raw) + (size_t)kStages * kStageBytes;
+    PairPipe<kStages> pipe;
+    pipe.open(behind, kEpilogueWarps, 1, 512, p.dev_status, p.wait_ns);
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
-    const int total_tiles = p.tiles * p.batch;
+    const int phases = 3 * p.steps;
 
     if (warp == 0) {
         if (lane == 0) {                                  // copies, both CTAs
             const uint32_t leader_full = map_to_cta(pipe.full, 0);
-            RingPos<STAGES> at;
+            RingPos<kStages> at;
             uint32_t fills = 0;
             bool ok = true;
-            for (int tile = pair; ok && tile < total_tiles; tile += npairs) {
-                int b, tr, tc;
-                tile_at<BN>(p, tile, &b, &tr, &tc);
-                const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM, col0 = tc * BN + (int)pipe.rank * cfg::kHalfRows;
-                for (int kb = 0; kb < p.kblocks; ++kb) {
-                    if (!(ok = pipe.wait(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
-                    const uint32_t dst = tiles_base + at.stage * cfg::kStageBytes;
-                    if (pipe.rank == 0) mbar_arrive_expect_tx(pipe.full + 8 * at.stage, 2 * cfg::kStageBytes);
-                    load_operand<TURNED_A>(dst, &map_a, leader_full + 8 * at.stage, kb, row0, kBM, b);
-                    load_operand<TURNED_B>(dst + kBM * 128, &map_b, leader_full + 8 * at.stage, kb, col0, cfg::kHalfRows, b);
-                    ++fills;
-                    at.next();
+            for (int ph = 0; ok && ph < phases; ++ph) {
+                const Phase q = phase_at(p, ph / 3, ph % 3);
+                if (pair >= q.tiles * p.batch) continue;
+                if (!(ok = wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag))) break;
+                asm volatile("fence.proxy.async;" ::: "memory");       // the other CTAs' stores, then this thread's bulk copies
+                const int half_rows = q.bn / 2;
+                for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs) {
+                    int b, tr, tc;
+                    tile_at(q, tile, &b, &tr, &tc);
+                    const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM, col0 = tc * q.bn + (int)pipe.rank * half_rows;
+                    for (int kb = 0; kb < q.kblocks; ++kb) {
+                        if (!(ok = pipe.wait(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
+                        const uint32_t dst = tiles_base + at.stage * kStageBytes;
+                        pipe.announce(at.stage, (uint32_t)(kBM + half_rows) * 128u);
+                        load_operand(dst, q.map_a, leader_full + 8 * at.stage, q.turned_a, kb, row0, kBM, b);
+                        load_operand(dst + kBM * 128, q.map_b, leader_full + 8 * at.stage, q.turned_b, kb, col0, half_rows, b);
+                        ++fills;
+                        at.next();
+                    }
                 }
             }
             *pipe.fills_issued = fills;
@@ -308,76 +382,95 @@ ns_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_cons
         }
     } else if (warp == 1) {
         if (lane == 0 && pipe.rank == 0) {                // MMAs, leader
-            RingPos<STAGES> at;
+            RingPos<kStages> at;
             uint32_t it = 0;                              // tile counter: buffer it & 1, its use number it >> 1
             bool ok = true;
-            for (int tile = pair; ok && tile < total_tiles; tile += npairs, ++it) {
-                const uint32_t buf = it & 1u;
-                if (!(ok = pipe.wait(pipe.tempty + 8 * buf, ((it >> 1) & 1u) ^ 1u, kDevTimeoutMma))) break;
-                for (int kb = 0; kb < p.kblocks; ++kb) {
-                    if (!(ok = pipe.wait(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
-                    tcgen05_fence_after();
-                    const uint32_t a_addr = tiles_base + at.stage * cfg::kStageBytes, b_addr = a_addr + kBM * 128;
-                    const uint64_t adesc = TURNED_A ? make_smem_desc_turned(a_addr) : make_smem_desc(a_addr);
-                    const uint64_t bdesc = TURNED_B ? make_smem_desc_turned(b_addr) : make_smem_desc(b_addr);
-                    // 16 inner entries: 32 bytes along a swizzle row, or 16 rows of 128 bytes
+            for (int ph = 0; ok && ph < phases; ++ph) {
+                const Phase q = phase_at(p, ph / 3, ph % 3);
+                const uint32_t idesc = make_idesc_f16(q.turned_a, q.turned_b, 2 * kBM, q.bn);
+                // 16 inner entries: 32 bytes along a swizzle row, or 16 rows of 128 bytes
+                const uint64_t step_a = q.turned_a ? 128 : 2, step_b = q.turned_b ? 128 : 2;
+                for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs, ++it) {
+                    const uint32_t buf = it & 1u;
+                    if (!(ok = pipe.wait(pipe.tempty + 8 * buf, ((it >> 1) & 1u) ^ 1u, kDevTimeoutMma))) break;
+                    for (int kb = 0; kb < q.kblocks; ++kb) {
+                        if (!(ok = pipe.wait(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
+                        tcgen05_fence_after();
+                        const uint32_t a_addr = tiles_base + at.stage * kStageBytes, b_addr = a_addr + kBM * 128;
+                        const uint64_t adesc = q.turned_a ? make_smem_desc_turned(a_addr) : make_smem_desc(a_addr);
+                        const uint64_t bdesc = q.turned_b ? make_smem_desc_turned(b_addr) : make_smem_desc(b_addr);
 #pragma unroll
-                    for (int k4 = 0; k4 < 4; ++k4)
-                        umma_f16_pair(pipe.tmem + buf * BN, adesc + (uint64_t)(k4 * (TURNED_A ? 128 : 2)), bdesc + (uint64_t)(k4 * (TURNED_B ? 128 : 2)), p.idesc,
-                                      (uint32_t)((kb | k4) != 0));
-                    umma_commit_pair(pipe.empty + 8 * at.stage, 3);
-                    at.next();
+                        for (int k4 = 0; k4 < 4; ++k4)
+                            umma_f16_pair(pipe.tmem + buf * 256, adesc + k4 * step_a, bdesc + k4 * step_b, idesc, (uint32_t)((kb | k4) != 0));
+                        umma_commit_pair(pipe.empty + 8 * at.stage, 3);
+                        at.next();
+                    }
+                    if (ok) umma_commit_pair(pipe.tfull + 8 * buf, 3);
                 }
-                if (ok) umma_commit_pair(pipe.tfull + 8 * buf, 3);
             }
             if (!ok) pipe.tell_peer();
         }
     } else {
         // Epilogue: warp w reads lanes 32 (w & 3) .. of TMEM (rows), columns of half (w - 2) / 4.
         const int half = (warp - 2) >> 2, quarter = warp & 3;
-        constexpr int NC = cfg::kCols;
-        const uint32_t turn = smem_u32(behind) + (uint32_t)cfg::kPipeBytes + (uint32_t)(warp - 2) * 4096;
+        const uint32_t turn = smem_u32(behind) + (uint32_t)kPipeBytes + (uint32_t)(warp - 2) * 4096;
         const uint32_t leader_tempty = map_to_cta(pipe.tempty, 0);
         uint32_t it = 0;
-        int shift_for = -1;
-        float g = 0.f;
         bool ok = true;
-        for (int tile = pair; ok && tile < total_tiles; tile += npairs, ++it) {
-            int b, tr, tc;
-            tile_at<BN>(p, tile, &b, &tr, &tc);
-            const uint32_t buf = it & 1u;
-            if (b != shift_for) {
-                g = shift_of(p, b);
-                shift_for = b;
+        for (int ph = 0; ph < phases; ++ph) {
+            const int step = ph / 3;
+            const Phase q = phase_at(p, step, ph % 3);
+            if (ok) {                                     // (without tiles too: a CTA is counted for a phase only after the phases before it)
+                ok = lane != 0 || wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag);
+                ok = __all_sync(0xffffffffu, ok);
             }
-            if (p.mode == kGram && tr == 0 && tc == 0 && pipe.rank == 0 && warp == 2 && lane == 0) p.shift[b] = g;
-            ok = __all_sync(0xffffffffu, pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue));
-            if (!ok) break;
-            tcgen05_fence_after();
-            const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM + quarter * 32, col0 = tc * BN + half * NC;
-            const bool mirror = (p.mode == kGram || p.mode == kPoly) && (tc + 1) * BN <= tr * 2 * kBM;      // below the diagonal block
-            const uint32_t taddr = pipe.tmem + ((uint32_t)(quarter * 32) << 16) + buf * BN + (uint32_t)(half * NC);
-            float sum = 0.f;
+            __threadfence();                              // lane 0 has seen the other CTAs' stores; the other lanes read them too
+            const int nc = q.bn / 2;
+            int shift_for = -1;
+            float g = 0.f;
+            for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs, ++it) {
+                int b, tr, tc;
+                tile_at(q, tile, &b, &tr, &tc);
+                const uint32_t buf = it & 1u;
+                if (b != shift_for) {
+                    g = shift_of(p, step, q.mode, b);
+                    shift_for = b;
+                }
+                if (q.mode == kGram && tr == 0 && tc == 0 && pipe.rank == 0 && warp == 2 && lane == 0) p.shift[b] = g;
+                ok = __all_sync(0xffffffffu, pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue));
+                if (!ok) break;
+                tcgen05_fence_after();
+                const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM + quarter * 32, col0 = tc * q.bn + half * nc;
+                const bool mirror = (q.mode == kGram || q.mode == kPoly) && (tc + 1) * q.bn <= tr * 2 * kBM;      // below the diagonal block
+                const uint32_t taddr = pipe.tmem + ((uint32_t)(quarter * 32) << 16) + buf * 256 + (uint32_t)(half * nc);
+                float sum = 0.f;
 #pragma unroll 1
-            for (int c = 0; c < NC; c += 32) {
-                uint32_t v[32];
-                tmem_ld32(taddr + c, v);
-                tmem_ld_wait();
-                if (c + 32 == NC) pipe.release_at(leader_tempty + 8 * buf);
-                if (row0 < p.M && col0 + c < p.N) sum += finish_block(p, v, turn, b, row0, col0 + c, mirror, g);
-                // one partial sum per 32 rows and 64 columns, whatever the tile width: results do not depend on that choice
-                if (p.mode == kUpdate && (c & 32)) {
+                for (int c = 0; c < nc; c += 32) {
+                    uint32_t v[32];
+                    tmem_ld32(taddr + c, v);
+                    tmem_ld_wait();
+                    if (c + 32 == nc) pipe.release_at(leader_tempty + 8 * buf);
+                    if (row0 < q.M && col0 + c < q.N) sum += finish_block(p, q, step, v, turn, b, row0, col0 + c, mirror, g);
+                    // one partial sum per 32 rows and 64 columns, whatever the tile width: results do not depend on that choice
+                    if (q.mode == kUpdate && (c & 32)) {
 #pragma unroll
-                    for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                    const int part_row = row0 >> 5, part_col = (col0 + c) >> 6, cols = (p.N + 63) >> 6;
-                    if (lane == 0 && row0 < p.M && part_col < cols) p.trace_out[(int64_t)b * p.trace_parts + (int64_t)part_row * cols + part_col] = sum * exp2f(-2 * kXExp);
-                    sum = 0.f;
+                        for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
+                        const int part_row = row0 >> 5, part_col = (col0 + c) >> 6, cols = (q.N + 63) >> 6;
+                        if (lane == 0 && row0 < q.M && part_col < cols)
+                            p.trace[(step + 1) & 1][(int64_t)b * p.trace_parts + (int64_t)part_row * cols + part_col] = sum * exp2f(-2 * kXExp);
+                        sum = 0.f;
+                    }
                 }
             }
+            // (always, also after a give-up: nobody waits for this CTA for longer than for the others)
+            asm volatile("fence.proxy.async;" ::: "memory");
+            __threadfence();
+            asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
+            if (warp == 2 && lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.phase_count) : "memory");
         }
         if (!ok && lane == 0) pipe.tell_peer();
     }
-    pipe.close(cfg::kTmemCols, cfg::kStageBytes);
+    pipe.close(512);
 }
 
 inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
@@ -385,52 +478,16 @@ inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 // Partial sums of the trace that an update of m x n matrices leaves.
 inline int64_t update_trace_parts(int64_t m, int64_t n) { return (m + 31) / 32 * ((n + 63) / 64); }
 
-// One operand of a product, rows x inner entries of `batch` matrices `stride` apart: element (r, k) at r ld + k, or at k ld + r if turned.
-struct Operand { const __half* p; int64_t rows, inner, ld, stride; bool turned; };
-
-bool make_half_map(CUtensorMap* map, const Operand& o, int64_t batch, int box_rows) {
+// rows x cols of `batch` matrices, padded rows; box = 64 x 64 of one matrix, which serves as 64 rows x 64 inner entries in either order.
+bool make_half_map(CUtensorMap* map, const __half* base, int64_t rows, int64_t cols, int64_t ld, int64_t batch) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
-    const cuuint64_t dims[3] = {(cuuint64_t)(o.turned ? o.rows : o.inner), (cuuint64_t)(o.turned ? o.inner : o.rows), (cuuint64_t)batch};
-    const cuuint64_t strides[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)o.stride * 2};
-    const cuuint32_t box[3] = {64, (cuuint32_t)(o.turned ? kBK : box_rows), 1};
+    const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
+    const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)(rows * ld) * 2};
+    const cuuint32_t box[3] = {64, 64, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
-    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(o.p), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
-}
-
-template <int BN, bool TURNED_A, bool TURNED_B>
-cudaError_t launch_tiles(NsGemm& q, const Operand& A, const Operand& B, int sm_count, cudaStream_t st, int* launches) {
-    using cfg = Cfg<BN>;
-    static int pairs_dev[kMaxDevices] = {};
-    int& max_pairs = pairs_dev[current_device_slot()];
-    if (!max_pairs) {
-        int pairs = 0;
-        cudaError_t err = resident_pairs(ns_gemm_pair_kernel<BN, TURNED_A, TURNED_B>, kGemmThreads, cfg::kSmem, sm_count, &pairs);
-        if (err != cudaSuccess) return err;
-        max_pairs = pairs;
-    }
-    CUtensorMap map_a, map_b;
-    if (!make_half_map(&map_a, A, q.batch, kBM) || !make_half_map(&map_b, B, q.batch, cfg::kHalfRows)) return cudaErrorInvalidValue;
-    q.tiles_r = (q.M + 2 * kBM - 1) / (2 * kBM);
-    q.tiles_c = (q.N + BN - 1) / BN;
-    constexpr int per = 2 * kBM / BN;
-    // (a square's last row tile has all of its column tiles, the others those up to the diagonal block)
-    const int64_t all = q.mode == kGram || q.mode == kPoly ? (int64_t)per * q.tiles_r * (q.tiles_r - 1) / 2 + q.tiles_c : (int64_t)q.tiles_r * q.tiles_c;
-    if (all * q.batch > INT32_MAX / 4) return cudaErrorInvalidValue;
-    q.tiles = (int)all;
-    q.idesc = make_idesc_f16(TURNED_A, TURNED_B, 2 * kBM, BN);
-    const int pairs = (int)(all * q.batch < max_pairs ? all * q.batch : max_pairs);
-    cudaError_t err = launch_chained(ns_gemm_pair_kernel<BN, TURNED_A, TURNED_B>, dim3(2 * pairs), dim3(kGemmThreads), cfg::kSmem, st, map_a, map_b, q);
-    if (err == cudaSuccess) ++*launches;
-    return err;
-}
-
-template <int BN>
-cudaError_t launch_width(NsGemm& q, const Operand& A, const Operand& B, int sm_count, cudaStream_t st, int* launches) {
-    if (A.turned) return launch_tiles<BN, true, true>(q, A, B, sm_count, st, launches);        // X^T X
-    if (B.turned) return launch_tiles<BN, false, true>(q, A, B, sm_count, st, launches);       // P X
-    return launch_tiles<BN, false, false>(q, A, B, sm_count, st, launches);
 }
 
 template <typename T>
@@ -442,7 +499,7 @@ cudaError_t launch_start(const NewtonSchulzArgs& a, cudaStream_t st, int* launch
     if (err != cudaSuccess) return err;
     err = launch_chained(start_kernel<T>, dim3((unsigned)(a.m < 1024 ? a.m : 1024), (unsigned)a.batch), dim3(kRowThreads), 0, st, (const T*)a.G, a.m, a.n, a.ldg,
                          a.stride_g, parts, blocks, a.eps, (__half*)(a.ws + l.off_hi[0]), (__half*)(a.ws + l.off_lo[0]), l.ldx,
-                         (float*)(a.ws + l.off_trace[0]));
+                         (float*)(a.ws + l.off_trace[0]), (uint32_t*)(a.ws + l.off_count));
     if (err == cudaSuccess) *launches += 2;
     return err;
 }
@@ -465,6 +522,7 @@ NewtonSchulzLayout newton_schulz_layout(int64_t batch, int64_t m, int64_t n, int
     int64_t off = round_up(offset, 256);
     auto take = [&](int64_t bytes) { int64_t o = off; off = round_up(off + bytes, 256); return o; };
     l.off_norm = take(8 * batch * l.norm_parts);
+    l.off_count = take(256);
     l.off_shift = take(4 * batch);
     for (int i = 0; i < 2; ++i) l.off_trace[i] = take(4 * batch * l.trace_parts);
     for (int i = 0; i < 2; ++i) {
@@ -482,57 +540,56 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
                       : a.type == kF16 ? launch_start<__half>(a, st, &launches[0]) : launch_start<__nv_bfloat16>(a, st, &launches[0]);
     if (err != cudaSuccess) return err;
     const NewtonSchulzLayout& l = a.lay;
-    const bool tall = a.m > a.n;
-    const int64_t s = tall ? a.n : a.m, L = tall ? a.m : a.n;
-    __half* gram = (__half*)(a.ws + l.off_gram);
-    __half* poly = (__half*)(a.ws + l.off_poly);
-    // Tile width of every product (see wide_tiles)
-    const int64_t rt = (s + 255) / 256, pairs = sm_count / 2;
-    auto width = [&](int64_t wide, int64_t narrow) { return wide_tiles(wide * a.batch, narrow * a.batch, pairs); };
-    const bool wide_square = width(rt * (rt - 1) / 2 + (s + 255) / 256, rt * (rt - 1) + (s + 127) / 128);
-    const int64_t mt = (a.m + 255) / 256;
-    const bool wide_update = width(mt * ((a.n + 255) / 256), mt * ((a.n + 127) / 128));
-    for (int k = 0; k < a.steps; ++k) {
-        const __half* hi = (const __half*)(a.ws + l.off_hi[k & 1]);
-        const int64_t sx = a.m * l.ldx, ss = s * l.lds;
-        const Operand x_rows = {hi, a.m, a.n, l.ldx, sx, false}, x_cols = {hi, a.n, a.m, l.ldx, sx, true};
-        NsGemm q = {};
-        q.batch = (int)a.batch;
-        q.short_side = (float)s;
-        q.a = a.coeffs[3 * k]; q.b = a.coeffs[3 * k + 1]; q.c = a.coeffs[3 * k + 2];
-        q.trace = k + 2 >= a.steps ? (const float*)(a.ws + l.off_trace[k & 1]) : nullptr;
-        q.trace_parts = k == 0 ? 1 : l.trace_parts;
-        q.shift = (float*)(a.ws + l.off_shift);
-        q.ldo = l.lds; q.stride_o = ss;
-        q.ldx = l.ldx; q.stride_x = sx;
-        q.dev_status = a.dev_status;
-        q.wait_ns = kWaitLimitNs;
-        auto run = [&](const Operand& A, const Operand& B, int64_t K, bool wide) {
-            q.M = (int)A.rows; q.N = (int)B.rows;
-            q.kblocks = (int)((K + kBK - 1) / kBK);
-            return wide ? launch_width<256>(q, A, B, sm_count, st, &launches[1]) : launch_width<128>(q, A, B, sm_count, st, &launches[1]);
-        };
-        // A' = X X^T - g I  (X^T X for a tall matrix)
-        q.mode = kGram;
-        q.out = gram;
-        if ((err = run(tall ? x_cols : x_rows, tall ? x_cols : x_rows, L, wide_square)) != cudaSuccess) return err;
-        // P = (b + 2 c g) A' + c A'^2
-        const Operand sq = {gram, s, s, l.lds, ss, false}, p = {poly, s, s, l.lds, ss, false};
-        q.mode = kPoly;
-        q.gram = gram; q.out = poly;
-        if ((err = run(sq, sq, s, wide_square)) != cudaSuccess) return err;
-        // X <- (a + b g + c g^2) X + P X  (X P for a tall matrix; P is symmetric)
-        q.mode = k + 1 == a.steps ? kLast : kUpdate;
-        q.hi = hi; q.lo = (const __half*)(a.ws + l.off_lo[k & 1]);
-        q.hi_out = (__half*)(a.ws + l.off_hi[(k + 1) & 1]);
-        q.lo_out = (__half*)(a.ws + l.off_lo[(k + 1) & 1]);
-        q.trace_out = (float*)(a.ws + l.off_trace[(k + 1) & 1]);
-        q.trace_parts = l.trace_parts;
-        q.last = (__nv_bfloat16*)a.O; q.ld_last = a.ldo; q.stride_last = a.stride_o;
-        q.last_vec = ((uintptr_t)a.O & 7) == 0 && a.ldo % 4 == 0 && a.stride_o % 4 == 0;
-        if ((err = run(tall ? x_rows : p, tall ? p : x_cols, s, wide_update)) != cudaSuccess) return err;
+    static int pairs_dev[kMaxDevices] = {};
+    int& max_pairs = pairs_dev[current_device_slot()];
+    if (!max_pairs) {
+        int pairs = 0;
+        if ((err = resident_pairs(ns_steps_kernel, kGemmThreads, kGemmSmem, sm_count, &pairs)) != cudaSuccess) return err;
+        max_pairs = pairs;
     }
-    return cudaSuccess;
+    NsParams p = {};
+    p.m = (int)a.m; p.n = (int)a.n; p.s = (int)(a.m < a.n ? a.m : a.n);
+    p.batch = (int)a.batch; p.steps = a.steps;
+    for (int i = 0; i < 3 * a.steps; ++i) p.coeffs[i] = a.coeffs[i];
+    for (int i = 0; i < 2; ++i) {
+        p.trace[i] = (float*)(a.ws + l.off_trace[i]);
+        p.hi[i] = (__half*)(a.ws + l.off_hi[i]);
+        p.lo[i] = (__half*)(a.ws + l.off_lo[i]);
+        if (!make_half_map(&p.x[i], p.hi[i], a.m, a.n, l.ldx, a.batch)) return cudaErrorInvalidValue;
+    }
+    p.trace_parts = l.trace_parts;
+    p.shift = (float*)(a.ws + l.off_shift);
+    p.gram = (__half*)(a.ws + l.off_gram);
+    p.poly = (__half*)(a.ws + l.off_poly);
+    p.lds = l.lds; p.ldx = l.ldx;
+    if (!make_half_map(&p.gram_map, p.gram, p.s, p.s, l.lds, a.batch) || !make_half_map(&p.poly_map, p.poly, p.s, p.s, l.lds, a.batch)) return cudaErrorInvalidValue;
+    p.out = (__nv_bfloat16*)a.O; p.ld_out = a.ldo; p.stride_out = a.stride_o;
+    p.out_vec = ((uintptr_t)a.O & 7) == 0 && a.ldo % 4 == 0 && a.stride_o % 4 == 0;
+    p.phase_count = (uint32_t*)(a.ws + l.off_count);
+    p.dev_status = a.dev_status;
+    p.wait_ns = kWaitLimitNs;
+    auto tiles_of = [](int64_t x, int64_t width) { return (x + width - 1) / width; };
+    const int64_t rt = tiles_of(p.s, 256), mt = tiles_of(a.m, 256);
+    if (tiles_of(p.s, 128) * (rt + 1) > INT32_MAX / 8 / a.batch || mt * tiles_of(a.n, 128) > INT32_MAX / 8 / a.batch) return cudaErrorInvalidValue;
+    const int64_t square[2] = {square_tiles((int)rt, (int)tiles_of(p.s, 128), 2) * a.batch, square_tiles((int)rt, (int)rt, 1) * a.batch};
+    const int64_t update[2] = {mt * tiles_of(a.n, 128) * a.batch, mt * tiles_of(a.n, 256) * a.batch};
+    p.wide_square = wide_tiles(square[1], square[0], max_pairs);
+    p.wide_update = wide_tiles(update[1], update[0], max_pairs);
+    const int64_t most = square[p.wide_square] > update[p.wide_update] ? square[p.wide_square] : update[p.wide_update];
+    const int pairs = (int)(most < max_pairs ? most : max_pairs);
+    cudaLaunchConfig_t c = {};
+    c.gridDim = dim3(2 * pairs);
+    c.blockDim = dim3(kGemmThreads);
+    c.dynamicSmemBytes = kGemmSmem;
+    c.stream = st;
+    cudaLaunchAttribute at[1];
+    at[0].id = cudaLaunchAttributeCooperative;
+    at[0].val.cooperative = 1;
+    c.attrs = at;
+    c.numAttrs = 1;
+    err = cudaLaunchKernelEx(&c, ns_steps_kernel, p);
+    if (err == cudaSuccess) ++launches[1];
+    return err;
 }
 
 }  // namespace gemm2m

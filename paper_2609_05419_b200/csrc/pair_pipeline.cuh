@@ -23,12 +23,13 @@ struct PairPipe {
     uint32_t full, empty, tfull, tempty, drain;      // shared-memory addresses of the barriers
     uint32_t* tmem_slot;
     volatile int* abort_flag;
-    volatile uint32_t* fills_issued;
+    volatile uint32_t* fills_issued;                 // by this CTA's producer, and the bytes that it loaded in the last fill of each stage
+    volatile uint32_t* fill_bytes;
     uint32_t rank, peer_abort, tmem;
     int* dev_status;
     unsigned long long wait_ns;
 
-    static constexpr size_t kBytes = 8 * (2 * STAGES + 5) + 16;
+    static constexpr size_t kBytes = 8 * (2 * STAGES + 5) + 16 + 4 * STAGES;
 
     // All threads.  `mem`: kBytes of shared memory, 8-byte aligned; warp 1 allocates the TMEM columns.  tfull_arrivals: the commit
     // and whatever else of this CTA an accumulator waits for before its epilogue.
@@ -42,6 +43,7 @@ struct PairPipe {
         tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
         abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
         fills_issued = reinterpret_cast<volatile uint32_t*>(tmem_slot + 2);
+        fill_bytes = reinterpret_cast<volatile uint32_t*>(tmem_slot + 3);
         rank = cluster_ctarank();
         dev_status = status;
         wait_ns = limit;
@@ -68,6 +70,11 @@ struct PairPipe {
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int code) const { return mbar_wait(bar, parity, abort_flag, dev_status, code, wait_ns); }
     // A role that gave up tells the peer; its own CTA's flag is set by the wait (or was seen there).
     __device__ __forceinline__ void tell_peer() const { st_cluster_u32(peer_abort, 1u); }
+    // Producer: `bytes` are about to be copied into this CTA's stage; the leader announces both CTAs' (they load alike).
+    __device__ __forceinline__ void announce(uint32_t stage, uint32_t bytes) const {
+        fill_bytes[stage] = bytes;
+        if (rank == 0) mbar_arrive_expect_tx(full + 8 * stage, 2 * bytes);
+    }
     // Epilogue, one warp: the accumulator buffer may be overwritten (`leader_tempty`: that buffer's barrier in the leader).
     __device__ __forceinline__ void release_at(uint32_t leader_tempty) const {
         tcgen05_fence_before();
@@ -79,7 +86,7 @@ struct PairPipe {
     // barrier of their own and waited for.  Copies still on their way credit the leader's full[stage]; the two producers are at
     // most STAGES fills apart, so each barrier is short of, or ahead by, at most one fill: the leader takes the missing peer bytes off,
     // or announces those it had not got to, and waits for the last fill of every stage.  These waits are bounded too.
-    __device__ __forceinline__ void close(uint32_t tmem_cols, uint32_t stage_bytes) {
+    __device__ __forceinline__ void close(uint32_t tmem_cols) {
         const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
         tcgen05_fence_before();
         __syncthreads();
@@ -93,8 +100,8 @@ struct PairPipe {
                 const uint32_t mine = *fills_issued, peers = ld_cluster_u32(map_to_cta(smem_u32(const_cast<uint32_t*>(fills_issued)), 1u));
                 for (uint32_t f = min(mine, peers); f < max(mine, peers); ++f) {
                     const uint32_t bar = full + 8 * (f % STAGES);
-                    if (peers < mine) mbar_complete_tx(bar, stage_bytes);
-                    else mbar_arrive_expect_tx(bar, stage_bytes);
+                    if (peers < mine) mbar_complete_tx(bar, fill_bytes[f % STAGES]);
+                    else mbar_arrive_expect_tx(bar, ld_cluster_u32(map_to_cta(smem_u32(const_cast<uint32_t*>(fill_bytes + f % STAGES)), 1u)));
                 }
                 const uint32_t fills = max(mine, peers);
                 for (uint32_t s = 0; s < (uint32_t)STAGES && s < fills; ++s) {
