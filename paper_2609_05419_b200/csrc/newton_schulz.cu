@@ -96,7 +96,12 @@ constexpr int kStages = 6;
 constexpr int kBoxBytes = 64 * 128;       // a copy: 64 rows x 64 inner entries, in either order
 constexpr int kStageBytes = 4 * kBoxBytes;
 constexpr int kEpilogueWarps = 8;
-constexpr int kGemmThreads = 64 + 32 * kEpilogueWarps;
+// Warps 0 and 1 copy operands and issue MMAs, 2 and 3 do nothing, 4 .. 11 are the epilogue, which holds a block's operands ahead and
+// needs more registers than an equal share (168): 128 x 40 + 256 x 232 = 384 x 168.
+constexpr int kFirstEpilogueWarp = 4;
+constexpr int kGemmThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
+constexpr int kLaunchRegs = 168, kPipeRegs = 40, kEpilogueRegs = 232;
+static_assert(128 * kPipeRegs + 32 * kEpilogueWarps * kEpilogueRegs <= kGemmThreads * kLaunchRegs, "register shares exceed what the block is launched with");
 constexpr int kMaxSteps = 64;
 constexpr size_t kPipeBytes = (PairPipe<kStages>::kBytes + 15) / 16 * 16;
 constexpr size_t kGemmSmem = (size_t)kStages * kStageBytes + 1024 + kPipeBytes + kEpilogueWarps * 4096;
@@ -213,33 +218,55 @@ __device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t targe
     return true;
 }
 
-struct alignas(8) Half4 { __half h[4]; };
 struct alignas(8) Bf4 { __nv_bfloat16 h[4]; };
 
-// 32 columns of 32 rows (v: this lane's row) of a phase's accumulator, at (row0, col0) of matrix b.  The values turn in shared memory
-// (`turn`, 4 KB per warp; 16-byte pieces XORed with the row), so that eight lanes have four columns each of one row and what is
-// read and written beside them is whole sectors.  What is read is asked for first, all at once: the stores might alias it, so
-// that nothing would move ahead of them by itself, and a round trip per row costs ten times the arithmetic.  Planes have
-// padded rows, so that four columns can always be touched; what lies in the padding is not used.
-__device__ __forceinline__ float finish_block(const NsParams& p, const Phase& q, int step, const uint32_t (&v)[32], uint32_t turn, int b, int row0, int col0, bool mirror, float g) {
-    const int lane = threadIdx.x & 31, piece = lane & 7, r0 = lane >> 3;
-    const int col = col0 + piece * 4;
-    const int rows = col < q.N ? min(32, q.M - row0) : 0;
+// What a lane reads beside a block of 32 x 32 accumulators: four columns each of eight rows of hi and lo (update), or of A' (polynomial).
+struct Beside { uint2 a[8], b[8]; };
+// A lane's place in a block at (row0, col0) of matrix b: eight lanes have one row's 32 columns.
+struct Place { int64_t at, step; int rows, col; };        // element offset of its first row, offset of every fourth row, rows of the block, first column
+__device__ __forceinline__ Place place_of(const NsParams& p, const Phase& q, int b, int row0, int col0) {
+    const int lane = threadIdx.x & 31;
     const bool square = q.mode == kGram || q.mode == kPoly;
     const int64_t ld = square ? p.lds : p.ldx;
-    const int64_t at0 = (int64_t)b * (square ? (int64_t)p.s * p.lds : (int64_t)p.m * p.ldx) + (int64_t)(row0 + r0) * ld + col;
-    Half4 in[8], in_lo[8];
-    if (q.mode != kGram) {
-        const __half* src = q.mode == kPoly ? p.gram : p.hi[step & 1];
+    Place w;
+    w.col = col0 + (lane & 7) * 4;
+    w.rows = w.col < q.N ? min(32, q.M - row0) : 0;
+    w.at = ((int64_t)b * (square ? p.s : p.m) + row0 + (lane >> 3)) * ld + w.col;
+    w.step = 4 * ld;
+    return w;
+}
+__device__ __forceinline__ uint2 ld_pair(const __half* p) { return *reinterpret_cast<const uint2*>(p); }
+__device__ __forceinline__ void load_beside(const NsParams& p, const Phase& q, int step, const Place& w, Beside& in) {
+    if (q.mode == kGram) return;
+    const int r0 = (threadIdx.x & 31) >> 3;
+    const __half* a = (q.mode == kPoly ? p.gram : p.hi[step & 1]) + w.at;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (r0 + 4 * i < rows) in[i] = *reinterpret_cast<const Half4*>(src + at0 + 4 * i * ld);
-    }
-    if (!square) {
+    for (int i = 0; i < 8; ++i)
+        if (r0 + 4 * i < w.rows) in.a[i] = ld_pair(a + i * w.step);
+    if (q.mode == kPoly) return;
+    const __half* l = p.lo[step & 1] + w.at;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (r0 + 4 * i < rows) in_lo[i] = *reinterpret_cast<const Half4*>(p.lo[step & 1] + at0 + 4 * i * ld);
-    }
+    for (int i = 0; i < 8; ++i)
+        if (r0 + 4 * i < w.rows) in.b[i] = ld_pair(l + i * w.step);
+}
+__device__ __forceinline__ void to_floats(uint2 v, float (&f)[4]) {
+    const float2 lo = __half22float2(*reinterpret_cast<const __half2*>(&v.x)), hi = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
+    f[0] = lo.x; f[1] = lo.y; f[2] = hi.x; f[3] = hi.y;
+}
+__device__ __forceinline__ uint2 to_halves(const float (&f)[4]) {
+    const __half2 lo = __floats2half2_rn(f[0], f[1]), hi = __floats2half2_rn(f[2], f[3]);
+    return make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+}
+
+// 32 columns of 32 rows (v: this lane's row) of a phase's accumulator, at (row0, col0) of matrix b.  The values turn in shared memory
+// (`turn`, 4 KB per warp; 16-byte pieces XORed with the row) so that what is read and written beside them is whole sectors.
+// `in` was read ahead; `next`, called between the arithmetic and the stores, reads ahead for the block after this one
+// (the compiler cannot move loads over stores that might alias them, and a round trip costs more than a block's arithmetic).
+// Planes have padded rows, so that four columns can always be touched; what lies in the padding is not used.
+template <typename Next>
+__device__ __forceinline__ float finish_block(const NsParams& p, const Phase& q, int step, const uint32_t (&v)[32], uint32_t turn, const Place& w, Beside& in,
+                                              int b, int row0, int col0, bool mirror, float g, Next next) {
+    const int lane = threadIdx.x & 31, piece = lane & 7, r0 = lane >> 3;
     __syncwarp();                                         // the previous block has been read
 #pragma unroll
     for (int i = 0; i < 8; ++i)
@@ -254,69 +281,101 @@ __device__ __forceinline__ float finish_block(const NsParams& p, const Phase& q,
                      : "r"(turn + (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4))) : "memory");
     }
     const float ca = p.coeffs[3 * step], cb = p.coeffs[3 * step + 1], cc = p.coeffs[3 * step + 2];
+    const Place here = w;
     float sum = 0.f;
-    if (square) {
-        __half* out = q.mode == kGram ? p.gram : p.poly;
-        const float lin = cb + 2.f * cc * g, sq = q.mode == kGram ? (float)(1.0 / (1 << (2 * kXExp - kSExp))) : cc * (float)(1.0 / (1 << kSExp));
-        const float diagonal = g * (float)(1 << kSExp);
-        __syncwarp();                                     // x has been read: the block's results take its place, 72 bytes per row
+    uint2 o[8];
+    if (q.mode == kGram || q.mode == kPoly) {
+        __half* out = (q.mode == kGram ? p.gram : p.poly);
+        if (q.mode == kGram) {
+            constexpr float kScale = 1.f / (float)(1 << (2 * kXExp - kSExp));
+            const float diagonal = g * (float)(1 << kSExp);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int r = r0 + 4 * i;
-            Half4 o;
+            for (int i = 0; i < 8; ++i) {
+                float f[4];
+                const int on = row0 + r0 + 4 * i - here.col;      // which of the four columns is the diagonal's
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                o.h[j] = __float2half_rn(q.mode == kGram ? x[i][j] * sq - (row0 + r == col + j ? diagonal : 0.f) : lin * __half2float(in[i].h[j]) + sq * x[i][j]);
-            if (r < rows) *reinterpret_cast<Half4*>(out + at0 + 4 * i * ld) = o;
-            if (mirror) {
-                const uint2 w = *reinterpret_cast<const uint2*>(&o);
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(turn + (uint32_t)(r * 72 + piece * 8)), "r"(w.x), "r"(w.y) : "memory");
+                for (int j = 0; j < 4; ++j) f[j] = x[i][j] * kScale - (on == j ? diagonal : 0.f);
+                o[i] = to_halves(f);
+            }
+        } else {
+            const float lin = cb + 2.f * cc * g, sq = cc * (1.f / (float)(1 << kSExp));
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                float f[4];
+                to_floats(in.a[i], f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f[j] = lin * f[j] + sq * x[i][j];
+                o[i] = to_halves(f);
             }
         }
-        if (mirror) {                                     // the same numbers at (column, row): two rows per lane, 16 lanes along a column
+        next();
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (r0 + 4 * i < here.rows) *reinterpret_cast<uint2*>(out + here.at + i * here.step) = o[i];
+        if (mirror) {                                     // the same numbers at (column, row): turned once more, 72 bytes per row
             __syncwarp();
-            const int r = (lane & 15) * 2;
-            __half* to = out + (int64_t)b * p.s * p.lds + row0 + r;
-            const int have = q.M - row0 - r;              // (the second row may lie in the padding)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(turn + (uint32_t)((r0 + 4 * i) * 72 + piece * 8)), "r"(o[i].x), "r"(o[i].y) : "memory");
+            __syncwarp();
+            const int r = (lane & 15) * 2;                // two rows per lane, 16 lanes along a column; the second row may lie in the padding
+            const int have = q.M - row0 - r;
+            __half* to = out + ((int64_t)b * p.s + col0 + (lane >> 4)) * p.lds + row0 + r;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
                 const int c = 2 * i + (lane >> 4);
                 uint16_t lo, hi;
                 asm volatile("ld.shared.u16 %0, [%1];" : "=h"(lo) : "r"(turn + (uint32_t)(r * 72 + c * 2)) : "memory");
                 asm volatile("ld.shared.u16 %0, [%1];" : "=h"(hi) : "r"(turn + (uint32_t)(r * 72 + 72 + c * 2)) : "memory");
-                if (have > 0 && col0 + c < q.N) *reinterpret_cast<uint32_t*>(to + (int64_t)(col0 + c) * p.lds) = (uint32_t)lo | ((uint32_t)hi << 16);
+                if (have > 0 && col0 + c < q.N) *reinterpret_cast<uint32_t*>(to + (int64_t)(2 * i) * p.lds) = (uint32_t)lo | ((uint32_t)hi << 16);
             }
         }
     } else {
         const float lin = ca + g * (cb + cc * g);
+        uint2 ol[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const int r = r0 + 4 * i;
-            if (r >= rows) continue;
-            float w[4];
+            float h[4], l[4], f[4];
+            to_floats(in.a[i], h);
+            to_floats(in.b[i], l);
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                w[j] = lin * (__half2float(in[i].h[j]) + __half2float(in_lo[i].h[j]) * (float)(1.0 / (1 << kLoExp))) + x[i][j] * (float)(1.0 / (1 << kSExp));
+            for (int j = 0; j < 4; ++j) f[j] = lin * (h[j] + l[j] * (1.f / (float)(1 << kLoExp))) + x[i][j] * (1.f / (float)(1 << kSExp));
             if (q.mode == kUpdate) {
-                Half4 ho, lo;
+                o[i] = to_halves(f);
+                to_floats(o[i], h);
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    ho.h[j] = __float2half_rn(w[j]);
-                    lo.h[j] = __float2half_rn((w[j] - __half2float(ho.h[j])) * (float)(1 << kLoExp));
-                    if (col + j < q.N) sum += w[j] * w[j];
+                    l[j] = (f[j] - h[j]) * (float)(1 << kLoExp);
+                    if (r0 + 4 * i < here.rows && here.col + j < q.N) sum += f[j] * f[j];
                 }
-                *reinterpret_cast<Half4*>(p.hi[(step + 1) & 1] + at0 + 4 * i * ld) = ho;
-                *reinterpret_cast<Half4*>(p.lo[(step + 1) & 1] + at0 + 4 * i * ld) = lo;
+                ol[i] = to_halves(l);
             } else {
-                __nv_bfloat16* d = p.out + (int64_t)b * p.stride_out + (int64_t)(row0 + r) * p.ld_out + col;
-                Bf4 o;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) o.h[j] = __float2bfloat16_rn(w[j] * (float)(1.0 / (1 << kXExp)));
-                if (p.out_vec && col + 4 <= q.N) *reinterpret_cast<Bf4*>(d) = o;
+                for (int j = 0; j < 4; ++j) x[i][j] = f[j] * (1.f / (float)(1 << kXExp));
+            }
+        }
+        next();
+        if (q.mode == kUpdate) {
+            __half *hi = p.hi[(step + 1) & 1] + here.at, *lo = p.lo[(step + 1) & 1] + here.at;
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r0 + 4 * i < here.rows) {
+                    *reinterpret_cast<uint2*>(hi + i * here.step) = o[i];
+                    *reinterpret_cast<uint2*>(lo + i * here.step) = ol[i];
+                }
+        } else {
+            __nv_bfloat16* d = p.out + (int64_t)b * p.stride_out + (int64_t)(row0 + r0) * p.ld_out + here.col;
+#pragma unroll
+            for (int i = 0; i < 8; ++i, d += 4 * p.ld_out) {
+                if (r0 + 4 * i >= here.rows) continue;
+                Bf4 f;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) f.h[j] = __float2bfloat16_rn(x[i][j]);
+                if (p.out_vec && here.col + 4 <= q.N) *reinterpret_cast<Bf4*>(d) = f;
                 else
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        if (col + j < q.N) d[j] = o.h[j];
+                        if (here.col + j < q.N) d[j] = f.h[j];
             }
         }
     }
@@ -350,8 +409,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
     const int pair = blockIdx.x >> 1, npairs = gridDim.x >> 1;
     const int phases = 3 * p.steps;
 
-    if (warp == 0) {
-        if (lane == 0) {                                  // copies, both CTAs
+    if (warp < kFirstEpilogueWarp) {
+        asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPipeRegs));
+        if (warp == 0 && lane == 0) {                     // copies, both CTAs
             const uint32_t leader_full = map_to_cta(pipe.full, 0);
             RingPos<kStages> at;
             uint32_t fills = 0;
@@ -360,7 +420,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                 const Phase q = phase_at(p, ph / 3, ph % 3);
                 if (pair >= q.tiles * p.batch) continue;
                 if (!(ok = wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag))) break;
-                asm volatile("fence.proxy.async;" ::: "memory");       // the other CTAs' stores, then this thread's bulk copies
+                asm volatile("fence.proxy.async.global;" ::: "memory");       // the other CTAs' stores, then this thread's bulk copies
                 const int half_rows = q.bn / 2;
                 for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs) {
                     int b, tr, tc;
@@ -379,9 +439,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             }
             *pipe.fills_issued = fills;
             if (!ok) pipe.tell_peer();
-        }
-    } else if (warp == 1) {
-        if (lane == 0 && pipe.rank == 0) {                // MMAs, leader
+        } else if (warp == 1 && lane == 0 && pipe.rank == 0) {      // MMAs, leader
             RingPos<kStages> at;
             uint32_t it = 0;                              // tile counter: buffer it & 1, its use number it >> 1
             bool ok = true;
@@ -411,9 +469,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             if (!ok) pipe.tell_peer();
         }
     } else {
-        // Epilogue: warp w reads lanes 32 (w & 3) .. of TMEM (rows), columns of half (w - 2) / 4.
-        const int half = (warp - 2) >> 2, quarter = warp & 3;
-        const uint32_t turn = smem_u32(behind) + (uint32_t)kPipeBytes + (uint32_t)(warp - 2) * 4096;
+        asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
+        // Epilogue: warp w reads lanes 32 (w & 3) .. of TMEM (rows), columns of half (w - 4) / 4.
+        const int half = (warp - kFirstEpilogueWarp) >> 2, quarter = warp & 3;
+        const uint32_t turn = smem_u32(behind) + (uint32_t)kPipeBytes + (uint32_t)(warp - kFirstEpilogueWarp) * 4096;
         const uint32_t leader_tempty = map_to_cta(pipe.tempty, 0);
         uint32_t it = 0;
         bool ok = true;
@@ -422,9 +481,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             const Phase q = phase_at(p, step, ph % 3);
             if (ok) {                                     // (without tiles too: a CTA is counted for a phase only after the phases before it)
                 ok = lane != 0 || wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag);
-                ok = __all_sync(0xffffffffu, ok);
+                ok = __all_sync(0xffffffffu, ok);         // lane 0 has acquired the other CTAs' stores, and the warp with it
             }
-            __threadfence();                              // lane 0 has seen the other CTAs' stores; the other lanes read them too
             const int nc = q.bn / 2;
             int shift_for = -1;
             float g = 0.f;
@@ -436,13 +494,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                     g = shift_of(p, step, q.mode, b);
                     shift_for = b;
                 }
-                if (q.mode == kGram && tr == 0 && tc == 0 && pipe.rank == 0 && warp == 2 && lane == 0) p.shift[b] = g;
-                ok = __all_sync(0xffffffffu, pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue));
-                if (!ok) break;
-                tcgen05_fence_after();
+                if (q.mode == kGram && tr == 0 && tc == 0 && pipe.rank == 0 && warp == kFirstEpilogueWarp && lane == 0) p.shift[b] = g;
                 const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM + quarter * 32, col0 = tc * q.bn + half * nc;
                 const bool mirror = (q.mode == kGram || q.mode == kPoly) && (tc + 1) * q.bn <= tr * 2 * kBM;      // below the diagonal block
                 const uint32_t taddr = pipe.tmem + ((uint32_t)(quarter * 32) << 16) + buf * 256 + (uint32_t)(half * nc);
+                Beside in;
+                Place w = place_of(p, q, b, row0, col0);
+                load_beside(p, q, step, w, in);           // on its way while the tile's last MMAs run
+                ok = __all_sync(0xffffffffu, pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue));
+                if (!ok) break;
+                tcgen05_fence_after();
                 float sum = 0.f;
 #pragma unroll 1
                 for (int c = 0; c < nc; c += 32) {
@@ -450,7 +511,13 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                     tmem_ld32(taddr + c, v);
                     tmem_ld_wait();
                     if (c + 32 == nc) pipe.release_at(leader_tempty + 8 * buf);
-                    if (row0 < q.M && col0 + c < q.N) sum += finish_block(p, q, step, v, turn, b, row0, col0 + c, mirror, g);
+                    if (row0 < q.M && col0 + c < q.N)
+                        sum += finish_block(p, q, step, v, turn, w, in, b, row0, col0 + c, mirror, g, [&]() {
+                            if (c + 32 < nc) {
+                                w = place_of(p, q, b, row0, col0 + c + 32);
+                                load_beside(p, q, step, w, in);
+                            }
+                        });
                     // one partial sum per 32 rows and 64 columns, whatever the tile width: results do not depend on that choice
                     if (q.mode == kUpdate && (c & 32)) {
 #pragma unroll
@@ -463,10 +530,12 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                 }
             }
             // (always, also after a give-up: nobody waits for this CTA for longer than for the others)
-            asm volatile("fence.proxy.async;" ::: "memory");
-            __threadfence();
             asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
-            if (warp == 2 && lane == 0) asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.phase_count) : "memory");
+            if (warp == kFirstEpilogueWarp && lane == 0) {      // what the barrier has collected is published as a whole, to bulk copies too
+                asm volatile("fence.proxy.async.global;" ::: "memory");
+                __threadfence();
+                asm volatile("red.release.gpu.global.add.u32 [%0], 1;" ::"l"(p.phase_count) : "memory");
+            }
         }
         if (!ok && lane == 0) pipe.tell_peer();
     }
