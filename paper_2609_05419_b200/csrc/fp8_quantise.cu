@@ -12,8 +12,6 @@
 // the column's group of 8 so that neither side has bank conflicts.
 #include "layer_ops.cuh"
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 #include <cuda_fp8.h>
 
 namespace gemm2m {
@@ -21,26 +19,6 @@ namespace gemm2m {
 namespace {
 
 constexpr int kThreads = 256;
-
-template <typename T> __device__ __forceinline__ float to_float(T v);
-template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_float<__half>(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
-
-// Eight consecutive entries of a row; those at or beyond `valid` read as zero.
-template <typename T>
-__device__ __forceinline__ void load8(const T* p, int64_t valid, bool vec, float (&v)[8]) {
-    if (vec && valid >= 8) {
-        T t[8];
-#pragma unroll
-        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(t)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = to_float<T>(t[i]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < valid ? to_float<T>(p[i]) : 0.f;
-    }
-}
 
 template <int FMT>
 __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {

@@ -4,6 +4,9 @@
 #pragma once
 #include "common.cuh"
 
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
 namespace gemm2m {
 
 constexpr int kScaleBlock = 128;          // entries along k that share a scale
@@ -49,5 +52,28 @@ struct NewtonSchulzArgs {
     int* dev_status;
 };
 cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaStream_t st, int launches[2]);
+
+#ifdef __CUDACC__
+template <typename T> __device__ __forceinline__ float to_float(T v);
+template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ float to_float<__half>(__half v) { return __half2float(v); }
+template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
+
+// Eight consecutive entries of a row; those at or beyond `valid` read as zero.
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, int64_t valid, bool vec, float (&v)[8]) {
+    if (vec && valid >= 8) {
+        T t[8];
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(t)[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = to_float<T>(t[i]);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < valid ? to_float<T>(p[i]) : 0.f;
+    }
+}
+
+#endif
 
 }  // namespace gemm2m

@@ -18,8 +18,6 @@
 #include "layer_ops.cuh"
 #include "pair_pipeline.cuh"
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
 
 namespace gemm2m {
 
@@ -28,13 +26,8 @@ namespace {
 constexpr int kXExp = 8;              // hi = rn16(2^8 X): entries of X are at most about 1.2
 constexpr int kLoExp = 11;            // lo = rn16(2^11 (2^8 X - hi))
 constexpr int kSExp = 4;              // A' and the polynomial are held times 2^4
-constexpr int kNormParts = 256;       // partial sums of |G|_F^2 per matrix
+constexpr int kNormParts = 592;       // partial sums of |G|_F^2 per matrix
 constexpr int kRowThreads = 256;
-
-template <typename T> __device__ __forceinline__ float to_float(T v);
-template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
-template <> __device__ __forceinline__ float to_float<__half>(__half v) { return __half2float(v); }
-template <> __device__ __forceinline__ float to_float<__nv_bfloat16>(__nv_bfloat16 v) { return __bfloat162float(v); }
 
 // Sum over the block in a fixed order; every thread gets it.
 __device__ __forceinline__ double block_sum(double v, double* scratch) {
@@ -48,26 +41,38 @@ __device__ __forceinline__ double block_sum(double v, double* scratch) {
     return s;
 }
 
+// The matrix is walked in groups of eight entries of a row, kUnroll groups per thread in flight (rows that are not 16-byte aligned are
+// read entry by entry).
+constexpr int kUnroll = 4;
+
 // |G|_F^2, one partial sum per block, in 64 bits (a square of a 32-bit number always fits).
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) norm_kernel(const T* G, int64_t m, int64_t n, int64_t ldg, int64_t stride_g, double* parts) {
+__global__ void __launch_bounds__(kRowThreads) norm_kernel(const T* G, int64_t groups, uint32_t per_row, int64_t n, int64_t ldg, int64_t stride_g, int vec, double* parts) {
     __shared__ double scratch[kRowThreads / 32];
     wait_for_prior_kernels();
     const T* g = G + (int64_t)blockIdx.y * stride_g;
+    const int64_t stride = (int64_t)gridDim.x * kRowThreads;
     double s = 0.0;
-    for (int64_t r = blockIdx.x; r < m; r += gridDim.x)
-        for (int64_t c = threadIdx.x; c < n; c += kRowThreads) {
-            const double v = (double)to_float<T>(g[r * ldg + c]);
-            s += v * v;
+    for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < groups; i += kUnroll * stride) {
+        float v[kUnroll][8];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t k = i + u * stride, row = k / per_row, col = (k - row * per_row) * 8;
+            load8<T>(g + row * ldg + col, k < groups ? n - col : 0, vec != 0, v[u]);
         }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += (double)v[u][j] * (double)v[u][j];
+    }
     s = block_sum(s, scratch);
     if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
 }
 
 // X_0 in two planes.  The first block of each matrix also leaves |X_0|_F^2, the trace of the first step.
 template <typename T>
-__global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t m, int64_t n, int64_t ldg, int64_t stride_g, const double* parts,
-                                                            int nparts, float eps, __half* hi, __half* lo, int64_t ldx, float* trace, uint32_t* phase_count) {
+__global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t groups, uint32_t per_row, int64_t m, int64_t n, int64_t ldg, int64_t stride_g, int vec,
+                                                            const double* parts, int nparts, float eps, __half* hi, __half* lo, int64_t ldx, float* trace, uint32_t* phase_count) {
     __shared__ double scratch[kRowThreads / 32];
     wait_for_prior_kernels();
     const int64_t b = blockIdx.y;
@@ -75,19 +80,38 @@ __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t 
     for (int i = threadIdx.x; i < nparts; i += kRowThreads) sq += parts[b * nparts + i];
     sq = block_sum(sq, scratch);
     const double norm = sqrt(sq) + (double)eps;
-    const double inv = norm > 0.0 ? (double)(1 << kXExp) / norm : 0.0;       // in 64 bits: 1 / norm of a tiny matrix overflows 32
+    const double inv = norm > 0.0 ? (double)(1 << kXExp) / norm : 0.0;
+    const bool in32 = inv > 1e-30 && inv < 1e30;           // 1 / norm of a tiny matrix overflows 32 bits
+    const float inv32 = (float)inv;
     if (blockIdx.x == 0 && threadIdx.x == 0) {
         if (b == 0) *phase_count = 0;
         trace[b] = norm > 0.0 ? (float)(sq / (norm * norm)) : 0.f;
     }
     const T* g = G + b * stride_g;
-    for (int64_t r = blockIdx.x; r < m; r += gridDim.x)
-        for (int64_t c = threadIdx.x; c < n; c += kRowThreads) {
-            const float x = (float)((double)to_float<T>(g[r * ldg + c]) * inv);
-            const __half h = __float2half_rn(x);
-            hi[(b * m + r) * ldx + c] = h;
-            lo[(b * m + r) * ldx + c] = __float2half_rn((x - __half2float(h)) * (float)(1 << kLoExp));
+    const int64_t stride = (int64_t)gridDim.x * kRowThreads;
+    for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < groups; i += kUnroll * stride) {
+        float v[kUnroll][8];
+        int64_t at[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t k = i + u * stride, row = k / per_row, col = (k - row * per_row) * 8;
+            load8<T>(g + row * ldg + col, k < groups ? n - col : 0, vec != 0, v[u]);
+            at[u] = k < groups ? (b * m + row) * ldx + col : -1;
         }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            if (at[u] < 0) continue;
+            __half h[8], l[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float x = in32 ? v[u][j] * inv32 : (float)((double)v[u][j] * inv);
+                h[j] = __float2half_rn(x);
+                l[j] = __float2half_rn((x - __half2float(h[j])) * (float)(1 << kLoExp));
+            }
+            *reinterpret_cast<uint4*>(hi + at[u]) = *reinterpret_cast<const uint4*>(h);      // (rows of the planes are padded)
+            *reinterpret_cast<uint4*>(lo + at[u]) = *reinterpret_cast<const uint4*>(l);
+        }
+    }
 }
 
 constexpr int kBM = 128;                  // rows of the first operand per CTA
@@ -111,7 +135,7 @@ enum Mode { kGram, kPoly, kUpdate, kLast };
 struct NsParams {
     CUtensorMap x[2], gram_map, poly_map;                 // the iterate's hi planes, A' and the polynomial
     int m, n, s, batch, steps;
-    int wide_square, wide_update;                         // tiles of 256 columns, otherwise of 128
+    int square_width, update_width;                       // columns of a tile: 256, 128 or 64
     float coeffs[3 * kMaxSteps];
     float* trace[2]; int64_t trace_parts;           // partial sums of |X|_F^2 (one in front of the first step)
     float* shift;                                         // g of every matrix: written with A', read by the rest of the step
@@ -134,7 +158,7 @@ __device__ __forceinline__ Phase phase_at(const NsParams& p, int step, int kind)
     Phase q;
     const bool tall = p.m > p.n;
     q.mode = kind == 0 ? kGram : kind == 1 ? kPoly : step + 1 == p.steps ? kLast : kUpdate;
-    q.bn = (kind == 2 ? p.wide_update : p.wide_square) ? 256 : 128;
+    q.bn = kind == 2 ? p.update_width : p.square_width;
     q.M = kind == 2 ? p.m : p.s;
     q.N = kind == 2 ? p.n : p.s;
     q.kblocks = ((kind == 0 ? (tall ? p.m : p.n) : p.s) + kBK - 1) / kBK;
@@ -199,13 +223,15 @@ __device__ __forceinline__ void tile_at(const Phase& q, int t, int* b, int* tr, 
     }
 }
 
-// Waits (bounded) until `target` CTAs in all have finished their phases, and sees what they wrote.
+// Waits (bounded) until `target` CTAs in all have finished their phases, and sees what they wrote.  (The look itself is relaxed: an
+// acquire every time would empty the SM's L1 under the warps that still work.)
 __device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t target, volatile int* abort_flag) {
     const unsigned long long t0 = global_timer_ns();
     for (uint32_t spins = 1;; ++spins) {
         uint32_t seen;
-        asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(p.phase_count) : "memory");
+        asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(p.phase_count) : "memory");
         if (seen >= target) break;
+        __nanosleep(40);
         if ((spins & 63u) == 0) {
             if (*abort_flag) return false;
             if (global_timer_ns() - t0 > p.wait_ns) {
@@ -215,6 +241,7 @@ __device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t targe
             }
         }
     }
+    asm volatile("fence.acq_rel.gpu;" ::: "memory");
     return true;
 }
 
@@ -429,7 +456,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                     for (int kb = 0; kb < q.kblocks; ++kb) {
                         if (!(ok = pipe.wait(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
                         const uint32_t dst = tiles_base + at.stage * kStageBytes;
-                        pipe.announce(at.stage, (uint32_t)(kBM + half_rows) * 128u);
+                        pipe.announce(at.stage, (uint32_t)(kBM + max(half_rows, 64)) * 128u);      // (a copy is 64 rows, also where half of them are used)
                         load_operand(dst, q.map_a, leader_full + 8 * at.stage, q.turned_a, kb, row0, kBM, b);
                         load_operand(dst + kBM * 128, q.map_b, leader_full + 8 * at.stage, q.turned_b, kb, col0, half_rows, b);
                         ++fills;
@@ -504,32 +531,30 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                 ok = __all_sync(0xffffffffu, pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue));
                 if (!ok) break;
                 tcgen05_fence_after();
-                float sum = 0.f;
 #pragma unroll 1
                 for (int c = 0; c < nc; c += 32) {
+                    float sum = 0.f;
                     uint32_t v[32];
                     tmem_ld32(taddr + c, v);
                     tmem_ld_wait();
                     if (c + 32 == nc) pipe.release_at(leader_tempty + 8 * buf);
                     if (row0 < q.M && col0 + c < q.N)
-                        sum += finish_block(p, q, step, v, turn, w, in, b, row0, col0 + c, mirror, g, [&]() {
+                        sum = finish_block(p, q, step, v, turn, w, in, b, row0, col0 + c, mirror, g, [&]() {
                             if (c + 32 < nc) {
                                 w = place_of(p, q, b, row0, col0 + c + 32);
                                 load_beside(p, q, step, w, in);
                             }
                         });
-                    // one partial sum per 32 rows and 64 columns, whatever the tile width: results do not depend on that choice
-                    if (q.mode == kUpdate && (c & 32)) {
+                    // one partial sum per block, whatever the tile width: results do not depend on that choice
+                    if (q.mode == kUpdate) {
 #pragma unroll
                         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
-                        const int part_row = row0 >> 5, part_col = (col0 + c) >> 6, cols = (q.N + 63) >> 6;
+                        const int part_row = row0 >> 5, part_col = (col0 + c) >> 5, cols = (q.N + 31) >> 5;
                         if (lane == 0 && row0 < q.M && part_col < cols)
-                            p.trace[(step + 1) & 1][(int64_t)b * p.trace_parts + (int64_t)part_row * cols + part_col] = sum * exp2f(-2 * kXExp);
-                        sum = 0.f;
+                            p.trace[(step + 1) & 1][(int64_t)b * p.trace_parts + (int64_t)part_row * cols + part_col] = sum * (1.f / (float)(1 << (2 * kXExp)));
                     }
                 }
             }
-            // (always, also after a give-up: nobody waits for this CTA for longer than for the others)
             asm volatile("bar.sync 1, %0;" ::"n"(32 * kEpilogueWarps) : "memory");
             if (warp == kFirstEpilogueWarp && lane == 0) {      // what the barrier has collected is published as a whole, to bulk copies too
                 asm volatile("fence.proxy.async.global;" ::: "memory");
@@ -545,7 +570,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
 inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
 // Partial sums of the trace that an update of m x n matrices leaves.
-inline int64_t update_trace_parts(int64_t m, int64_t n) { return (m + 31) / 32 * ((n + 63) / 64); }
+inline int64_t update_trace_parts(int64_t m, int64_t n) { return (m + 31) / 32 * ((n + 31) / 32); }
 
 // rows x cols of `batch` matrices, padded rows; box = 64 x 64 of one matrix, which serves as 64 rows x 64 inner entries in either order.
 bool make_half_map(CUtensorMap* map, const __half* base, int64_t rows, int64_t cols, int64_t ld, int64_t batch) {
@@ -563,20 +588,34 @@ template <typename T>
 cudaError_t launch_start(const NewtonSchulzArgs& a, cudaStream_t st, int* launches) {
     const NewtonSchulzLayout& l = a.lay;
     double* parts = (double*)(a.ws + l.off_norm);
-    const int blocks = (int)(a.m < kNormParts ? a.m : kNormParts);
-    cudaError_t err = launch_chained(norm_kernel<T>, dim3(blocks, (unsigned)a.batch), dim3(kRowThreads), 0, st, (const T*)a.G, a.m, a.n, a.ldg, a.stride_g, parts);
+    const uint32_t per_row = (uint32_t)((a.n + 7) / 8);
+    const int64_t groups = a.m * per_row, needed = (groups + kRowThreads - 1) / kRowThreads;
+    const int vec = ((uintptr_t)a.G & 15) == 0 && a.ldg * sizeof(T) % 16 == 0 && a.stride_g * sizeof(T) % 16 == 0;
+    // (by the matrix alone, so that its sums do not depend on the batch it is in; eight groups or more per thread)
+    const int blocks = (int)((needed + 7) / 8 < kNormParts ? (needed + 7) / 8 : kNormParts);
+    cudaError_t err = launch_chained(norm_kernel<T>, dim3(blocks, (unsigned)a.batch), dim3(kRowThreads), 0, st, (const T*)a.G, groups, per_row, a.n, a.ldg, a.stride_g, vec, parts);
     if (err != cudaSuccess) return err;
-    err = launch_chained(start_kernel<T>, dim3((unsigned)(a.m < 1024 ? a.m : 1024), (unsigned)a.batch), dim3(kRowThreads), 0, st, (const T*)a.G, a.m, a.n, a.ldg,
-                         a.stride_g, parts, blocks, a.eps, (__half*)(a.ws + l.off_hi[0]), (__half*)(a.ws + l.off_lo[0]), l.ldx,
-                         (float*)(a.ws + l.off_trace[0]), (uint32_t*)(a.ws + l.off_count));
+    const int start_blocks = (int)((needed + kUnroll - 1) / kUnroll < 1024 ? (needed + kUnroll - 1) / kUnroll : 1024);
+    err = launch_chained(start_kernel<T>, dim3(start_blocks, (unsigned)a.batch), dim3(kRowThreads), 0, st, (const T*)a.G, groups, per_row, a.m, a.n, a.ldg, a.stride_g, vec,
+                         parts, blocks, a.eps, (__half*)(a.ws + l.off_hi[0]), (__half*)(a.ws + l.off_lo[0]), l.ldx, (float*)(a.ws + l.off_trace[0]),
+                         (uint32_t*)(a.ws + l.off_count));
     if (err == cudaSuccess) *launches += 2;
     return err;
 }
 
-// Whether a product's tiles are 256 or 128 columns wide: whichever makes the last pair finish first, a narrow tile counted as
-// 0.55 of a wide one (half the MMAs, three quarters of the operand bytes).
-bool wide_tiles(int64_t wide, int64_t narrow, int64_t pairs) {
-    return (double)((wide + pairs - 1) / pairs) <= 0.55 * (double)((narrow + pairs - 1) / pairs);
+// Columns of a product's tiles (index 0, 1, 2: 64, 128, 256), by the time of the pair that finishes last.  A tile's copies and MMAs take, per 64
+// inner entries, what the SMs can draw from L2 (about 46 bytes per SM and cycle at 1.7 GHz: 710 cycles for a wide tile's 32 KB per
+// CTA, 580 for the others' 24 KB); its epilogue about 3300 cycles per 32 columns of a warp.  The longer of the two counts for every
+// tile, the shorter once.
+int best_width(const int64_t (&tiles)[3], int64_t kblocks, int64_t pairs) {
+    int best = 0;
+    double least = 0.0;
+    for (int w = 0; w < 3; ++w) {
+        const double rounds = (double)((tiles[w] + pairs - 1) / pairs), feed = (double)kblocks * (w == 2 ? 710.0 : 580.0), finish = 3300.0 * (double)(1 << w);
+        const double cost = rounds * (feed > finish ? feed : finish) + (feed > finish ? finish : feed);
+        if (w == 0 || cost < least) { best = w; least = cost; }
+    }
+    return best;
 }
 
 }  // namespace
@@ -639,12 +678,17 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
     p.wait_ns = kWaitLimitNs;
     auto tiles_of = [](int64_t x, int64_t width) { return (x + width - 1) / width; };
     const int64_t rt = tiles_of(p.s, 256), mt = tiles_of(a.m, 256);
-    if (tiles_of(p.s, 128) * (rt + 1) > INT32_MAX / 8 / a.batch || mt * tiles_of(a.n, 128) > INT32_MAX / 8 / a.batch) return cudaErrorInvalidValue;
-    const int64_t square[2] = {square_tiles((int)rt, (int)tiles_of(p.s, 128), 2) * a.batch, square_tiles((int)rt, (int)rt, 1) * a.batch};
-    const int64_t update[2] = {mt * tiles_of(a.n, 128) * a.batch, mt * tiles_of(a.n, 256) * a.batch};
-    p.wide_square = wide_tiles(square[1], square[0], max_pairs);
-    p.wide_update = wide_tiles(update[1], update[0], max_pairs);
-    const int64_t most = square[p.wide_square] > update[p.wide_update] ? square[p.wide_square] : update[p.wide_update];
+    if (tiles_of(p.s, 64) * (rt + 1) > INT32_MAX / 8 / a.batch || mt * tiles_of(a.n, 64) > INT32_MAX / 8 / a.batch) return cudaErrorInvalidValue;
+    int64_t square[3], update[3];
+    for (int w = 0; w < 3; ++w) {
+        square[w] = square_tiles((int)rt, (int)tiles_of(p.s, 64 << w), 4 >> w) * a.batch;
+        update[w] = mt * tiles_of(a.n, 64 << w) * a.batch;
+    }
+    const int64_t long_side = a.m < a.n ? a.n : a.m;
+    const int ws = best_width(square, tiles_of((p.s + long_side) / 2, kBK), max_pairs), wu = best_width(update, tiles_of(p.s, kBK), max_pairs);
+    p.square_width = 64 << ws;
+    p.update_width = 64 << wu;
+    const int64_t most = square[ws] > update[wu] ? square[ws] : update[wu];
     const int pairs = (int)(most < max_pairs ? most : max_pairs);
     cudaLaunchConfig_t c = {};
     c.gridDim = dim3(2 * pairs);
