@@ -133,7 +133,7 @@ constexpr size_t kGemmSmem = (size_t)kStages * kStageBytes + 1024 + kPipeBytes +
 enum Mode { kGram, kPoly, kUpdate, kLast };
 
 struct NsParams {
-    CUtensorMap x[2], gram_map, poly_map;                 // the iterate's hi planes, A' and the polynomial
+    CUtensorMap x[2][2], gram_map[2], poly_map[2];        // the iterate's hi planes, A' and the polynomial, in boxes of 64 and of 128 rows
     int m, n, s, batch, steps;
     int square_width, update_width;                       // columns of a tile: 256, 128 or 64
     float coeffs[3 * kMaxSteps];
@@ -167,9 +167,9 @@ __device__ __forceinline__ Phase phase_at(const NsParams& p, int step, int kind)
     q.tiles = kind == 2 ? q.tiles_r * q.tiles_c : square_tiles(q.tiles_r, q.tiles_c, 2 * kBM / q.bn);
     q.turned_a = kind == 0 && tall;                       // X^T X contracts along the rows of X
     q.turned_b = (kind == 0 && tall) || (kind == 2 && !tall);
-    const CUtensorMap* x = &p.x[step & 1];
-    q.map_a = kind == 0 ? x : kind == 1 ? &p.gram_map : tall ? x : &p.poly_map;
-    q.map_b = kind == 0 ? x : kind == 1 ? &p.gram_map : tall ? &p.poly_map : x;
+    const CUtensorMap* x = p.x[step & 1];
+    q.map_a = kind == 0 ? x : kind == 1 ? p.gram_map : tall ? x : p.poly_map;
+    q.map_b = kind == 0 ? x : kind == 1 ? p.gram_map : tall ? p.poly_map : x;
     return q;
 }
 
@@ -196,8 +196,12 @@ __device__ __forceinline__ uint64_t make_smem_desc_turned(uint32_t addr) {
     d |= (uint64_t)2 << 61;
     return d;
 }
-// `rows` rows from row0 and one stage of the inner dimension, 64 rows per copy.
+// `rows` rows from row0 and one stage of the inner dimension: in one copy where 128 rows follow one another, else 64 rows per copy.
 __device__ __forceinline__ void load_operand(uint32_t dst, const CUtensorMap* map, uint32_t bar, bool turned, int kb, int row0, int rows, int b) {
+    if (!turned && rows == 128) {
+        tma_load_3d_pair(dst, map + 1, bar, kb * kBK, row0, b);
+        return;
+    }
     for (int r = 0; r < rows; r += 64, dst += kBoxBytes) {
         if (turned) tma_load_3d_pair(dst, map, bar, row0 + r, kb * kBK, b);
         else tma_load_3d_pair(dst, map, bar, kb * kBK, row0 + r, b);
@@ -446,6 +450,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             for (int ph = 0; ok && ph < phases; ++ph) {
                 const Phase q = phase_at(p, ph / 3, ph % 3);
                 if (pair >= q.tiles * p.batch) continue;
+                asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_a) : "memory");
+                asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_b) : "memory");
                 if (!(ok = wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag))) break;
                 asm volatile("fence.proxy.async.global;" ::: "memory");       // the other CTAs' stores, then this thread's bulk copies
                 const int half_rows = q.bn / 2;
@@ -572,13 +578,13 @@ inline int64_t round_up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 // Partial sums of the trace that an update of m x n matrices leaves.
 inline int64_t update_trace_parts(int64_t m, int64_t n) { return (m + 31) / 32 * ((n + 31) / 32); }
 
-// rows x cols of `batch` matrices, padded rows; box = 64 x 64 of one matrix, which serves as 64 rows x 64 inner entries in either order.
-bool make_half_map(CUtensorMap* map, const __half* base, int64_t rows, int64_t cols, int64_t ld, int64_t batch) {
+// rows x cols of `batch` matrices, padded rows; box = box_rows x 64 of one matrix (64 x 64 serves as rows x inner entries in either order).
+bool make_half_map(CUtensorMap* map, const __half* base, int64_t rows, int64_t cols, int64_t ld, int64_t batch, int box_rows) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) return false;
     const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)batch};
     const cuuint64_t strides[2] = {(cuuint64_t)ld * 2, (cuuint64_t)(rows * ld) * 2};
-    const cuuint32_t box[3] = {64, 64, 1};
+    const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1};
     const cuuint32_t estr[3] = {1, 1, 1};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_FLOAT16, 3, const_cast<__half*>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -663,14 +669,17 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
         p.trace[i] = (float*)(a.ws + l.off_trace[i]);
         p.hi[i] = (__half*)(a.ws + l.off_hi[i]);
         p.lo[i] = (__half*)(a.ws + l.off_lo[i]);
-        if (!make_half_map(&p.x[i], p.hi[i], a.m, a.n, l.ldx, a.batch)) return cudaErrorInvalidValue;
+        for (int w = 0; w < 2; ++w)
+            if (!make_half_map(&p.x[i][w], p.hi[i], a.m, a.n, l.ldx, a.batch, 64 << w)) return cudaErrorInvalidValue;
     }
     p.trace_parts = l.trace_parts;
     p.shift = (float*)(a.ws + l.off_shift);
     p.gram = (__half*)(a.ws + l.off_gram);
     p.poly = (__half*)(a.ws + l.off_poly);
     p.lds = l.lds; p.ldx = l.ldx;
-    if (!make_half_map(&p.gram_map, p.gram, p.s, p.s, l.lds, a.batch) || !make_half_map(&p.poly_map, p.poly, p.s, p.s, l.lds, a.batch)) return cudaErrorInvalidValue;
+    for (int w = 0; w < 2; ++w)
+        if (!make_half_map(&p.gram_map[w], p.gram, p.s, p.s, l.lds, a.batch, 64 << w) || !make_half_map(&p.poly_map[w], p.poly, p.s, p.s, l.lds, a.batch, 64 << w))
+            return cudaErrorInvalidValue;
     p.out = (__nv_bfloat16*)a.O; p.ld_out = a.ldo; p.stride_out = a.stride_o;
     p.out_vec = ((uintptr_t)a.O & 7) == 0 && a.ldo % 4 == 0 && a.stride_o % 4 == 0;
     p.phase_count = (uint32_t*)(a.ws + l.off_count);
