@@ -49,7 +49,7 @@ __device__ __forceinline__ void store8(uint8_t* p, uint2 v, int64_t valid) {
 }
 
 template <typename T, int FMT, bool TILE, bool BOTH>
-__global__ void __launch_bounds__(kThreads) fp8_quantise_kernel(const QuantiseArgs a, int col_tiles, int vec) {
+__global__ void __launch_bounds__(kThreads, sizeof(T) == 4 || (BOTH && !TILE) ? 2 : 3) fp8_quantise_kernel(const QuantiseArgs a, int col_tiles, int vec) {
     __shared__ uint32_t warp_top[8][128];
     __shared__ __align__(16) uint2 turned[BOTH ? 128 : 1][16];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -60,20 +60,31 @@ __global__ void __launch_bounds__(kThreads) fp8_quantise_kernel(const QuantiseAr
     const int64_t valid = a.cols - col0;
     wait_for_prior_kernels();
 
+    Raw8<T> raw[8];
+    const T* src = (const T*)a.X + row0 * a.ldx + col0;
+    if (vec && (tile_r + 1) * 128 <= a.rows && (tile_c + 1) * 128 <= a.cols) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) raw[i] = load8<T>(src + i * a.ldx);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) raw[i] = load8_part<T>(src + i * a.ldx, row0 + i < a.rows ? valid : 0);
+    }
     float x[8][8];
     uint32_t top_row[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        if (row0 + i < a.rows) load8<T>((const T*)a.X + (row0 + i) * a.ldx + col0, valid, vec != 0, x[i]);
-        else
+    for (int i = 0; i < 8; ++i) to_floats8<T>(raw[i], x[i]);
+    uint32_t top_col[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) x[i][j] = 0.f;
-    }
+    for (int j = 0; j < 8; ++j) top_col[j] = 0;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         top_row[i] = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top_row[i] = max(top_row[i], __float_as_uint(x[i][j]) & 0x7fffffffu);
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t size = __float_as_uint(x[i][j]) & 0x7fffffffu;
+            top_row[i] = max(top_row[i], size);
+            if (BOTH && !TILE) top_col[j] = max(top_col[j], size);
+        }
     }
     float inv_row[8];
     if (TILE) {
@@ -94,16 +105,24 @@ __global__ void __launch_bounds__(kThreads) fp8_quantise_kernel(const QuantiseAr
             if (BOTH) a.St[tile_r * a.ldst + tile_c] = s;
         }
     } else if (a.Q) {
+        // Row maxima over 16 lanes, halving the rows that a lane keeps with every exchange: lane g of the 16 ends with row g / 2, forms
+        // its scale (two divisions, not sixteen) and hands the inverse back.
 #pragma unroll
-        for (int d = 8; d > 0; d >>= 1)
+        for (int d = 8, keep = 4; d > 1; d >>= 1, keep >>= 1) {
+            const bool upper = (lane & d) != 0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) top_row[i] = max(top_row[i], __shfl_xor_sync(0xffffffffu, top_row[i], d));
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float s;
-            scales<FMT>(top_row[i], &s, &inv_row[i]);
-            if (group == i && row0 + i < a.rows) a.S[tile_c * a.lds + row0 + i] = s;
+            for (int i = 0; i < keep; ++i) {
+                const uint32_t mine = upper ? top_row[i + keep] : top_row[i], theirs = upper ? top_row[i] : top_row[i + keep];
+                top_row[i] = max(mine, __shfl_xor_sync(0xffffffffu, theirs, d));
+            }
         }
+        top_row[0] = max(top_row[0], __shfl_xor_sync(0xffffffffu, top_row[0], 1));
+        float s, inv;
+        scales<FMT>(top_row[0], &s, &inv);
+        const int64_t row = row0 + (group >> 1);
+        if (!(lane & 1) && row < a.rows) a.S[tile_c * a.lds + row] = s;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) inv_row[i] = __shfl_sync(0xffffffffu, inv, (lane & 16) | (2 * i));
     }
     if (a.Q && valid > 0) {
 #pragma unroll
@@ -119,17 +138,11 @@ __global__ void __launch_bounds__(kThreads) fp8_quantise_kernel(const QuantiseAr
 #pragma unroll
             for (int j = 0; j < 8; ++j) inv_col[j] = inv_row[0];
         } else {
-            uint32_t top[8];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                top[j] = 0;
-#pragma unroll
-                for (int i = 0; i < 8; ++i) top[j] = max(top[j], __float_as_uint(x[i][j]) & 0x7fffffffu);
-                top[j] = max(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16));
-            }
+            for (int j = 0; j < 8; ++j) top_col[j] = max(top_col[j], __shfl_xor_sync(0xffffffffu, top_col[j], 16));
             if (lane < 16) {
-                *reinterpret_cast<uint4*>(&warp_top[warp][group * 8]) = make_uint4(top[0], top[1], top[2], top[3]);
-                *reinterpret_cast<uint4*>(&warp_top[warp][group * 8 + 4]) = make_uint4(top[4], top[5], top[6], top[7]);
+                *reinterpret_cast<uint4*>(&warp_top[warp][group * 8]) = make_uint4(top_col[0], top_col[1], top_col[2], top_col[3]);
+                *reinterpret_cast<uint4*>(&warp_top[warp][group * 8 + 4]) = make_uint4(top_col[4], top_col[5], top_col[6], top_col[7]);
             }
             __syncthreads();
             // one thread per column forms the scale and leaves the inverse in row 0 of the table

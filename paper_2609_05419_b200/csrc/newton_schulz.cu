@@ -45,6 +45,27 @@ __device__ __forceinline__ double block_sum(double v, double* scratch) {
 // read entry by entry).
 constexpr int kUnroll = 4;
 
+// Groups i, i + stride, ..: their entries, and (at) where they go in a plane with rows of ldx, -1 behind the last group.
+template <typename T>
+__device__ __forceinline__ void load_groups(Raw8<T> (&raw)[kUnroll], int64_t* at, const T* g, int64_t i, int64_t stride, int64_t groups, uint32_t per_row, int64_t n,
+                                            int64_t ldg, int vec, int64_t ldx) {
+    if (vec && i + (kUnroll - 1) * stride < groups) {      // vec: every group is whole and aligned
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t k = i + u * stride, row = k / per_row, col = (k - row * per_row) * 8;
+            raw[u] = load8<T>(g + row * ldg + col);
+            if (at) at[u] = row * ldx + col;
+        }
+    } else {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int64_t k = i + u * stride, row = k / per_row, col = (k - row * per_row) * 8;
+            raw[u] = load8_part<T>(g + row * ldg + col, k < groups ? n - col : 0);
+            if (at) at[u] = k < groups ? row * ldx + col : -1;
+        }
+    }
+}
+
 // |G|_F^2, one partial sum per block, in 64 bits (a square of a 32-bit number always fits).
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) norm_kernel(const T* G, int64_t groups, uint32_t per_row, int64_t n, int64_t ldg, int64_t stride_g, int vec, double* parts) {
@@ -54,16 +75,15 @@ __global__ void __launch_bounds__(kRowThreads) norm_kernel(const T* G, int64_t g
     const int64_t stride = (int64_t)gridDim.x * kRowThreads;
     double s = 0.0;
     for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < groups; i += kUnroll * stride) {
-        float v[kUnroll][8];
+        Raw8<T> raw[kUnroll];
+        load_groups<T>(raw, nullptr, g, i, stride, groups, per_row, n, ldg, vec, 0);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            const int64_t k = i + u * stride, row = k / per_row, col = (k - row * per_row) * 8;
-            load8<T>(g + row * ldg + col, k < groups ? n - col : 0, vec != 0, v[u]);
+            float v[8];
+            to_floats8<T>(raw[u], v);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += (double)v[j] * (double)v[j];
         }
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u)
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s += (double)v[u][j] * (double)v[u][j];
     }
     s = block_sum(s, scratch);
     if (threadIdx.x == 0) parts[(int64_t)blockIdx.y * gridDim.x + blockIdx.x] = s;
@@ -90,26 +110,23 @@ __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t 
     const T* g = G + b * stride_g;
     const int64_t stride = (int64_t)gridDim.x * kRowThreads;
     for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < groups; i += kUnroll * stride) {
-        float v[kUnroll][8];
+        Raw8<T> raw[kUnroll];
         int64_t at[kUnroll];
-#pragma unroll
-        for (int u = 0; u < kUnroll; ++u) {
-            const int64_t k = i + u * stride, row = k / per_row, col = (k - row * per_row) * 8;
-            load8<T>(g + row * ldg + col, k < groups ? n - col : 0, vec != 0, v[u]);
-            at[u] = k < groups ? (b * m + row) * ldx + col : -1;
-        }
+        load_groups<T>(raw, at, g, i, stride, groups, per_row, n, ldg, vec, ldx);
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
             if (at[u] < 0) continue;
+            float v[8];
+            to_floats8<T>(raw[u], v);
             __half h[8], l[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float x = in32 ? v[u][j] * inv32 : (float)((double)v[u][j] * inv);
+                const float x = in32 ? v[j] * inv32 : (float)((double)v[j] * inv);
                 h[j] = __float2half_rn(x);
                 l[j] = __float2half_rn((x - __half2float(h[j])) * (float)(1 << kLoExp));
             }
-            *reinterpret_cast<uint4*>(hi + at[u]) = *reinterpret_cast<const uint4*>(h);      // (rows of the planes are padded)
-            *reinterpret_cast<uint4*>(lo + at[u]) = *reinterpret_cast<const uint4*>(l);
+            *reinterpret_cast<uint4*>(hi + b * m * ldx + at[u]) = *reinterpret_cast<const uint4*>(h);      // (rows of the planes are padded)
+            *reinterpret_cast<uint4*>(lo + b * m * ldx + at[u]) = *reinterpret_cast<const uint4*>(l);
         }
     }
 }
@@ -613,7 +630,7 @@ cudaError_t launch_start(const NewtonSchulzArgs& a, cudaStream_t st, int* launch
     double* parts = (double*)(a.ws + l.off_norm);
     const uint32_t per_row = (uint32_t)((a.n + 7) / 8);
     const int64_t groups = a.m * per_row, needed = (groups + kRowThreads - 1) / kRowThreads;
-    const int vec = ((uintptr_t)a.G & 15) == 0 && a.ldg * sizeof(T) % 16 == 0 && a.stride_g * sizeof(T) % 16 == 0;
+    const int vec = a.n % 8 == 0 && ((uintptr_t)a.G & 15) == 0 && a.ldg * sizeof(T) % 16 == 0 && a.stride_g * sizeof(T) % 16 == 0;
     // (by the matrix alone, so that its sums do not depend on the batch it is in; eight groups or more per thread)
     const int blocks = (int)((needed + 7) / 8 < kNormParts ? (needed + 7) / 8 : kNormParts);
     cudaError_t err = launch_chained(norm_kernel<T>, dim3(blocks, (unsigned)a.batch), dim3(kRowThreads), 0, st, (const T*)a.G, groups, per_row, a.n, a.ldg, a.stride_g, vec, parts);
