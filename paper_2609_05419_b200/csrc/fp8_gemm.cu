@@ -10,8 +10,7 @@
 #include "layer_ops.cuh"
 #include "pair_pipeline.cuh"
 
-#include <cuda_bf16.h>
-#include <cuda_fp16.h>
+#include <cmath>
 
 namespace gemm2m {
 
@@ -26,22 +25,25 @@ constexpr int kThreads = 32 * (kFirstEpilogueWarp + kEpilogueWarps);
 constexpr int kLaunchRegs = 168, kPipeRegs = 40, kEpilogueRegs = 232;
 static_assert(128 * kPipeRegs + 32 * kEpilogueWarps * kEpilogueRegs <= kThreads * kLaunchRegs, "register shares exceed what the block is launched with");
 
-// Ring of scale slots, one per block; a slot is written 3 blocks ahead.  A block's scales are there when its tfull barrier completes (the
-// two scale warps arrive on it next to the commit).  They turn to block g after tfull of block g - 2: the MMAs of g - 2 were issued
-// after every epilogue warp had released block g - 4, so all of them are through with block g - 5, whose slot is that of g + 3.
-constexpr int kSlots = 8, kAhead = 3, kScaleWarps = 2;
+// Ring of scale slots, one per block; a slot is written kAhead blocks ahead.  A block's scales are there when its tfull barrier completes
+// (the two scale warps arrive on it next to the commit).  They turn to block g after tfull of block g - NB (NB accumulators): the MMAs of
+// that block were issued after every epilogue warp had released block g - 2 NB, so all of them are through with g - 2 NB - 1 and
+// earlier ones: kSlots >= kAhead + 2 NB + 1.
+constexpr int kSlots = 16, kAhead = 3, kScaleWarps = 2;
 
 template <int BN, bool COLS>
 struct Cfg {
     static constexpr int kHalfRows = BN / 2;                          // rows of B per CTA
     static constexpr int kStageBytes = (kBM + kHalfRows) * kGemmBK;
-    static constexpr int kStages = 5;
+    static constexpr int kStages = BN == 256 ? 5 : 6;
     static constexpr int kCols = BN / 2;                              // columns per epilogue warp: totals per thread
-    static constexpr uint32_t kTmemCols = 2 * BN;
+    static constexpr int kBuffers = 512 / BN;
+    static_assert(kSlots >= kAhead + 2 * kBuffers + 1, "scale ring");
+    static constexpr uint32_t kTmemCols = 512;
     static constexpr int kSlotFloats = kBM + (COLS ? BN : 2);         // scales of one block: 128 rows, and the columns or their two halves
     static constexpr int kSlotBytes = (kSlotFloats * 4 + 15) / 16 * 16;
     static constexpr size_t kScaleBytes = (size_t)kSlots * kSlotBytes;
-    static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + kScaleBytes + PairPipe<kStages>::kBytes + 16 + kEpilogueWarps * 4096;
+    static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + kScaleBytes + PairPipe<kStages, kBuffers>::kBytes + 16 + kEpilogueWarps * 4096;
 };
 
 struct Fp8GemmParams {
@@ -153,7 +155,8 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     const uint32_t tiles_base = (raw + 1023u) & ~1023u;
     unsigned char* behind = smem_raw + (tiles_base - raw) + (size_t)STAGES * cfg::kStageBytes;
     const uint32_t scale_ring = smem_u32(behind);
-    PairPipe<STAGES> pipe;
+    constexpr int NB = cfg::kBuffers;
+    PairPipe<STAGES, NB> pipe;
     pipe.open(behind + cfg::kScaleBytes, kEpilogueWarps, 1 + kScaleWarps, cfg::kTmemCols, p.dev_status, p.wait_ns);
     wait_for_prior_kernels();
 
@@ -186,12 +189,12 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             if (!ok) pipe.tell_peer();
         } else if (warp == 1 && lane == 0 && pipe.rank == 0) {      // MMAs, leader
             RingPos<STAGES> at;
-            uint32_t it = 0;                              // block counter over all tiles: buffer it & 1, its use number it >> 1
+            uint32_t it = 0;                              // block counter over all tiles: buffer it % NB, its use number it / NB
             bool ok = true;
             for (int tile = pair; ok && tile < total_tiles; tile += npairs)
                 for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
-                    const uint32_t buf = it & 1u;
-                    if (!(ok = pipe.wait(pipe.tempty + 8 * buf, ((it >> 1) & 1u) ^ 1u, kDevTimeoutMma) &&
+                    const uint32_t buf = it % NB;
+                    if (!(ok = pipe.wait(pipe.tempty + 8 * buf, ((it / NB) & 1u) ^ 1u, kDevTimeoutMma) &&
                                pipe.wait(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
                     tcgen05_fence_after();
                     const uint32_t a_addr = tiles_base + at.stage * cfg::kStageBytes;
@@ -236,8 +239,8 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             const uint32_t blocks = pair < total_tiles ? (uint32_t)((total_tiles - pair + npairs - 1) / npairs) * (uint32_t)p.kblocks : 0u;
             bool ok = true;
             for (uint32_t g = 0; g < blocks; ++g) {
-                const uint32_t bar = pipe.tfull + 8 * (g & 1u);
-                if (g >= 2 && !(ok = __all_sync(0xffffffffu, pipe.wait(bar, ((g >> 1) & 1u) ^ 1u, kDevTimeoutProducer)))) break;
+                const uint32_t bar = pipe.tfull + 8 * (g % NB);
+                if (g >= NB && !(ok = __all_sync(0xffffffffu, pipe.wait(bar, ((g / NB) & 1u) ^ 1u, kDevTimeoutProducer)))) break;
                 fetch();
                 asm volatile("cp.async.wait_group %0;" ::"n"(kAhead) : "memory");
                 __syncwarp();
@@ -254,7 +257,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         const uint32_t row_slot = scale_ring + (uint32_t)(quarter * 32 + lane) * 4;
         const uint32_t col_slot = scale_ring + (uint32_t)(kBM + (COLS ? half * NC : half)) * 4;
         const uint32_t taddr = pipe.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)(half * NC);
-        const uint32_t turn = smem_u32(behind) + (uint32_t)(cfg::kScaleBytes + PairPipe<STAGES>::kBytes + 15) / 16 * 16 + (uint32_t)(warp - kFirstEpilogueWarp) * 4096;
+        const uint32_t turn = smem_u32(behind) + (uint32_t)(cfg::kScaleBytes + PairPipe<STAGES, NB>::kBytes + 15) / 16 * 16 + (uint32_t)(warp - kFirstEpilogueWarp) * 4096;
         const uint32_t leader_tempty = map_to_cta(pipe.tempty, 0);
         uint32_t it = 0;
         bool ok = true;
@@ -267,9 +270,9 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 #pragma unroll
             for (int i = 0; i < NC; ++i) acc[i] = 0.f;
             for (int kb = p.kblocks; kb > 0; --kb, ++it) {
-                const uint32_t buf = it & 1u;
+                const uint32_t buf = it % NB;
                 // (a wait that gives up is acted on at the end of the tile: every later one then returns at once)
-                ok &= pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue);
+                ok &= pipe.wait(pipe.tfull + 8 * buf, (it / NB) & 1u, kDevTimeoutEpilogue);
                 tcgen05_fence_after();
                 const uint32_t slot = (it & (kSlots - 1)) * cfg::kSlotBytes, col_scale = col_slot + slot;
                 float scale = lds(row_slot + slot);
@@ -578,15 +581,28 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         cluster_sync_all();                      // every rank's totals are there
         if (warp >= 4) {                         // this rank's share of the columns, added in the order of the ranks
             const int row = (int)threadIdx.x - 128, l = l0 + row;
-            const int from = N * rank / S, to = N * (rank + 1) / S;
-            if (l < p.lanes)
-                for (int j = from; j < to && c0 + j < p.cols; ++j) {
-                    float s = 0.f;
-                    for (int q = 0; q < S; ++q)
-                        s += __uint_as_float(ld_cluster_u32(map_to_cta(tiles_base + (uint32_t)(j * kBM + row) * 4, (uint32_t)q)));
-                    const int64_t dj = (int64_t)l * p.d_lane + (int64_t)(c0 + j) * p.d_col, cj = (int64_t)l * p.c_lane + (int64_t)(c0 + j) * p.c_col;
-                    ((T*)p.D)[dj] = to_type<T>(s + (p.C ? from_type<T>(((const T*)p.C)[cj]) : 0.f));
+            // (S, a power of two up to 8, divides 16: sixteen remote loads in flight are 16 / S whole columns)
+            const int from = N / S * rank;
+#pragma unroll 1
+            for (int t0 = 0; t0 < N; t0 += 16) {
+                float v[16], s = 0.f;
+                const int j0 = from + t0 / S;
+                if (c0 + j0 >= p.cols) break;
+#pragma unroll
+                for (int u = 0; u < 16; ++u)
+                    v[u] = __uint_as_float(ld_cluster_u32(map_to_cta(tiles_base + (uint32_t)((j0 + u / S) * kBM + row) * 4, (uint32_t)(u & (S - 1)))));
+#pragma unroll
+                for (int u = 0; u < 16; ++u) {
+                    s += v[u];
+                    if (((u + 1) & (S - 1)) != 0) continue;
+                    const int j = c0 + j0 + u / S;
+                    if (l < p.lanes && j < p.cols) {
+                        const int64_t dj = (int64_t)l * p.d_lane + (int64_t)j * p.d_col, cj = (int64_t)l * p.c_lane + (int64_t)j * p.c_col;
+                        ((T*)p.D)[dj] = to_type<T>(s + (p.C ? from_type<T>(((const T*)p.C)[cj]) : 0.f));
+                    }
+                    s = 0.f;
                 }
+            }
         }
         cluster_sync_all();                      // nobody leaves while its totals are being read
     }
@@ -596,14 +612,19 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     }
 }
 
-// Whether the 256 x 256 tiles of CTA pairs are used.
-bool takes_pair(const Fp8GemmArgs& a, int sm_count) {
-    const int64_t tiles = ((a.m + 255) / 256) * ((a.n + 255) / 256);
-    return a.m > 64 && a.n > 64 && tiles >= sm_count / 2;
+// Time of a product in microseconds by each kind of tile, from measurements (B200, 1.7 to 1.9 GHz): `round` tiles run at once, each takes
+// so much per block of k and for its output, and a launch takes the rest.  (256 x 256 tiles per pair: 1024 x 4096 x 4096, one round of 32 blocks, 27 us,
+// 2048^3 18 us; 256 x 128: 512 x 4096 x 4096 21 us, 1001 x 1999 x 1100, nine blocks, 14 us; CTAs of their own, 128 x 128 with k split in
+// four: 128 x 4096 x 4096 16 us, 256 x 4096 x 4096 split in two 21.5 us.)
+double pair_cost(const Fp8GemmArgs& a, int width, int sm_count) {
+    const double tiles = (double)((a.m + 255) / 256) * (double)((a.n + width - 1) / width), rounds = std::ceil(tiles / (sm_count / 2));
+    const double blocks = (double)((a.k + kScaleBlock - 1) / kScaleBlock), cols = a.B.block == 1;
+    if (width == 256) return 9.0 + rounds * (blocks * (0.53 + 0.17 * cols) + 2.0);
+    return 9.0 + rounds * (blocks * ((rounds > 1 ? 0.40 : 0.30) + 0.17 * cols) + 1.5);
 }
 
 // How often the blocks of k are split: the least number of rounds of CTAs, each weighed by its length, over the SMs; at least two blocks each.
-int thin_split(int64_t tiles, int64_t kblocks, int sm_count) {
+int thin_split(int64_t tiles, int64_t kblocks, int sm_count, double* cost_out) {
     int best = 1;
     double best_cost = 1e30;
     for (int S = 1; S <= kMostSplit; S *= 2) {
@@ -612,6 +633,7 @@ int thin_split(int64_t tiles, int64_t kblocks, int sm_count) {
         const double cost = (double)rounds * ((double)((kblocks + S - 1) / S) + 6.0);      // a round's fixed part is about six blocks
         if (cost < best_cost * 0.999) { best = S; best_cost = cost; }
     }
+    if (cost_out) *cost_out = best_cost;
     return best;
 }
 
@@ -641,18 +663,30 @@ cudaError_t launch_thin(const Fp8GemmArgs& a, bool swapped, int sm_count, cudaSt
     p.dev_status = a.dev_status;
     p.wait_ns = kWaitLimitNs;
     const int64_t tiles = (int64_t)p.lane_tiles * ((p.cols + N - 1) / N);
-    const int S = thin_split(tiles, p.kblocks, sm_count);
+    const int S = thin_split(tiles, p.kblocks, sm_count, nullptr);
     if (tiles * S > INT32_MAX) return cudaErrorInvalidValue;
     cudaError_t err = launch_chained_cluster(fp8_gemm_thin_kernel<T, N>, dim3((unsigned)(tiles * S)), dim3(kThinThreads), cfg::kSmem, S, st, map_l, map_c, p);
     if (err == cudaSuccess) ++*launches;
     return err;
 }
 
+template <typename T, int BN>
+cudaError_t launch_pair_scales(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
+    return a.B.block == 1 ? launch_pair<T, BN, true>(a, sm_count, st, launches) : launch_pair<T, BN, false>(a, sm_count, st, launches);
+}
+
 template <typename T>
 cudaError_t launch_typed(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
-    if (takes_pair(a, sm_count)) return a.B.block == 1 ? launch_pair<T, 256, true>(a, sm_count, st, launches) : launch_pair<T, 256, false>(a, sm_count, st, launches);
     const bool swapped = !(a.n <= 64 && a.m > a.n);        // lanes run along the rows of B, so that stores run along rows of D, unless B has few
-    const int64_t cols = swapped ? a.m : a.n;
+    const int64_t cols = swapped ? a.m : a.n, lanes = swapped ? a.n : a.m;
+    if (cols > 64) {                                       // (up to 64 columns a narrower tile reads the lane operand once, which is all there is to do)
+        double thin;
+        thin_split((lanes + kBM - 1) / kBM * ((cols + 127) / 128), (a.k + kScaleBlock - 1) / kScaleBlock, sm_count, &thin);
+        thin = 8.5 + 0.53 * thin;
+        const double wide = pair_cost(a, 256, sm_count), narrow = pair_cost(a, 128, sm_count);
+        if (wide <= narrow && wide <= thin) return launch_pair_scales<T, 256>(a, sm_count, st, launches);
+        if (narrow <= thin) return launch_pair_scales<T, 128>(a, sm_count, st, launches);
+    }
     if (cols <= 16) return launch_thin<T, 16>(a, swapped, sm_count, st, launches);
     if (cols <= 32) return launch_thin<T, 32>(a, swapped, sm_count, st, launches);
     if (cols <= 64) return launch_thin<T, 64>(a, swapped, sm_count, st, launches);

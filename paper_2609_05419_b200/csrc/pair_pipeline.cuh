@@ -18,7 +18,8 @@ __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
-template <int STAGES>
+// STAGES of operands, BUFFERS of accumulators.
+template <int STAGES, int BUFFERS = 2>
 struct PairPipe {
     uint32_t full, empty, tfull, tempty, drain;      // shared-memory addresses of the barriers
     uint32_t* tmem_slot;
@@ -29,7 +30,7 @@ struct PairPipe {
     int* dev_status;
     unsigned long long wait_ns;
 
-    static constexpr size_t kBytes = 8 * (2 * STAGES + 5) + 16 + 4 * STAGES;
+    static constexpr size_t kBytes = 8 * (2 * STAGES + 2 * BUFFERS + 1) + 16 + 4 * STAGES;
 
     // All threads.  `mem`: kBytes of shared memory, 8-byte aligned; warp 1 allocates the TMEM columns.  tfull_arrivals: the commit
     // and whatever else of this CTA an accumulator waits for before its epilogue.
@@ -38,9 +39,9 @@ struct PairPipe {
         full = smem_u32(bars);
         empty = full + 8 * STAGES;
         tfull = empty + 8 * STAGES;
-        tempty = tfull + 16;
-        drain = tempty + 16;
-        tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
+        tempty = tfull + 8 * BUFFERS;
+        drain = tempty + 8 * BUFFERS;
+        tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 2 * BUFFERS + 1);
         abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
         fills_issued = reinterpret_cast<volatile uint32_t*>(tmem_slot + 2);
         fill_bytes = reinterpret_cast<volatile uint32_t*>(tmem_slot + 3);
@@ -49,7 +50,7 @@ struct PairPipe {
         wait_ns = limit;
         if (threadIdx.x == 0) {
             for (int s = 0; s < STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
-            for (int a = 0; a < 2; ++a) { mbar_init(tfull + 8 * a, tfull_arrivals); mbar_init(tempty + 8 * a, 2 * epilogue_warps); }
+            for (int a = 0; a < BUFFERS; ++a) { mbar_init(tfull + 8 * a, tfull_arrivals); mbar_init(tempty + 8 * a, 2 * epilogue_warps); }
             mbar_init(drain, 1);
             *abort_flag = 0;
             *fills_issued = 0;
