@@ -166,7 +166,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
 
     if (warp < kFirstEpilogueWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPipeRegs));
-        if (warp == 0 && lane == 0) {                     // copies, both CTAs
+        if (warp == 0) {                                  // copies, both CTAs
             const uint32_t leader_full = map_to_cta(pipe.full, 0);
             RingPos<STAGES> at;
             uint32_t fills = 0;
@@ -176,37 +176,43 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
                 tile_at(p, tile, &tr, &tc);
                 const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM, col0 = tc * BN + (int)pipe.rank * cfg::kHalfRows;
                 for (int kb = 0; kb < p.kblocks; ++kb) {
-                    if (!(ok = pipe.wait(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
+                    if (!(ok = pipe.wait_warp(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
                     const uint32_t dst = tiles_base + at.stage * cfg::kStageBytes;
-                    pipe.announce(at.stage, cfg::kStageBytes);
-                    tma_load_2d_pair(dst, &map_a, leader_full + 8 * at.stage, kb * kGemmBK, row0);
-                    tma_load_2d_pair(dst + kBM * kGemmBK, &map_b, leader_full + 8 * at.stage, kb * kGemmBK, col0);
+                    if (elect_one()) {
+                        pipe.announce(at.stage, cfg::kStageBytes);
+                        tma_load_2d_pair(dst, &map_a, leader_full + 8 * at.stage, kb * kGemmBK, row0);
+                        tma_load_2d_pair(dst + kBM * kGemmBK, &map_b, leader_full + 8 * at.stage, kb * kGemmBK, col0);
+                    }
+                    __syncwarp();
                     ++fills;
                     at.next();
                 }
             }
-            *pipe.fills_issued = fills;
-            if (!ok) pipe.tell_peer();
-        } else if (warp == 1 && lane == 0 && pipe.rank == 0) {      // MMAs, leader
+            if (lane == 0) *pipe.fills_issued = fills;
+            if (!ok && lane == 0) pipe.tell_peer();
+        } else if (warp == 1 && pipe.rank == 0) {         // MMAs, leader
             RingPos<STAGES> at;
             uint32_t it = 0;                              // block counter over all tiles: buffer it % NB, its use number it / NB
             bool ok = true;
             for (int tile = pair; ok && tile < total_tiles; tile += npairs)
                 for (int kb = 0; kb < p.kblocks; ++kb, ++it) {
                     const uint32_t buf = it % NB;
-                    if (!(ok = pipe.wait(pipe.tempty + 8 * buf, ((it / NB) & 1u) ^ 1u, kDevTimeoutMma) &&
-                               pipe.wait(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
+                    if (!(ok = pipe.wait_warp(pipe.tempty + 8 * buf, ((it / NB) & 1u) ^ 1u, kDevTimeoutMma) &&
+                               pipe.wait_warp(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
                     tcgen05_fence_after();
                     const uint32_t a_addr = tiles_base + at.stage * cfg::kStageBytes;
                     const uint64_t adesc = make_smem_desc(a_addr), bdesc = make_smem_desc(a_addr + kBM * kGemmBK);
+                    if (elect_one()) {
 #pragma unroll
-                    for (int k4 = 0; k4 < 4; ++k4)
-                        umma_f8_pair(pipe.tmem + buf * BN, adesc + (uint64_t)(k4 * 2), bdesc + (uint64_t)(k4 * 2), p.idesc, (uint32_t)(k4 != 0));
-                    umma_commit_pair(pipe.empty + 8 * at.stage, 3);
-                    umma_commit_pair(pipe.tfull + 8 * buf, 3);
+                        for (int k4 = 0; k4 < 4; ++k4)
+                            umma_f8_pair(pipe.tmem + buf * BN, adesc + (uint64_t)(k4 * 2), bdesc + (uint64_t)(k4 * 2), p.idesc, (uint32_t)(k4 != 0));
+                        umma_commit_pair(pipe.tfull + 8 * buf, 3);
+                        umma_commit_pair(pipe.empty + 8 * at.stage, 3);
+                    }
+                    __syncwarp();
                     at.next();
                 }
-            if (!ok) pipe.tell_peer();
+            if (!ok && lane == 0) pipe.tell_peer();
         } else if (warp >= 2) {                           // scales, both CTAs: asynchronous 4-byte copies, one group per block
             const int t = threadIdx.x - 64;
             int tile = pair, kb = 0, row0 = 0, col0 = 0;  // next block to fetch
@@ -452,35 +458,37 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
 
     float acc[N];
     if (warp == 0) {
-        if (lane == 0) {
-            RingPos<STAGES> at;
-            int kb = 0;
-            for (; kb < blocks; ++kb) {
-                if (!wait(empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer)) break;
-                const uint32_t dst = tiles_base + at.stage * cfg::kStageBytes, bar = full + 8 * at.stage;
+        RingPos<STAGES> at;
+        int kb = 0;
+        for (; kb < blocks; ++kb) {
+            if (!__all_sync(0xffffffffu, wait(empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
+            const uint32_t dst = tiles_base + at.stage * cfg::kStageBytes, bar = full + 8 * at.stage;
+            if (elect_one()) {
                 mbar_arrive_expect_tx(bar, cfg::kStageBytes);
                 tma_load_2d(dst, &map_l, bar, (kb0 + kb) * kGemmBK, l0);
                 tma_load_2d(dst + kBM * kGemmBK, &map_c, bar, (kb0 + kb) * kGemmBK, c0);
-                at.next();
             }
-            *fills_issued = (uint32_t)kb;
+            __syncwarp();
+            at.next();
         }
+        if (lane == 0) *fills_issued = (uint32_t)kb;
     } else if (warp == 1) {
-        if (lane == 0) {
-            RingPos<STAGES> at;
-            for (int kb = 0; kb < blocks; ++kb) {
-                const uint32_t buf = kb % kThinBuffers, use = kb / kThinBuffers;
-                if (!wait(tempty + 8 * buf, (use & 1u) ^ 1u, kDevTimeoutMma) || !wait(full + 8 * at.stage, at.phase, kDevTimeoutMma)) break;
-                tcgen05_fence_after();
-                const uint32_t a_addr = tiles_base + at.stage * cfg::kStageBytes;
-                const uint64_t adesc = make_smem_desc(a_addr), bdesc = make_smem_desc(a_addr + kBM * kGemmBK);
+        RingPos<STAGES> at;
+        for (int kb = 0; kb < blocks; ++kb) {
+            const uint32_t buf = kb % kThinBuffers, use = kb / kThinBuffers;
+            if (!__all_sync(0xffffffffu, wait(tempty + 8 * buf, (use & 1u) ^ 1u, kDevTimeoutMma) && wait(full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
+            tcgen05_fence_after();
+            const uint32_t a_addr = tiles_base + at.stage * cfg::kStageBytes;
+            const uint64_t adesc = make_smem_desc(a_addr), bdesc = make_smem_desc(a_addr + kBM * kGemmBK);
+            if (elect_one()) {
 #pragma unroll
                 for (int k4 = 0; k4 < 4; ++k4)
                     umma_f8(tmem + buf * N, adesc + (uint64_t)(k4 * 2), bdesc + (uint64_t)(k4 * 2), p.idesc, (uint32_t)(k4 != 0));
-                umma_commit(empty + 8 * at.stage);
                 umma_commit(tfull + 8 * buf);
-                at.next();
+                umma_commit(empty + 8 * at.stage);
             }
+            __syncwarp();
+            at.next();
         }
     } else if (warp < 4) {                       // scales: asynchronous 4-byte copies, one group per block
         const int t = threadIdx.x - 64;
@@ -564,8 +572,8 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     tcgen05_fence_before();
     __syncthreads();
     if (*abort_flag) {                           // nothing may be in flight when shared memory and TMEM go away; both waits are bounded
-        if (warp == 1 && lane == 0) {
-            umma_commit(drain);
+        if (warp == 1) {
+            if (elect_one()) umma_commit(drain);         // by the lane that issued the MMAs
             mbar_wait_quiet(drain, 0, kDrainLimitNs);
         }
         if (warp == 0 && lane == 0) {

@@ -463,7 +463,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
 
     if (warp < kFirstEpilogueWarp) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kPipeRegs));
-        if (warp == 0 && lane == 0) {                     // copies, both CTAs
+        if (warp == 0) {                                  // copies, both CTAs
             const uint32_t leader_full = map_to_cta(pipe.full, 0);
             RingPos<kStages> at;
             uint32_t fills = 0;
@@ -473,7 +473,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                 if (pair >= q.tiles * p.batch) continue;
                 asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_a) : "memory");
                 asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_b) : "memory");
-                if (!(ok = wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag))) break;
+                if (!(ok = __all_sync(0xffffffffu, wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag)))) break;
                 asm volatile("fence.proxy.async.global;" ::: "memory");       // the other CTAs' stores, then this thread's bulk copies
                 const int half_rows = q.bn / 2;
                 for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs) {
@@ -481,19 +481,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                     tile_at(q, tile, &b, &tr, &tc);
                     const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM, col0 = tc * q.bn + (int)pipe.rank * half_rows;
                     for (int kb = 0; kb < q.kblocks; ++kb) {
-                        if (!(ok = pipe.wait(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
+                        if (!(ok = pipe.wait_warp(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
                         const uint32_t dst = tiles_base + at.stage * kStageBytes;
-                        pipe.announce(at.stage, (uint32_t)(kBM + max(half_rows, 64)) * 128u);      // (a copy is 64 rows, also where half of them are used)
-                        load_operand(dst, q.map_a, leader_full + 8 * at.stage, q.turned_a, kb, row0, kBM, b);
-                        load_operand(dst + kBM * 128, q.map_b, leader_full + 8 * at.stage, q.turned_b, kb, col0, half_rows, b);
+                        if (elect_one()) {
+                            pipe.announce(at.stage, (uint32_t)(kBM + max(half_rows, 64)) * 128u);      // (a copy is 64 rows, also where half of them are used)
+                            load_operand(dst, q.map_a, leader_full + 8 * at.stage, q.turned_a, kb, row0, kBM, b);
+                            load_operand(dst + kBM * 128, q.map_b, leader_full + 8 * at.stage, q.turned_b, kb, col0, half_rows, b);
+                        }
+                        __syncwarp();
                         ++fills;
                         at.next();
                     }
                 }
             }
-            *pipe.fills_issued = fills;
-            if (!ok) pipe.tell_peer();
-        } else if (warp == 1 && lane == 0 && pipe.rank == 0) {      // MMAs, leader
+            if (lane == 0) *pipe.fills_issued = fills;
+            if (!ok && lane == 0) pipe.tell_peer();
+        } else if (warp == 1 && pipe.rank == 0) {         // MMAs, leader
             RingPos<kStages> at;
             uint32_t it = 0;                              // tile counter: buffer it & 1, its use number it >> 1
             bool ok = true;
@@ -504,23 +507,27 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                 const uint64_t step_a = q.turned_a ? 128 : 2, step_b = q.turned_b ? 128 : 2;
                 for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs, ++it) {
                     const uint32_t buf = it & 1u;
-                    if (!(ok = pipe.wait(pipe.tempty + 8 * buf, ((it >> 1) & 1u) ^ 1u, kDevTimeoutMma))) break;
+                    if (!(ok = pipe.wait_warp(pipe.tempty + 8 * buf, ((it >> 1) & 1u) ^ 1u, kDevTimeoutMma))) break;
                     for (int kb = 0; kb < q.kblocks; ++kb) {
-                        if (!(ok = pipe.wait(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
+                        if (!(ok = pipe.wait_warp(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
                         tcgen05_fence_after();
                         const uint32_t a_addr = tiles_base + at.stage * kStageBytes, b_addr = a_addr + kBM * 128;
                         const uint64_t adesc = q.turned_a ? make_smem_desc_turned(a_addr) : make_smem_desc(a_addr);
                         const uint64_t bdesc = q.turned_b ? make_smem_desc_turned(b_addr) : make_smem_desc(b_addr);
+                        if (elect_one()) {
 #pragma unroll
-                        for (int k4 = 0; k4 < 4; ++k4)
-                            umma_f16_pair(pipe.tmem + buf * 256, adesc + k4 * step_a, bdesc + k4 * step_b, idesc, (uint32_t)((kb | k4) != 0));
-                        umma_commit_pair(pipe.empty + 8 * at.stage, 3);
+                            for (int k4 = 0; k4 < 4; ++k4)
+                                umma_f16_pair(pipe.tmem + buf * 256, adesc + k4 * step_a, bdesc + k4 * step_b, idesc, (uint32_t)((kb | k4) != 0));
+                            umma_commit_pair(pipe.empty + 8 * at.stage, 3);
+                        }
+                        __syncwarp();
                         at.next();
                     }
-                    if (ok) umma_commit_pair(pipe.tfull + 8 * buf, 3);
+                    if (ok && elect_one()) umma_commit_pair(pipe.tfull + 8 * buf, 3);
+                    __syncwarp();
                 }
             }
-            if (!ok) pipe.tell_peer();
+            if (!ok && lane == 0) pipe.tell_peer();
         }
     } else {
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));

@@ -18,6 +18,15 @@ __device__ __forceinline__ void mbar_arrive_relaxed(uint32_t cluster_addr) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_addr) : "memory");
 }
 
+// One lane of a converged warp, the same every time.  The loops that issue copies and MMAs run converged and pick their lane around
+// the instructions only: a loop that one lane runs alone costs 350 cycles per stage of two copies (the compiler guards every
+// instruction that takes uniform operands), a converged one 190.
+__device__ __forceinline__ bool elect_one() {
+    uint32_t one;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(one));
+    return one != 0;
+}
+
 // STAGES of operands, BUFFERS of accumulators.
 template <int STAGES, int BUFFERS = 2>
 struct PairPipe {
@@ -69,6 +78,8 @@ struct PairPipe {
         peer_abort = map_to_cta(smem_u32(const_cast<int*>(abort_flag)), rank ^ 1u);
     }
     __device__ __forceinline__ bool wait(uint32_t bar, uint32_t parity, int code) const { return mbar_wait(bar, parity, abort_flag, dev_status, code, wait_ns); }
+    // The same for a converged warp, which stays so.
+    __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, int code) const { return __all_sync(0xffffffffu, wait(bar, parity, code)); }
     // A role that gave up tells the peer; its own CTA's flag is set by the wait (or was seen there).
     __device__ __forceinline__ void tell_peer() const { st_cluster_u32(peer_abort, 1u); }
     // Producer: `bytes` are about to be copied into this CTA's stage; the leader announces both CTAs' (they load alike).
@@ -93,8 +104,8 @@ struct PairPipe {
         __syncthreads();
         cluster_sync_all();
         if (*abort_flag) {                               // both CTAs agree: a flag is set in both before this point
-            if (warp == 1 && lane == 0 && rank == 0) {
-                umma_commit_pair(drain, 1);
+            if (warp == 1 && rank == 0) {
+                if (elect_one()) umma_commit_pair(drain, 1);      // by the lane that issued the MMAs
                 mbar_wait_quiet(drain, 0, kDrainLimitNs);
             }
             if (warp == 0 && lane == 0 && rank == 0) {
