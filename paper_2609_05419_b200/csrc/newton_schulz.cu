@@ -250,13 +250,13 @@ __device__ __forceinline__ void tile_at(const Phase& q, int t, int* b, int* tr, 
 
 // Waits (bounded) until `target` CTAs in all have finished their phases, and sees what they wrote.  (The look itself is relaxed: an
 // acquire every time would empty the SM's L1 under the warps that still work.)
-__device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t target, volatile int* abort_flag) {
+__device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t target, volatile int* abort_flag, bool patient) {
     const unsigned long long t0 = global_timer_ns();
     for (uint32_t spins = 1;; ++spins) {
         uint32_t seen;
         asm volatile("ld.relaxed.gpu.global.u32 %0, [%1];" : "=r"(seen) : "l"(p.phase_count) : "memory");
         if (seen >= target) break;
-        __nanosleep(40);
+        if (patient) __nanosleep(100);                    // (the epilogue warps have the first tile's products to wait for; the copies have not)
         if ((spins & 63u) == 0) {
             if (*abort_flag) return false;
             if (global_timer_ns() - t0 > p.wait_ns) {
@@ -471,14 +471,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             for (int ph = 0; ok && ph < phases; ++ph) {
                 const Phase q = phase_at(p, ph / 3, ph % 3);
                 if (pair >= q.tiles * p.batch) continue;
+                const int half_rows = q.bn / 2;
+                int b, tr, tc;
+                tile_at(q, pair, &b, &tr, &tc);
                 asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_a) : "memory");
                 asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_b) : "memory");
-                if (!(ok = __all_sync(0xffffffffu, wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag)))) break;
+                if (!(ok = __all_sync(0xffffffffu, wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag, false)))) break;
                 asm volatile("fence.proxy.async.global;" ::: "memory");       // the other CTAs' stores, then this thread's bulk copies
-                const int half_rows = q.bn / 2;
                 for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs) {
-                    int b, tr, tc;
-                    tile_at(q, tile, &b, &tr, &tc);
+                    if (tile != pair) tile_at(q, tile, &b, &tr, &tc);
                     const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM, col0 = tc * q.bn + (int)pipe.rank * half_rows;
                     for (int kb = 0; kb < q.kblocks; ++kb) {
                         if (!(ok = pipe.wait_warp(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
@@ -541,7 +542,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             const int step = ph / 3;
             const Phase q = phase_at(p, step, ph % 3);
             if (ok) {                                     // (without tiles too: a CTA is counted for a phase only after the phases before it)
-                ok = lane != 0 || wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag);
+                ok = lane != 0 || wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag, true);
                 ok = __all_sync(0xffffffffu, ok);         // lane 0 has acquired the other CTAs' stores, and the warp with it
             }
             const int nc = q.bn / 2;
