@@ -384,6 +384,7 @@ __device__ __forceinline__ float finish_block(const NsParams& p, const Phase& q,
         }
     } else {
         const float lin = ca + g * (cb + cc * g);
+        const bool traced = step + 3 >= p.steps;          // the next step is one of the last two, which shift
         uint2 ol[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -398,7 +399,7 @@ __device__ __forceinline__ float finish_block(const NsParams& p, const Phase& q,
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     l[j] = (f[j] - h[j]) * (float)(1 << kLoExp);
-                    if (r0 + 4 * i < here.rows && here.col + j < q.N) sum += f[j] * f[j];
+                    if (traced && r0 + 4 * i < here.rows && here.col + j < q.N) sum += f[j] * f[j];
                 }
                 ol[i] = to_halves(l);
             } else {
@@ -581,7 +582,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                             }
                         });
                     // one partial sum per block, whatever the tile width: results do not depend on that choice
-                    if (q.mode == kUpdate) {
+                    if (q.mode == kUpdate && step + 3 >= p.steps) {
 #pragma unroll
                         for (int d = 16; d > 0; d >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, d);
                         const int part_row = row0 >> 5, part_col = (col0 + c) >> 5, cols = (q.N + 31) >> 5;
@@ -651,15 +652,14 @@ cudaError_t launch_start(const NewtonSchulzArgs& a, cudaStream_t st, int* launch
     return err;
 }
 
-// Columns of a product's tiles (index 0, 1, 2: 64, 128, 256), by the time of the pair that finishes last.  A tile's copies and MMAs take, per 64
-// inner entries, what the SMs can draw from L2 (about 46 bytes per SM and cycle at 1.7 GHz: 710 cycles for a wide tile's 32 KB per
-// CTA, 580 for the others' 24 KB); its epilogue about 3300 cycles per 32 columns of a warp.  The longer of the two counts for every
-// tile, the shorter once.
+// Columns of a product's tiles (index 0, 1, 2: 64, 128, 256), by the time of the pair that finishes last.  A tile's copies and MMAs take,
+// per 64 inner entries, about 370, 400 or 560 cycles (1000 x 4096: 370 for 64 columns; 4096^2, all SMs: 560 for 256), its epilogue
+// 3600 per 32 columns of a warp.  The longer of the two counts for every tile, the shorter once.
 int best_width(const int64_t (&tiles)[3], int64_t kblocks, int64_t pairs) {
     int best = 0;
     double least = 0.0;
     for (int w = 0; w < 3; ++w) {
-        const double rounds = (double)((tiles[w] + pairs - 1) / pairs), feed = (double)kblocks * (w == 2 ? 710.0 : 580.0), finish = 3300.0 * (double)(1 << w);
+        const double rounds = (double)((tiles[w] + pairs - 1) / pairs), feed = (double)kblocks * (w == 2 ? 560.0 : w == 1 ? 400.0 : 370.0), finish = 3600.0 * (double)(1 << w);
         const double cost = rounds * (feed > finish ? feed : finish) + (feed > finish ? finish : feed);
         if (w == 0 || cost < least) { best = w; least = cost; }
     }
