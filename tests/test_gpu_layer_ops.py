@@ -148,6 +148,35 @@ def test_product(m, n, k, ab, bb):
         check_product(m, n, k, ab, bb)
 
 
+# more tiles than fit the GPU at once, in tiles of either width, with ragged edges
+@pytest.mark.parametrize("m,n,k", [(2100, 1300, 700), (4100, 4300, 257), (2500, 2600, 1000), (9000, 200, 384), (130, 20000, 130)])
+@pytest.mark.parametrize("bb,dtype", [(128, torch.bfloat16), (1, torch.float32)])
+def test_product_of_many_tiles(m, n, k, bb, dtype):
+    with Workspace(b.workspace_bytes(b.OP_FP8_GEMM, m, n, k, 1)):
+        check_product(m, n, k, 1, bb, dtype=dtype, add=bb == 1)
+
+
+def test_offsets_beyond_32_bits():
+    m, n, k = 66000, 33100, 48                                    # m n > 2^31
+    qa, sa = operand(m, k, 1, b.E4M3, 91)
+    qb, sb = operand(n, k, 128, b.E4M3, 92)
+    d = torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+    with Workspace(b.workspace_bytes(b.OP_FP8_GEMM, m, n, k, 1)):
+        b.fp8_gemm(qa, sa, qb, sb, d)
+    rows = torch.tensor([0, 1, 32767, 64999, m - 1], device="cuda")
+    want = (qa[rows].double() * sa[rows].double()) @ (qb.double() * spread(sb, 128, n, k)).t()
+    assert float((d[rows].double() - want).abs().max()) <= 2.0 ** -7 * float(want.abs().max())
+    q, s = b.fp8_empty(m, n)
+    qt, st = b.fp8_empty(n, m)
+    b.fp8_quantise(d, q, s, qt, st)                               # the last rows and columns against a call of their own
+    q1, s1 = b.fp8_empty(100, n)
+    b.fp8_quantise(d[-100:], q1, s1)
+    assert torch.equal(q[-100:].view(torch.uint8), q1.view(torch.uint8)) and torch.equal(s[-100:], s1)
+    q2, s2 = b.fp8_empty(100, m)
+    b.fp8_quantise(d[:, -100:], None, None, q2, s2)
+    assert torch.equal(qt[-100:].view(torch.uint8), q2.view(torch.uint8)) and torch.equal(st[-100:], s2)
+
+
 @pytest.mark.parametrize("m,n,k", [(3, 300, 700), (200, 300, 700), (600, 1030, 900)])
 @pytest.mark.parametrize("fa,fb", [(b.E5M2, b.E4M3), (b.E4M3, b.E5M2), (b.E5M2, b.E5M2)])
 @pytest.mark.parametrize("dtype", [torch.float32, torch.float16])
@@ -264,6 +293,18 @@ def check_newton_schulz(g, o, **how):
     assert rel <= ns_room(g.numel()), rel
 
 
+# several tiles per pair, every tile width, both orientations, many matrices
+@pytest.mark.parametrize("batch,m,n", [(1, 1500, 2300), (1, 2304, 1100), (40, 200, 260), (12, 700, 600), (1, 2500, 2500)])
+def test_newton_schulz_of_many_tiles(batch, m, n):
+    g = torch.stack([update(m, n, "flat" if i % 2 else "falling", 100 + i) for i in range(batch)])
+    o = torch.full((batch, m, n), float("nan"), dtype=torch.bfloat16, device="cuda")
+    with Workspace(b.workspace_bytes(b.OP_NEWTON_SCHULZ, m, n, batch, 1)):
+        b.newton_schulz(g, o)
+        b.device_status()
+    for i in range(0, batch, 5):
+        check_newton_schulz(g[i], o[i])
+
+
 NS_SHAPES = [(1, 1), (1, 200), (130, 1), (2, 3), (17, 17), (64, 64), (100, 300), (300, 100), (128, 256), (257, 129), (256, 256), (511, 700), (1030, 520)]
 
 
@@ -330,6 +371,39 @@ def test_newton_schulz_in_place_tiny_huge_and_non_finite(m, n):
             h[3, 5] = bad
             b.newton_schulz(h, o)
             assert bool(torch.isnan(o).all())
+
+
+def test_one_graph_of_copies_quantisation_product_and_newton_schulz():
+    m, n, k = 200, 300, 256
+    x, w = torch.randn(m, k, device="cuda"), torch.randn(n, k, device="cuda")
+    staged, qa, sa = torch.empty_like(x), *b.fp8_empty(m, k)
+    qb, sb = b.fp8_empty(n, k, block_rows=128)
+    d, o = torch.empty(m, n, device="cuda"), torch.empty(m, n, dtype=torch.bfloat16, device="cuda")
+
+    def step():
+        staged.copy_(x)                                             # a copy in front of a kernel that is launched as a dependent
+        b.fp8_quantise(staged, qa, sa)
+        b.fp8_quantise(w, qb, sb, block_rows=128)
+        b.fp8_gemm(qa, sa, qb, sb, d)
+        b.newton_schulz(d, o)
+
+    with Workspace(max(b.workspace_bytes(b.OP_FP8_GEMM, m, n, k, 1), b.workspace_bytes(b.OP_NEWTON_SCHULZ, m, n, 1, 1))):
+        step()
+        want = o.clone()
+        x2 = torch.randn(m, k, device="cuda")
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want)                                 # bit for bit, and again with other inputs
+        x.copy_(x2)
+        graph.replay()
+        got = o.clone()
+        step()
+        b.device_status()
+        assert torch.equal(o, got) and not torch.equal(got, want)
 
 
 def test_newton_schulz_singular_values_and_small_workspace():
