@@ -145,7 +145,7 @@ constexpr int kLaunchRegs = 168, kPipeRegs = 40, kEpilogueRegs = 232;
 static_assert(128 * kPipeRegs + 32 * kEpilogueWarps * kEpilogueRegs <= kGemmThreads * kLaunchRegs, "register shares exceed what the block is launched with");
 constexpr int kMaxSteps = 64;
 constexpr size_t kPipeBytes = (PairPipe<kStages>::kBytes + 15) / 16 * 16;
-constexpr size_t kGemmSmem = (size_t)kStages * kStageBytes + 1024 + kPipeBytes + kEpilogueWarps * 4096;
+constexpr size_t kGemmSmem = (size_t)kStages * kStageBytes + 1024 + kPipeBytes;
 
 enum Mode { kGram, kPoly, kUpdate, kLast };
 
@@ -270,165 +270,124 @@ __device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t targe
     return true;
 }
 
-struct alignas(8) Bf4 { __nv_bfloat16 h[4]; };
+// A block of 32 x 32 accumulators is finished row by row: a lane has one row's 32 columns, 64 bytes of a half-precision plane, which it
+// reads and writes as two whole sectors.  (Planes have padded rows, so that 32 columns can always be touched; what lies in the padding
+// is not used.  Turning the block in shared memory so that eight lanes share a row takes as many sectors and twice the
+// instructions.)
+struct Row32 { uint32_t w[16]; };                         // 32 halves
+__device__ __forceinline__ void load_row(const __half* p, Row32& r) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 8)
+        asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                     : "=r"(r.w[i]), "=r"(r.w[i + 1]), "=r"(r.w[i + 2]), "=r"(r.w[i + 3]), "=r"(r.w[i + 4]), "=r"(r.w[i + 5]), "=r"(r.w[i + 6]), "=r"(r.w[i + 7])
+                     : "l"(p + 2 * i) : "memory");
+}
+__device__ __forceinline__ void store_row(__half* p, const Row32& r) {
+#pragma unroll
+    for (int i = 0; i < 16; i += 8)
+        asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 2 * i), "r"(r.w[i]), "r"(r.w[i + 1]), "r"(r.w[i + 2]), "r"(r.w[i + 3]),
+                     "r"(r.w[i + 4]), "r"(r.w[i + 5]), "r"(r.w[i + 6]), "r"(r.w[i + 7]) : "memory");
+}
+__device__ __forceinline__ float2 to_floats(uint32_t v) { return __half22float2(*reinterpret_cast<const __half2*>(&v)); }
+__device__ __forceinline__ uint32_t to_halves(float x, float y) {
+    const __half2 h = __floats2half2_rn(x, y);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 
-// What a lane reads beside a block of 32 x 32 accumulators: four columns each of eight rows of hi and lo (update), or of A' (polynomial).
-struct Beside { uint2 a[8], b[8]; };
-// A lane's place in a block at (row0, col0) of matrix b: eight lanes have one row's 32 columns.
-struct Place { int64_t at, step; int rows, col; };        // element offset of its first row, offset of every fourth row, rows of the block, first column
-__device__ __forceinline__ Place place_of(const NsParams& p, const Phase& q, int b, int row0, int col0) {
-    const int lane = threadIdx.x & 31;
+// What a row reads beside its accumulators: hi and lo (update), or A' (polynomial); `at`: its element offset in the planes.
+struct Beside { Row32 a, b; };
+__device__ __forceinline__ int64_t place_of(const NsParams& p, const Phase& q, int b, int row, int col) {
     const bool square = q.mode == kGram || q.mode == kPoly;
-    const int64_t ld = square ? p.lds : p.ldx;
-    Place w;
-    w.col = col0 + (lane & 7) * 4;
-    w.rows = w.col < q.N ? min(32, q.M - row0) : 0;
-    w.at = ((int64_t)b * (square ? p.s : p.m) + row0 + (lane >> 3)) * ld + w.col;
-    w.step = 4 * ld;
-    return w;
+    return ((int64_t)b * (square ? p.s : p.m) + row) * (square ? p.lds : p.ldx) + col;
 }
-__device__ __forceinline__ uint2 ld_pair(const __half* p) { return *reinterpret_cast<const uint2*>(p); }
-__device__ __forceinline__ void load_beside(const NsParams& p, const Phase& q, int step, const Place& w, Beside& in) {
+__device__ __forceinline__ void load_beside(const NsParams& p, const Phase& q, int step, int64_t at, Beside& in) {
     if (q.mode == kGram) return;
-    const int r0 = (threadIdx.x & 31) >> 3;
-    const __half* a = (q.mode == kPoly ? p.gram : p.hi[step & 1]) + w.at;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (r0 + 4 * i < w.rows) in.a[i] = ld_pair(a + i * w.step);
-    if (q.mode == kPoly) return;
-    const __half* l = p.lo[step & 1] + w.at;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (r0 + 4 * i < w.rows) in.b[i] = ld_pair(l + i * w.step);
-}
-__device__ __forceinline__ void to_floats(uint2 v, float (&f)[4]) {
-    const float2 lo = __half22float2(*reinterpret_cast<const __half2*>(&v.x)), hi = __half22float2(*reinterpret_cast<const __half2*>(&v.y));
-    f[0] = lo.x; f[1] = lo.y; f[2] = hi.x; f[3] = hi.y;
-}
-__device__ __forceinline__ uint2 to_halves(const float (&f)[4]) {
-    const __half2 lo = __floats2half2_rn(f[0], f[1]), hi = __floats2half2_rn(f[2], f[3]);
-    return make_uint2(*reinterpret_cast<const uint32_t*>(&lo), *reinterpret_cast<const uint32_t*>(&hi));
+    load_row((q.mode == kPoly ? p.gram : p.hi[step & 1]) + at, in.a);
+    if (q.mode != kPoly) load_row(p.lo[step & 1] + at, in.b);
 }
 
-// 32 columns of 32 rows (v: this lane's row) of a phase's accumulator, at (row0, col0) of matrix b.  The values turn in shared memory
-// (`turn`, 4 KB per warp; 16-byte pieces XORed with the row) so that what is read and written beside them is whole sectors.
-// `in` was read ahead; `next`, called between the arithmetic and the stores, reads ahead for the block after this one
-// (the compiler cannot move loads over stores that might alias them, and a round trip costs more than a block's arithmetic).
-// Planes have padded rows, so that four columns can always be touched; what lies in the padding is not used.
+// Row `row` and columns [col0, col0 + 32) of a phase's accumulators (v) of matrix b.  `in` was read ahead; `next`, called between the
+// arithmetic and the stores, reads ahead for the block after this one (the compiler cannot move loads over stores that might
+// alias them, and a round trip costs more than a block's arithmetic).  Whole warps: a lane whose row does not exist takes part in
+// the exchange.  Returns the row's sum of squares where the next step needs it.
 template <typename Next>
-__device__ __forceinline__ float finish_block(const NsParams& p, const Phase& q, int step, const uint32_t (&v)[32], uint32_t turn, const Place& w, Beside& in,
-                                              int b, int row0, int col0, bool mirror, float g, Next next) {
-    const int lane = threadIdx.x & 31, piece = lane & 7, r0 = lane >> 3;
-    __syncwarp();                                         // the previous block has been read
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-        asm volatile("st.shared.v4.b32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (uint32_t)(lane * 128 + ((i ^ (lane & 7)) << 4))), "r"(v[4 * i]), "r"(v[4 * i + 1]),
-                     "r"(v[4 * i + 2]), "r"(v[4 * i + 3]) : "memory");
-    __syncwarp();
-    float x[8][4];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = r0 + 4 * i;
-        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[i][0]), "=f"(x[i][1]), "=f"(x[i][2]), "=f"(x[i][3])
-                     : "r"(turn + (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4))) : "memory");
-    }
+__device__ __forceinline__ float finish_row(const NsParams& p, const Phase& q, int step, const uint32_t (&v)[32], int64_t at, Beside& in, int b, int row, int col0, bool mirror,
+                                            float g, Next next) {
     const float ca = p.coeffs[3 * step], cb = p.coeffs[3 * step + 1], cc = p.coeffs[3 * step + 2];
-    const Place here = w;
+    const bool have = row < q.M;
     float sum = 0.f;
-    uint2 o[8];
+    Row32 o;
     if (q.mode == kGram || q.mode == kPoly) {
-        __half* out = (q.mode == kGram ? p.gram : p.poly);
+        __half* out = q.mode == kGram ? p.gram : p.poly;
         if (q.mode == kGram) {
             constexpr float kScale = 1.f / (float)(1 << (2 * kXExp - kSExp));
             const float diagonal = g * (float)(1 << kSExp);
+            const int on = row - col0;                    // which of the 32 columns is the diagonal's
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float f[4];
-                const int on = row0 + r0 + 4 * i - here.col;      // which of the four columns is the diagonal's
-#pragma unroll
-                for (int j = 0; j < 4; ++j) f[j] = x[i][j] * kScale - (on == j ? diagonal : 0.f);
-                o[i] = to_halves(f);
-            }
+            for (int i = 0; i < 16; ++i)
+                o.w[i] = to_halves(__uint_as_float(v[2 * i]) * kScale - (on == 2 * i ? diagonal : 0.f), __uint_as_float(v[2 * i + 1]) * kScale - (on == 2 * i + 1 ? diagonal : 0.f));
         } else {
             const float lin = cb + 2.f * cc * g, sq = cc * (1.f / (float)(1 << kSExp));
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                float f[4];
-                to_floats(in.a[i], f);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) f[j] = lin * f[j] + sq * x[i][j];
-                o[i] = to_halves(f);
+            for (int i = 0; i < 16; ++i) {
+                const float2 s = to_floats(in.a.w[i]);
+                o.w[i] = to_halves(lin * s.x + sq * __uint_as_float(v[2 * i]), lin * s.y + sq * __uint_as_float(v[2 * i + 1]));
             }
         }
         next();
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (r0 + 4 * i < here.rows) *reinterpret_cast<uint2*>(out + here.at + i * here.step) = o[i];
-        if (mirror) {                                     // the same numbers at (column, row): turned once more, 72 bytes per row
-            __syncwarp();
-#pragma unroll
-            for (int i = 0; i < 8; ++i)
-                asm volatile("st.shared.v2.b32 [%0], {%1, %2};" ::"r"(turn + (uint32_t)((r0 + 4 * i) * 72 + piece * 8)), "r"(o[i].x), "r"(o[i].y) : "memory");
-            __syncwarp();
-            const int r = (lane & 15) * 2;                // two rows per lane, 16 lanes along a column; the second row may lie in the padding
-            const int have = q.M - row0 - r;
-            __half* to = out + ((int64_t)b * p.s + col0 + (lane >> 4)) * p.lds + row0 + r;
+        if (have) store_row(out + at, o);
+        if (mirror) {                                     // the same numbers at (column, row): neighbouring lanes trade, so that each stores two rows of a column
+            const bool odd = threadIdx.x & 1;             // (the second row may lie in the padding)
+            __half* to = out + ((int64_t)b * p.s + col0 + odd) * p.lds + (row & ~1);
+            const bool pair = (row & ~1) < q.M;
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
-                const int c = 2 * i + (lane >> 4);
-                uint16_t lo, hi;
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(lo) : "r"(turn + (uint32_t)(r * 72 + c * 2)) : "memory");
-                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(hi) : "r"(turn + (uint32_t)(r * 72 + 72 + c * 2)) : "memory");
-                if (have > 0 && col0 + c < q.N) *reinterpret_cast<uint32_t*>(to + (int64_t)(2 * i) * p.lds) = (uint32_t)lo | ((uint32_t)hi << 16);
+                const uint32_t theirs = __shfl_xor_sync(0xffffffffu, o.w[i], 1);
+                const uint32_t w = odd ? __byte_perm(theirs, o.w[i], 0x7632) : __byte_perm(o.w[i], theirs, 0x5410);
+                if (pair && col0 + 2 * i + odd < q.N) *reinterpret_cast<uint32_t*>(to + (int64_t)(2 * i) * p.lds) = w;
             }
         }
     } else {
-        const float lin = ca + g * (cb + cc * g);
+        const float lin = ca + g * (cb + cc * g), lin_lo = lin * (1.f / (float)(1 << kLoExp));
         const bool traced = step + 3 >= p.steps;          // the next step is one of the last two, which shift
-        uint2 ol[8];
+        Row32 ol;
+        float f[32];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            float h[4], l[4], f[4];
-            to_floats(in.a[i], h);
-            to_floats(in.b[i], l);
+        for (int i = 0; i < 16; ++i) {
+            const float2 h = to_floats(in.a.w[i]), l = to_floats(in.b.w[i]);
+            f[2 * i] = lin * h.x + (lin_lo * l.x + __uint_as_float(v[2 * i]) * (1.f / (float)(1 << kSExp)));
+            f[2 * i + 1] = lin * h.y + (lin_lo * l.y + __uint_as_float(v[2 * i + 1]) * (1.f / (float)(1 << kSExp)));
+        }
+        if (q.mode == kUpdate) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) f[j] = lin * (h[j] + l[j] * (1.f / (float)(1 << kLoExp))) + x[i][j] * (1.f / (float)(1 << kSExp));
-            if (q.mode == kUpdate) {
-                o[i] = to_halves(f);
-                to_floats(o[i], h);
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    l[j] = (f[j] - h[j]) * (float)(1 << kLoExp);
-                    if (traced && r0 + 4 * i < here.rows && here.col + j < q.N) sum += f[j] * f[j];
-                }
-                ol[i] = to_halves(l);
-            } else {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[i][j] = f[j] * (1.f / (float)(1 << kXExp));
+            for (int i = 0; i < 16; ++i) {
+                o.w[i] = to_halves(f[2 * i], f[2 * i + 1]);
+                const float2 h = to_floats(o.w[i]);
+                ol.w[i] = to_halves((f[2 * i] - h.x) * (float)(1 << kLoExp), (f[2 * i + 1] - h.y) * (float)(1 << kLoExp));
             }
+            if (traced && have)
+#pragma unroll
+                for (int i = 0; i < 32; ++i) sum += col0 + i < q.N ? f[i] * f[i] : 0.f;
         }
         next();
-        if (q.mode == kUpdate) {
-            __half *hi = p.hi[(step + 1) & 1] + here.at, *lo = p.lo[(step + 1) & 1] + here.at;
+        if (q.mode == kUpdate && have) {
+            store_row(p.hi[(step + 1) & 1] + at, o);
+            store_row(p.lo[(step + 1) & 1] + at, ol);
+        } else if (have) {
+            __nv_bfloat16* d = p.out + (int64_t)b * p.stride_out + (int64_t)row * p.ld_out + col0;
+            constexpr float kScale = 1.f / (float)(1 << kXExp);
+            if (p.out_vec && col0 + 32 <= q.N) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (r0 + 4 * i < here.rows) {
-                    *reinterpret_cast<uint2*>(hi + i * here.step) = o[i];
-                    *reinterpret_cast<uint2*>(lo + i * here.step) = ol[i];
+                for (int i = 0; i < 32; i += 8) {
+                    __nv_bfloat162 w[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) w[j] = __floats2bfloat162_rn(f[i + 2 * j] * kScale, f[i + 2 * j + 1] * kScale);
+                    *reinterpret_cast<uint4*>(d + i) = *reinterpret_cast<const uint4*>(w);
                 }
-        } else {
-            __nv_bfloat16* d = p.out + (int64_t)b * p.stride_out + (int64_t)(row0 + r0) * p.ld_out + here.col;
+            } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i, d += 4 * p.ld_out) {
-                if (r0 + 4 * i >= here.rows) continue;
-                Bf4 f;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) f.h[j] = __float2bfloat16_rn(x[i][j]);
-                if (p.out_vec && here.col + 4 <= q.N) *reinterpret_cast<Bf4*>(d) = f;
-                else
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-                        if (here.col + j < q.N) d[j] = f.h[j];
+                for (int i = 0; i < 32; ++i)
+                    if (col0 + i < q.N) d[i] = __float2bfloat16_rn(f[i] * kScale);
             }
         }
     }
@@ -535,7 +494,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
         asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kEpilogueRegs));
         // Epilogue: warp w reads lanes 32 (w & 3) .. of TMEM (rows), columns of half (w - 4) / 4.
         const int half = (warp - kFirstEpilogueWarp) >> 2, quarter = warp & 3;
-        const uint32_t turn = smem_u32(behind) + (uint32_t)kPipeBytes + (uint32_t)(warp - kFirstEpilogueWarp) * 4096;
         const uint32_t leader_tempty = map_to_cta(pipe.tempty, 0);
         uint32_t it = 0;
         bool ok = true;
@@ -561,25 +519,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                 const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM + quarter * 32, col0 = tc * q.bn + half * nc;
                 const bool mirror = (q.mode == kGram || q.mode == kPoly) && (tc + 1) * q.bn <= tr * 2 * kBM;      // below the diagonal block
                 const uint32_t taddr = pipe.tmem + ((uint32_t)(quarter * 32) << 16) + buf * 256 + (uint32_t)(half * nc);
+                const int row = row0 + lane;
                 Beside in;
-                Place w = place_of(p, q, b, row0, col0);
-                load_beside(p, q, step, w, in);           // on its way while the tile's last MMAs run
+                int64_t at = place_of(p, q, b, row, col0);
+                if (row < q.M && col0 < q.N) load_beside(p, q, step, at, in);      // on its way while the tile's last MMAs run
                 ok = __all_sync(0xffffffffu, pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue));
                 if (!ok) break;
                 tcgen05_fence_after();
 #pragma unroll 1
-                for (int c = 0; c < nc; c += 32) {
+                for (int c = 0; c < nc; c += 32, at += 32) {
                     float sum = 0.f;
                     uint32_t v[32];
                     tmem_ld32(taddr + c, v);
                     tmem_ld_wait();
                     if (c + 32 == nc) pipe.release_at(leader_tempty + 8 * buf);
                     if (row0 < q.M && col0 + c < q.N)
-                        sum = finish_block(p, q, step, v, turn, w, in, b, row0, col0 + c, mirror, g, [&]() {
-                            if (c + 32 < nc) {
-                                w = place_of(p, q, b, row0, col0 + c + 32);
-                                load_beside(p, q, step, w, in);
-                            }
+                        sum = finish_row(p, q, step, v, at, in, b, row, col0 + c, mirror, g, [&]() {
+                            if (c + 32 < nc && col0 + c + 32 < q.N && row < q.M) load_beside(p, q, step, at + 32, in);
                         });
                     // one partial sum per block, whatever the tile width: results do not depend on that choice
                     if (q.mode == kUpdate && step + 3 >= p.steps) {
@@ -724,7 +680,7 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
         if (!make_half_map(&p.gram_map[w], p.gram, p.s, p.s, l.lds, a.batch, 64 << w) || !make_half_map(&p.poly_map[w], p.poly, p.s, p.s, l.lds, a.batch, 64 << w))
             return cudaErrorInvalidValue;
     p.out = (__nv_bfloat16*)a.O; p.ld_out = a.ldo; p.stride_out = a.stride_o;
-    p.out_vec = ((uintptr_t)a.O & 7) == 0 && a.ldo % 4 == 0 && a.stride_o % 4 == 0;
+    p.out_vec = ((uintptr_t)a.O & 15) == 0 && a.ldo % 8 == 0 && a.stride_o % 8 == 0;
     p.phase_count = (uint32_t*)(a.ws + l.off_count);
     p.dev_status = a.dev_status;
     p.wait_ns = kWaitLimitNs;
