@@ -133,7 +133,7 @@ __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t 
 
 constexpr int kBM = 128;                  // rows of the first operand per CTA
 constexpr int kBK = 64;                   // 16-bit entries of the inner dimension per stage: one 128-byte swizzle row
-constexpr int kStages = 6;
+constexpr int kStages = 5;
 constexpr int kBoxBytes = 64 * 128;       // a copy: 64 rows x 64 inner entries, in either order
 constexpr int kStageBytes = 4 * kBoxBytes;
 constexpr int kEpilogueWarps = 8;
@@ -610,12 +610,12 @@ cudaError_t launch_start(const NewtonSchulzArgs& a, cudaStream_t st, int* launch
 
 // Columns of a product's tiles (index 0, 1, 2: 64, 128, 256), by the time of the pair that finishes last.  A tile's copies and MMAs take,
 // per 64 inner entries, about 370, 400 or 560 cycles (1000 x 4096: 370 for 64 columns; 4096^2, all SMs: 560 for 256), its epilogue
-// 3600 per 32 columns of a warp.  The longer of the two counts for every tile, the shorter once.
+// 1500 per 32 columns of a warp.  The longer of the two counts for every tile, the shorter once.
 int best_width(const int64_t (&tiles)[3], int64_t kblocks, int64_t pairs) {
     int best = 0;
     double least = 0.0;
     for (int w = 0; w < 3; ++w) {
-        const double rounds = (double)((tiles[w] + pairs - 1) / pairs), feed = (double)kblocks * (w == 2 ? 560.0 : w == 1 ? 400.0 : 370.0), finish = 3600.0 * (double)(1 << w);
+        const double rounds = (double)((tiles[w] + pairs - 1) / pairs), feed = (double)kblocks * (w == 2 ? 560.0 : w == 1 ? 400.0 : 370.0), finish = 1500.0 * (double)(1 << w);
         const double cost = rounds * (feed > finish ? feed : finish) + (feed > finish ? finish : feed);
         if (w == 0 || cost < least) { best = w; least = cost; }
     }
