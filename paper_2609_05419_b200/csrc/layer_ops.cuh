@@ -38,8 +38,9 @@ cudaError_t launch_fp8_gemm(const Fp8GemmArgs& a, int sm_count, cudaStream_t st,
 // Newton-Schulz iteration on `batch` matrices (see newton_schulz.cu for the arithmetic and the workspace).
 struct NewtonSchulzLayout {
     int64_t ldx, lds;                     // leading dimensions of the iterate and of the short-side squares, in elements
-    int64_t off_norm, off_count, off_shift, off_trace[2], off_hi[2], off_lo[2], off_gram, off_poly, total;      // bytes from the start of the workspace
+    int64_t off_norm, off_count, off_shift, off_trace[2], off_hi[2], off_lo[2], off_gram, off_poly, off_part, off_part_count, total;      // bytes from the start of the workspace
     int64_t norm_parts, trace_parts;      // partial sums per matrix
+    int splits; int64_t part_counts;      // pieces of the first product's inner dimension, and counters of finished ones
 };
 NewtonSchulzLayout newton_schulz_layout(int64_t batch, int64_t m, int64_t n, int64_t offset);
 struct NewtonSchulzArgs {

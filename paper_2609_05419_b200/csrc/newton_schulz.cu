@@ -92,7 +92,8 @@ __global__ void __launch_bounds__(kRowThreads) norm_kernel(const T* G, int64_t g
 // X_0 in two planes.  The first block of each matrix also leaves |X_0|_F^2, the trace of the first step.
 template <typename T>
 __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t groups, uint32_t per_row, int64_t m, int64_t n, int64_t ldg, int64_t stride_g, int vec,
-                                                            const double* parts, int nparts, float eps, __half* hi, __half* lo, int64_t ldx, float* trace, uint32_t* phase_count) {
+                                                            const double* parts, int nparts, float eps, __half* hi, __half* lo, int64_t ldx, float* trace, uint32_t* phase_count, uint32_t* part_count,
+                                                            int64_t part_counts) {
     __shared__ double scratch[kRowThreads / 32];
     wait_for_prior_kernels();
     const int64_t b = blockIdx.y;
@@ -107,6 +108,8 @@ __global__ void __launch_bounds__(kRowThreads) start_kernel(const T* G, int64_t 
         if (b == 0) *phase_count = 0;
         trace[b] = norm > 0.0 ? (float)(sq / (norm * norm)) : 0.f;
     }
+    if (b == 0)
+        for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < part_counts; i += (int64_t)gridDim.x * kRowThreads) part_count[i] = 0;
     const T* g = G + b * stride_g;
     const int64_t stride = (int64_t)gridDim.x * kRowThreads;
     for (int64_t i = (int64_t)blockIdx.x * kRowThreads + threadIdx.x; i < groups; i += kUnroll * stride) {
@@ -157,6 +160,7 @@ struct NsParams {
     int square_width, update_width;                       // columns of a tile: 256, 128 or 64
     float coeffs[3 * kMaxSteps];
     float* trace[2]; int64_t trace_parts;           // partial sums of |X|_F^2 (one in front of the first step)
+    int splits; float* part; uint32_t* part_count;        // A' in pieces along its inner dimension (see kGram's epilogue)
     float* shift;                                         // g of every matrix: written with A', read by the rest of the step
     __half *gram, *poly; int64_t lds;                     // s x s, times 2^kSExp
     __half *hi[2], *lo[2]; int64_t ldx;                   // m x n
@@ -169,10 +173,12 @@ struct NsParams {
 // One product of a step: kind 0 A' = X X^T - g I, 1 P = (b + 2 c g) A' + c A'^2, 2 X <- (a + b g + c g^2) X + P X.
 struct Phase {
     int mode, M, N, kblocks, bn, tiles_r, tiles_c, tiles;
+    int splits, items;                                    // pieces of the inner dimension per tile; tiles and pieces of all matrices
     bool turned_a, turned_b;
     const CUtensorMap *map_a, *map_b;
 };
 __host__ __device__ inline int square_tiles(int tiles_r, int tiles_c, int per) { return per * tiles_r * (tiles_r - 1) / 2 + tiles_c; }
+template <bool PIECES>
 __device__ __forceinline__ Phase phase_at(const NsParams& p, int step, int kind) {
     Phase q;
     const bool tall = p.m > p.n;
@@ -184,6 +190,8 @@ __device__ __forceinline__ Phase phase_at(const NsParams& p, int step, int kind)
     q.tiles_r = (q.M + 2 * kBM - 1) / (2 * kBM);
     q.tiles_c = (q.N + q.bn - 1) / q.bn;
     q.tiles = kind == 2 ? q.tiles_r * q.tiles_c : square_tiles(q.tiles_r, q.tiles_c, 2 * kBM / q.bn);
+    q.splits = PIECES && kind == 0 ? p.splits : 1;
+    q.items = q.tiles * p.batch * q.splits;
     q.turned_a = kind == 0 && tall;                       // X^T X contracts along the rows of X
     q.turned_b = (kind == 0 && tall) || (kind == 2 && !tall);
     const CUtensorMap* x = p.x[step & 1];
@@ -268,6 +276,12 @@ __device__ __forceinline__ bool wait_for_phase(const NsParams& p, uint32_t targe
     }
     asm volatile("fence.acq_rel.gpu;" ::: "memory");
     return true;
+}
+
+// Blocks of the inner dimension of piece `split`.
+__device__ __forceinline__ void piece_of(const Phase& q, int split, int* from, int* to) {
+    *from = (int)((int64_t)q.kblocks * split / q.splits);
+    *to = (int)((int64_t)q.kblocks * (split + 1) / q.splits);
 }
 
 // A block of 32 x 32 accumulators is finished row by row: a lane has one row's 32 columns, 64 bytes of a half-precision plane, which it
@@ -409,6 +423,8 @@ __device__ __forceinline__ float shift_of(const NsParams& p, int step, int mode,
 // All steps in one launch.  The CTA pairs share a phase's tiles; a phase begins when every CTA has finished the one before (a counter
 // in the workspace, which every CTA adds to; the launch is cooperative).  Without launches in between, what is left between
 // two phases is the counter's round trip and the filling of the pipeline.
+// PIECES: the first product's inner dimension is split (a kernel of its own, for the others are 4 % slower with that path in it).
+template <bool PIECES>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_steps_kernel(const __grid_constant__ NsParams p) {
     extern __shared__ unsigned char smem_raw[];
     const uint32_t raw = smem_u32(smem_raw);
@@ -429,19 +445,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             uint32_t fills = 0;
             bool ok = true;
             for (int ph = 0; ok && ph < phases; ++ph) {
-                const Phase q = phase_at(p, ph / 3, ph % 3);
-                if (pair >= q.tiles * p.batch) continue;
+                const Phase q = phase_at<PIECES>(p, ph / 3, ph % 3);
+                if (pair >= q.items) continue;
                 const int half_rows = q.bn / 2;
-                int b, tr, tc;
-                tile_at(q, pair, &b, &tr, &tc);
+                int b, tr, tc, from, to;
+                tile_at(q, pair / q.splits, &b, &tr, &tc);
+                piece_of(q, pair % q.splits, &from, &to);
                 asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_a) : "memory");
                 asm volatile("prefetch.tensormap [%0];" ::"l"(q.map_b) : "memory");
                 if (!(ok = __all_sync(0xffffffffu, wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag, false)))) break;
                 asm volatile("fence.proxy.async.global;" ::: "memory");       // the other CTAs' stores, then this thread's bulk copies
-                for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs) {
-                    if (tile != pair) tile_at(q, tile, &b, &tr, &tc);
+                for (int item = pair; ok && item < q.items; item += npairs) {
+                    if (item != pair) {
+                        tile_at(q, item / q.splits, &b, &tr, &tc);
+                        piece_of(q, item % q.splits, &from, &to);
+                    }
                     const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM, col0 = tc * q.bn + (int)pipe.rank * half_rows;
-                    for (int kb = 0; kb < q.kblocks; ++kb) {
+                    for (int kb = from; kb < to; ++kb) {
                         if (!(ok = pipe.wait_warp(pipe.empty + 8 * at.stage, at.phase ^ 1u, kDevTimeoutProducer))) break;
                         const uint32_t dst = tiles_base + at.stage * kStageBytes;
                         if (elect_one()) {
@@ -462,14 +482,16 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             uint32_t it = 0;                              // tile counter: buffer it & 1, its use number it >> 1
             bool ok = true;
             for (int ph = 0; ok && ph < phases; ++ph) {
-                const Phase q = phase_at(p, ph / 3, ph % 3);
+                const Phase q = phase_at<PIECES>(p, ph / 3, ph % 3);
                 const uint32_t idesc = make_idesc_f16(q.turned_a, q.turned_b, 2 * kBM, q.bn);
                 // 16 inner entries: 32 bytes along a swizzle row, or 16 rows of 128 bytes
                 const uint64_t step_a = q.turned_a ? 128 : 2, step_b = q.turned_b ? 128 : 2;
-                for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs, ++it) {
+                for (int item = pair; ok && item < q.items; item += npairs, ++it) {
                     const uint32_t buf = it & 1u;
+                    int from, to;
+                    piece_of(q, item % q.splits, &from, &to);
                     if (!(ok = pipe.wait_warp(pipe.tempty + 8 * buf, ((it >> 1) & 1u) ^ 1u, kDevTimeoutMma))) break;
-                    for (int kb = 0; kb < q.kblocks; ++kb) {
+                    for (int kb = from; kb < to; ++kb) {
                         if (!(ok = pipe.wait_warp(pipe.full + 8 * at.stage, at.phase, kDevTimeoutMma))) break;
                         tcgen05_fence_after();
                         const uint32_t a_addr = tiles_base + at.stage * kStageBytes, b_addr = a_addr + kBM * 128;
@@ -478,7 +500,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                         if (elect_one()) {
 #pragma unroll
                             for (int k4 = 0; k4 < 4; ++k4)
-                                umma_f16_pair(pipe.tmem + buf * 256, adesc + k4 * step_a, bdesc + k4 * step_b, idesc, (uint32_t)((kb | k4) != 0));
+                                umma_f16_pair(pipe.tmem + buf * 256, adesc + k4 * step_a, bdesc + k4 * step_b, idesc, (uint32_t)(kb != from || k4 != 0));
                             umma_commit_pair(pipe.empty + 8 * at.stage, 3);
                         }
                         __syncwarp();
@@ -499,7 +521,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
         bool ok = true;
         for (int ph = 0; ph < phases; ++ph) {
             const int step = ph / 3;
-            const Phase q = phase_at(p, step, ph % 3);
+            const Phase q = phase_at<PIECES>(p, step, ph % 3);
             if (ok) {                                     // (without tiles too: a CTA is counted for a phase only after the phases before it)
                 ok = lane != 0 || wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag, true);
                 ok = __all_sync(0xffffffffu, ok);         // lane 0 has acquired the other CTAs' stores, and the warp with it
@@ -507,15 +529,15 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             const int nc = q.bn / 2;
             int shift_for = -1;
             float g = 0.f;
-            for (int tile = pair; ok && tile < q.tiles * p.batch; tile += npairs, ++it) {
+            for (int item = pair; ok && item < q.items; item += npairs, ++it) {
                 int b, tr, tc;
-                tile_at(q, tile, &b, &tr, &tc);
+                tile_at(q, item / q.splits, &b, &tr, &tc);
                 const uint32_t buf = it & 1u;
                 if (b != shift_for) {
                     g = shift_of(p, step, q.mode, b);
                     shift_for = b;
                 }
-                if (q.mode == kGram && tr == 0 && tc == 0 && pipe.rank == 0 && warp == kFirstEpilogueWarp && lane == 0) p.shift[b] = g;
+                if (q.mode == kGram && tr == 0 && tc == 0 && item % q.splits == 0 && pipe.rank == 0 && warp == kFirstEpilogueWarp && lane == 0) p.shift[b] = g;
                 const int row0 = tr * (2 * kBM) + (int)pipe.rank * kBM + quarter * 32, col0 = tc * q.bn + half * nc;
                 const bool mirror = (q.mode == kGram || q.mode == kPoly) && (tc + 1) * q.bn <= tr * 2 * kBM;      // below the diagonal block
                 const uint32_t taddr = pipe.tmem + ((uint32_t)(quarter * 32) << 16) + buf * 256 + (uint32_t)(half * nc);
@@ -526,13 +548,51 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                 ok = __all_sync(0xffffffffu, pipe.wait(pipe.tfull + 8 * buf, (it >> 1) & 1u, kDevTimeoutEpilogue));
                 if (!ok) break;
                 tcgen05_fence_after();
+                // A tile in pieces: every warp leaves its rows' sums of a piece in memory and counts itself; the last one of a tile's
+                // pieces adds them all, in the order of the pieces whoever is last, and finishes the rows.
+                const int64_t rows_id = ((int64_t)(item / q.splits) * 2 + pipe.rank) * kEpilogueWarps + (warp - kFirstEpilogueWarp);
+                float* part = p.part + rows_id * q.splits * 32 * nc + lane;
+                if (PIECES && q.splits > 1) {
+#pragma unroll 1
+                    for (int c = 0; c < nc; c += 32) {
+                        uint32_t v[32];
+                        tmem_ld32(taddr + c, v);
+                        tmem_ld_wait();
+                        float* to = part + (item % q.splits * nc + c) * 32;
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) to[j * 32] = __uint_as_float(v[j]);
+                    }
+                    pipe.release_at(leader_tempty + 8 * buf);
+                    __threadfence();
+                    __syncwarp();
+                    uint32_t before = 0;
+                    if (lane == 0) before = atomicAdd(p.part_count + rows_id, 1u);
+                    before = __shfl_sync(0xffffffffu, before, 0);
+                    if (before + 1 != (uint32_t)q.splits) continue;
+                    __threadfence();
+                    if (lane == 0) p.part_count[rows_id] = 0;      // for the next step, which begins behind a phase's end
+                }
 #pragma unroll 1
                 for (int c = 0; c < nc; c += 32, at += 32) {
                     float sum = 0.f;
                     uint32_t v[32];
-                    tmem_ld32(taddr + c, v);
-                    tmem_ld_wait();
-                    if (c + 32 == nc) pipe.release_at(leader_tempty + 8 * buf);
+                    if (PIECES && q.splits > 1) {
+                        const float* from = part + c * 32;
+                        float f[32];
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) f[j] = from[j * 32];
+                        for (int s = 1; s < q.splits; ++s) {
+                            from += nc * 32;
+#pragma unroll
+                            for (int j = 0; j < 32; ++j) f[j] += from[j * 32];
+                        }
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(f[j]);
+                    } else {
+                        tmem_ld32(taddr + c, v);
+                        tmem_ld_wait();
+                        if (c + 32 == nc) pipe.release_at(leader_tempty + 8 * buf);
+                    }
                     if (row0 < q.M && col0 + c < q.N)
                         sum = finish_row(p, q, step, v, at, in, b, row, col0 + c, mirror, g, [&]() {
                             if (c + 32 < nc && col0 + c + 32 < q.N && row < q.M) load_beside(p, q, step, at + 32, in);
@@ -603,7 +663,7 @@ cudaError_t launch_start(const NewtonSchulzArgs& a, cudaStream_t st, int* launch
     const int start_blocks = (int)((needed + kUnroll - 1) / kUnroll < 1024 ? (needed + kUnroll - 1) / kUnroll : 1024);
     err = launch_chained(start_kernel<T>, dim3(start_blocks, (unsigned)a.batch), dim3(kRowThreads), 0, st, (const T*)a.G, groups, per_row, a.m, a.n, a.ldg, a.stride_g, vec,
                          parts, blocks, a.eps, (__half*)(a.ws + l.off_hi[0]), (__half*)(a.ws + l.off_lo[0]), l.ldx, (float*)(a.ws + l.off_trace[0]),
-                         (uint32_t*)(a.ws + l.off_count));
+                         (uint32_t*)(a.ws + l.off_count), (uint32_t*)(a.ws + l.off_part_count), l.part_counts);
     if (err == cudaSuccess) *launches += 2;
     return err;
 }
@@ -620,6 +680,20 @@ int best_width(const int64_t (&tiles)[3], int64_t kblocks, int64_t pairs) {
         if (w == 0 || cost < least) { best = w; least = cost; }
     }
     return best;
+}
+
+// Tiles of an s x s square in tiles of 64 << w columns.
+int64_t tiles_of_square(int64_t s, int w) { return square_tiles((int)((s + 255) / 256), (int)((s + (64 << w) - 1) / (64 << w)), 4 >> w); }
+
+// Pieces of the inner dimension of X X^T, where a square of few tiles has a long one: as many as let one matrix's tiles, 128 columns wide,
+// fill 74 pairs, at most 8, with 12 blocks of 64 or more each, and four or none (a piece costs the writing and reading of its sums).
+// By the matrix alone: the pieces are part of the order of summation.  256 x 8000, eight pieces: 152 us against 223 in one;
+// 1000 x 4096, three: 228 against 227; 8 of 200 x 1500, two: 193 against 184.
+int splits_of(int64_t s, int64_t long_side) {
+    int64_t most = 74 / tiles_of_square(s, 1);
+    const int64_t blocks = (long_side + kBK - 1) / kBK;
+    if (most > blocks / 12) most = blocks / 12;
+    return (int)(most < 4 ? 1 : most > 8 ? 8 : most);
 }
 
 }  // namespace
@@ -643,6 +717,15 @@ NewtonSchulzLayout newton_schulz_layout(int64_t batch, int64_t m, int64_t n, int
     }
     l.off_gram = take(2 * batch * s * l.lds);
     l.off_poly = take(2 * batch * s * l.lds);
+    l.splits = splits_of(s, m < n ? n : m);
+    int64_t area = 0;
+    l.part_counts = 0;
+    if (l.splits > 1) {
+        for (int w = 0; w < 3; ++w) area = area > tiles_of_square(s, w) * 256 * (64 << w) ? area : tiles_of_square(s, w) * 256 * (64 << w);
+        l.part_counts = tiles_of_square(s, 0) * 2 * kEpilogueWarps * batch;
+    }
+    l.off_part = take(4 * area * l.splits * batch);
+    l.off_part_count = take(4 * l.part_counts);
     l.total = off;
     return l;
 }
@@ -652,11 +735,12 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
                       : a.type == kF16 ? launch_start<__half>(a, st, &launches[0]) : launch_start<__nv_bfloat16>(a, st, &launches[0]);
     if (err != cudaSuccess) return err;
     const NewtonSchulzLayout& l = a.lay;
-    static int pairs_dev[kMaxDevices] = {};
-    int& max_pairs = pairs_dev[current_device_slot()];
+    static int pairs_dev[2][kMaxDevices] = {};
+    const auto kernel = l.splits > 1 ? ns_steps_kernel<true> : ns_steps_kernel<false>;
+    int& max_pairs = pairs_dev[l.splits > 1][current_device_slot()];
     if (!max_pairs) {
         int pairs = 0;
-        if ((err = resident_pairs(ns_steps_kernel, kGemmThreads, kGemmSmem, sm_count, &pairs)) != cudaSuccess) return err;
+        if ((err = resident_pairs(kernel, kGemmThreads, kGemmSmem, sm_count, &pairs)) != cudaSuccess) return err;
         max_pairs = pairs;
     }
     NsParams p = {};
@@ -672,6 +756,9 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
                 return cudaErrorInvalidValue;
     }
     p.trace_parts = l.trace_parts;
+    p.splits = l.splits;
+    p.part = (float*)(a.ws + l.off_part);
+    p.part_count = (uint32_t*)(a.ws + l.off_part_count);
     p.shift = (float*)(a.ws + l.off_shift);
     p.gram = (__half*)(a.ws + l.off_gram);
     p.poly = (__half*)(a.ws + l.off_poly);
@@ -689,11 +776,11 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
     if (tiles_of(p.s, 64) * (rt + 1) > INT32_MAX / 8 / a.batch || mt * tiles_of(a.n, 64) > INT32_MAX / 8 / a.batch) return cudaErrorInvalidValue;
     int64_t square[3], update[3];
     for (int w = 0; w < 3; ++w) {
-        square[w] = square_tiles((int)rt, (int)tiles_of(p.s, 64 << w), 4 >> w) * a.batch;
+        square[w] = tiles_of_square(p.s, w) * l.splits * a.batch;
         update[w] = mt * tiles_of(a.n, 64 << w) * a.batch;
     }
     const int64_t long_side = a.m < a.n ? a.n : a.m;
-    const int ws = best_width(square, tiles_of((p.s + long_side) / 2, kBK), max_pairs), wu = best_width(update, tiles_of(p.s, kBK), max_pairs);
+    const int ws = best_width(square, tiles_of((p.s + long_side / l.splits) / 2, kBK), max_pairs), wu = best_width(update, tiles_of(p.s, kBK), max_pairs);
     p.square_width = 64 << ws;
     p.update_width = 64 << wu;
     const int64_t most = square[ws] > update[wu] ? square[ws] : update[wu];
@@ -708,7 +795,7 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
     at[0].val.cooperative = 1;
     c.attrs = at;
     c.numAttrs = 1;
-    err = cudaLaunchKernelEx(&c, ns_steps_kernel, p);
+    err = cudaLaunchKernelEx(&c, kernel, p);
     if (err == cudaSuccess) ++launches[1];
     return err;
 }

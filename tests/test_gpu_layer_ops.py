@@ -294,7 +294,7 @@ def check_newton_schulz(g, o, **how):
 
 
 # several tiles per pair, every tile width, both orientations, many matrices
-@pytest.mark.parametrize("batch,m,n", [(1, 1500, 2300), (1, 2304, 1100), (40, 200, 260), (12, 700, 600), (1, 2500, 2500)])
+@pytest.mark.parametrize("batch,m,n", [(1, 1500, 2300), (1, 2304, 1100), (40, 200, 260), (12, 700, 600), (1, 2500, 2500), (1, 200, 6100), (6, 3900, 130)])
 def test_newton_schulz_of_many_tiles(batch, m, n):
     g = torch.stack([update(m, n, "flat" if i % 2 else "falling", 100 + i) for i in range(batch)])
     o = torch.full((batch, m, n), float("nan"), dtype=torch.bfloat16, device="cuda")
@@ -329,7 +329,7 @@ def test_newton_schulz_steps_and_coefficients(steps, coeffs):
     check_newton_schulz(g, o, steps=steps, coeffs=coeffs)
 
 
-@pytest.mark.parametrize("m,n", [(96, 200), (300, 140), (520, 520)])
+@pytest.mark.parametrize("m,n", [(96, 200), (300, 140), (520, 520), (150, 4000)])
 def test_newton_schulz_batch_strides_and_independence(m, n):
     batch, ld = 5, n + 13
     store = torch.zeros(batch, m + 2, ld, device="cuda")
