@@ -95,41 +95,46 @@ template <> __device__ __forceinline__ __nv_bfloat16 to_type<__nv_bfloat16>(floa
 // below m and n exist.  Through `turn`, 4 KB of shared memory per warp, 32 columns at a time: a lane writes its row's 128 bytes,
 // 16-byte pieces XORed with the row, and then eight lanes store one row's 32 columns side by side (whole 32-byte
 // sectors; a lane storing along its own row would leave half-written sectors of 32 rows per instruction).
-template <typename T, int NC>
+template <typename T, int NC, bool ADD>
 __device__ __forceinline__ void store_rows(const float (&v)[NC], uint32_t turn, const T* C, int64_t ldc, T* D, int64_t ldd, int row0, int col0, int m, int n, bool vec) {
     const int lane = threadIdx.x & 31, piece = lane & 7;
     struct alignas(4 * sizeof(T)) Four { T t[4]; };
 #pragma unroll
     for (int c = 0; c < NC; c += 32) {
+        const int col = col0 + c + piece * 4, first = lane >> 3;
+        const int rows = col < n ? min(32, m - row0) : 0;
+        const bool whole = vec && col + 4 <= n;
+        // ADD: what is added is asked for at once (row by row, each load would wait for the store before it: 265 against 228 us for
+        // 4096 x 4096 x 8192 added to a 32-bit C).  Without it the loop is kept short: it is fetched anew for every tile.
+        Four in[8];
+        if (ADD && whole)
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (first + 4 * i < rows) in[i] = *reinterpret_cast<const Four*>(C + (int64_t)(row0 + first + 4 * i) * ldc + col);
         __syncwarp();                                     // the previous columns have been read
 #pragma unroll
         for (int q = 0; q < 8; ++q)
             asm volatile("st.shared.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(turn + (uint32_t)(lane * 128 + ((q ^ (lane & 7)) << 4))), "f"(v[c + 4 * q]),
                          "f"(v[c + 4 * q + 1]), "f"(v[c + 4 * q + 2]), "f"(v[c + 4 * q + 3]) : "memory");
         __syncwarp();
-        const int col = col0 + c + piece * 4;
-        const int rows = col < n ? min(32, m - row0) : 0;
-#pragma unroll 2
-        for (int r = lane >> 3; r < rows; r += 4) {       // (kept short: this code is fetched anew for every tile)
+#pragma unroll(ADD ? 8 : 2)
+        for (int i = 0; i < 8; ++i) {
+            const int r = first + 4 * i;
+            if (r >= rows) continue;
             float x[4];
             asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[0]), "=f"(x[1]), "=f"(x[2]), "=f"(x[3])
                          : "r"(turn + (uint32_t)(r * 128 + ((piece ^ (r & 7)) << 4))) : "memory");
             T* d = D + (int64_t)(row0 + r) * ldd + col;
-            const T* s = C ? C + (int64_t)(row0 + r) * ldc + col : nullptr;
-            if (vec && col + 4 <= n) {
+            if (whole) {
                 Four f;
-                if (s) {
-                    f = *reinterpret_cast<const Four*>(s);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] += from_type<T>(f.t[j]);
-                }
-#pragma unroll
-                for (int j = 0; j < 4; ++j) f.t[j] = to_type<T>(x[j]);
+                for (int j = 0; j < 4; ++j) f.t[j] = to_type<T>(ADD ? x[j] + from_type<T>(in[i].t[j]) : x[j]);
                 *reinterpret_cast<Four*>(d) = f;
             } else {
+                const T* s = C + (int64_t)(row0 + r) * ldc + col;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
-                    if (col + j < n) d[j] = to_type<T>(x[j] + (s ? from_type<T>(s[j]) : 0.f));
+                    if (col + j < n) d[j] = to_type<T>(ADD ? x[j] + from_type<T>(s[j]) : x[j]);
             }
         }
     }
@@ -144,8 +149,8 @@ __device__ __forceinline__ float lds(uint32_t addr) {
     return v;
 }
 
-// T: type of C and D.  COLS: B has a scale per row (of B; column of D) and block, otherwise one per 128 rows.
-template <typename T, int BN, bool COLS>
+// T: type of C and D.  ADD: C is added.  COLS: B has a scale per row (of B; column of D) and block, otherwise one per 128 rows.
+template <typename T, int BN, bool COLS, bool ADD>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kThreads, 1)
 fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Fp8GemmParams p) {
     using cfg = Cfg<BN, COLS>;
@@ -309,7 +314,7 @@ fp8_gemm_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             }
             ok = __all_sync(0xffffffffu, ok);
             if (ok && row0 < p.m && col0 < p.n) {
-                store_rows<T, NC>(acc, turn, (const T*)p.C, p.ldc, (T*)p.D, p.ldd, row0, col0, p.m, p.n, p.vec != 0);
+                store_rows<T, NC, ADD>(acc, turn, (const T*)p.C, p.ldc, (T*)p.D, p.ldd, row0, col0, p.m, p.n, p.vec != 0);
             }
         }
         if (!ok && lane == 0) pipe.tell_peer();
@@ -329,13 +334,13 @@ bool make_byte_map(CUtensorMap* map, const uint8_t* base, int64_t rows, int64_t 
               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <typename T, int BN, bool COLS>
+template <typename T, int BN, bool COLS, bool ADD>
 cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
     static int pairs_dev[kMaxDevices] = {};
     int& max_pairs = pairs_dev[current_device_slot()];
     if (!max_pairs) {
         int pairs = 0;
-        cudaError_t err = resident_pairs(fp8_gemm_pair_kernel<T, BN, COLS>, kThreads, Cfg<BN, COLS>::kSmem, sm_count, &pairs);
+        cudaError_t err = resident_pairs(fp8_gemm_pair_kernel<T, BN, COLS, ADD>, kThreads, Cfg<BN, COLS>::kSmem, sm_count, &pairs);
         if (err != cudaSuccess) return err;
         max_pairs = pairs;
     }
@@ -357,7 +362,7 @@ cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int
     p.dev_status = a.dev_status;
     p.wait_ns = kWaitLimitNs;
     const int pairs = (int)(tr * tc < max_pairs ? tr * tc : max_pairs);
-    cudaError_t err = launch_chained(fp8_gemm_pair_kernel<T, BN, COLS>, dim3(2 * pairs), dim3(kThreads), Cfg<BN, COLS>::kSmem, st, map_a, map_b, p);
+    cudaError_t err = launch_chained(fp8_gemm_pair_kernel<T, BN, COLS, ADD>, dim3(2 * pairs), dim3(kThreads), Cfg<BN, COLS>::kSmem, st, map_a, map_b, p);
     if (err == cudaSuccess) ++*launches;
     return err;
 }
@@ -680,7 +685,8 @@ cudaError_t launch_thin(const Fp8GemmArgs& a, bool swapped, int sm_count, cudaSt
 
 template <typename T, int BN>
 cudaError_t launch_pair_scales(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
-    return a.B.block == 1 ? launch_pair<T, BN, true>(a, sm_count, st, launches) : launch_pair<T, BN, false>(a, sm_count, st, launches);
+    if (a.C) return a.B.block == 1 ? launch_pair<T, BN, true, true>(a, sm_count, st, launches) : launch_pair<T, BN, false, true>(a, sm_count, st, launches);
+    return a.B.block == 1 ? launch_pair<T, BN, true, false>(a, sm_count, st, launches) : launch_pair<T, BN, false, false>(a, sm_count, st, launches);
 }
 
 template <typename T>
