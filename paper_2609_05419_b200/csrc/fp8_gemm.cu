@@ -4,9 +4,14 @@
 //
 // A block of 128 entries is one 128-byte swizzle row, so one pipeline stage, so four MMAs (K = 32).  Since the scales differ from
 // block to block, the tensor core's accumulator holds one block's sums only: it is written afresh every four MMAs, into two TMEM buffers in
-// turn, and eight epilogue warps per CTA read each back, multiply by the scales and add to totals in registers (128 per
-// thread) while the other buffer is being filled.  256 x 256 tiles per CTA pair: the four MMAs of a block take 512 cycles, the
-// 128 x 256 multiply-adds of a CTA's half 256 cycles of the FP32 pipes (512 with a scale per column), as packed pairs.
+// turn (four of a narrow tile), and eight epilogue warps per CTA read each back, multiply by the scales and add to totals in registers (128
+// per thread) while the next is being filled.  256 x 256 tiles per CTA pair: the four MMAs of a block take 512 cycles, the
+// 128 x 256 multiply-adds of a CTA's half 256 issue slots of the FP32 pipes.  What bounds it is neither: a block takes about 1000
+// cycles, the way from the commit through the epilogue warps (wait, scales, four TMEM loads, 128 multiply-adds, two warps per scheduler) back
+// to the released buffer, during which each buffer is out of the tensor core's hands.  8192^3 to bf16: 519 us (2.12 PFLOP/s), tensor
+// pipe 45 % active; 4096 x 4096 x 8192 with a scale per column: 183 us.  Measured and not kept: packed pairs (f32x2) in
+// place of scalar multiply-adds, whose register pairs the compiler feeds with moves (620 us); sixteen epilogue warps of 64 columns (590);
+// the wide tile in two parts of 128 columns with two buffers each (577: the first operand is read twice).
 #include "layer_ops.cuh"
 #include "pair_pipeline.cuh"
 
@@ -40,7 +45,7 @@ struct Cfg {
     static constexpr int kBuffers = 512 / BN;
     static_assert(kSlots >= kAhead + 2 * kBuffers + 1, "scale ring");
     static constexpr uint32_t kTmemCols = 512;
-    static constexpr int kSlotFloats = kBM + (COLS ? BN : 2);         // scales of one block: 128 rows, and the columns or their two halves
+    static constexpr int kSlotFloats = kBM + (COLS ? BN : 2);         // scales of one block: 128 rows, and the columns or their halves
     static constexpr int kSlotBytes = (kSlotFloats * 4 + 15) / 16 * 16;
     static constexpr size_t kScaleBytes = (size_t)kSlots * kSlotBytes;
     static constexpr size_t kSmem = (size_t)kStages * kStageBytes + 1024 + kScaleBytes + PairPipe<kStages, kBuffers>::kBytes + 16 + kEpilogueWarps * 4096;
