@@ -380,11 +380,13 @@ cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int
 
 constexpr int kThinBuffers = 4;                  // accumulators of N columns
 constexpr int kThinSlots = 16, kThinAhead = 6;   // scales turn to block g after tfull of g - 4, so every warp is through with g - 9; slot of g + 6 - 16
-constexpr int kThinThreads = 256;                // copies, MMAs, two scale warps, four epilogue warps
-constexpr int kMostSplit = 8;
 
 template <int N>
 struct ThinCfg {
+    // Epilogue warps, four per part of the columns: eight from 64 columns on (48 x 16384 x 4096: 16.6 us, with four 19.3).
+    static constexpr int kWarps = N >= 64 ? 8 : 4;
+    static constexpr int kCols = N / (kWarps / 4);
+    static constexpr int kThreads = 128 + 32 * kWarps;     // copies, MMAs, two scale warps, epilogue
     static constexpr int kStageBytes = (kBM + N) * kGemmBK;
     static constexpr int kStages = N == 128 ? 6 : 8;
     static constexpr int kSlotBytes = (kBM + N) * 4;
@@ -425,7 +427,7 @@ __device__ __forceinline__ uint32_t cluster_size() {
 }
 
 template <typename T, int N>
-__global__ void __launch_bounds__(kThinThreads, 1)
+__global__ void __launch_bounds__(ThinCfg<N>::kThreads, 1)
 fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_constant__ CUtensorMap map_c, const __grid_constant__ ThinParams p) {
     using cfg = ThinCfg<N>;
     constexpr int STAGES = cfg::kStages;
@@ -448,7 +450,7 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < STAGES; ++s) { mbar_init(full + 8 * s, 1); mbar_init(empty + 8 * s, 1); }
-        for (int a = 0; a < kThinBuffers; ++a) { mbar_init(tfull + 8 * a, 1 + kScaleWarps); mbar_init(tempty + 8 * a, 4); }
+        for (int a = 0; a < kThinBuffers; ++a) { mbar_init(tfull + 8 * a, 1 + kScaleWarps); mbar_init(tempty + 8 * a, cfg::kWarps); }
         mbar_init(drain, 1);
         *abort_flag = 0;
         *fills_issued = 0;
@@ -466,7 +468,8 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     wait_for_prior_kernels();
     auto wait = [&](uint32_t bar, uint32_t parity, int code) { return mbar_wait(bar, parity, abort_flag, p.dev_status, code, p.wait_ns); };
 
-    float acc[N];
+    constexpr int NC = cfg::kCols;
+    float acc[NC];
     if (warp == 0) {
         RingPos<STAGES> at;
         int kb = 0;
@@ -528,10 +531,10 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else {                                     // epilogue: lane = row of the lane operand
-        const int quarter = warp & 3;
-        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16);
+        const int quarter = warp & 3, from = ((warp >> 2) - 1) * NC;      // this warp's rows, and its columns of the tile
+        const uint32_t taddr = tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)from;
 #pragma unroll
-        for (int j = 0; j < N; ++j) acc[j] = 0.f;
+        for (int j = 0; j < NC; ++j) acc[j] = 0.f;
         bool ok = true;
         for (int kb = 0; kb < blocks; ++kb) {
             const uint32_t buf = kb % kThinBuffers, slot = scale_ring + (uint32_t)(kb % kThinSlots) * cfg::kSlotBytes;
@@ -539,14 +542,14 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             tcgen05_fence_after();
             const float scale = lds(slot + (quarter * 32 + lane) * 4);
             const uint64_t s2 = pack2(scale, scale);
-            constexpr int P = N < 32 ? N : 32;
+            constexpr int P = NC < 32 ? NC : 32;
 #pragma unroll
-            for (int c = 0; c < N; c += P) {
+            for (int c = 0; c < NC; c += P) {
                 uint32_t v[P];
                 if constexpr (P == 32) tmem_ld32(taddr + buf * N + c, v);
                 else tmem_ld16(taddr + buf * N + c, v);
                 tmem_ld_wait();
-                if (c + P == N) {
+                if (c + P == NC) {
                     tcgen05_fence_before();
                     __syncwarp();
                     if (lane == 0) mbar_arrive(tempty + 8 * buf);
@@ -555,7 +558,7 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
                 for (int i = 0; i < P; i += 4) {
                     uint64_t f, g;
                     float s[4];
-                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f), "=l"(g) : "r"(slot + (kBM + c + i) * 4));
+                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f), "=l"(g) : "r"(slot + (kBM + from + c + i) * 4));
                     unpack2(mul2(s2, f), &s[0], &s[1]);
                     unpack2(mul2(s2, g), &s[2], &s[3]);
 #pragma unroll
@@ -567,15 +570,17 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
             float* totals = reinterpret_cast<float*>(smem_raw + (tiles_base - raw));
             if (ok)
 #pragma unroll
-                for (int j = 0; j < N; ++j) totals[j * kBM + quarter * 32 + lane] = acc[j];
+                for (int j = 0; j < NC; ++j) totals[(from + j) * kBM + quarter * 32 + lane] = acc[j];
         } else if (ok) {
             const int l = l0 + quarter * 32 + lane;
             if (l < p.lanes) {
                 const T* cp = (const T*)p.C + (int64_t)l * p.c_lane;
                 T* dp = (T*)p.D + (int64_t)l * p.d_lane;
 #pragma unroll
-                for (int j = 0; j < N; ++j)
-                    if (c0 + j < p.cols) dp[(int64_t)(c0 + j) * p.d_col] = to_type<T>(acc[j] + (p.C ? from_type<T>(cp[(int64_t)(c0 + j) * p.c_col]) : 0.f));
+                for (int j = 0; j < NC; ++j) {
+                    const int col = c0 + from + j;
+                    if (col < p.cols) dp[(int64_t)col * p.d_col] = to_type<T>(acc[j] + (p.C ? from_type<T>(cp[(int64_t)col * p.c_col]) : 0.f));
+                }
             }
         }
     }
@@ -598,11 +603,11 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
     if (S > 1) {
         cluster_sync_all();                      // every rank's totals are there
         if (warp >= 4) {                         // this rank's share of the columns, added in the order of the ranks
-            const int row = (int)threadIdx.x - 128, l = l0 + row;
+            const int row = ((int)threadIdx.x - 128) & 127, l = l0 + row;
             // (S, a power of two up to 8, divides 16: sixteen remote loads in flight are 16 / S whole columns)
             const int from = N / S * rank;
 #pragma unroll 1
-            for (int t0 = 0; t0 < N; t0 += 16) {
+            for (int t0 = ((warp >> 2) - 1) * 16; t0 < N; t0 += 4 * cfg::kWarps) {      // 16 loads at a time, in turn between the parts
                 float v[16], s = 0.f;
                 const int j0 = from + t0 / S;
                 if (c0 + j0 >= p.cols) break;
@@ -633,7 +638,7 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
 // Time of a product in microseconds by each kind of tile, from measurements (B200, 1.7 to 1.9 GHz): `round` tiles run at once, each takes
 // so much per block of k and for its output, and a launch takes the rest.  (256 x 256 tiles per pair: 1024 x 4096 x 4096, one round of 32 blocks, 27 us,
 // 2048^3 18 us; 256 x 128: 512 x 4096 x 4096 21 us, 1001 x 1999 x 1100, nine blocks, 14 us; CTAs of their own, 128 x 128 with k split in
-// four: 128 x 4096 x 4096 16 us, 256 x 4096 x 4096 split in two 21.5 us.)
+// four: 128 x 4096 x 4096 13.7 us, 1024 x 1024 x 8192 split in two 23.4 us.)
 double pair_cost(const Fp8GemmArgs& a, int width, int sm_count) {
     const double tiles = (double)((a.m + 255) / 256) * (double)((a.n + width - 1) / width), rounds = std::ceil(tiles / (sm_count / 2));
     const double blocks = (double)((a.k + kScaleBlock - 1) / kScaleBlock), cols = a.B.block == 1;
@@ -641,13 +646,47 @@ double pair_cost(const Fp8GemmArgs& a, int width, int sm_count) {
     return 9.0 + rounds * (blocks * ((rounds > 1 ? 0.40 : 0.30) + 0.17 * cols) + 1.5);
 }
 
-// How often the blocks of k are split: the least number of rounds of CTAs, each weighed by its length, over the SMs; at least two blocks each.
-int thin_split(int64_t tiles, int64_t kblocks, int sm_count, double* cost_out) {
+// CTAs of clusters of 1, 2, 4 and 8 (index: logarithm) that are resident at once: larger clusters leave SMs of a GPC without a place.
+// One CTA per SM for every column count, so that one kernel speaks for all.
+struct ThinCapacity { int ctas[4]; };
+cudaError_t thin_capacity(int sm_count, ThinCapacity* out) {
+    static ThinCapacity known[kMaxDevices] = {};
+    ThinCapacity& k = known[current_device_slot()];
+    if (!k.ctas[0]) {
+        using cfg = ThinCfg<128>;
+        cudaError_t err = cudaFuncSetAttribute(fp8_gemm_thin_kernel<float, 128>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)cfg::kSmem);
+        if (err != cudaSuccess) return err;
+        ThinCapacity c = {{sm_count, 0, 0, 0}};
+        for (int i = 1; i < 4; ++i) {
+            cudaLaunchConfig_t qc = {};
+            qc.gridDim = dim3((unsigned)(sm_count >> i << i));
+            qc.blockDim = dim3(cfg::kThreads);
+            qc.dynamicSmemBytes = cfg::kSmem;
+            cudaLaunchAttribute qa[1];
+            qa[0].id = cudaLaunchAttributeClusterDimension;
+            qa[0].val.clusterDim.x = 1u << i;
+            qa[0].val.clusterDim.y = 1;
+            qa[0].val.clusterDim.z = 1;
+            qc.attrs = qa;
+            qc.numAttrs = 1;
+            int clusters = 0;
+            if ((err = cudaOccupancyMaxActiveClusters(&clusters, fp8_gemm_thin_kernel<float, 128>, &qc)) != cudaSuccess) return err;
+            c.ctas[i] = clusters << i;
+        }
+        k = c;
+    }
+    *out = k;
+    return cudaSuccess;
+}
+
+// How often the blocks of k are split: the least number of rounds of CTAs, each weighed by its length; at least two blocks each.
+int thin_split(int64_t tiles, int64_t kblocks, const ThinCapacity& room, double* cost_out) {
     int best = 1;
     double best_cost = 1e30;
-    for (int S = 1; S <= kMostSplit; S *= 2) {
-        if (S > 1 && kblocks < 2 * S) break;
-        const int64_t rounds = (tiles * S + sm_count - 1) / sm_count;
+    for (int i = 0; i < 4; ++i) {
+        const int S = 1 << i;
+        if (S > 1 && (kblocks < 2 * S || room.ctas[i] == 0)) break;
+        const int64_t rounds = (tiles * S + room.ctas[i] - 1) / room.ctas[i];
         const double cost = (double)rounds * ((double)((kblocks + S - 1) / S) + 6.0);      // a round's fixed part is about six blocks
         if (cost < best_cost * 0.999) { best = S; best_cost = cost; }
     }
@@ -656,7 +695,7 @@ int thin_split(int64_t tiles, int64_t kblocks, int sm_count, double* cost_out) {
 }
 
 template <typename T, int N>
-cudaError_t launch_thin(const Fp8GemmArgs& a, bool swapped, int sm_count, cudaStream_t st, int* launches) {
+cudaError_t launch_thin(const Fp8GemmArgs& a, bool swapped, const ThinCapacity& room, cudaStream_t st, int* launches) {
     using cfg = ThinCfg<N>;
     static bool ready_dev[kMaxDevices] = {};
     bool& ready = ready_dev[current_device_slot()];
@@ -681,9 +720,9 @@ cudaError_t launch_thin(const Fp8GemmArgs& a, bool swapped, int sm_count, cudaSt
     p.dev_status = a.dev_status;
     p.wait_ns = kWaitLimitNs;
     const int64_t tiles = (int64_t)p.lane_tiles * ((p.cols + N - 1) / N);
-    const int S = thin_split(tiles, p.kblocks, sm_count, nullptr);
+    const int S = thin_split(tiles, p.kblocks, room, nullptr);
     if (tiles * S > INT32_MAX) return cudaErrorInvalidValue;
-    cudaError_t err = launch_chained_cluster(fp8_gemm_thin_kernel<T, N>, dim3((unsigned)(tiles * S)), dim3(kThinThreads), cfg::kSmem, S, st, map_l, map_c, p);
+    cudaError_t err = launch_chained_cluster(fp8_gemm_thin_kernel<T, N>, dim3((unsigned)(tiles * S)), dim3(cfg::kThreads), cfg::kSmem, S, st, map_l, map_c, p);
     if (err == cudaSuccess) ++*launches;
     return err;
 }
@@ -698,18 +737,20 @@ template <typename T>
 cudaError_t launch_typed(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int* launches) {
     const bool swapped = !(a.n <= 64 && a.m > a.n);        // lanes run along the rows of B, so that stores run along rows of D, unless B has few
     const int64_t cols = swapped ? a.m : a.n, lanes = swapped ? a.n : a.m;
+    ThinCapacity room;
+    if (cudaError_t err = thin_capacity(sm_count, &room)) return err;
     if (cols > 64) {                                       // (up to 64 columns a narrower tile reads the lane operand once, which is all there is to do)
         double thin;
-        thin_split((lanes + kBM - 1) / kBM * ((cols + 127) / 128), (a.k + kScaleBlock - 1) / kScaleBlock, sm_count, &thin);
-        thin = 8.5 + 0.53 * thin;
+        thin_split((lanes + kBM - 1) / kBM * ((cols + 127) / 128), (a.k + kScaleBlock - 1) / kScaleBlock, room, &thin);
+        thin = 8.0 + 0.40 * thin;
         const double wide = pair_cost(a, 256, sm_count), narrow = pair_cost(a, 128, sm_count);
         if (wide <= narrow && wide <= thin) return launch_pair_scales<T, 256>(a, sm_count, st, launches);
         if (narrow <= thin) return launch_pair_scales<T, 128>(a, sm_count, st, launches);
     }
-    if (cols <= 16) return launch_thin<T, 16>(a, swapped, sm_count, st, launches);
-    if (cols <= 32) return launch_thin<T, 32>(a, swapped, sm_count, st, launches);
-    if (cols <= 64) return launch_thin<T, 64>(a, swapped, sm_count, st, launches);
-    return launch_thin<T, 128>(a, swapped, sm_count, st, launches);
+    if (cols <= 16) return launch_thin<T, 16>(a, swapped, room, st, launches);
+    if (cols <= 32) return launch_thin<T, 32>(a, swapped, room, st, launches);
+    if (cols <= 64) return launch_thin<T, 64>(a, swapped, room, st, launches);
+    return launch_thin<T, 128>(a, swapped, room, st, launches);
 }
 
 }  // namespace
