@@ -377,6 +377,8 @@ cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int
 // the lane operand (the weights, for tokens) x N rows of the column operand, N = 16, 32, 64 or 128, and the blocks of k split over a cluster
 // of S CTAs, whose totals are added through distributed shared memory in the order of the ranks.  The lane operand is
 // what such a product has to read; all stages of the ring are requested at once, so that every SM has 130 to 190 KB on its way.
+// 1 x 4096 x 4096 (16.8 MB of weights, split in four): 6 to 7 us on the device, of which set-up 0.7, first bytes 0.5 (from L2; 2 from HBM), eight
+// blocks 2.6, the join 1.6; 48 x 16384 x 4096 (67 MB): 16.6 us, 4.1 TB/s.
 
 constexpr int kThinBuffers = 4;                  // accumulators of N columns
 constexpr int kThinSlots = 16, kThinAhead = 6;   // scales turn to block g after tfull of g - 4, so every warp is through with g - 9; slot of g + 6 - 16
