@@ -384,6 +384,7 @@ def _stream_of(stream):
 
 _FP8 = (E4M3, E5M2)
 _FLOATS = (F32, F16, BF16)
+_NO_FORM = (None, 0, None, 0)
 
 
 def fp8_empty(rows, cols, fmt=E4M3, block_rows=1, device="cuda"):
@@ -399,21 +400,18 @@ def fp8_quantise(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None)
     px, tx, rows, cols, ldx = _rowmajor(X, "X", _FLOATS)
     if block_rows not in (1, 128):
         raise ValueError("block_rows: need 1 or 128")
-    blocks = lambda v, b: -(-v // b)
-    fits = lambda width: -(-max(width, 1) // 16) * 16
-    big = max(rows, cols, 1)
-    fmt, form, form_t = None, (None, fits(cols), None, big), (None, fits(rows), None, big)
+    fmt, form, form_t = None, _NO_FORM, _NO_FORM
     if Q is not None:
         pq, fmt, r, c, ldq = _rowmajor(Q, "Q", _FP8)
-        if (r, c) != (rows, cols) or S is None:
+        if r != rows or c != cols or S is None:
             raise ValueError("Q, S: shape mismatch")
-        form = (pq, ldq) + _scales(S, "S", blocks(rows, block_rows), blocks(cols, 128))
+        form = (pq, ldq, *_scales(S, "S", rows if block_rows == 1 else -(-rows // 128), -(-cols // 128)))
     if Qt is not None:
         pq, fmt_t, r, c, ldq = _rowmajor(Qt, "Qt", _FP8)
-        if (r, c) != (cols, rows) or St is None or fmt not in (None, fmt_t):
+        if r != cols or c != rows or St is None or fmt not in (None, fmt_t):
             raise ValueError("Qt, St: shape or type mismatch")
         fmt = fmt_t
-        form_t = (pq, ldq) + _scales(St, "St", blocks(cols, block_rows), blocks(rows, 128))
+        form_t = (pq, ldq, *_scales(St, "St", cols if block_rows == 1 else -(-cols // 128), -(-rows // 128)))
     if fmt is None:
         raise ValueError("need Q and S, or Qt and St")
     _check(lib().gemm2m_fp8_quantise(rows, cols, px, tx, ldx, fmt, block_rows, *form, *form_t, _stream_of(stream)), "gemm2m_fp8_quantise")
