@@ -375,7 +375,11 @@ def _scales(t, name, rows, cols):
     step, ld = t.stride()
     if rows > 1 and step != 1:
         raise ValueError(f"{name}: need column-major storage (stride 1 along dim 0), e.g. torch.empty(cols, rows).t()")
-    return t.data_ptr(), ld if cols > 1 and ld > 0 else max(rows, 1)
+    if cols <= 1 or rows == 0:                      # the stride of a single column says nothing
+        return t.data_ptr(), max(rows, 1)
+    if ld < rows:                                   # an expanded column of scales: the kernels read (or write) one column per block
+        raise ValueError(f"{name}: columns of scales overlap (stride {ld} along dim 1, {rows} rows); store one scale per block")
+    return t.data_ptr(), ld
 
 
 def _stream_of(stream):

@@ -1,0 +1,80 @@
+"""What the binding of the layer operators passes on to the library, and what it refuses: no GPU is touched, CPU tensors stand in for
+CUDA ones and the library is replaced by a recorder."""
+import pytest
+import torch
+
+from paper_2609_05419_b200 import binding as b
+
+
+class Standin:
+    """A CPU tensor that says it is a CUDA one."""
+    is_cuda = True
+
+    def __init__(self, tensor, device=0):
+        self.tensor, self.index = tensor, device
+
+    def __getattr__(self, name):
+        return getattr(self.tensor, name)
+
+    def get_device(self):
+        return self.index
+
+
+@pytest.fixture
+def calls(monkeypatch):
+    """Calls that would have reached the library: (name, arguments) each."""
+    seen = []
+
+    class Recorder:
+        def __getattr__(self, name):
+            return lambda *args: seen.append((name, args)) or b.OK
+
+    monkeypatch.setattr(b, "lib", Recorder)
+    monkeypatch.setattr(b, "_current_stream", lambda: 0)
+    return seen
+
+
+def matrix(rows, cols, block=1, **where):
+    q, s = b.fp8_empty(rows, cols, b.E4M3, block, device="cpu")
+    return Standin(q, **where), Standin(s, **where)
+
+
+def dense(rows, cols, dtype=torch.float32, **where):
+    return Standin(torch.zeros(rows, cols, dtype=dtype), **where)
+
+
+# ------------------------------------------------------------------------------------- scales with a stride below their rows
+# one scale per row for all of k, spelled as an expanded column: memory holds one column of scales, not one per block
+@pytest.mark.parametrize("m", [1, 2, 300])
+@pytest.mark.parametrize("side", ["A", "B"])
+def test_product_refuses_expanded_scales(calls, m, side):
+    k = 500
+    qa, sa = matrix(m, k)
+    qb, sb = matrix(m, k)
+    one = Standin(torch.ones(m, 1).expand(m, 4))
+    sa, sb = (one, sb) if side == "A" else (sa, one)
+    with pytest.raises(ValueError):
+        b.fp8_gemm(qa, sa, qb, sb, dense(m, m), b_block=1)
+    assert not calls
+
+
+@pytest.mark.parametrize("rows", [1, 300])
+def test_quantise_refuses_to_write_expanded_scales(calls, rows):
+    q, _ = matrix(rows, 500)
+    with pytest.raises(ValueError):
+        b.fp8_quantise(dense(rows, 500), q, Standin(torch.ones(rows, 1).expand(rows, 4)))
+    if rows > 128:                                             # transposed form with a scale per 128 x 128: 4 x 3 of them
+        qt, _ = matrix(500, rows, 128)
+        with pytest.raises(ValueError):
+            b.fp8_quantise(dense(rows, 500), None, None, qt, Standin(torch.ones(4, 1).expand(4, 3)), block_rows=128)
+    assert not calls
+
+
+def test_scales_pass_their_own_leading_dimension(calls):
+    for rows, cols, want in ((300, 500, 300), (1, 500, 1), (300, 100, 300), (1, 1, 1)):
+        q, s = matrix(rows, cols)
+        b.fp8_quantise(dense(rows, cols), q, s)
+        assert calls[-1][1][10] == want                        # lds
+    wide = Standin(torch.zeros(4, 400).t()[:300])               # columns further apart than their rows
+    b.fp8_quantise(dense(300, 500), matrix(300, 500)[0], wide)
+    assert calls[-1][1][10] == 400
