@@ -131,7 +131,7 @@ def _colmajor(t, name):
     if rows > 1 and t.stride(0) != 1:
         raise ValueError(f"{name}: need column-major storage (stride 1 along dim 0), e.g. torch.empty(cols, rows).t()")
     ld = t.stride(1) if cols > 1 else max(rows, 1)
-    return ctypes.c_void_p(t.data_ptr()), rows, cols, max(ld, 1)
+    return ctypes.c_void_p(t.data_ptr()), rows, cols, ld if rows > 0 else max(ld, 1)      # (0: an expanded row, which the library refuses)
 
 
 def max_moduli():
@@ -203,7 +203,7 @@ def _colmajor_host(t, name):
     if rows > 1 and t.stride(0) != 1:
         raise ValueError(f"{name}: need column-major storage (stride 1 along dim 0), e.g. torch.empty(cols, rows).t()")
     ld = t.stride(1) if cols > 1 else max(rows, 1)
-    return ctypes.c_void_p(t.data_ptr()), rows, cols, max(ld, 1)
+    return ctypes.c_void_p(t.data_ptr()), rows, cols, ld if rows > 0 else max(ld, 1)      # (0: an expanded row, which the library refuses)
 
 
 def zgemm2m_host(A, B, C, nmod=16, stream=None):
