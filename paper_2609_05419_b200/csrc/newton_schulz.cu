@@ -691,6 +691,7 @@ int64_t tiles_of_square(int64_t s, int w) { return square_tiles((int)((s + 255) 
 // By the matrix alone: the pieces are part of the order of summation.  256 x 8000, eight pieces: 152 us against 223 in one;
 // 1000 x 4096, three: 228 against 227; 8 of 200 x 1500, two: 193 against 184.
 int splits_of(int64_t s, int64_t long_side) {
+    if (s == 0) return 1;                                 // (no tiles: a workspace is asked for, nothing is launched)
     int64_t most = 74 / tiles_of_square(s, 1);
     const int64_t blocks = (long_side + kBK - 1) / kBK;
     if (most > blocks / 12) most = blocks / 12;

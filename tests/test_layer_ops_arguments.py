@@ -1,9 +1,16 @@
 """What the binding of the layer operators passes on to the library, and what it refuses: no GPU is touched, CPU tensors stand in for
 CUDA ones and the library is replaced by a recorder."""
+import ast
+import os
+import subprocess
+import sys
+
 import pytest
 import torch
 
 from paper_2609_05419_b200 import binding as b
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 class Standin:
@@ -78,3 +85,16 @@ def test_scales_pass_their_own_leading_dimension(calls):
     wide = Standin(torch.zeros(4, 400).t()[:300])               # columns further apart than their rows
     b.fp8_quantise(dense(300, 500), matrix(300, 500)[0], wide)
     assert calls[-1][1][10] == 400
+
+
+# ------------------------------------------------------------------------------------------------------------ sizes of nothing
+# (in a process of its own: an arithmetic signal would end the test run)
+@pytest.mark.parametrize("op", ["OP_NEWTON_SCHULZ", "OP_FP8_GEMM"])
+def test_workspace_sizes_of_empty_matrices(op):
+    code = ("from paper_2609_05419_b200 import binding as b\n"
+            f"op = b.{op}\n"
+            "print([b.workspace_bytes(op, *size, 1) for size in ((0, 8, 1), (8, 0, 1), (0, 0, 1), (0, 0, 0), (8, 8, 0), (8, 8, 1))])")
+    done = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert done.returncode == 0, (done.returncode, done.stderr)
+    sizes = ast.literal_eval(done.stdout)
+    assert all(256 <= v <= sizes[-1] for v in sizes)
