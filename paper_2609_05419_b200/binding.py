@@ -362,7 +362,7 @@ def _rowmajor(t, name, allowed):
     ld, step = t.stride()
     if cols > 1 and step != 1:
         raise ValueError(f"{name}: need row-major storage (stride 1 along dim 1)")
-    if rows <= 1:                                   # the stride of a single row says nothing
+    if rows <= 1 or cols == 0:                      # the stride of a single row, or of rows without entries, says nothing
         ld = (max(cols, 1) + 15) // 16 * 16
     return t.data_ptr(), _type_of(t, name, allowed), rows, cols, ld
 

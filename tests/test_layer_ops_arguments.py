@@ -98,3 +98,22 @@ def test_workspace_sizes_of_empty_matrices(op):
     assert done.returncode == 0, (done.returncode, done.stderr)
     sizes = ast.literal_eval(done.stdout)
     assert all(256 <= v <= sizes[-1] for v in sizes)
+
+
+# a batch without tokens: both forms of X, the forward product, and the weight gradient whose inner dimension is empty
+@pytest.mark.parametrize("rows,cols", [(0, 40), (40, 0), (0, 0), (1, 0), (0, 1)])
+def test_empty_matrices_have_leading_dimensions_that_the_library_takes(calls, rows, cols):
+    q, s = matrix(rows, cols)
+    qt, st = matrix(cols, rows)
+    b.fp8_quantise(dense(rows, cols), q, s, qt, st)
+    _, args = calls[-1]
+    ldx, ldq, ldqt = args[4], args[8], args[12]
+    assert ldx >= max(cols, 1) and ldq >= max(cols, 1) and ldq % 16 == 0 and ldqt >= max(rows, 1) and ldqt % 16 == 0
+    for (a, sa), n in ((matrix(rows, cols), 24), (matrix(24, rows), 8)):
+        m, k = a.shape
+        bq, sb = matrix(n, k)
+        b.fp8_gemm(a, sa, bq, sb, dense(m, n), C=dense(m, n), b_block=1)
+        _, args = calls[-1]
+        for ld, scales, count in ((args[5], args[7], m), (args[11], args[13], n)):
+            assert ld >= max(k, 1) and ld % 16 == 0 and scales >= max(count, 1)
+        assert args[16] >= n and args[19] >= n                  # ldc, ldd
