@@ -525,7 +525,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
             const Phase q = phase_at<PIECES>(p, step, ph % 3);
             if (ok) {                                     // (without tiles too: a CTA is counted for a phase only after the phases before it)
                 ok = lane != 0 || wait_for_phase(p, (uint32_t)ph * gridDim.x, pipe.abort_flag, true);
-                ok = __all_sync(0xffffffffu, ok);         // lane 0 has acquired the other CTAs' stores, and the warp with it
+                ok = __all_sync(0xffffffffu, ok);
+                __syncwarp();                             // lane 0 has acquired the other CTAs' stores; this orders the other lanes' reads behind it (a vote does not)
             }
             const int nc = q.bn / 2;
             int shift_for = -1;
@@ -571,6 +572,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kGemmThreads, 1) ns_
                     before = __shfl_sync(0xffffffffu, before, 0);
                     if (before + 1 != (uint32_t)q.splits) continue;
                     __threadfence();
+                    __syncwarp();                         // lane 0 has seen the other pieces counted; its fence orders the other lanes' reads too
                     if (lane == 0) p.part_count[rows_id] = 0;      // for the next step, which begins behind a phase's end
                 }
 #pragma unroll 1
