@@ -261,7 +261,8 @@ int gemm2m_fp8_quantise(int64_t rows, int64_t cols, const void* X, int type, int
  * a_block, b_block = 1 (a scale per row and block) or 128 (per 128 x 128 block); the formats may differ.  C and D are m x n of
  * the same type (F32, F16, BF16), row-major; C may be NULL (nothing is added) or D itself (then ldc = ldd), not otherwise overlap D.  Block sums and
  * their total are held in 32 bits, and rounded once.  m = 1 (one token) is an ordinary size.  k = 0 gives D = C, or zero.
- * A NaN scale makes the rows (columns) of D that it belongs to NaN.
+ * A NaN scale makes the rows (columns) of D that it belongs to NaN.  Where SA SB would leave the 32-bit range, a block's sum is multiplied
+ * by one scale after the other, so that only results outside that range are lost, for scales from 2^-94 to 2^89.
  * Forward: X quantised with 1-row blocks, W (out x in) with 128: Y = X W^T.  Input gradient: dY with 1-row blocks, Qt of W.
  * Weight gradient: dW = Qt of dY times Qt of X, block 1 on both sides, C = D = the 32-bit sum over micro-batches.
  * Workspace: GEMM2M_OP_FP8_GEMM. */

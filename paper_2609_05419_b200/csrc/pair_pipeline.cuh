@@ -152,13 +152,11 @@ __device__ __forceinline__ uint64_t pack2(float a, float b) {
     asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
     return r;
 }
-__device__ __forceinline__ void unpack2(uint64_t v, float* a, float* b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(*a), "=f"(*b) : "l"(v)); }
 // (volatile: stays behind the wait for the TMEM load that fills its operand)
 __device__ __forceinline__ void fma1(float& acc, float x, float y) { asm volatile("fma.rn.f32 %0, %1, %2, %0;" : "+f"(acc) : "f"(x), "f"(y)); }
-__device__ __forceinline__ uint64_t mul2(uint64_t x, uint64_t y) {
-    uint64_t r;
-    asm volatile("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(x), "l"(y));
-    return r;
+// (a, b) times (y, y), as bit patterns in.
+__device__ __forceinline__ void mul_pair(uint32_t a, uint32_t b, uint64_t y, float* x0, float* x1) {
+    asm volatile("{\n\t.reg .b64 t;\n\tmov.b64 t, {%2, %3};\n\tmul.rn.f32x2 t, t, %4;\n\tmov.b64 {%0, %1}, t;\n\t}" : "=f"(*x0), "=f"(*x1) : "r"(a), "r"(b), "l"(y));
 }
 
 // Most CTA pairs that are resident at once.

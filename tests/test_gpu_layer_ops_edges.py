@@ -31,3 +31,50 @@ def test_a_batch_without_tokens():
         b.fp8_gemm(*forms["dy"][2:], *forms["x"][2:], dw, b_block=1)                # nothing added: zero
         assert bool((dw == 0).all())
         b.device_status()
+
+
+# ------------------------------------------------------------------------------------------------- products of scales of any size
+# shapes that reach every kind of tile: few rows (16, 32, 64 columns; k in one piece and split), 128 x 128 with k split, pairs 256 and 128 wide
+SCALE_SHAPES = [(4, 600, 512), (30, 20000, 300), (50, 600, 1100), (200, 260, 1100), (600, 600, 300), (2500, 2600, 300)]
+
+
+@pytest.mark.parametrize("m,n,k", SCALE_SHAPES)
+@pytest.mark.parametrize("bb", [128, 1])
+@pytest.mark.parametrize("sizes", [(1e22, 1e17), (1e17, 1e22), (1e30, 1e30), (1e-30, 1e-30)])
+def test_zero_sums_stay_zero_whatever_their_scales(m, n, k, bb, sizes):
+    qa, sa = operand(m, k, 1, b.E4M3, 31)
+    qb, sb = operand(n, k, bb, b.E4M3, 32)
+    first = min(128, k)
+    qa[:, 1:first:2] = 0                                           # block 0: no entry of A meets one of B
+    qb[:, 0:first:2] = 0
+    sa[:, 0], sb[:, 0] = sizes
+    for c in (None, torch.randn(m, n, generator=gen(33), device="cuda")):
+        d = torch.full((m, n), float("nan"), device="cuda")
+        with Workspace(b.workspace_bytes(b.OP_FP8_GEMM, m, n, k, 1)):
+            b.fp8_gemm(qa, sa, qb, sb, d, C=c, b_block=bb)
+            b.device_status()
+        a, w = qa[:, first:].double() * spread(sa[:, 1:], 1, m, k - first), qb[:, first:].double() * spread(sb[:, 1:], bb, n, k - first)
+        exact, size = a @ w.t() + (0.0 if c is None else c.double()), a.abs() @ w.abs().t() + (0.0 if c is None else c.double().abs())
+        # as for every product: block sums 128 x 2^-23 of the magnitudes, the scales, blocks and C 2^-24 each
+        assert bool(((d.double() - exact).abs() <= size * (128 * 2.0 ** -23 + 13 * 2.0 ** -24)).all())
+
+
+@pytest.mark.parametrize("m,n,k", SCALE_SHAPES)
+@pytest.mark.parametrize("bb", [128, 1])
+@pytest.mark.parametrize("sizes", [(1e-21, 1e-22), (3e-30, 1e-14), (1e-14, 3e-30), (1e28, 1e-31), (1e-31, 1e28)])
+def test_scales_whose_product_is_subnormal_or_far_apart(m, n, k, bb, sizes):
+    qa, sa = operand(m, k, 1, b.E4M3, 41)
+    qb, sb = operand(n, k, bb, b.E4M3, 42)
+    qa.view(torch.uint8).bitwise_and_(0x7f)                        # all of one sign: sums of 128 products are above 2^16
+    qb.view(torch.uint8).bitwise_and_(0x7f)
+    sa *= sizes[0] * 1e3
+    sb *= sizes[1] * 1e3
+    sa[::2] /= sizes[0] * 1e3                                      # every other row has ordinary scales
+    d = torch.full((m, n), float("nan"), device="cuda")
+    with Workspace(b.workspace_bytes(b.OP_FP8_GEMM, m, n, k, 1)):
+        b.fp8_gemm(qa, sa, qb, sb, d, b_block=bb)
+        b.device_status()
+    exact = (qa.double() * spread(sa, 1, m, k)) @ (qb.double() * spread(sb, bb, n, k)).t()
+    # nothing cancels; results that are themselves subnormal are right to half of the smallest spacing per addition
+    room = exact * (128 * 2.0 ** -23 + 13 * 2.0 ** -24) + 13 * 2.0 ** -149
+    assert bool(((d.double() - exact).abs() <= room).all())
