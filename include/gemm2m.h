@@ -274,8 +274,9 @@ int gemm2m_fp8_gemm(int64_t m, int64_t n, int64_t k, const void* A, int a_fmt, i
  * stride_g / stride_o elements apart: X_0 = G / (|G|_F + eps), then X <- a X + (b A + c A^2) X with A = X X^T (m <= n; the same
  * polynomial with X^T X from the right for m > n), O = X rounded to bf16.  G: F32 / F16 / BF16, any alignment; O: BF16, may be G.
  * coeffs: host pointer to (a, b, c) of each step, or NULL for (3.4445, -4.7750, 2.0315) in every step, which drives the singular
- * values towards 1 (into about [0.7, 1.2]).  The coefficients must keep the singular values below about 100.  Products run on
- * 16-bit operands with 32-bit sums; before its rounding O is within about 2e-3 (relative, Frobenius norm;
+ * values towards 1 (into about [0.7, 1.2]).  Products run on 16-bit operands with 32-bit sums, which sets the range of the coefficients:
+ * in front of every step the singular values must be below 64 (the first step's are at most 1), and |b s^2 + c s^4| below 2000 for every s
+ * up to the largest of them.  Outside this range operands may overflow, and O then holds Inf or NaN.  Before its rounding O is within about 2e-3 (relative, Frobenius norm;
  * 4e-3 for sides below 20) of the exact iteration.
  * A zero matrix gives zero (for eps > 0 or = 0), a matrix with an Inf or NaN gives NaN throughout.  Results do not depend on the
  * batch a matrix is in.  Workspace: GEMM2M_OP_NEWTON_SCHULZ with (m, n, batch). */

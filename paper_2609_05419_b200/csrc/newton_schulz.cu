@@ -24,9 +24,9 @@ namespace gemm2m {
 
 namespace {
 
-constexpr int kXExp = 8;              // hi = rn16(2^8 X): entries of X are at most about 1.2
+constexpr int kXExp = 8;              // hi = rn16(2^8 X): entries of X are at most about 1.2; 255 fit
 constexpr int kLoExp = 11;            // lo = rn16(2^11 (2^8 X - hi))
-constexpr int kSExp = 4;              // A' and the polynomial are held times 2^4
+constexpr int kSExp = 4;              // A' and the polynomial are held times 2^4: entries up to 4094 fit, so singular values below 64
 constexpr int kNormParts = 592;       // partial sums of |G|_F^2 per matrix
 constexpr int kRowThreads = 256;
 

@@ -78,3 +78,27 @@ def test_scales_whose_product_is_subnormal_or_far_apart(m, n, k, bb, sizes):
     # nothing cancels; results that are themselves subnormal are right to half of the smallest spacing per addition
     room = exact * (128 * 2.0 ** -23 + 13 * 2.0 ** -24) + 13 * 2.0 ** -149
     assert bool(((d.double() - exact).abs() <= room).all())
+
+
+# ------------------------------------------------------------------------------------- Newton-Schulz: coefficients and their range
+def newton_schulz(g, steps, coeffs=None):
+    o = torch.full(g.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+    with Workspace(b.workspace_bytes(b.OP_NEWTON_SCHULZ, *g.shape, 1, 1)):
+        b.newton_schulz(g, o, steps=steps, coeffs=coeffs)
+        b.device_status()
+    return o
+
+
+def relative_error(g, steps, coeffs=None):
+    want = plain_newton_schulz(g, steps, coeffs)
+    return float(torch.linalg.vector_norm(newton_schulz(g, steps, coeffs).double() - want) / torch.linalg.vector_norm(want))
+
+
+# matrices of rank one, whose singular value 1 reaches 60 in front of a step, or whose polynomial reaches 1960 in the last one: the stated
+# limits are 64 and 2000.  Room: 2.5e-3 as documented for such slopes, and the rounding to bf16 (2^-8 of an entry, 2^-9 over many)
+@pytest.mark.parametrize("m,n", [(1, 40), (30, 1), (30, 40), (300, 200)])
+@pytest.mark.parametrize("coeffs", [[(60.0, 0.0, 0.0)] + [(1.0, 0.0, 0.0)] * 3, [(1.0, 0.0, 0.0)] * 2 + [(60.0, 0.0, 0.0), (1.0, -1e-4, 0.0)],
+                                    [(6.5, 0.0, 0.0), (0.0, 0.0, 1.1)], [(1.0, 0.0, 0.0), (6.5, 0.0, 0.0), (1.0, 0.0, 1.1)]])
+def test_newton_schulz_just_inside_its_range(m, n, coeffs):
+    g = torch.randn(m, 1, generator=gen(51), device="cuda") @ torch.randn(1, n, generator=gen(52), device="cuda")
+    assert relative_error(g, len(coeffs), coeffs) <= 2.5e-3 + (2.0 ** -8 if m * n < 64 else 2.0 ** -9)
