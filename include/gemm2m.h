@@ -276,8 +276,14 @@ int gemm2m_fp8_gemm(int64_t m, int64_t n, int64_t k, const void* A, int a_fmt, i
  * coeffs: host pointer to (a, b, c) of each step, or NULL for (3.4445, -4.7750, 2.0315) in every step, which drives the singular
  * values towards 1 (into about [0.7, 1.2]).  Products run on 16-bit operands with 32-bit sums, which sets the range of the coefficients:
  * in front of every step the singular values must be below 64 (the first step's are at most 1), and |b s^2 + c s^4| below 2000 for every s
- * up to the largest of them.  Outside this range operands may overflow, and O then holds Inf or NaN.  Before its rounding O is within about 2e-3 (relative, Frobenius norm;
- * 4e-3 for sides below 20) of the exact iteration.
+ * up to the largest of them.  Outside this range operands may overflow, and O then holds Inf or NaN.
+ * Accuracy: every step rounds by up to 2^-11 of the iterate's norm, and the later steps multiply that by their slopes (a where singular
+ * values are small, a + 3 b s^2 + 5 c s^4 elsewhere).  Against the exact iteration, before the rounding to bf16 (relative, Frobenius norm): the
+ * default coefficients 2.5e-3 for up to five steps (1e-2 for sides below 64), 1e-2 for ten, several 1e-2 from twenty steps on, where directions
+ * that G does not have are filled by what was rounded; coefficients that only contract, (1.5, -0.5, 0) or (1.875, -1.25, 0.375), 1e-3
+ * for up to twelve steps; sets that begin as steeply as (8.3, -23.6, 17.3) 1e-2 (5e-2 for sides below 20) if they leave room above the largest singular value
+ * (damped by 1 %: a / 1.01, b / 1.01^3, c / 1.01^5), and 1e-1 or worse if singular values can reach the end of the interval that the set is
+ * made for, where slopes are 10 in several steps.
  * A zero matrix gives zero (for eps > 0 or = 0), a matrix with an Inf or NaN gives NaN throughout.  Results do not depend on the
  * batch a matrix is in.  Workspace: GEMM2M_OP_NEWTON_SCHULZ with (m, n, batch). */
 int gemm2m_newton_schulz(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* O, int64_t ldo,

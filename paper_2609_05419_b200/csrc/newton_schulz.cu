@@ -9,9 +9,11 @@
 // exactly, and g = trace(A) / s makes A' (what is rounded) smallest.  trace(A) = |X|_F^2 comes from the step before, as one
 // partial sum per tile, added in a fixed order by every reader.  (Earlier steps keep g = 0: there P = b A + c A^2 vanishes on the
 // directions where X does, so that it lets none of hi's rounding into them, which a shift would, to be multiplied by a in every
-// later step.)  All planes are scaled by powers of two into the middle of the 16-bit range.  Against 64 bits the result (of this
-// arithmetic, on the CPU) is off by 4e-4 .. 1.1e-3 of its norm for sides from 64 up (flat, k^-1/2 and k^-1 spectra, full rank and a third of it; up to 4e-3 for sides
-// below 20), before its rounding to bf16 (1.7e-3); rounding the iterate to 16 bits instead costs up to 2e-2, all planes in bf16 up to 2e-1.
+// later step.)  All planes are scaled by powers of two into the middle of the 16-bit range.  Against 64 bits the result of five
+// default steps (this arithmetic on the CPU, before the rounding to bf16, which is 1.7e-3) is off by 4e-4 .. 2.4e-3 of its norm for sides from 64 up
+// (flat, k^-1/2 and k^-1 spectra, full rank and a third of it; rows and singular values down to 1e-3 of the largest), by up to 5e-3 between 20 and
+// 64 and 9e-3 below; rounding the iterate to 16 bits instead costs up to 2e-2, all planes in bf16 up to 2e-1.  More steps, or coefficients
+// with steeper slopes, multiply the rounding of the steps before: ten default steps 8e-3, 1 % damped steep sets 5e-3, undamped ones 4e-2 and more.
 //
 // Work.  A and A^2 are symmetric: only tiles on and below the diagonal are computed, and written twice.  Per step
 // s^2 l + s^3 + 2 s^2 l operations.  One cooperative launch runs all steps (ns_steps_kernel).  4096^2, five steps: 1.16 ms, tensor pipe 63 %

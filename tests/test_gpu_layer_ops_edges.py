@@ -102,3 +102,45 @@ def relative_error(g, steps, coeffs=None):
 def test_newton_schulz_just_inside_its_range(m, n, coeffs):
     g = torch.randn(m, 1, generator=gen(51), device="cuda") @ torch.randn(1, n, generator=gen(52), device="cuda")
     assert relative_error(g, len(coeffs), coeffs) <= 2.5e-3 + (2.0 ** -8 if m * n < 64 else 2.0 ** -9)
+
+
+# ------------------------------------------------------------------------------ Newton-Schulz: accuracy by coefficients and steps
+# Each step rounds by up to 2^-11 of the iterate, and later steps multiply that by their slopes; the bounds are the documented ones.
+STEEP = [(8.29, -23.6, 17.3), (4.11, -2.95, 0.545), (3.95, -2.91, 0.552), (3.32, -2.49, 0.510), (2.30, -1.67, 0.419)]
+DAMPED = [(p / 1.01, q / 1.01 ** 3, r / 1.01 ** 5) for p, q, r in STEEP[:-1]] + STEEP[-1:]      # 1 % inside the interval that they are made for
+
+
+def spectrum(kind, m=256, n=400):
+    g = torch.randn(m, n, generator=gen(61), device="cuda")
+    if kind == "diagonal":                                          # 1 .. 1e-3
+        g = torch.zeros(m, n, device="cuda")
+        g[range(m), range(m)] = torch.logspace(0, -3, m, device="cuda")
+    elif kind == "few large rows":
+        g[8:] *= 1e-3
+    return g
+
+
+@pytest.mark.parametrize("kind", ["normal", "diagonal", "few large rows"])
+@pytest.mark.parametrize("steps,coeffs,bound", [(1, None, 2.5e-3), (3, None, 2.5e-3), (5, None, 2.5e-3), (10, None, 1e-2), (5, DAMPED, 1e-2),
+                                                (8, (1.5, -0.5, 0.0), 1e-3), (12, (1.875, -1.25, 0.375), 1e-3)])
+def test_newton_schulz_accuracy(kind, steps, coeffs, bound):
+    assert relative_error(spectrum(kind), steps, coeffs) <= bound + 2.0 ** -9
+
+
+@pytest.mark.parametrize("kind", ["normal", "diagonal"])
+def test_newton_schulz_accuracy_of_coefficients_at_the_edge_of_their_interval(kind):
+    assert relative_error(spectrum(kind), 5, STEEP) <= 1e-1
+
+
+@pytest.mark.parametrize("steps", [20, 64])
+def test_newton_schulz_many_default_steps(steps):
+    assert relative_error(spectrum("normal"), steps) <= 1e-1
+    s = torch.linalg.svdvals(newton_schulz(spectrum("diagonal"), steps).double())
+    assert 0.6 < float(s.min()) and float(s.max()) < 1.3            # the default coefficients keep them in about [0.7, 1.2]
+
+
+@pytest.mark.parametrize("m,n", [(1, 5), (3, 3), (8, 19), (19, 5)])
+def test_newton_schulz_accuracy_of_small_sides(m, n):
+    for seed in range(8):
+        g = torch.randn(m, n, generator=gen(70 + seed), device="cuda")
+        assert relative_error(g, 5) <= 1e-2 + 2.0 ** -8
