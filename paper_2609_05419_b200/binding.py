@@ -99,20 +99,31 @@ def _check(status, where):
         raise Gemm2mError(status, where)
 
 
-_raw_stream = None
+_raw_device = _raw_stream = None
 
 
-def _current_stream():
-    """Handle of torch's current stream.  torch's own look-up by device index takes 0.1 us, a Stream object 3 us."""
+def _current_device():
+    """Index of torch's current device, by torch's own look-up (0.1 us) once it is initialised."""
+    global _raw_device
+    if _raw_device is None:
+        import torch
+        device = getattr(torch._C, "_cuda_getDevice", None)
+        if not device or not torch.cuda.is_initialized():
+            return torch.cuda.current_device()
+        _raw_device = device
+    return _raw_device()
+
+
+def _current_stream(device=None):
+    """Handle of torch's current stream on the current device.  torch's own look-up by device index takes 0.1 us, a Stream object 3 us."""
     global _raw_stream
     if _raw_stream is None:
         import torch
-        raw, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
-        if raw and device and torch.cuda.is_initialized():
-            _raw_stream = lambda: raw(device())
-        else:
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if not raw or not torch.cuda.is_initialized():
             return torch.cuda.current_stream().cuda_stream
-    return _raw_stream()
+        _raw_stream = raw
+    return _raw_stream(_current_device() if device is None else device)
 
 
 def _stream_ptr(stream):
@@ -353,11 +364,19 @@ def _type_of(t, name, allowed):
     return code
 
 
-def _rowmajor(t, name, allowed):
+def _launch_device(t, name):
+    """Index of the device that a call with `t` runs on: the current one, which `t` has to lie on."""
+    device = t.get_device()                         # (-1: not a CUDA tensor)
+    if device < 0 or device != _current_device():
+        raise ValueError(f"{name}: need a CUDA tensor on the current device")
+    return device
+
+
+def _rowmajor(t, name, allowed, device):
     """(pointer, type code, rows, cols, leading dimension) of a 2-D CUDA tensor with contiguous rows."""
     shape = t.shape
-    if len(shape) != 2 or not t.is_cuda:
-        raise ValueError(f"{name}: need a 2-D CUDA tensor")
+    if len(shape) != 2 or t.get_device() != device:
+        raise ValueError(f"{name}: need a 2-D CUDA tensor on the current device")
     rows, cols = shape
     ld, step = t.stride()
     if cols > 1 and step != 1:
@@ -367,10 +386,10 @@ def _rowmajor(t, name, allowed):
     return t.data_ptr(), _type_of(t, name, allowed), rows, cols, ld
 
 
-def _scales(t, name, rows, cols):
+def _scales(t, name, rows, cols, device):
     """(pointer, leading dimension) of a column-major float32 scale matrix of the given shape."""
-    if t.shape != (rows, cols) or not t.is_cuda:
-        raise ValueError(f"{name}: need a CUDA tensor of shape {(rows, cols)}")
+    if t.shape != (rows, cols) or t.get_device() != device:
+        raise ValueError(f"{name}: need a CUDA tensor of shape {(rows, cols)} on the current device")
     _type_of(t, name, (F32,))
     step, ld = t.stride()
     if rows > 1 and step != 1:
@@ -382,8 +401,8 @@ def _scales(t, name, rows, cols):
     return t.data_ptr(), ld
 
 
-def _stream_of(stream):
-    return _current_stream() if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
+def _stream_of(stream, device):
+    return _current_stream(device) if stream is None else stream if isinstance(stream, int) else stream.cuda_stream
 
 
 _FP8 = (E4M3, E5M2)
@@ -401,51 +420,54 @@ def fp8_empty(rows, cols, fmt=E4M3, block_rows=1, device="cuda"):
 
 def fp8_quantise(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None):
     """X (row-major, float32 / float16 / bfloat16) to 8-bit values Q with scales S, and / or its transpose Qt with scales St."""
-    px, tx, rows, cols, ldx = _rowmajor(X, "X", _FLOATS)
+    device = _launch_device(X, "X")
+    px, tx, rows, cols, ldx = _rowmajor(X, "X", _FLOATS, device)
     if block_rows not in (1, 128):
         raise ValueError("block_rows: need 1 or 128")
     fmt, form, form_t = None, _NO_FORM, _NO_FORM
     if Q is not None:
-        pq, fmt, r, c, ldq = _rowmajor(Q, "Q", _FP8)
+        pq, fmt, r, c, ldq = _rowmajor(Q, "Q", _FP8, device)
         if r != rows or c != cols or S is None:
             raise ValueError("Q, S: shape mismatch")
-        form = (pq, ldq, *_scales(S, "S", rows if block_rows == 1 else -(-rows // 128), -(-cols // 128)))
+        form = (pq, ldq, *_scales(S, "S", rows if block_rows == 1 else -(-rows // 128), -(-cols // 128), device))
     if Qt is not None:
-        pq, fmt_t, r, c, ldq = _rowmajor(Qt, "Qt", _FP8)
+        pq, fmt_t, r, c, ldq = _rowmajor(Qt, "Qt", _FP8, device)
         if r != cols or c != rows or St is None or fmt not in (None, fmt_t):
             raise ValueError("Qt, St: shape or type mismatch")
         fmt = fmt_t
-        form_t = (pq, ldq, *_scales(St, "St", cols if block_rows == 1 else -(-cols // 128), -(-rows // 128)))
+        form_t = (pq, ldq, *_scales(St, "St", cols if block_rows == 1 else -(-cols // 128), -(-rows // 128), device))
     if fmt is None:
         raise ValueError("need Q and S, or Qt and St")
-    _check(lib().gemm2m_fp8_quantise(rows, cols, px, tx, ldx, fmt, block_rows, *form, *form_t, _stream_of(stream)), "gemm2m_fp8_quantise")
+    _check(lib().gemm2m_fp8_quantise(rows, cols, px, tx, ldx, fmt, block_rows, *form, *form_t, _stream_of(stream, device)), "gemm2m_fp8_quantise")
 
 
 def fp8_gemm(A, SA, B, SB, D, C=None, a_block=1, b_block=128, stream=None):
     """D = C + A B^T with A (m x k), B (n x k) in 8 bits and their scales; D, C float32 / float16 / bfloat16 (C may be D)."""
-    pa, fa, m, k, lda = _rowmajor(A, "A", _FP8)
-    pb, fb, n, k2, ldb = _rowmajor(B, "B", _FP8)
-    pd, td, md, nd, ldd = _rowmajor(D, "D", _FLOATS)
+    device = _launch_device(A, "A")
+    pa, fa, m, k, lda = _rowmajor(A, "A", _FP8, device)
+    pb, fb, n, k2, ldb = _rowmajor(B, "B", _FP8, device)
+    pd, td, md, nd, ldd = _rowmajor(D, "D", _FLOATS, device)
     if k != k2 or (md, nd) != (m, n):
         raise ValueError("shape mismatch")
     if a_block not in (1, 128) or b_block not in (1, 128):
         raise ValueError("a_block, b_block: need 1 or 128")
     kb = -(-k // 128)
-    sa, ldsa = _scales(SA, "SA", -(-m // a_block), kb)
-    sb, ldsb = _scales(SB, "SB", -(-n // b_block), kb)
+    sa, ldsa = _scales(SA, "SA", -(-m // a_block), kb, device)
+    sb, ldsb = _scales(SB, "SB", -(-n // b_block), kb, device)
     pc, ldc = None, ldd
     if C is not None:
-        pc, tc, mc, nc, ldc = _rowmajor(C, "C", _FLOATS)
+        pc, tc, mc, nc, ldc = _rowmajor(C, "C", _FLOATS, device)
         if (mc, nc) != (m, n) or tc != td:
             raise ValueError("C: need the shape and type of D")
     _check(lib().gemm2m_fp8_gemm(m, n, k, pa, fa, lda, sa, ldsa, a_block, pb, fb, ldb, sb, ldsb, b_block, pc, ldc, pd, td, ldd,
-                                 _stream_of(stream)), "gemm2m_fp8_gemm")
+                                 _stream_of(stream, device)), "gemm2m_fp8_gemm")
 
 
 def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
     """O (bfloat16) = G orthogonalised by Newton-Schulz steps; 2-D, or 3-D for a batch.  coeffs: (a, b, c), or one such per step."""
-    if G.dim() not in (2, 3) or not G.is_cuda or not O.is_cuda or O.shape != G.shape:
-        raise ValueError("G, O: need CUDA tensors of the same 2-D or 3-D shape")
+    device = _launch_device(G, "G")
+    if G.dim() not in (2, 3) or O.get_device() != device or O.shape != G.shape:
+        raise ValueError("G, O: need CUDA tensors of the same 2-D or 3-D shape on the current device")
     tg = _type_of(G, "G", _FLOATS)
     _type_of(O, "O", (BF16,))
     batch = G.shape[0] if G.dim() == 3 else 1
@@ -461,7 +483,7 @@ def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
             raise ValueError("coeffs: need (a, b, c), or one such per step")
         co = ctypes.cast((ctypes.c_float * (3 * steps))(*[float(v) for r in rows for v in r]), ctypes.c_void_p)
     _check(lib().gemm2m_newton_schulz(batch, m, n, G.data_ptr(), tg, ld(G), stride(G), O.data_ptr(), ld(O), stride(O), steps, co, eps,
-                                      _stream_of(stream)), "gemm2m_newton_schulz")
+                                      _stream_of(stream, device)), "gemm2m_newton_schulz")
 
 
 def device_status(stream=None):

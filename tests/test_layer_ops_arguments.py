@@ -37,7 +37,8 @@ def calls(monkeypatch):
             return lambda *args: seen.append((name, args)) or b.OK
 
     monkeypatch.setattr(b, "lib", Recorder)
-    monkeypatch.setattr(b, "_current_stream", lambda: 0)
+    monkeypatch.setattr(b, "_current_stream", lambda *device: 0)
+    monkeypatch.setattr(b, "_current_device", lambda: 0, raising=False)
     return seen
 
 
@@ -117,3 +118,44 @@ def test_empty_matrices_have_leading_dimensions_that_the_library_takes(calls, ro
         for ld, scales, count in ((args[5], args[7], m), (args[11], args[13], n)):
             assert ld >= max(k, 1) and ld % 16 == 0 and scales >= max(count, 1)
         assert args[16] >= n and args[19] >= n                  # ldc, ldd
+
+
+# ------------------------------------------------------------------------------------------------ tensors on more than one device
+def quantise_operands():
+    return dense(300, 500), *matrix(300, 500), *matrix(500, 300)
+
+
+def product_operands():
+    return *matrix(300, 500), *matrix(200, 500), dense(300, 200), dense(300, 200)
+
+
+def newton_schulz_operands():
+    return dense(30, 50), dense(30, 50, torch.bfloat16)
+
+
+def run(name, t):
+    if name == "product":
+        b.fp8_gemm(*t[:5], C=t[5], b_block=1)
+    else:
+        {"quantise": b.fp8_quantise, "newton_schulz": b.newton_schulz}[name](*t)
+
+
+@pytest.mark.parametrize("name,make", [("quantise", quantise_operands), ("product", product_operands), ("newton_schulz", newton_schulz_operands)])
+def test_every_operand_lies_on_the_current_device(calls, monkeypatch, name, make):
+    run(name, make())
+    assert len(calls) == 1
+    for i in range(len(make())):
+        for elsewhere in (1, -1):
+            operands = make()
+            operands[i].index = elsewhere
+            with pytest.raises(ValueError):
+                run(name, operands)
+    operands = make()
+    for t in operands:
+        t.index = 1
+    with pytest.raises(ValueError):
+        run(name, operands)
+    assert len(calls) == 1
+    monkeypatch.setattr(b, "_current_device", lambda: 1)
+    run(name, operands)
+    assert len(calls) == 2
