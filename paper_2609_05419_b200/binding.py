@@ -436,8 +436,8 @@ def fp8_quantise(X, Q=None, S=None, Qt=None, St=None, block_rows=1, stream=None)
             raise ValueError("Qt, St: shape or type mismatch")
         fmt = fmt_t
         form_t = (pq, ldq, *_scales(St, "St", cols if block_rows == 1 else -(-cols // 128), -(-rows // 128), device))
-    if fmt is None:
-        raise ValueError("need Q and S, or Qt and St")
+    if fmt is None or (Q is None and S is not None) or (Qt is None and St is not None):
+        raise ValueError("need Q and S, or Qt and St, or all four")
     _check(lib().gemm2m_fp8_quantise(rows, cols, px, tx, ldx, fmt, block_rows, *form, *form_t, _stream_of(stream, device)), "gemm2m_fp8_quantise")
 
 

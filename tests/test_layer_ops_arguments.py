@@ -159,3 +159,14 @@ def test_every_operand_lies_on_the_current_device(calls, monkeypatch, name, make
     monkeypatch.setattr(b, "_current_device", lambda: 1)
     run(name, operands)
     assert len(calls) == 2
+
+
+# ------------------------------------------------------------------------------------------------------- halves of an output form
+def test_quantise_refuses_scales_without_their_values(calls):
+    q, s = matrix(300, 500)
+    qt, st = matrix(500, 300)
+    x = dense(300, 500)
+    for args in ((None, s, qt, st), (q, s, None, st), (q, None, qt, st), (q, s, qt, None), (None, s, None, None), ()):
+        with pytest.raises(ValueError):
+            b.fp8_quantise(x, *args)
+    assert not calls
