@@ -144,3 +144,34 @@ def test_newton_schulz_accuracy_of_small_sides(m, n):
     for seed in range(8):
         g = torch.randn(m, n, generator=gen(70 + seed), device="cuda")
         assert relative_error(g, 5) <= 1e-2 + 2.0 ** -8
+
+
+# ------------------------------------------------------------------------------------------------ workspaces that hold anything
+# every bit set: NaN as 16-bit and 32-bit numbers, also in the padding of the planes and in the counters
+@pytest.mark.parametrize("batch,m,n", [(1, 1, 7), (1, 33, 130), (1, 130, 33), (3, 300, 200), (2, 200, 300), (1, 200, 6100), (1, 6100, 200), (1, 700, 513)])
+@pytest.mark.parametrize("steps", [1, 2, 5])
+def test_newton_schulz_on_a_workspace_of_nan(batch, m, n, steps):
+    g = torch.randn(batch, m, n, generator=gen(81), device="cuda")
+    outs = []
+    for fill in (0, 255):
+        with Workspace(b.workspace_bytes(b.OP_NEWTON_SCHULZ, m, n, batch, 1)) as ws:
+            ws.buf[256:] = fill
+            o = torch.full(g.shape, float("nan"), dtype=torch.bfloat16, device="cuda")
+            b.newton_schulz(g, o, steps=steps)
+            b.device_status()
+        outs.append(o)
+    assert bool(torch.isfinite(outs[0]).all()) and torch.equal(*outs)
+
+
+def test_product_on_a_workspace_of_nan():
+    qa, sa = operand(200, 300, 1, b.E4M3, 91)
+    qb, sb = operand(260, 300, 128, b.E4M3, 92)
+    outs = []
+    for fill in (0, 255):
+        with Workspace(b.workspace_bytes(b.OP_FP8_GEMM, 200, 260, 300, 1)) as ws:
+            ws.buf[256:] = fill
+            d = torch.full((200, 260), float("nan"), device="cuda")
+            b.fp8_gemm(qa, sa, qb, sb, d)
+            b.device_status()
+        outs.append(d)
+    assert bool(torch.isfinite(outs[0]).all()) and torch.equal(*outs)
