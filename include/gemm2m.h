@@ -327,6 +327,9 @@ int gemm2m_workspace_layout(int op, int64_t m, int64_t n, int64_t k, int nmod, g
  * its code in the workspace's status word and the kernel returns; gemm2m_device_status() then reports
  * GEMM2M_ERR_DEVICE_TIMEOUT once and clears the word.  Needs a registered workspace (GEMM2M_ERR_WORKSPACE otherwise). */
 int gemm2m_debug_wait_selftest(uint64_t budget_ns, void* stream);
+/* Limit (ns) of the device-side waits of gemm2m_newton_schulz for these sizes: it grows with the work of a step, which a wait may have to
+ * outlast.  0 for sizes that the call refuses. */
+uint64_t gemm2m_debug_newton_schulz_wait_ns(int64_t batch, int64_t m, int64_t n);
 /* Which int8 GEMM kernel later calls use: 0 = the tcgen05 kernel on CTA pairs (default), 1 = a plain CUDA-core check
  * kernel kept only so that tests can tell a fault in the tensor-core kernel from one in the pre/post kernels. */
 int gemm2m_debug_set_gemm_kernel(int which);

@@ -80,6 +80,7 @@ def lib():
     L.gemm2m_workspace_layout.argtypes = [i32, i64, i64, i64, i32, ctypes.POINTER(Layout)]
     L.gemm2m_debug_set_gemm_kernel.argtypes = [i32]
     L.gemm2m_debug_wait_selftest.argtypes = [ctypes.c_uint64, vp]
+    L.gemm2m_debug_newton_schulz_wait_ns.argtypes, L.gemm2m_debug_newton_schulz_wait_ns.restype = [i64] * 3, ctypes.c_uint64
     L.gemm2m_debug_set_panels.argtypes = [i32]
     L.dgemm_ozaki2.argtypes = [i64, i64, i64, vp, i64, vp, i64, vp, i64, i32, vp]
     L.gemm2m_debug_tables_real.argtypes = [i32, i64] + [vp] * 10
@@ -506,6 +507,10 @@ def last_launch_count():
     per = (ctypes.c_int * 4)()
     total = int(lib().gemm2m_last_launch_count(per))
     return total, [int(x) for x in per]
+
+
+def debug_newton_schulz_wait_ns(batch, m, n):
+    return int(lib().gemm2m_debug_newton_schulz_wait_ns(batch, m, n))
 
 
 def debug_wait_selftest(budget_ns, stream=None):

@@ -993,6 +993,10 @@ int gemm2m_debug_wait_selftest(uint64_t budget_ns, void* stream) {
     return GEMM2M_OK;
 }
 
+uint64_t gemm2m_debug_newton_schulz_wait_ns(int64_t batch, int64_t m, int64_t n) {
+    return newton_schulz_sizes_ok(batch, m, n) ? newton_schulz_wait_ns(batch, m, n) : 0;
+}
+
 int gemm2m_set_profiling(int enabled) {
     std::lock_guard<std::mutex> lock(g.mu);
     g.profiling = enabled ? 1 : 0;

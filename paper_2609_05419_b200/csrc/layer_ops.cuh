@@ -53,6 +53,7 @@ struct NewtonSchulzArgs {
     int* dev_status;
 };
 cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaStream_t st, int launches[2]);
+unsigned long long newton_schulz_wait_ns(int64_t batch, int64_t m, int64_t n);      // limit of its device-side waits
 
 #ifdef __CUDACC__
 template <typename T> __device__ __forceinline__ float to_float(T v);

@@ -736,6 +736,13 @@ NewtonSchulzLayout newton_schulz_layout(int64_t batch, int64_t m, int64_t n, int
     return l;
 }
 
+// Waits last as long as a phase: the largest product has 2 s^2 l operations per matrix, here allowed a rate of 10^14 per second (a tenth of what
+// it runs at) on top of the limit of every wait.  (100000^2 bf16 in place takes 140 GB and 2 s per phase.)
+unsigned long long newton_schulz_wait_ns(int64_t batch, int64_t m, int64_t n) {
+    const double s = (double)(m < n ? m : n), l = (double)(m < n ? n : m);
+    return kWaitLimitNs + (unsigned long long)(2.0 * s * s * l * (double)batch / 1e5);
+}
+
 cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaStream_t st, int launches[2]) {
     cudaError_t err = a.type == kF32 ? launch_start<float>(a, st, &launches[0])
                       : a.type == kF16 ? launch_start<__half>(a, st, &launches[0]) : launch_start<__nv_bfloat16>(a, st, &launches[0]);
@@ -776,7 +783,7 @@ cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaSt
     p.out_vec = ((uintptr_t)a.O & 15) == 0 && a.ldo % 8 == 0 && a.stride_o % 8 == 0;
     p.phase_count = (uint32_t*)(a.ws + l.off_count);
     p.dev_status = a.dev_status;
-    p.wait_ns = kWaitLimitNs;
+    p.wait_ns = newton_schulz_wait_ns(a.batch, a.m, a.n);
     auto tiles_of = [](int64_t x, int64_t width) { return (x + width - 1) / width; };
     const int64_t rt = tiles_of(p.s, 256), mt = tiles_of(a.m, 256);
     if (tiles_of(p.s, 64) * (rt + 1) > INT32_MAX / 8 / a.batch || mt * tiles_of(a.n, 64) > INT32_MAX / 8 / a.batch) return cudaErrorInvalidValue;

@@ -170,3 +170,13 @@ def test_quantise_refuses_scales_without_their_values(calls):
         with pytest.raises(ValueError):
             b.fp8_quantise(x, *args)
     assert not calls
+
+
+# ------------------------------------------------------------------------------------------------------- limits of device-side waits
+# a CTA without tiles waits for a whole product, 2 s^2 l operations, at no less than 5e14 per second (a third of the 16-bit rate)
+@pytest.mark.parametrize("batch,m,n", [(1, 1, 1), (1, 300, 200), (16, 1024, 1024), (1, 16384, 4096), (1, 40000, 130000), (1, 110000, 100000), (3, 65536, 20000)])
+def test_newton_schulz_waits_outlast_a_step(batch, m, n):
+    limit, product = b.debug_newton_schulz_wait_ns(batch, m, n) * 1e-9, 2.0 * min(m, n) ** 2 * max(m, n) * batch
+    assert limit >= 1.0 + product / 5e14
+    assert limit <= 2.5 + product / 5e13                           # and end all the same
+    assert b.debug_newton_schulz_wait_ns(1, -1, 4) == 0
