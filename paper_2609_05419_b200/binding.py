@@ -479,7 +479,8 @@ def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
     stride = lambda t: t.stride(0) if batch > 1 and t.dim() == 3 else m * max(n, 1)
     co = None
     if coeffs is not None:
-        rows = [coeffs] * steps if not hasattr(coeffs[0], "__len__") else list(coeffs)
+        first = coeffs[0]
+        rows = [coeffs] * steps if not hasattr(first, "__len__") or getattr(first, "ndim", 1) == 0 else list(coeffs)      # (an entry of a tensor has both)
         if len(rows) != steps or any(len(r) != 3 for r in rows):
             raise ValueError("coeffs: need (a, b, c), or one such per step")
         co = ctypes.cast((ctypes.c_float * (3 * steps))(*[float(v) for r in rows for v in r]), ctypes.c_void_p)

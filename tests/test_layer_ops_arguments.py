@@ -1,10 +1,12 @@
 """What the binding of the layer operators passes on to the library, and what it refuses: no GPU is touched, CPU tensors stand in for
 CUDA ones and the library is replaced by a recorder."""
 import ast
+import ctypes
 import os
 import subprocess
 import sys
 
+import numpy as np
 import pytest
 import torch
 
@@ -180,3 +182,17 @@ def test_newton_schulz_waits_outlast_a_step(batch, m, n):
     assert limit >= 1.0 + product / 5e14
     assert limit <= 2.5 + product / 5e13                           # and end all the same
     assert b.debug_newton_schulz_wait_ns(1, -1, 4) == 0
+
+
+# ----------------------------------------------------------------------------------------------------------- coefficients as arrays
+@pytest.mark.parametrize("steps", [3, 5])
+@pytest.mark.parametrize("kind", [tuple, list, np.array, torch.tensor])
+def test_newton_schulz_coefficients_in_any_container(calls, kind, steps):
+    one, each = (1.5, -0.5, 0.25), [(i + 1.5, i - 0.5, i + 0.25) for i in range(steps)]
+    for coeffs, rows in ((one, [one] * steps), (each, each)):
+        b.newton_schulz(*newton_schulz_operands(), steps=steps, coeffs=kind(coeffs))
+        passed = ctypes.cast(calls[-1][1][11], ctypes.POINTER(ctypes.c_float))
+        assert [passed[i] for i in range(3 * steps)] == [v for row in rows for v in row]
+    for bad in (one[:2], each[1:], [row[:2] for row in each]):
+        with pytest.raises(ValueError):
+            b.newton_schulz(*newton_schulz_operands(), steps=steps, coeffs=kind(bad))
