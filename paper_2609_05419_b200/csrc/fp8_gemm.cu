@@ -8,10 +8,11 @@
 // per thread) while the next is being filled.  256 x 256 tiles per CTA pair: the four MMAs of a block take 512 cycles, the
 // 128 x 256 multiply-adds of a CTA's half 256 issue slots of the FP32 pipes.  What bounds it is neither: a block takes about 1000
 // cycles, the way from the commit through the epilogue warps (wait, scales, four TMEM loads, 128 multiply-adds, two warps per scheduler) back
-// to the released buffer, during which each buffer is out of the tensor core's hands.  8192^3 to bf16: 519 us (2.12 PFLOP/s), tensor
-// pipe 45 % active; 4096 x 4096 x 8192 with a scale per column: 183 us.  Measured and not kept: packed pairs (f32x2) in
-// place of scalar multiply-adds, whose register pairs the compiler feeds with moves (620 us); sixteen epilogue warps of 64 columns (590);
-// the wide tile in two parts of 128 columns with two buffers each (577: the first operand is read twice).
+// to the released buffer, during which each buffer is out of the tensor core's hands.  8192^3 to bf16: 504 us in a short run (2.18 PFLOP/s), 585 in
+// a steady stream of calls at the board's power limit; 4096 x 4096 x 8192 with a scale per column: 177 and 203 us.  8192 x 4096 x 4096: tensor
+// pipe 49 % active.  Measured and not kept, against 519 us then: packed pairs (f32x2) in place of scalar multiply-adds, whose register pairs
+// the compiler feeds with moves (620 us); sixteen epilogue warps of 64 columns (590); the wide tile in two parts of 128 columns with two
+// buffers each (577: the first operand is read twice).
 #include "layer_ops.cuh"
 #include "pair_pipeline.cuh"
 
@@ -399,14 +400,14 @@ cudaError_t launch_pair(const Fp8GemmArgs& a, int sm_count, cudaStream_t st, int
 // of S CTAs, whose totals are added through distributed shared memory in the order of the ranks.  The lane operand is
 // what such a product has to read; all stages of the ring are requested at once, so that every SM has 130 to 190 KB on its way.
 // 1 x 4096 x 4096 (16.8 MB of weights, split in four): 6 to 7 us on the device, of which set-up 0.7, first bytes 0.5 (from L2; 2 from HBM), eight
-// blocks 2.6, the join 1.6; 48 x 16384 x 4096 (67 MB): 16.6 us, 4.1 TB/s.
+// blocks 2.6, the join 1.6; 48 x 16384 x 4096 (67 MB): 18.2 us from HBM, 3.7 TB/s.
 
 constexpr int kThinBuffers = 4;                  // accumulators of N columns
 constexpr int kThinSlots = 16, kThinAhead = 6;   // scales turn to block g after tfull of g - 4, so every warp is through with g - 9; slot of g + 6 - 16
 
 template <int N>
 struct ThinCfg {
-    // Epilogue warps, four per part of the columns: eight from 64 columns on (48 x 16384 x 4096: 16.6 us, with four 19.3).
+    // Epilogue warps, four per part of the columns: eight from 64 columns on (48 x 16384 x 4096 on the same operands: 16.6 us, with four 19.3).
     static constexpr int kWarps = N >= 64 ? 8 : 4;
     static constexpr int kCols = N / (kWarps / 4);
     static constexpr int kThreads = 128 + 32 * kWarps;     // copies, MMAs, two scale warps, epilogue
@@ -660,7 +661,7 @@ fp8_gemm_thin_kernel(const __grid_constant__ CUtensorMap map_l, const __grid_con
 // Time of a product in microseconds by each kind of tile, from measurements (B200, 1.7 to 1.9 GHz): `round` tiles run at once, each takes
 // so much per block of k and for its output, and a launch takes the rest.  (256 x 256 tiles per pair: 1024 x 4096 x 4096, one round of 32 blocks, 27 us,
 // 2048^3 18 us; 256 x 128: 512 x 4096 x 4096 21 us, 1001 x 1999 x 1100, nine blocks, 14 us; CTAs of their own, 128 x 128 with k split in
-// four: 128 x 4096 x 4096 13.7 us, 1024 x 1024 x 8192 split in two 23.4 us.)
+// four: 128 x 4096 x 4096 13.7 us, 1024 x 1024 x 8192 split in two 23.4 us; each a call by itself.  In a stream of calls: 23, 15, 18, 12, 13, 24.)
 double pair_cost(const Fp8GemmArgs& a, int width, int sm_count) {
     const double tiles = (double)((a.m + 255) / 256) * (double)((a.n + width - 1) / width), rounds = std::ceil(tiles / (sm_count / 2));
     const double blocks = (double)((a.k + kScaleBlock - 1) / kScaleBlock), cols = a.B.block == 1;

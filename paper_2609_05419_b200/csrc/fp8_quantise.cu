@@ -11,8 +11,9 @@
 // shared memory.  The transposed form turns in shared memory, in 8-byte pieces (8 rows of a column) whose position is XORed with
 // the column's group of 8 so that neither side has bank conflicts.
 //
-// Bound by HBM where a tile has one scale (8192^2 f32, both forms: 62.9 us, 6.4 TB/s) and by its instructions where every row and
-// column has one (8192 x 4096 bf16, both forms: 33.6 us, 4.0 TB/s; 8192^2 bf16, rows only: 35.7 us, 5.6 TB/s).
+// Bound by HBM where a tile has one scale (8192^2 f32, both forms: 62.9 us, 6.4 TB/s).  Where every row and column has one, neither HBM
+// (62 % of its rate) nor the issue slots (55 %) are full: a block's loads, arithmetic and stores follow one another, and 16 warps per SM do not
+// cover the waits for the loads (8192 x 4096 bf16, both forms: 33.5 us, 4.1 TB/s; 8192^2 bf16, rows only, 24 warps: 35.4 us, 5.7 TB/s).
 #include "layer_ops.cuh"
 
 #include <cuda_fp8.h>

@@ -16,8 +16,9 @@
 // with steeper slopes, multiply the rounding of the steps before: ten default steps 8e-3, 1 % damped steep sets 5e-3, undamped ones 4e-2 and more.
 //
 // Work.  A and A^2 are symmetric: only tiles on and below the diagonal are computed, and written twice.  Per step
-// s^2 l + s^3 + 2 s^2 l operations.  One cooperative launch runs all steps (ns_steps_kernel).  4096^2, five steps: 1.16 ms, tensor pipe 63 %
-// active, 1.18 PFLOP/s of the operations above; 16384 x 4096 in 32 bits: 3.7 to 4.3 ms (the board's power limit).  Small
+// s^2 l + s^3 + 2 s^2 l operations.  One cooperative launch runs all steps (ns_steps_kernel).  4096^2, five steps: 1.16 to 1.21 ms in a short run, tensor
+// pipe 63 % active, 1.18 PFLOP/s of the operations above, and 1.41 ms in a steady stream of calls at the board's power limit; 16384 x 4096 in 32 bits:
+// 3.8 and 4.4 ms; 16 x 1024^2: 553 and 637 us.  Small
 // matrices are bound by the chain of each of the 15 products (counter, first copies, MMAs, epilogue, fence: about 5 us).
 #include "layer_ops.cuh"
 #include "pair_pipeline.cuh"
