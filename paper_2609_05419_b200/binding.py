@@ -135,10 +135,19 @@ def _stream_ptr(stream):
     return ctypes.c_void_p(stream.cuda_stream)
 
 
+def _launch_device(t, name):
+    """Index of the device that a call with `t` runs on: the current one, which `t` has to lie on."""
+    device = t.get_device()                         # (-1: not a CUDA tensor)
+    if device < 0 or device != _current_device():
+        raise ValueError(f"{name}: need a CUDA tensor on the current device")
+    return device
+
+
 def _colmajor(t, name):
     """(pointer, rows, cols, leading dimension) of a 2-D CUDA tensor stored column-major."""
-    if t.dim() != 2 or not t.is_cuda:
+    if t.dim() != 2:
         raise ValueError(f"{name}: need a 2-D CUDA tensor")
+    _launch_device(t, name)
     rows, cols = t.shape
     if rows > 1 and t.stride(0) != 1:
         raise ValueError(f"{name}: need column-major storage (stride 1 along dim 0), e.g. torch.empty(cols, rows).t()")
@@ -171,10 +180,11 @@ def workspace_layout(op, m, n, k, nmod):
 
 
 def set_workspace(tensor):
-    """Register a torch uint8 CUDA tensor (kept alive by the caller) as the library's workspace; None unregisters."""
+    """Register a torch uint8 CUDA tensor (kept alive by the caller) as the library's workspace on the current device; None unregisters."""
     if tensor is None:
         _check(lib().gemm2m_set_workspace(None, 0), "gemm2m_set_workspace")
     else:
+        _launch_device(tensor, "workspace")
         _check(lib().gemm2m_set_workspace(ctypes.c_void_p(tensor.data_ptr()), tensor.numel() * tensor.element_size()),
                "gemm2m_set_workspace")
 
@@ -318,7 +328,8 @@ def zscale_exponents_static(A, e, nmod=16, stream=None):
     pa, m, k, lda = _colmajor(A, "A")
     if m > STATIC_MAX_ROWS:
         raise ValueError(f"zscale_exponents_static: {m} rows exceed the built-in scratch ({STATIC_MAX_ROWS} rows)")
-    if e.numel() != m or not e.is_cuda or e.element_size() != 4 or not e.is_contiguous():
+    _launch_device(e, "e")
+    if e.numel() != m or e.element_size() != 4 or not e.is_contiguous():
         raise ValueError("e: need a contiguous int32 CUDA tensor with one entry per row of A")
     _check(lib().gemm2m_zscale_exponents_static(m, k, pa, lda, nmod, ctypes.c_void_p(e.data_ptr()), _stream_ptr(stream)),
            "gemm2m_zscale_exponents_static")
@@ -363,14 +374,6 @@ def _type_of(t, name, allowed):
     if code not in allowed:
         raise ValueError(f"{name}: unsupported type {t.dtype}")
     return code
-
-
-def _launch_device(t, name):
-    """Index of the device that a call with `t` runs on: the current one, which `t` has to lie on."""
-    device = t.get_device()                         # (-1: not a CUDA tensor)
-    if device < 0 or device != _current_device():
-        raise ValueError(f"{name}: need a CUDA tensor on the current device")
-    return device
 
 
 def _rowmajor(t, name, allowed, device):
