@@ -76,7 +76,8 @@ typedef enum {
     GEMM2M_OP_GAUSSIAN_INT = 0, GEMM2M_OP_ZGEMM = 1, GEMM2M_OP_CGEMM = 2, GEMM2M_OP_ZHERK = 3,
     GEMM2M_OP_ZHER2K = 4, GEMM2M_OP_DSYRK = 5, GEMM2M_OP_DSYR2K = 6, GEMM2M_OP_DGEMM_OZAKI2 = 7,
     GEMM2M_OP_ZGEMM_EISENSTEIN = 8, GEMM2M_OP_ZGEMM_HOST = 9,
-    GEMM2M_OP_FP8_GEMM = 10, GEMM2M_OP_NEWTON_SCHULZ = 11       /* layer operators, below; k = batch for the latter, nmod is ignored */
+    GEMM2M_OP_FP8_GEMM = 10, GEMM2M_OP_NEWTON_SCHULZ = 11,      /* layer operators, below; k = batch for the latter, nmod is ignored */
+    GEMM2M_OP_RMS_NORM = 12, GEMM2M_OP_RMS_NORM_BACKWARD = 13   /* m = rows, n = columns, k is ignored */
 } gemm2m_op;
 
 /* Element types of the layer operators.  E4M3 and E5M2 are the 8-bit formats with 4 / 5 exponent bits and largest finite
@@ -288,6 +289,27 @@ int gemm2m_fp8_gemm(int64_t m, int64_t n, int64_t k, const void* A, int a_fmt, i
  * batch a matrix is in.  Workspace: GEMM2M_OP_NEWTON_SCHULZ with (m, n, batch). */
 int gemm2m_newton_schulz(int64_t batch, int64_t m, int64_t n, const void* G, int type, int64_t ldg, int64_t stride_g, void* O, int64_t ldo,
                          int64_t stride_o, int steps, const float* coeffs, float eps, void* stream);
+
+/* Root-mean-square norm of the rows of H = X + R, as operands of the 8-bit products (rows x cols, cols <= 32768; X, R, H, Y of the same type F32 / F16 /
+ * BF16, any alignment and stride; W: cols weights of type w_type, NULL for ones):
+ *   H = X + R rounded to its type (R NULL: H = X);  rstd_i = 1 / sqrt(mean_j H_ij^2 + eps);  N_ij = H_ij rstd_i W_j, held in 32 bits.
+ * Outputs, each may be NULL, at least one is not: H, Y = N rounded, rstd (rows), and N quantised exactly as gemm2m_fp8_quantise does it with
+ * block_rows = 1 (fmt E4M3 / E5M2): Q, S with blocks along the rows, Qt, St with blocks along the columns.  H may be X or R, entry on entry; no
+ * other output may overlap an input.  The norm reads H as stored.  A row whose sum of squares leaves the 32-bit range gives zeros (NaN where
+ * H is infinite); a NaN makes its row NaN, and the scales of the blocks that it is in.
+ * Workspace: GEMM2M_OP_RMS_NORM with (rows, cols), needed for Qt where rstd is NULL. */
+int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t ldx, const void* R, int64_t ldr, const void* W, int w_type, float eps,
+                    void* H, int64_t ldh, void* Y, int64_t ldy, int fmt, void* Q, int64_t ldq, float* S, int64_t lds, void* Qt, int64_t ldqt,
+                    float* St, int64_t ldst, float* rstd, void* stream);
+
+/* Gradients of gemm2m_rms_norm from dY, the gradient of N (an 8-bit form's gradient is that of the values it stands for), with H and rstd as the
+ * forward pass left them: with n = H rstd,
+ *   dX = rstd (dY W - n mean_j(dY W n)) + dR,   dW = sum_i dY n, or dW + that sum where `add` is not 0.
+ * dX is the gradient of X and of R alike; dR (may be NULL) is the gradient that reached H along the residual path.  dY, H, dR, dX: same type, dX may be
+ * any of the others, entry on entry.  dW (32 bits, may be NULL) is summed in 32 bits and a fixed order.
+ * Workspace: GEMM2M_OP_RMS_NORM_BACKWARD with (rows, cols), needed for dW. */
+int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int type, int64_t lddy, const void* H, int64_t ldh, const void* W, int w_type,
+                             const float* rstd, const void* dR, int64_t lddr, void* dX, int64_t lddx, float* dW, int add, void* stream);
 
 /* Waits for `stream` and returns GEMM2M_ERR_DEVICE_TIMEOUT if a kernel of an earlier call on the registered
  * workspace gave up a bounded wait (its results are then invalid), GEMM2M_ERR_CUDA on a CUDA error, else OK. */

@@ -14,6 +14,7 @@ OP_GAUSSIAN_INT, OP_ZGEMM, OP_CGEMM, OP_ZHERK, OP_ZHER2K, OP_DSYRK, OP_DSYR2K, O
 OP_ZGEMM_EISENSTEIN = 8
 OP_ZGEMM_HOST = 9
 OP_FP8_GEMM, OP_NEWTON_SCHULZ = 10, 11
+OP_RMS_NORM, OP_RMS_NORM_BACKWARD = 12, 13
 F32, F16, BF16, E4M3, E5M2 = 0, 1, 2, 3, 4              # gemm2m_type
 OK = 0
 ERR_ARG, ERR_NMOD, ERR_WORKSPACE, ERR_CUDA, ERR_ARCH, ERR_DEVICE_TIMEOUT = 1, 2, 3, 4, 5, 6     # gemm2m_status
@@ -91,6 +92,8 @@ def lib():
     L.gemm2m_fp8_quantise.argtypes = [i64, i64, vp, i32, i64, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp]
     L.gemm2m_fp8_gemm.argtypes = [i64, i64, i64] + [vp, i32, i64, vp, i64, i32] * 2 + [vp, i64, vp, i32, i64, vp]
     L.gemm2m_newton_schulz.argtypes = [i64, i64, i64, vp, i32, i64, i64, vp, i64, i64, i32, vp, ctypes.c_float, vp]
+    L.gemm2m_rms_norm.argtypes = [i64, i64, vp, i32, i64, vp, i64, vp, i32, ctypes.c_float] + [vp, i64] * 2 + [i32] + [vp, i64] * 4 + [vp, vp]
+    L.gemm2m_rms_norm_backward.argtypes = [i64, i64, vp, i32, i64, vp, i64, vp, i32, vp, vp, i64, vp, i64, vp, i32, vp]
     _lib = L
     return L
 
@@ -489,6 +492,72 @@ def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
         co = ctypes.cast((ctypes.c_float * (3 * steps))(*[float(v) for r in rows for v in r]), ctypes.c_void_p)
     _check(lib().gemm2m_newton_schulz(batch, m, n, G.data_ptr(), tg, ld(G), stride(G), O.data_ptr(), ld(O), stride(O), steps, co, eps,
                                       _stream_of(stream, device)), "gemm2m_newton_schulz")
+
+
+def _like(t, name, shape, kind, device):
+    """(pointer, leading dimension) of a matrix that has to have this shape and type, (None, 0) for None."""
+    if t is None:
+        return None, 0
+    p, code, rows, cols, ld = _rowmajor(t, name, _FLOATS, device)
+    if (rows, cols) != shape or code != kind:
+        raise ValueError(f"{name}: shape or type mismatch")
+    return p, ld
+
+
+def _vector(t, name, size, allowed, device):
+    """(pointer, type code) of a contiguous vector, (None, F32) for None."""
+    if t is None:
+        return None, F32
+    if t.dim() != 1 or t.shape[0] != size or t.get_device() != device or (size > 1 and t.stride(0) != 1):
+        raise ValueError(f"{name}: need a contiguous CUDA tensor of {size} entries on the current device")
+    return t.data_ptr(), _type_of(t, name, allowed)
+
+
+def _fp8_form(Q, S, names, rows, cols, device):
+    """(format or None, (pointer, ld, scales, ld)) of an 8-bit form with 1 x 128 blocks that may be absent."""
+    if Q is None and S is None:
+        return None, _NO_FORM
+    if Q is None or S is None:
+        raise ValueError(f"{names}: need both or neither")
+    p, fmt, r, c, ld = _rowmajor(Q, names, _FP8, device)
+    if (r, c) != (rows, cols):
+        raise ValueError(f"{names}: shape mismatch")
+    return fmt, (p, ld, *_scales(S, names, rows, -(-cols // 128), device))
+
+
+def rms_norm(X, W=None, R=None, H=None, Y=None, Q=None, S=None, Qt=None, St=None, rstd=None, eps=1e-6, stream=None):
+    """Root-mean-square norm of the rows of H = X + R with weights W, into any of H, Y (type of X), 8-bit Q with scales S, the
+    transposed Qt with St (both as fp8_empty lays them out), rstd (float32, one per row)."""
+    device = _launch_device(X, "X")
+    px, tx, rows, cols, ldx = _rowmajor(X, "X", _FLOATS, device)
+    shape = (rows, cols)
+    pr, ldr = _like(R, "R", shape, tx, device)
+    ph, ldh = _like(H, "H", shape, tx, device)
+    py, ldy = _like(Y, "Y", shape, tx, device)
+    pw, tw = _vector(W, "W", cols, _FLOATS, device)
+    fmt, form = _fp8_form(Q, S, "Q, S", rows, cols, device)
+    fmt_t, form_t = _fp8_form(Qt, St, "Qt, St", cols, rows, device)
+    if fmt is not None and fmt_t is not None and fmt != fmt_t:
+        raise ValueError("Q, Qt: types differ")
+    fmt = fmt if fmt is not None else fmt_t if fmt_t is not None else E4M3
+    _check(lib().gemm2m_rms_norm(rows, cols, px, tx, ldx, pr, ldr, pw, tw, eps, ph, ldh, py, ldy, fmt, *form, *form_t,
+                                 _vector(rstd, "rstd", rows, (F32,), device)[0], _stream_of(stream, device)), "gemm2m_rms_norm")
+
+
+def rms_norm_backward(dY, H, W, rstd, dX, dR=None, dW=None, add=False, stream=None):
+    """dX = the gradient of rms_norm's X (and R) from dY, joined with dR; dW (float32) = the gradient of W, added to dW for add=True.
+    H and rstd as rms_norm left them; W None: ones."""
+    device = _launch_device(dY, "dY")
+    pg, tg, rows, cols, ldg = _rowmajor(dY, "dY", _FLOATS, device)
+    shape = (rows, cols)
+    if H is None or dX is None or rstd is None:
+        raise ValueError("need H, rstd and dX")
+    ph, ldh = _like(H, "H", shape, tg, device)
+    px, ldx = _like(dX, "dX", shape, tg, device)
+    pr, ldr = _like(dR, "dR", shape, tg, device)
+    pw, tw = _vector(W, "W", cols, _FLOATS, device)
+    _check(lib().gemm2m_rms_norm_backward(rows, cols, pg, tg, ldg, ph, ldh, pw, tw, _vector(rstd, "rstd", rows, (F32,), device)[0], pr, ldr, px, ldx,
+                                          _vector(dW, "dW", cols, (F32,), device)[0], 1 if add else 0, _stream_of(stream, device)), "gemm2m_rms_norm_backward")
 
 
 def device_status(stream=None):

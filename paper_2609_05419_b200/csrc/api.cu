@@ -196,6 +196,22 @@ bool newton_schulz_sizes_ok(int64_t batch, int64_t m, int64_t n) {
     return batch >= 0 && batch <= 65535 && m >= 0 && n >= 0 && m <= kMaxNsSide && n <= kMaxNsSide;
 }
 
+bool norm_sizes_ok(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kMaxCoord && cols >= 0 && cols <= kMaxNormCols; }
+size_t rms_norm_bytes(int64_t rows) { return (size_t)(kLayerOpsOffset + round_up(4 * rows, 256)); }      // rstd, where the caller does not keep it
+size_t rms_norm_backward_bytes(int64_t rows, int64_t cols) {
+    return (size_t)(kLayerOpsOffset + (rows && cols ? round_up(4 * cols * rms_norm_backward_parts(rows, cols), 256) : 0));
+}
+bool float_type(int type) { return type >= GEMM2M_F32 && type <= GEMM2M_BF16; }
+// A row-major matrix that may be absent.
+bool rows_ok(const void* p, int64_t ld, int64_t cols) { return !p || ld >= (cols > 1 ? cols : 1); }
+// An 8-bit matrix with its column-major scales (`scale_rows` of them per column): both there or neither.
+bool fp8_form_ok(const void* Q, int64_t ldq, const float* S, int64_t lds, int64_t width, int64_t scale_rows) {
+    if (!Q || !S) return !Q && !S;
+    return ldq >= (width > 1 ? width : 1) && ldq % 16 == 0 && ((uintptr_t)Q & 15) == 0 && lds >= (scale_rows > 1 ? scale_rows : 1);
+}
+// An output may lie where an input does, entry on entry.
+bool in_place_ok(const void* out, int64_t ldo, const void* in, int64_t ldi) { return !out || out != in || ldo == ldi; }
+
 constexpr int64_t kMaxRows = 65535LL * 32;   // grid.y limit of the residue kernels
 
 // hex: the Eisenstein variant's lattice rounding in front of the same residue arithmetic (complex double only).
@@ -556,6 +572,8 @@ int gemm2m_modulus(int j, int* m, int* s) {
 size_t gemm2m_workspace_bytes(int op, int64_t m, int64_t n, int64_t k, int nmod) {
     if (op == GEMM2M_OP_FP8_GEMM) return fp8_sizes_ok(m, n, k) ? (size_t)kLayerOpsOffset : 0;
     if (op == GEMM2M_OP_NEWTON_SCHULZ) return newton_schulz_sizes_ok(k, m, n) ? (size_t)newton_schulz_layout(k, m, n, kLayerOpsOffset).total : 0;
+    if (op == GEMM2M_OP_RMS_NORM) return norm_sizes_ok(m, n) ? rms_norm_bytes(m) : 0;
+    if (op == GEMM2M_OP_RMS_NORM_BACKWARD) return norm_sizes_ok(m, n) ? rms_norm_backward_bytes(m, n) : 0;
     Carve c;
     if (op == GEMM2M_OP_GAUSSIAN_INT && nmod > 8) return 0;
     if (!carve(op, m, n, k, nmod, &c)) return 0;
@@ -967,6 +985,62 @@ int gemm2m_newton_schulz(int64_t batch, int64_t m, int64_t n, const void* G, int
     CK(ph.end(st));
     g.launches[1] = launches[0];
     g.launches[2] = launches[1];
+    ph.done();
+    return GEMM2M_OK;
+}
+
+int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t ldx, const void* R, int64_t ldr, const void* W, int w_type, float eps,
+                    void* H, int64_t ldh, void* Y, int64_t ldy, int fmt, void* Q, int64_t ldq, float* S, int64_t lds, void* Qt, int64_t ldqt,
+                    float* St, int64_t ldst, float* rstd, void* stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    if (!norm_sizes_ok(rows, cols) || !float_type(type) || (W && !float_type(w_type)) || !(eps >= 0.f)) return GEMM2M_ERR_ARG;
+    if (ldx < (cols > 1 ? cols : 1) || !rows_ok(R, ldr, cols) || !rows_ok(H, ldh, cols) || !rows_ok(Y, ldy, cols)) return GEMM2M_ERR_ARG;
+    if (!in_place_ok(H, ldh, X, ldx) || !in_place_ok(H, ldh, R, ldr) || (Y && (Y == X || Y == R || Y == H))) return GEMM2M_ERR_ARG;
+    if ((Q || Qt) && fmt != GEMM2M_E4M3 && fmt != GEMM2M_E5M2) return GEMM2M_ERR_ARG;
+    if (!fp8_form_ok(Q, ldq, S, lds, cols, rows) || !fp8_form_ok(Qt, ldqt, St, ldst, rows, cols)) return GEMM2M_ERR_ARG;
+    if (!H && !Y && !Q && !Qt && !rstd) return GEMM2M_ERR_ARG;
+    if (rows == 0 || cols == 0) return GEMM2M_OK;
+    if (!X || ((rows + 127) / 128) * ((cols + 127) / 128) > INT32_MAX) return GEMM2M_ERR_ARG;
+    if (int s = check_device()) return s;
+    if (Qt && !rstd) {
+        if (!D().ws || D().ws_bytes < rms_norm_bytes(rows)) return GEMM2M_ERR_WORKSPACE;
+        rstd = (float*)((char*)D().ws + kLayerOpsOffset);
+    }
+    cudaStream_t st = (cudaStream_t)stream;
+    Phases ph;
+    if (int s = begin_call(&ph)) return s;
+    const RmsNormArgs a = {rows, cols, X, type, ldx, R, ldr, W, w_type, eps, H, ldh, Y, ldy, fmt, (uint8_t*)Q, ldq, S, lds, (uint8_t*)Qt, ldqt, St, ldst, rstd};
+    CK(ph.begin(1, st));
+    CK(launch_rms_norm(a, st, &g.launches[1]));
+    CK(ph.end(st));
+    ph.done();
+    return GEMM2M_OK;
+}
+
+int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int type, int64_t lddy, const void* H, int64_t ldh, const void* W, int w_type,
+                             const float* rstd, const void* dR, int64_t lddr, void* dX, int64_t lddx, float* dW, int add, void* stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    if (!norm_sizes_ok(rows, cols) || !float_type(type) || (W && !float_type(w_type))) return GEMM2M_ERR_ARG;
+    const int64_t least = cols > 1 ? cols : 1;
+    if (lddy < least || ldh < least || lddx < least || !rows_ok(dR, lddr, cols)) return GEMM2M_ERR_ARG;
+    if (!in_place_ok(dX, lddx, dY, lddy) || !in_place_ok(dX, lddx, H, ldh) || !in_place_ok(dX, lddx, dR, lddr)) return GEMM2M_ERR_ARG;
+    if (cols == 0 || (rows == 0 && (!dW || add))) return GEMM2M_OK;
+    if (rows && (!dY || !H || !rstd || !dX)) return GEMM2M_ERR_ARG;
+    if (int s = check_device()) return s;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (rows == 0) {                     // a sum over no rows
+        std::memset(g.launches, 0, sizeof(g.launches));
+        CK(cudaMemsetAsync(dW, 0, (size_t)cols * 4, st));
+        return GEMM2M_OK;
+    }
+    if (dW && (!D().ws || D().ws_bytes < rms_norm_backward_bytes(rows, cols))) return GEMM2M_ERR_WORKSPACE;
+    Phases ph;
+    if (int s = begin_call(&ph)) return s;
+    const RmsNormBackwardArgs a = {rows, cols, dY, type, lddy, H, ldh, W, w_type, rstd, dR, lddr, dX, lddx, dW, add,
+                                   dW ? (float*)((char*)D().ws + kLayerOpsOffset) : nullptr, rms_norm_backward_parts(rows, cols)};
+    CK(ph.begin(2, st));
+    CK(launch_rms_norm_backward(a, st, &g.launches[2]));
+    CK(ph.end(st));
     ph.done();
     return GEMM2M_OK;
 }

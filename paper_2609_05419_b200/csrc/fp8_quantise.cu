@@ -14,43 +14,13 @@
 // Bound by HBM where a tile has one scale (8192^2 f32, both forms: 62.9 us, 6.4 TB/s).  Where every row and column has one, neither HBM
 // (62 % of its rate) nor the issue slots (55 %) are full: a block's loads, arithmetic and stores follow one another, and 16 warps per SM do not
 // cover the waits for the loads (8192 x 4096 bf16, both forms: 33.5 us, 4.1 TB/s; 8192^2 bf16, rows only, 24 warps: 35.4 us, 5.7 TB/s).
-#include "layer_ops.cuh"
-
-#include <cuda_fp8.h>
+#include "fp8_pack.cuh"
 
 namespace gemm2m {
 
 namespace {
 
 constexpr int kThreads = 256;
-
-template <int FMT>
-__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
-    constexpr __nv_fp8_interpretation_t kind = FMT == kE4M3 ? __NV_E4M3 : __NV_E5M2;
-    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, kind);
-    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, kind);
-    return lo | (hi << 16);
-}
-
-// Scale and inverse scale of a block from the bit pattern of its largest magnitude.
-template <int FMT>
-__device__ __forceinline__ void scales(uint32_t top, float* s, float* inv) {
-    constexpr float kMax = FMT == kE4M3 ? 448.f : 57344.f;
-    const float u = fmaxf(__uint_as_float(top), kLeastMax);
-    const bool finite = top < 0x7f800000u;
-    *s = finite ? __fdiv_rn(u, kMax) : __uint_as_float(0x7fffffffu);
-    *inv = finite ? __fdiv_rn(kMax, u) : 0.f;
-}
-
-__device__ __forceinline__ void store8(uint8_t* p, uint2 v, int64_t valid) {
-    if (valid >= 8) {
-        *reinterpret_cast<uint2*>(p) = v;
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (i < valid) p[i] = (uint8_t)((i < 4 ? v.x : v.y) >> (8 * (i & 3)));
-    }
-}
 
 template <typename T, int FMT, bool TILE, bool BOTH>
 __global__ void __launch_bounds__(kThreads, sizeof(T) == 4 || (BOTH && !TILE) ? 2 : 3) fp8_quantise_kernel(const QuantiseArgs a, int col_tiles, int vec) {

@@ -10,6 +10,7 @@
 namespace gemm2m {
 
 constexpr int kScaleBlock = 128;          // entries along k that share a scale
+constexpr int kSms = 148;                  // of a B200: grids that decide how sums are cut go by this, not by the device at hand
 constexpr float kLeastMax = 0x1p-100f;    // smallest block maximum: keeps MAX / maximum finite, and gives a block of zeros a scale
 
 // Element types, numbered as in gemm2m_type.
@@ -55,6 +56,35 @@ struct NewtonSchulzArgs {
 cudaError_t launch_newton_schulz(const NewtonSchulzArgs& a, int sm_count, cudaStream_t st, int launches[2]);
 unsigned long long newton_schulz_wait_ns(int64_t batch, int64_t m, int64_t n);      // limit of its device-side waits
 
+// Root-mean-square norm of the rows of H = X + R (rms_norm.cu); any of the outputs may be null.
+constexpr int64_t kMaxNormCols = 32768;   // a row is held in the registers of one block
+struct RmsNormArgs {
+    int64_t rows, cols;
+    const void* X; int type; int64_t ldx;                    // X, R, H, Y: the same type
+    const void* R; int64_t ldr;
+    const void* W; int w_type; float eps;                    // null: ones
+    void* H; int64_t ldh;
+    void* Y; int64_t ldy;
+    int fmt;
+    uint8_t* Q; int64_t ldq; float* S; int64_t lds;
+    uint8_t* Qt; int64_t ldqt; float* St; int64_t ldst;
+    float* rstd;                                             // needed for Qt
+};
+cudaError_t launch_rms_norm(const RmsNormArgs& a, cudaStream_t st, int* launches);
+struct RmsNormBackwardArgs {
+    int64_t rows, cols;
+    const void* dY; int type; int64_t lddy;                  // dY, H, dR, dX: the same type
+    const void* H; int64_t ldh;
+    const void* W; int w_type;
+    const float* rstd;
+    const void* dR; int64_t lddr;
+    void* dX; int64_t lddx;
+    float* dW; int add;
+    float* part; int64_t parts;                              // workspace: partial sums of dW
+};
+int64_t rms_norm_backward_parts(int64_t rows, int64_t cols);      // rows of partial sums of dW
+cudaError_t launch_rms_norm_backward(const RmsNormBackwardArgs& a, cudaStream_t st, int* launches);
+
 #ifdef __CUDACC__
 template <typename T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }
@@ -70,6 +100,14 @@ __device__ __forceinline__ Raw8<T> load8(const T* p) {
     Raw8<T> r;
 #pragma unroll
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = __ldg(reinterpret_cast<const uint4*>(p) + i);
+    return r;
+}
+// The same of memory that the kernel also writes (an output in the place of an input): not through the read-only path.
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8_rw(const T* p) {
+    Raw8<T> r;
+#pragma unroll
+    for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const uint4*>(p)[i];
     return r;
 }
 template <typename T>
@@ -90,6 +128,32 @@ __device__ __forceinline__ void to_floats8(const Raw8<T>& r, float (&v)[8]) {
     const T* t = reinterpret_cast<const T*>(&r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = to_float<T>(t[i]);
+}
+template <typename T> __device__ __forceinline__ T from_float(float v);
+template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
+template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
+template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+// Eight values rounded to T; a whole aligned group, or the first `valid` entries one by one.
+template <typename T>
+__device__ __forceinline__ void store8_as(T* p, const float (&v)[8], bool whole, int64_t valid) {
+    Raw8<T> r;
+    T* t = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t[i] = from_float<T>(v[i]);
+    if (whole) {
+#pragma unroll
+        for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = r.w[i];
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < valid) p[i] = t[i];
+    }
+}
+// Eight entries of a vector of any floating type (type code known at run time).
+__device__ __forceinline__ void load8_any(const void* p, int type, int64_t at, int64_t valid, bool whole, float (&v)[8]) {
+    if (type == kF32) to_floats8<float>(whole ? load8<float>((const float*)p + at) : load8_part<float>((const float*)p + at, valid), v);
+    else if (type == kF16) to_floats8<__half>(whole ? load8<__half>((const __half*)p + at) : load8_part<__half>((const __half*)p + at, valid), v);
+    else to_floats8<__nv_bfloat16>(whole ? load8<__nv_bfloat16>((const __nv_bfloat16*)p + at) : load8_part<__nv_bfloat16>((const __nv_bfloat16*)p + at, valid), v);
 }
 
 #endif
