@@ -77,7 +77,8 @@ typedef enum {
     GEMM2M_OP_ZHER2K = 4, GEMM2M_OP_DSYRK = 5, GEMM2M_OP_DSYR2K = 6, GEMM2M_OP_DGEMM_OZAKI2 = 7,
     GEMM2M_OP_ZGEMM_EISENSTEIN = 8, GEMM2M_OP_ZGEMM_HOST = 9,
     GEMM2M_OP_FP8_GEMM = 10, GEMM2M_OP_NEWTON_SCHULZ = 11,      /* layer operators, below; k = batch for the latter, nmod is ignored */
-    GEMM2M_OP_RMS_NORM = 12, GEMM2M_OP_RMS_NORM_BACKWARD = 13   /* m = rows, n = columns, k is ignored */
+    GEMM2M_OP_RMS_NORM = 12, GEMM2M_OP_RMS_NORM_BACKWARD = 13,  /* m = rows, n = columns, k is ignored */
+    GEMM2M_OP_CLIP_GRADIENTS = 14      /* m = number of tensors */
 } gemm2m_op;
 
 /* Element types of the layer operators.  E4M3 and E5M2 are the 8-bit formats with 4 / 5 exponent bits and largest finite
@@ -310,6 +311,18 @@ int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t
  * Workspace: GEMM2M_OP_RMS_NORM_BACKWARD with (rows, cols), needed for dW. */
 int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int type, int64_t lddy, const void* H, int64_t ldh, const void* W, int w_type,
                              const float* rstd, const void* dR, int64_t lddr, void* dX, int64_t lddx, float* dW, int add, void* stream);
+
+/* Common 2-norm of `count` tensors (up to 2^20 of up to 2^40 entries, types F32 / F16 / BF16 mixed as they come), and the tensors scaled down where it is above
+ * max_norm:
+ *   norm = sqrt(sum of all squares), summed in 64 bits over sums of 8 in 32 bits (all in 64 where those would leave their range);
+ *   factor = 1 where max_norm >= norm + eps, otherwise max_norm / (norm + eps), and NaN for a NaN norm;  O_i = G_i factor, rounded to its type.
+ * Host arrays of `count` entries each: device pointers G_i and O_i, types, rows, columns and leading dimensions (row-major; rows = 1 for any contiguous tensor;
+ * empty tensors may have null pointers).  O = NULL, or O_i = G_i with the same leading dimension: in place; otherwise no output may overlap another output or
+ * an input (views of one matrix side by side do not).  In place nothing is written where the factor is 1.  norm: device pointer to one float (Inf
+ * where the norm is above the 32-bit range; the factor is formed from 64 bits), may be NULL.  max_norm may be infinite: with every tensor in place, the norm alone is formed.  The order of the sums goes by the tensors' sizes alone.
+ * Workspace: GEMM2M_OP_CLIP_GRADIENTS with m = count. */
+int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, const int* types, const int64_t* rows, const int64_t* cols, const int64_t* ldg,
+                          const int64_t* ldo, float max_norm, float eps, float* norm, void* stream);
 
 /* Waits for `stream` and returns GEMM2M_ERR_DEVICE_TIMEOUT if a kernel of an earlier call on the registered
  * workspace gave up a bounded wait (its results are then invalid), GEMM2M_ERR_CUDA on a CUDA error, else OK. */

@@ -14,7 +14,7 @@ OP_GAUSSIAN_INT, OP_ZGEMM, OP_CGEMM, OP_ZHERK, OP_ZHER2K, OP_DSYRK, OP_DSYR2K, O
 OP_ZGEMM_EISENSTEIN = 8
 OP_ZGEMM_HOST = 9
 OP_FP8_GEMM, OP_NEWTON_SCHULZ = 10, 11
-OP_RMS_NORM, OP_RMS_NORM_BACKWARD = 12, 13
+OP_RMS_NORM, OP_RMS_NORM_BACKWARD, OP_CLIP_GRADIENTS = 12, 13, 14
 F32, F16, BF16, E4M3, E5M2 = 0, 1, 2, 3, 4              # gemm2m_type
 OK = 0
 ERR_ARG, ERR_NMOD, ERR_WORKSPACE, ERR_CUDA, ERR_ARCH, ERR_DEVICE_TIMEOUT = 1, 2, 3, 4, 5, 6     # gemm2m_status
@@ -94,6 +94,7 @@ def lib():
     L.gemm2m_newton_schulz.argtypes = [i64, i64, i64, vp, i32, i64, i64, vp, i64, i64, i32, vp, ctypes.c_float, vp]
     L.gemm2m_rms_norm.argtypes = [i64, i64, vp, i32, i64, vp, i64, vp, i32, ctypes.c_float] + [vp, i64] * 2 + [i32] + [vp, i64] * 4 + [vp, vp]
     L.gemm2m_rms_norm_backward.argtypes = [i64, i64, vp, i32, i64, vp, i64, vp, i32, vp, vp, i64, vp, i64, vp, i32, vp]
+    L.gemm2m_clip_gradients.argtypes = [i64] + [vp] * 7 + [ctypes.c_float, ctypes.c_float, vp, vp]
     _lib = L
     return L
 
@@ -558,6 +559,60 @@ def rms_norm_backward(dY, H, W, rstd, dX, dR=None, dW=None, add=False, stream=No
     pw, tw = _vector(W, "W", cols, _FLOATS, device)
     _check(lib().gemm2m_rms_norm_backward(rows, cols, pg, tg, ldg, ph, ldh, pw, tw, _vector(rstd, "rstd", rows, (F32,), device)[0], pr, ldr, px, ldx,
                                           _vector(dW, "dW", cols, (F32,), device)[0], 1 if add else 0, _stream_of(stream, device)), "gemm2m_rms_norm_backward")
+
+
+def _rows_of(t, name, device):
+    """(pointer, type code, rows, columns, leading dimension) of a float tensor of any shape: dense in any order of its axes, or 2-D with rows apart."""
+    if t.get_device() != device:
+        raise ValueError(f"{name}: need CUDA tensors on the current device")
+    code = _type_of(t, name, _FLOATS)
+    if t.is_contiguous():
+        size = t.numel()
+        return t.data_ptr(), code, 1, size, size
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 2 and strides[1] == 1 and strides[0] >= shape[1]:
+        return t.data_ptr(), code, shape[0], shape[1], strides[0]
+    dense = 1
+    for stride, size in sorted(zip(strides, shape)):
+        if size > 1:
+            if stride != dense:
+                raise ValueError(f"{name}: need tensors that are dense, or 2-D with contiguous rows")
+            dense *= size
+    return t.data_ptr(), code, 1, dense, dense
+
+
+def clip_gradients(grads, max_norm, out=None, norm=None, eps=1e-6, stream=None):
+    """Common 2-norm of a list of tensors (float32 / float16 / bfloat16) into `norm` (float32, one entry), and the tensors times
+    min(1, max_norm / (norm + eps)), in place or into the list `out`.  max_norm = inf: the norm alone, unless there is an `out`."""
+    grads = list(grads)
+    count = len(grads)
+    device = _current_device()
+    if norm is not None:
+        if norm.numel() != 1 or norm.get_device() != device:
+            raise ValueError("norm: need a CUDA tensor of one entry on the current device")
+        _type_of(norm, "norm", (F32,))
+    rows = [_rows_of(t, "grads", device) for t in grads]
+    array = lambda kind, values: (kind * max(count, 1))(*values)
+    i64 = ctypes.c_int64
+    p_out = ld_out = None
+    if out is not None:
+        out = list(out)
+        if len(out) != count:
+            raise ValueError("out: need as many tensors as grads")
+        outs = [_rows_of(t, "out", device) for t in out]
+        for i, (g, o) in enumerate(zip(grads, out)):
+            if g.shape != o.shape or rows[i][1] != outs[i][1]:
+                raise ValueError("out: shape or type mismatch")
+            if rows[i][2:] != outs[i][2:] or any(size > 1 and a != c for size, a, c in zip(g.shape, g.stride(), o.stride())):
+                # the same order of entries, with rows of their own distance
+                if g.dim() != 2 or any(t.shape[1] > 1 and t.stride(1) != 1 for t in (g, o)):
+                    raise ValueError("out: need the order of the gradient's axes in memory")
+                m, n = g.shape
+                rows[i], outs[i] = ((*r[:2], m, n, t.stride(0) if m > 1 else n) for r, t in ((rows[i], g), (outs[i], o)))
+        p_out, ld_out = array(ctypes.c_void_p, [r[0] for r in outs]), array(i64, [r[4] for r in outs])
+    _check(lib().gemm2m_clip_gradients(count, array(ctypes.c_void_p, [r[0] for r in rows]), p_out, array(ctypes.c_int, [r[1] for r in rows]),
+                                       *(array(i64, [r[k] for r in rows]) for k in (2, 3, 4)), ld_out, max_norm, eps,
+                                       None if norm is None else norm.data_ptr(), _stream_of(stream, device)), "gemm2m_clip_gradients")
 
 
 def device_status(stream=None):

@@ -5,9 +5,12 @@
 #include "common.cuh"
 #include "layer_ops.cuh"
 
+#include <algorithm>
+#include <cmath>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
+#include <vector>
 
 using namespace gemm2m;
 
@@ -202,15 +205,56 @@ size_t rms_norm_backward_bytes(int64_t rows, int64_t cols) {
     return (size_t)(kLayerOpsOffset + (rows && cols ? round_up(4 * cols * rms_norm_backward_parts(rows, cols), 256) : 0));
 }
 bool float_type(int type) { return type >= GEMM2M_F32 && type <= GEMM2M_BF16; }
+// An address that entries of `size` bytes can have (or none): a misplaced one would be a fault on the device.
+bool placed(const void* p, size_t size) { return (uintptr_t)p % size == 0; }
+size_t float_size(int type) { return type == GEMM2M_F32 ? 4 : 2; }
 // A row-major matrix that may be absent.
-bool rows_ok(const void* p, int64_t ld, int64_t cols) { return !p || ld >= (cols > 1 ? cols : 1); }
+bool rows_ok(const void* p, int type, int64_t ld, int64_t cols) { return !p || (ld >= (cols > 1 ? cols : 1) && placed(p, float_size(type))); }
 // An 8-bit matrix with its column-major scales (`scale_rows` of them per column): both there or neither.
 bool fp8_form_ok(const void* Q, int64_t ldq, const float* S, int64_t lds, int64_t width, int64_t scale_rows) {
     if (!Q || !S) return !Q && !S;
-    return ldq >= (width > 1 ? width : 1) && ldq % 16 == 0 && ((uintptr_t)Q & 15) == 0 && lds >= (scale_rows > 1 ? scale_rows : 1);
+    return placed(S, 4) && ldq >= (width > 1 ? width : 1) && ldq % 16 == 0 && ((uintptr_t)Q & 15) == 0 && lds >= (scale_rows > 1 ? scale_rows : 1);
 }
 // An output may lie where an input does, entry on entry.
 bool in_place_ok(const void* out, int64_t ldo, const void* in, int64_t ldi) { return !out || out != in || ldo == ldi; }
+
+constexpr int64_t kMaxGradients = 1 << 20, kMaxGradient = 1LL << 40;      // tensors of a call, entries of one
+size_t clip_bytes(int64_t count) { return (size_t)(kLayerOpsOffset + round_up(8 * clip_partials(count), 256)); }
+
+// Memory that a tensor spans, to find outputs that overlap something else.
+struct Span { uintptr_t begin, end; int64_t row, width; bool written; };      // bytes; row = distance of rows, width = of entries in a row
+bool spans_meet(const Span& a, const Span& b) {          // a.begin <= b.begin < a.end
+    if (a.row != b.row || a.row == a.width || b.row == b.width) return true;
+    const int64_t at = (int64_t)(b.begin - a.begin) % a.row;       // views of one matrix side by side: where b's rows begin between a's
+    return at < a.width || at + b.width > a.row;
+}
+bool gradients_apart(const std::vector<GradTensor>& t) {
+    std::vector<Span> spans;
+    spans.reserve(2 * t.size());
+    for (const GradTensor& x : t) {
+        if (x.rows * x.cols == 0) continue;
+        const int64_t es = x.type == GEMM2M_F32 ? 4 : 2;
+        auto span = [&](const void* p, int64_t ld, bool written) {
+            const uintptr_t begin = (uintptr_t)p;
+            spans.push_back({begin, begin + (uintptr_t)(((x.rows - 1) * ld + x.cols) * es), ld * es, x.cols * es, written});
+        };
+        span(x.o, x.ldo, true);
+        if (x.o != x.g) span(x.g, x.ldg, false);
+    }
+    std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
+    std::vector<const Span*> open;                       // spans that have not ended yet
+    for (const Span& s : spans) {
+        size_t kept = 0;
+        for (const Span* o : open) {
+            if (o->end <= s.begin) continue;
+            if ((o->written || s.written) && spans_meet(*o, s)) return false;
+            open[kept++] = o;
+        }
+        open.resize(kept);
+        open.push_back(&s);
+    }
+    return true;
+}
 
 constexpr int64_t kMaxRows = 65535LL * 32;   // grid.y limit of the residue kernels
 
@@ -574,6 +618,7 @@ size_t gemm2m_workspace_bytes(int op, int64_t m, int64_t n, int64_t k, int nmod)
     if (op == GEMM2M_OP_NEWTON_SCHULZ) return newton_schulz_sizes_ok(k, m, n) ? (size_t)newton_schulz_layout(k, m, n, kLayerOpsOffset).total : 0;
     if (op == GEMM2M_OP_RMS_NORM) return norm_sizes_ok(m, n) ? rms_norm_bytes(m) : 0;
     if (op == GEMM2M_OP_RMS_NORM_BACKWARD) return norm_sizes_ok(m, n) ? rms_norm_backward_bytes(m, n) : 0;
+    if (op == GEMM2M_OP_CLIP_GRADIENTS) return m >= 0 && m <= kMaxGradients ? clip_bytes(m) : 0;
     Carve c;
     if (op == GEMM2M_OP_GAUSSIAN_INT && nmod > 8) return 0;
     if (!carve(op, m, n, k, nmod, &c)) return 0;
@@ -994,7 +1039,8 @@ int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t
                     float* St, int64_t ldst, float* rstd, void* stream) {
     std::lock_guard<std::mutex> lock(g.mu);
     if (!norm_sizes_ok(rows, cols) || !float_type(type) || (W && !float_type(w_type)) || !(eps >= 0.f)) return GEMM2M_ERR_ARG;
-    if (ldx < (cols > 1 ? cols : 1) || !rows_ok(R, ldr, cols) || !rows_ok(H, ldh, cols) || !rows_ok(Y, ldy, cols)) return GEMM2M_ERR_ARG;
+    if (ldx < (cols > 1 ? cols : 1) || !rows_ok(X, type, ldx, cols) || !rows_ok(R, type, ldr, cols) || !rows_ok(H, type, ldh, cols) ||
+        !rows_ok(Y, type, ldy, cols) || !placed(rstd, 4) || (W && !placed(W, float_size(w_type)))) return GEMM2M_ERR_ARG;
     if (!in_place_ok(H, ldh, X, ldx) || !in_place_ok(H, ldh, R, ldr) || (Y && (Y == X || Y == R || Y == H))) return GEMM2M_ERR_ARG;
     if ((Q || Qt) && fmt != GEMM2M_E4M3 && fmt != GEMM2M_E5M2) return GEMM2M_ERR_ARG;
     if (!fp8_form_ok(Q, ldq, S, lds, cols, rows) || !fp8_form_ok(Qt, ldqt, St, ldst, rows, cols)) return GEMM2M_ERR_ARG;
@@ -1021,7 +1067,9 @@ int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int typ
     std::lock_guard<std::mutex> lock(g.mu);
     if (!norm_sizes_ok(rows, cols) || !float_type(type) || (W && !float_type(w_type))) return GEMM2M_ERR_ARG;
     const int64_t least = cols > 1 ? cols : 1;
-    if (lddy < least || ldh < least || lddx < least || !rows_ok(dR, lddr, cols)) return GEMM2M_ERR_ARG;
+    if (lddy < least || ldh < least || lddx < least || !rows_ok(dR, type, lddr, cols)) return GEMM2M_ERR_ARG;
+    if (!placed(dY, float_size(type)) || !placed(H, float_size(type)) || !placed(dX, float_size(type))) return GEMM2M_ERR_ARG;
+    if (!placed(rstd, 4) || !placed(dW, 4) || (W && !placed(W, float_size(w_type)))) return GEMM2M_ERR_ARG;
     if (!in_place_ok(dX, lddx, dY, lddy) || !in_place_ok(dX, lddx, H, ldh) || !in_place_ok(dX, lddx, dR, lddr)) return GEMM2M_ERR_ARG;
     if (cols == 0 || (rows == 0 && (!dW || add))) return GEMM2M_OK;
     if (rows && (!dY || !H || !rstd || !dX)) return GEMM2M_ERR_ARG;
@@ -1042,6 +1090,49 @@ int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int typ
     CK(ph.end(st));
     ph.done();
     return GEMM2M_OK;
+}
+
+int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, const int* types, const int64_t* rows, const int64_t* cols, const int64_t* ldg,
+                          const int64_t* ldo, float max_norm, float eps, float* norm, void* stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    if (count < 0 || count > kMaxGradients || !(max_norm >= 0.f) || !(eps >= 0.f) || !placed(norm, 4)) return GEMM2M_ERR_ARG;
+    if (count && (!G || !types || !rows || !cols || !ldg || (O && !ldo))) return GEMM2M_ERR_ARG;
+    try {
+        std::vector<GradTensor> t((size_t)count);
+        bool in_place = true;
+        for (int64_t i = 0; i < count; ++i) {
+            if (!float_type(types[i]) || rows[i] < 0 || cols[i] < 0 || rows[i] > kMaxGradient || cols[i] > kMaxGradient) return GEMM2M_ERR_ARG;
+            t[i] = {G[i], O ? O[i] : (void*)G[i], rows[i], cols[i], ldg[i], O ? ldo[i] : ldg[i], types[i]};
+            GradTensor& x = t[i];
+            if (x.rows == 0 || x.cols == 0) continue;
+            if (!placed(x.g, float_size(x.type)) || !placed(x.o, float_size(x.type))) return GEMM2M_ERR_ARG;
+            if (!x.g || !x.o || x.rows > kMaxGradient / x.cols) return GEMM2M_ERR_ARG;
+            if (x.rows > 1) {
+                if (x.ldg < x.cols || x.ldo < x.cols || x.ldg > kMaxGradient || x.ldo > kMaxGradient) return GEMM2M_ERR_ARG;
+                if (x.ldg == x.cols && x.ldo == x.cols) x.cols *= x.rows, x.rows = 1;
+                else if (x.cols > INT32_MAX) return GEMM2M_ERR_ARG;
+            }
+            if (x.rows == 1) x.ldg = x.ldo = x.cols;
+            if (!in_place_ok(x.o, x.ldo, x.g, x.ldg)) return GEMM2M_ERR_ARG;
+            in_place = in_place && x.o == x.g;
+        }
+        const bool scale = !(in_place && std::isinf(max_norm));      // nothing is ever scaled: the norm alone
+        if (scale && !gradients_apart(t)) return GEMM2M_ERR_ARG;
+        if (int s = check_device()) return s;
+        if (!D().ws || D().ws_bytes < clip_bytes(count)) return GEMM2M_ERR_WORKSPACE;
+        cudaStream_t st = (cudaStream_t)stream;
+        Phases ph;
+        if (int s = begin_call(&ph)) return s;
+        int launches[2] = {0, 0};
+        CK(ph.begin(1, st));
+        CK(launch_clip_gradients(t.data(), count, scale, max_norm, eps, norm, (double*)((char*)D().ws + kLayerOpsOffset), st, launches));
+        CK(ph.end(st));
+        g.launches[1] = launches[0] + launches[1];
+        ph.done();
+        return GEMM2M_OK;
+    } catch (...) {                      // no memory on the host for the list
+        return GEMM2M_ERR_ARG;
+    }
 }
 
 int gemm2m_device_status(void* stream) {

@@ -1,0 +1,234 @@
+// Common 2-norm of many tensors, and the tensors scaled down where it is above a limit.
+//
+// norm = sqrt(sum over all tensors and entries of g^2); factor = 1 where max_norm >= norm + eps, else max_norm / (norm + eps) (NaN for a NaN norm),
+// formed in 64 bits and rounded to 32; o = rn(g factor).
+//
+// Tensors are cut into chunks of 8192 entries, dealt out in turn to the blocks of one launch for up to 512 tensors, which it gets as a kernel parameter
+// (nothing to copy first; captured by value).  First launch: every thread sums squares of 8 entries in 32 bits and these sums in 64 bits, every block
+// leaves one number.  Second launch: every block adds those up, in the same order, and scales its chunks, last chunk first: those are still
+// in the on-chip cache where all of them do not fit.
+#include "layer_ops.cuh"
+
+namespace gemm2m {
+
+namespace {
+
+constexpr int kChunk = 8192, kClipThreads = 256, kBlocks = 4 * kSms, kFew = 64, kMany = 512;
+
+struct Entry {
+    const void* g; void* o;
+    int64_t size, ldg, ldo;
+    int32_t cols;                         // of a row, 0 where all entries are contiguous
+    uint32_t first;                       // number of its first chunk
+    int32_t type, vec;                    // vec: groups of 8 entries are aligned, in g and in o
+};
+template <int N> struct Table { Entry t[N]; int32_t count; uint32_t chunks; };
+
+__device__ __forceinline__ int64_t place(const Entry& e, int64_t i, int64_t ld) {
+    if (!e.cols) return i;
+    const int64_t row = i / e.cols;
+    return row * ld + (i - row * e.cols);
+}
+
+// Sum of the squares of eight entries.  In 32 bits where neither the largest can overflow nor what underflows can matter (squares below 2^-126 against a sum of
+// 2^-100 or more: less than its rounding); otherwise, and for sums that are not finite, in 64 bits.
+__device__ __forceinline__ double squares8(const float (&v)[8]) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s += v[j] * v[j];
+    if (s >= 0x1p-100f && s <= 0x1p126f) return (double)s;
+    double d = 0.0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) d += (double)v[j] * (double)v[j];
+    return d;
+}
+
+__device__ __forceinline__ double block_sum(double v, double* warps) {
+#pragma unroll
+    for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
+    if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = 0.0;
+#pragma unroll
+    for (int w = 0; w < kClipThreads / 32; ++w) v += warps[w];
+    return v;
+}
+
+// The entry that chunk c belongs to.
+template <int N>
+__device__ __forceinline__ const Entry& entry_of(const Table<N>& t, uint32_t c) {
+    int lo = 0, hi = t.count;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.t[mid].first <= c) lo = mid;
+        else hi = mid;
+    }
+    return t.t[lo];
+}
+
+// The four groups of eight entries of a chunk that a thread deals with.
+template <typename T, typename F>
+__device__ __forceinline__ void for_chunk(const Entry& e, uint32_t c, F&& f) {
+    const int64_t base = (int64_t)(c - e.first) * kChunk;
+    const T* g = (const T*)e.g;
+    constexpr int kGroups = kChunk / (8 * kClipThreads);
+    if (e.vec && base + kChunk <= e.size) {
+        Raw8<T> raw[kGroups];
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) raw[k] = load8_rw<T>(g + place(e, base + (k * kClipThreads + threadIdx.x) * 8, e.ldg));
+#pragma unroll
+        for (int k = 0; k < kGroups; ++k) {
+            float v[8];
+            to_floats8<T>(raw[k], v);
+            f(v, base + (k * kClipThreads + threadIdx.x) * 8, 8);
+        }
+        return;
+    }
+    // neighbouring threads take neighbouring entries
+#pragma unroll 1
+    for (int k = 0; k < kGroups; ++k) {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t i = base + (k * 8 + j) * kClipThreads + threadIdx.x;
+            v[j] = i < e.size ? to_float<T>(g[place(e, i, e.ldg)]) : 0.f;
+        }
+        f(v, base + k * 8 * kClipThreads + threadIdx.x, 0);
+    }
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) squares_kernel(const __grid_constant__ Table<N> t, double* partials) {
+    __shared__ double warps[kClipThreads / 32];
+    wait_for_prior_kernels();
+    double sum = 0.0;
+    auto add = [&](const float (&v)[8], int64_t, int) { sum += squares8(v); };
+    for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+        const Entry& e = entry_of(t, c);
+        if (e.type == kF32) for_chunk<float>(e, c, add);
+        else if (e.type == kF16) for_chunk<__half>(e, c, add);
+        else for_chunk<__nv_bfloat16>(e, c, add);
+    }
+    sum = block_sum(sum, warps);
+    if (threadIdx.x == 0) partials[blockIdx.x] = sum;
+}
+
+// The sum of all partial sums, in an order that goes by their number alone.
+__device__ __forceinline__ double total_of(const double* partials, int64_t count, double* warps) {
+    double v = 0.0;
+    for (int64_t i = threadIdx.x; i < count; i += kClipThreads) v += partials[i];
+    return block_sum(v, warps);
+}
+
+__global__ void __launch_bounds__(kClipThreads) fold_kernel(const double* partials, int64_t count, double* total, float* norm) {
+    __shared__ double warps[kClipThreads / 32];
+    wait_for_prior_kernels();
+    const double sum = total_of(partials, count, warps);
+    if (threadIdx.x) return;
+    *total = sum;
+    if (norm) *norm = (float)sqrt(sum);
+}
+
+template <int N>
+__global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_constant__ Table<N> t, const double* partials, int64_t count, float max_norm, float eps, float* norm) {
+    __shared__ double warps[kClipThreads / 32];
+    wait_for_prior_kernels();
+    const double size = sqrt(total_of(partials, count, warps));
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)size;
+    const double room = size + (double)eps;
+    const float factor = (double)max_norm >= room ? 1.f : (float)((double)max_norm / room);      // (NaN: the second)
+    for (uint32_t i = blockIdx.x; i < t.chunks; i += gridDim.x) {
+        const uint32_t c = t.chunks - 1 - i;
+        const Entry& e = entry_of(t, c);
+        if (factor == 1.f && e.o == e.g) continue;
+        auto scale = [&](auto kind) {
+            using T = decltype(kind);
+            for_chunk<T>(e, c, [&](const float (&v)[8], int64_t at, int whole) {
+                float out[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) out[j] = v[j] * factor;
+                if (whole) {
+                    store8_as<T>((T*)e.o + place(e, at, e.ldo), out, true, 8);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (at + j * kClipThreads < e.size) ((T*)e.o)[place(e, at + j * kClipThreads, e.ldo)] = from_float<T>(out[j]);
+                }
+            });
+        };
+        if (e.type == kF32) scale(float());
+        else if (e.type == kF16) scale(__half());
+        else scale(__nv_bfloat16());
+    }
+}
+
+// Up to N tensors as a kernel parameter; returns how many were taken.
+template <int N>
+int64_t fill(Table<N>* t, const GradTensor* g, int64_t count) {
+    t->count = 0;
+    t->chunks = 0;
+    int64_t i = 0;
+    for (; i < count && t->count < N; ++i) {
+        const int64_t size = g[i].rows * g[i].cols;
+        if (size == 0) continue;
+        const int es = g[i].type == kF32 ? 4 : 2;
+        const bool flat = g[i].rows == 1 || (g[i].ldg == g[i].cols && g[i].ldo == g[i].cols);
+        const bool rows_vec = flat || (g[i].cols % 8 == 0 && g[i].ldg * es % 16 == 0 && g[i].ldo * es % 16 == 0);
+        const bool vec = rows_vec && (((uintptr_t)g[i].g | (uintptr_t)g[i].o) & 15) == 0;
+        t->t[t->count++] = {g[i].g, g[i].o, size, g[i].ldg, g[i].ldo, flat ? 0 : (int32_t)g[i].cols, t->chunks, g[i].type, vec ? 1 : 0};
+        t->chunks += (uint32_t)((size + kChunk - 1) / kChunk);
+    }
+    return i;
+}
+
+int blocks_for(uint32_t chunks) { return chunks < (uint32_t)kBlocks ? (int)chunks : kBlocks; }
+
+template <int N>
+cudaError_t launch_all(const GradTensor* g, int64_t count, bool scale, float max_norm, float eps, float* norm, double* partials, cudaStream_t st, int launches[2]) {
+    Table<N> t;
+    double* total = partials;
+    double* part = partials + 1;
+    int64_t parts = 0;
+    int tables = 0;
+    for (int64_t i = 0; i < count; ++tables) {
+        i += fill(&t, g + i, count - i);
+        if (t.chunks == 0) continue;
+        const int blocks = blocks_for(t.chunks);
+        cudaError_t err = launch_chained(squares_kernel<N>, dim3(blocks), dim3(kClipThreads), 0, st, t, part + parts);
+        if (err != cudaSuccess) return err;
+        parts += blocks;
+        ++launches[0];
+    }
+    // with several tables, or no tensor to scale, one block adds the partial sums up
+    if (tables != 1 || !scale || parts == 0) {
+        cudaError_t err = launch_chained(fold_kernel, dim3(1), dim3(kClipThreads), 0, st, (const double*)part, parts, total, norm);
+        if (err != cudaSuccess) return err;
+        ++launches[0];
+        part = total;
+        parts = 1;
+        norm = nullptr;
+    }
+    if (!scale) return cudaSuccess;
+    for (int64_t i = 0; i < count;) {
+        if (tables != 1) i += fill(&t, g + i, count - i);
+        else i = count;
+        if (t.chunks == 0) continue;
+        cudaError_t err = launch_chained(scale_kernel<N>, dim3(blocks_for(t.chunks)), dim3(kClipThreads), 0, st, t, (const double*)part, parts, max_norm, eps, norm);
+        if (err != cudaSuccess) return err;
+        ++launches[1];
+    }
+    return cudaSuccess;
+}
+
+}  // namespace
+
+int64_t clip_partials(int64_t count) { return 1 + (count / kMany + 1) * kBlocks; }
+
+cudaError_t launch_clip_gradients(const GradTensor* t, int64_t count, bool scale, float max_norm, float eps, float* norm, double* partials, cudaStream_t st,
+                                  int launches[2]) {
+    // a parameter of 4 KB or one of 30 KB, which costs more to launch
+    if (count <= kFew) return launch_all<kFew>(t, count, scale, max_norm, eps, norm, partials, st, launches);
+    return launch_all<kMany>(t, count, scale, max_norm, eps, norm, partials, st, launches);
+}
+
+}  // namespace gemm2m

@@ -85,6 +85,17 @@ struct RmsNormBackwardArgs {
 int64_t rms_norm_backward_parts(int64_t rows, int64_t cols);      // rows of partial sums of dW
 cudaError_t launch_rms_norm_backward(const RmsNormBackwardArgs& a, cudaStream_t st, int* launches);
 
+// Common 2-norm of many tensors, and the tensors scaled down where it is above a limit (clip_gradients.cu).
+struct GradTensor {
+    const void* g; void* o;               // o == g: in place
+    int64_t rows, cols, ldg, ldo;         // row-major; rows = 1 where the entries are contiguous
+    int type;
+};
+int64_t clip_partials(int64_t count);     // doubles of workspace for that many tensors
+// norm: device float or null.  scale = false: the norm alone, no tensor is written.
+cudaError_t launch_clip_gradients(const GradTensor* t, int64_t count, bool scale, float max_norm, float eps, float* norm, double* partials, cudaStream_t st,
+                                  int launches[2]);
+
 #ifdef __CUDACC__
 template <typename T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }

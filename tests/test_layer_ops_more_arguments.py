@@ -28,7 +28,8 @@ def _norm(rows=4, cols=4, X=one, type=b.BF16, ldx=4, R=null, ldr=4, W=null, w_ty
                                  dict(W=one, w_type=b.E5M2), dict(R=two, ldr=3), dict(H=two, ldh=3), dict(Y=two, ldy=3), dict(eps=-1.0), dict(eps=float("nan")),
                                  dict(fmt=b.BF16), dict(ldq=24), dict(ldq=0), dict(Q=264), dict(lds=3), dict(S=null), dict(Q=null), dict(Q=null, S=null),
                                  dict(Qt=one), dict(St=one), dict(Qt=one, St=one, ldqt=8), dict(Qt=one, St=one, ldst=3), dict(Qt=8, St=one), dict(X=null),
-                                 dict(H=one, ldh=8), dict(R=two, H=two, ldr=8), dict(Y=one), dict(R=two, Y=two), dict(H=two, Y=two)])
+                                 dict(X=258, ldx=8, type=b.F32), dict(R=513), dict(W=258), dict(H=515), dict(Y=511), dict(S=258), dict(rstd=254),
+                                 dict(Qt=one, St=two + 2), dict(H=one, ldh=8), dict(R=two, H=two, ldr=8), dict(Y=one), dict(R=two, Y=two), dict(H=two, Y=two)])
 def test_norm_refuses(bad):
     assert _norm(**bad) == ARG
 
@@ -43,6 +44,7 @@ def _back(rows=4, cols=4, dY=one, type=b.F32, lddy=4, H=two, ldh=4, W=null, w_ty
 
 @pytest.mark.parametrize("bad", [dict(rows=-1), dict(cols=-1), dict(cols=32769, lddy=40000, ldh=40000, lddx=40000), dict(type=b.E5M2), dict(W=one, w_type=7), dict(lddy=3),
                                  dict(ldh=3), dict(lddx=3), dict(dR=one, lddr=3), dict(dY=null), dict(H=null), dict(rstd=null), dict(dX=null),
+                                 dict(dY=258), dict(H=257), dict(W=258), dict(rstd=255), dict(dR=514), dict(dX=514), dict(dW=258),
                                  dict(dX=one, lddx=8), dict(dX=two, lddx=8), dict(dR=768, dX=768, lddx=8)])
 def test_norm_backward_refuses(bad):
     assert _back(**bad) == ARG
@@ -107,4 +109,102 @@ def test_norm_refuses_halves_of_forms_and_mixed_formats(calls):  # noqa: F811
     for missing in ("H", "rstd", "dX"):
         with pytest.raises(ValueError):
             b.rms_norm_backward(**{**backward_operands(), missing: None})
+    assert not calls
+
+
+# ----------------------------------------------------------------------------------------------------------- gradient clipping
+def _clip(tensors, max_norm=1.0, eps=1e-6, norm=null, in_place=False, count=None):
+    """tensors: (G, O, type, rows, cols, ldg, ldo) each."""
+    n = max(len(tensors), 1)
+    column = lambda kind, k: (kind * n)(*[t[k] for t in tensors])
+    vp, i64 = ctypes.c_void_p, ctypes.c_int64
+    return b.lib().gemm2m_clip_gradients(len(tensors) if count is None else count, column(vp, 0), null if in_place else column(vp, 1), column(ctypes.c_int, 2),
+                                         *(column(i64, k) for k in (3, 4, 5)), null if in_place else column(i64, 6), max_norm, eps, norm, null)
+
+
+def _tensor(G=4096, O=8192, type=b.F32, rows=4, cols=4, ldg=4, ldo=4):
+    return G, O, type, rows, cols, ldg, ldo
+
+
+def refused(status):
+    """(a call whose arguments are fine fails on this machine for want of a device, or of a workspace)"""
+    return status == ARG
+
+
+@pytest.mark.parametrize("bad", [dict(G=null), dict(O=null), dict(type=b.E4M3), dict(rows=-1), dict(cols=-1), dict(ldg=3), dict(ldo=3), dict(rows=2 ** 30, cols=2 ** 30, ldg=2 ** 30, ldo=2 ** 30),
+                                 dict(G=4098), dict(O=8190), dict(type=b.BF16, G=4097), dict(O=4096, ldo=5), dict(O=4100), dict(O=4096 + 60)])
+def test_clip_refuses_a_tensor(bad):
+    assert not refused(_clip([_tensor()]))
+    assert refused(_clip([_tensor(**bad)]))
+
+
+def test_clip_refuses_numbers():
+    for bad in (dict(max_norm=-1.0), dict(max_norm=float("nan")), dict(eps=-1.0), dict(eps=float("nan")), dict(norm=258), dict(count=-1), dict(count=2 ** 20 + 1)):
+        assert refused(_clip([_tensor()], **bad))
+    for fine in (dict(max_norm=0.0), dict(max_norm=float("inf")), dict(eps=0.0), dict(in_place=True)):
+        assert not refused(_clip([_tensor()], **fine))
+
+
+def test_clip_refuses_outputs_that_overlap():
+    a = _tensor()
+    assert not refused(_clip([a, _tensor(G=4096, O=8192 + 64)]))              # the same gradient twice, into places of their own
+    assert refused(_clip([a, a]))                                            # the same output twice
+    assert refused(_clip([_tensor(O=4096), _tensor(O=4096)]))                # in place, twice
+    assert refused(_clip([a, _tensor(G=4096 + 32)], in_place=True))
+    assert refused(_clip([a, _tensor(G=8192 + 16, O=4 * 4096)]))             # another's input
+    assert refused(_clip([a, _tensor(O=8192 + 60)]))
+    assert not refused(_clip([a, _tensor(G=4096 + 64)], in_place=True))
+    assert not refused(_clip([_tensor(rows=0, G=null, O=null), a, _tensor(cols=0)]))
+    # views of one matrix of 20 columns side by side, and ones that share a column
+    view = lambda at, cols: _tensor(G=4096 + 4 * at, rows=5, cols=cols, ldg=20)
+    assert not refused(_clip([view(0, 8), view(8, 10), view(18, 2)], in_place=True))
+    assert not refused(_clip([view(18, 2), view(8, 10), view(0, 8)], in_place=True))
+    assert refused(_clip([view(0, 9), view(8, 10)], in_place=True))
+    assert refused(_clip([view(0, 4), view(18, 4)], in_place=True))           # around the end of a row
+    assert refused(_clip([view(0, 8), view(24, 8)], in_place=True))          # a row further on, four columns shared
+    assert not refused(_clip([view(0, 8), view(28, 8)], in_place=True))      # a row further on, other columns
+    assert refused(_clip([view(0, 8), _tensor(G=4096 + 32, rows=1, cols=60)], in_place=True))
+    # a long span over many short ones
+    assert refused(_clip([_tensor(G=4096, rows=1, cols=1000)] + [_tensor(G=9000 + 16 * i, rows=1, cols=4) for i in range(5)] + [_tensor(G=4096 + 3996, rows=1, cols=1)],
+                         in_place=True))
+
+
+def test_clip_workspace_sizes():
+    size = lambda n: b.workspace_bytes(b.OP_CLIP_GRADIENTS, n, 1, 1, 1)
+    assert 256 <= size(0) <= size(1) <= size(1000) < 10 ** 6 and size(-1) == 0 and size(2 ** 20 + 1) == 0 and size(2 ** 20) > size(1000)
+
+
+def test_clip_passes_every_tensor_on(calls):  # noqa: F811
+    read = lambda p, n: [int(v or 0) for v in p[:n]]
+    whole = torch.zeros(6, 40)
+    grads = [dense(5, 7), Standin(torch.zeros(3, 4, dtype=torch.bfloat16)), Standin(whole[:, 8:20]), Standin(torch.zeros(8, 9).t()), Standin(torch.zeros(())),
+             Standin(torch.zeros(2, 3, 4).permute(2, 0, 1))]
+    b.clip_gradients(grads, 2.0, norm=vector(1))
+    _, a = calls[-1]
+    assert a[0] == 6 and a[2] is None and a[7] is None and (a[8], a[9]) == (2.0, 1e-6)
+    assert read(a[1], 6) == [t.data_ptr() for t in grads] and read(a[3], 6) == [b.F32, b.BF16] + [b.F32] * 4
+    assert read(a[4], 6) == [1, 1, 6, 1, 1, 1] and read(a[5], 6) == [35, 12, 12, 72, 1, 24] and read(a[6], 6)[2] == 40
+    # into outputs whose rows are further apart, or closer together
+    outs = [Standin(torch.zeros(5, 20)[:, :7]), dense(3, 4, torch.bfloat16), dense(6, 12), Standin(torch.zeros(8, 9).t()), Standin(torch.zeros(())),
+            Standin(torch.zeros(2, 3, 4).permute(2, 0, 1))]
+    b.clip_gradients(grads, 2.0, out=outs)
+    _, a = calls[-1]
+    assert read(a[4], 6) == [5, 1, 6, 1, 1, 1] and read(a[5], 6) == [7, 12, 12, 72, 1, 24]
+    assert read(a[6], 6)[0] == 7 and read(a[7], 6)[0] == 20 and read(a[6], 6)[2] == 40 and read(a[7], 6)[2] == 12
+
+
+def test_clip_refuses_tensors_that_it_cannot_walk(calls):  # noqa: F811
+    fine = dense(6, 8)
+    for bad in (Standin(torch.zeros(6, 16)[:, ::2]), Standin(torch.zeros(6, 1).expand(6, 8)), Standin(torch.zeros(4, 6, 8)[:, :5]), Standin(torch.zeros(16)[::2]),
+                Standin(torch.zeros(6, 8, dtype=torch.float64)), dense(6, 8, device=1), dense(6, 8, device=-1)):
+        with pytest.raises(ValueError):
+            b.clip_gradients([fine, bad], 1.0)
+        with pytest.raises(ValueError):
+            b.clip_gradients([fine], 1.0, out=[bad])
+    for out in ([], [dense(6, 9)], [dense(6, 8, torch.bfloat16)], [Standin(torch.zeros(8, 6).t())], [fine, fine]):
+        with pytest.raises(ValueError):
+            b.clip_gradients([fine], 1.0, out=out)
+    for norm in (vector(2), vector(1, torch.float64), vector(1, device=1)):
+        with pytest.raises(ValueError):
+            b.clip_gradients([fine], 1.0, norm=norm)
     assert not calls
