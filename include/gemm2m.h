@@ -78,7 +78,8 @@ typedef enum {
     GEMM2M_OP_ZGEMM_EISENSTEIN = 8, GEMM2M_OP_ZGEMM_HOST = 9,
     GEMM2M_OP_FP8_GEMM = 10, GEMM2M_OP_NEWTON_SCHULZ = 11,      /* layer operators, below; k = batch for the latter, nmod is ignored */
     GEMM2M_OP_RMS_NORM = 12, GEMM2M_OP_RMS_NORM_BACKWARD = 13,  /* m = rows, n = columns, k is ignored */
-    GEMM2M_OP_CLIP_GRADIENTS = 14      /* m = number of tensors */
+    GEMM2M_OP_CLIP_GRADIENTS = 14,     /* m = number of tensors */
+    GEMM2M_OP_ADAPTER_ADD = 15         /* m = tokens, n = rank, k = adapters */
 } gemm2m_op;
 
 /* Element types of the layer operators.  E4M3 and E5M2 are the 8-bit formats with 4 / 5 exponent bits and largest finite
@@ -323,6 +324,20 @@ int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int typ
  * Workspace: GEMM2M_OP_CLIP_GRADIENTS with m = count. */
 int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, const int* types, const int64_t* rows, const int64_t* cols, const int64_t* ldg,
                           const int64_t* ldo, float max_norm, float eps, float* norm, void* stream);
+
+/* Low-rank updates of many requests' adapters beside a shared projection, row by row (token by token):
+ *   D_t = C_t + s_a (X_t A_a^T) B_a^T,  a = index[t].
+ * X: tokens x k; A_a (rank x k) and B_a (n x rank) of `adapters` (<= 16384) adapters, stride_a / stride_b elements apart; X, A, B of the same type F16 /
+ * BF16.  rank <= 128; ranks (device, `adapters` entries, may be NULL): adapter a uses the first ranks[a] rows of A_a and columns of B_a, and nothing beyond them is
+ * read.  index: device, one entry per token, in any order; a token whose entry is not in [0, adapters) has no adapter: D_t = C_t.  scales: device, one
+ * per adapter, NULL for ones.  C and D: tokens x n of type d_type (F32 / F16 / BF16); C may be NULL (zero) or D itself (then ldc = ldd), not otherwise overlap D;
+ * with C = D rows without an adapter are not touched.  Any alignment and stride.  k = 0 or rank = 0 adds nothing.
+ * X A^T is summed and held in 32 bits (and multiplied by B as two 16-bit numbers, 2^-17 of its largest entry in a row), D is rounded once.  A token's
+ * result does not depend on the other tokens, beyond their number.
+ * Workspace: GEMM2M_OP_ADAPTER_ADD with (tokens, rank, adapters). */
+int gemm2m_adapter_add(int64_t tokens, int64_t n, int64_t k, int adapters, int rank, const void* X, int type, int64_t ldx, const void* A, int64_t lda,
+                       int64_t stride_a, const void* B, int64_t ldb, int64_t stride_b, const int32_t* index, const float* scales, const int32_t* ranks,
+                       const void* C, int64_t ldc, void* D, int d_type, int64_t ldd, void* stream);
 
 /* Waits for `stream` and returns GEMM2M_ERR_DEVICE_TIMEOUT if a kernel of an earlier call on the registered
  * workspace gave up a bounded wait (its results are then invalid), GEMM2M_ERR_CUDA on a CUDA error, else OK. */

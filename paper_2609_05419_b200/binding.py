@@ -14,7 +14,7 @@ OP_GAUSSIAN_INT, OP_ZGEMM, OP_CGEMM, OP_ZHERK, OP_ZHER2K, OP_DSYRK, OP_DSYR2K, O
 OP_ZGEMM_EISENSTEIN = 8
 OP_ZGEMM_HOST = 9
 OP_FP8_GEMM, OP_NEWTON_SCHULZ = 10, 11
-OP_RMS_NORM, OP_RMS_NORM_BACKWARD, OP_CLIP_GRADIENTS = 12, 13, 14
+OP_RMS_NORM, OP_RMS_NORM_BACKWARD, OP_CLIP_GRADIENTS, OP_ADAPTER_ADD = 12, 13, 14, 15
 F32, F16, BF16, E4M3, E5M2 = 0, 1, 2, 3, 4              # gemm2m_type
 OK = 0
 ERR_ARG, ERR_NMOD, ERR_WORKSPACE, ERR_CUDA, ERR_ARCH, ERR_DEVICE_TIMEOUT = 1, 2, 3, 4, 5, 6     # gemm2m_status
@@ -95,6 +95,7 @@ def lib():
     L.gemm2m_rms_norm.argtypes = [i64, i64, vp, i32, i64, vp, i64, vp, i32, ctypes.c_float] + [vp, i64] * 2 + [i32] + [vp, i64] * 4 + [vp, vp]
     L.gemm2m_rms_norm_backward.argtypes = [i64, i64, vp, i32, i64, vp, i64, vp, i32, vp, vp, i64, vp, i64, vp, i32, vp]
     L.gemm2m_clip_gradients.argtypes = [i64] + [vp] * 7 + [ctypes.c_float, ctypes.c_float, vp, vp]
+    L.gemm2m_adapter_add.argtypes = [i64, i64, i64, i32, i32, vp, i32, i64] + [vp, i64, i64] * 2 + [vp] * 3 + [vp, i64, vp, i32, i64, vp]
     _lib = L
     return L
 
@@ -613,6 +614,46 @@ def clip_gradients(grads, max_norm, out=None, norm=None, eps=1e-6, stream=None):
     _check(lib().gemm2m_clip_gradients(count, array(ctypes.c_void_p, [r[0] for r in rows]), p_out, array(ctypes.c_int, [r[1] for r in rows]),
                                        *(array(i64, [r[k] for r in rows]) for k in (2, 3, 4)), ld_out, max_norm, eps,
                                        None if norm is None else norm.data_ptr(), _stream_of(stream, device)), "gemm2m_clip_gradients")
+
+
+def _stack(t, name, kind, device):
+    """(pointer, matrices, rows, cols, leading dimension, stride) of a 3-D CUDA tensor of row-major matrices."""
+    if t.dim() != 3 or t.get_device() != device:
+        raise ValueError(f"{name}: need a 3-D CUDA tensor on the current device")
+    _type_of(t, name, (kind,))
+    many, rows, cols = t.shape
+    stride, ld, step = t.stride()
+    if cols > 1 and step != 1:
+        raise ValueError(f"{name}: need row-major storage (stride 1 along the last dim)")
+    if rows <= 1 or cols == 0:
+        ld = max(cols, 1)
+    return t.data_ptr(), many, rows, cols, ld, stride if many > 1 else rows * max(cols, 1)
+
+
+def adapter_add(X, A, B, index, D, C=None, scales=None, ranks=None, stream=None):
+    """D[t] = C[t] + scales[a] (X[t] A[a]^T) B[a]^T with a = index[t] (int32; no adapter where it is not an index of A): X tokens x k,
+    A adapters x rank x k, B adapters x n x rank in float16 / bfloat16; D, C float32 / float16 / bfloat16 (C may be D, or None for zero).
+    ranks (int32): how many rows of A[a] and columns of B[a] are in use."""
+    import torch
+    device = _launch_device(X, "X")
+    px, tx, tokens, k, ldx = _rowmajor(X, "X", (F16, BF16), device)
+    pa, many, rank, k2, lda, stride_a = _stack(A, "A", tx, device)
+    pb, many2, n, rank2, ldb, stride_b = _stack(B, "B", tx, device)
+    pd, td, md, nd, ldd = _rowmajor(D, "D", _FLOATS, device)
+    if k2 != k or many2 != many or rank2 != rank or (md, nd) != (tokens, n):
+        raise ValueError("shape mismatch")
+    pc, ldc = _like(C, "C", (tokens, n), td, device)
+    pointers = []
+    for t, name, size in ((index, "index", tokens), (ranks, "ranks", many)):
+        if t is None and name == "ranks":
+            pointers.append(None)
+            continue
+        if t.dim() != 1 or t.shape[0] != size or t.dtype != torch.int32 or t.get_device() != device or (size > 1 and t.stride(0) != 1):
+            raise ValueError(f"{name}: need a contiguous int32 CUDA tensor of {size} entries on the current device")
+        pointers.append(t.data_ptr())
+    _check(lib().gemm2m_adapter_add(tokens, n, k, many, rank, px, tx, ldx, pa, lda, stride_a, pb, ldb, stride_b, pointers[0],
+                                    _vector(scales, "scales", many, (F32,), device)[0], pointers[1], pc, ldc, pd, td, ldd, _stream_of(stream, device)),
+           "gemm2m_adapter_add")
 
 
 def device_status(stream=None):

@@ -221,6 +221,10 @@ bool in_place_ok(const void* out, int64_t ldo, const void* in, int64_t ldi) { re
 constexpr int64_t kMaxGradients = 1 << 20, kMaxGradient = 1LL << 40;      // tensors of a call, entries of one
 size_t clip_bytes(int64_t count) { return (size_t)(kLayerOpsOffset + round_up(8 * clip_partials(count), 256)); }
 
+bool adapter_sizes_ok(int64_t tokens, int64_t rank, int64_t adapters) {
+    return tokens >= 0 && tokens <= kMaxCoord && rank >= 0 && rank <= kMaxRank && adapters >= 0 && adapters <= kMaxAdapters;
+}
+
 // Memory that a tensor spans, to find outputs that overlap something else.
 struct Span { uintptr_t begin, end; int64_t row, width; bool written; };      // bytes; row = distance of rows, width = of entries in a row
 bool spans_meet(const Span& a, const Span& b) {          // a.begin <= b.begin < a.end
@@ -619,6 +623,7 @@ size_t gemm2m_workspace_bytes(int op, int64_t m, int64_t n, int64_t k, int nmod)
     if (op == GEMM2M_OP_RMS_NORM) return norm_sizes_ok(m, n) ? rms_norm_bytes(m) : 0;
     if (op == GEMM2M_OP_RMS_NORM_BACKWARD) return norm_sizes_ok(m, n) ? rms_norm_backward_bytes(m, n) : 0;
     if (op == GEMM2M_OP_CLIP_GRADIENTS) return m >= 0 && m <= kMaxGradients ? clip_bytes(m) : 0;
+    if (op == GEMM2M_OP_ADAPTER_ADD) return adapter_sizes_ok(m, n, k) ? (size_t)(kLayerOpsOffset + adapter_bytes(m, (int)n, (int)k)) : 0;
     Carve c;
     if (op == GEMM2M_OP_GAUSSIAN_INT && nmod > 8) return 0;
     if (!carve(op, m, n, k, nmod, &c)) return 0;
@@ -1133,6 +1138,45 @@ int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, c
     } catch (...) {                      // no memory on the host for the list
         return GEMM2M_ERR_ARG;
     }
+}
+
+int gemm2m_adapter_add(int64_t tokens, int64_t n, int64_t k, int adapters, int rank, const void* X, int type, int64_t ldx, const void* A, int64_t lda,
+                       int64_t stride_a, const void* B, int64_t ldb, int64_t stride_b, const int32_t* index, const float* scales, const int32_t* ranks,
+                       const void* C, int64_t ldc, void* D, int d_type, int64_t ldd, void* stream) {
+    std::lock_guard<std::mutex> lock(g.mu);
+    if (!fp8_sizes_ok(tokens, n, k) || !adapter_sizes_ok(tokens, rank, adapters)) return GEMM2M_ERR_ARG;
+    if ((type != GEMM2M_F16 && type != GEMM2M_BF16) || !float_type(d_type)) return GEMM2M_ERR_ARG;
+    const int64_t width_k = k > 1 ? k : 1, width_n = n > 1 ? n : 1, width_r = rank > 1 ? rank : 1;
+    if (ldx < width_k || lda < width_k || ldb < width_r || ldd < width_n || (C && ldc < width_n)) return GEMM2M_ERR_ARG;
+    if (adapters > 1 && (stride_a < 0 || stride_b < 0)) return GEMM2M_ERR_ARG;
+    if (!placed(X, 2) || !placed(A, 2) || !placed(B, 2) || !placed(index, 4) || !placed(scales, 4) || !placed(ranks, 4)) return GEMM2M_ERR_ARG;
+    if (!placed(C, float_size(d_type)) || !placed(D, float_size(d_type)) || !in_place_ok(D, ldd, C, ldc)) return GEMM2M_ERR_ARG;
+    if (tokens == 0 || n == 0) return GEMM2M_OK;
+    const bool nothing = k == 0 || rank == 0 || adapters == 0;
+    if (!D || (!nothing && (!X || !A || !B || !index))) return GEMM2M_ERR_ARG;
+    if (int s = check_device()) return s;
+    cudaStream_t st = (cudaStream_t)stream;
+    const size_t es = float_size(d_type);
+    if (nothing) {                       // D = C, or zero
+        std::memset(g.launches, 0, sizeof(g.launches));
+        if (!C) CK(cudaMemset2DAsync(D, (size_t)ldd * es, 0, (size_t)n * es, (size_t)tokens, st));
+        else if (C != D) CK(cudaMemcpy2DAsync(D, (size_t)ldd * es, C, (size_t)ldc * es, (size_t)n * es, (size_t)tokens, cudaMemcpyDeviceToDevice, st));
+        return GEMM2M_OK;
+    }
+    DevState& dev = g.dev[g.cur];
+    if (!dev.ws || dev.ws_bytes < (size_t)(kLayerOpsOffset + adapter_bytes(tokens, rank, adapters))) return GEMM2M_ERR_WORKSPACE;
+    Phases ph;
+    if (int s = begin_call(&ph)) return s;
+    const AdapterArgs a = {tokens, n, k, adapters, rank, X, type, ldx, A, lda, stride_a, B, ldb, stride_b, index, scales, ranks, C, ldc, D, d_type, ldd,
+                           (char*)dev.ws + kLayerOpsOffset};
+    int launches[2] = {0, 0};
+    CK(ph.begin(2, st));
+    CK(launch_adapter_add(a, st, launches));
+    CK(ph.end(st));
+    g.launches[1] = launches[0];
+    g.launches[2] = launches[1];
+    ph.done();
+    return GEMM2M_OK;
 }
 
 int gemm2m_device_status(void* stream) {

@@ -96,6 +96,22 @@ int64_t clip_partials(int64_t count);     // doubles of workspace for that many 
 cudaError_t launch_clip_gradients(const GradTensor* t, int64_t count, bool scale, float max_norm, float eps, float* norm, double* partials, cudaStream_t st,
                                   int launches[2]);
 
+// Low-rank updates of many adapters, added to what a shared projection wrote (adapters.cu).
+constexpr int kMaxRank = 128, kMaxAdapters = 16384;
+struct AdapterArgs {
+    int64_t tokens, n, k;
+    int adapters, rank;
+    const void* X; int type; int64_t ldx;                    // X, A, B: the same 16-bit type
+    const void* A; int64_t lda, stride_a;                    // adapter a: rank x k
+    const void* B; int64_t ldb, stride_b;                    // adapter a: n x rank
+    const int32_t* index; const float* scales; const int32_t* ranks;
+    const void* C; int64_t ldc;
+    void* D; int d_type; int64_t ldd;
+    char* ws;
+};
+int64_t adapter_bytes(int64_t tokens, int rank, int adapters);      // workspace
+cudaError_t launch_adapter_add(const AdapterArgs& a, cudaStream_t st, int launches[2]);
+
 #ifdef __CUDACC__
 template <typename T> __device__ __forceinline__ float to_float(T v);
 template <> __device__ __forceinline__ float to_float<float>(float v) { return v; }

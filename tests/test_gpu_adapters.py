@@ -1,0 +1,275 @@
+"""Low-rank updates of many adapters on the GPU against a plain implementation in 64 bits."""
+import math
+
+import pytest
+import torch
+
+from paper_2609_05419_b200 import binding as b
+
+pytestmark = pytest.mark.gpu
+
+from gpu_util import Workspace  # noqa: E402
+
+STEP = {torch.float32: 2.0 ** -24, torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}      # half a step, relative
+LEAST = {torch.float32: 2.0 ** -149, torch.float16: 2.0 ** -25, torch.bfloat16: 2.0 ** -134}  # half the smallest spacing, or more
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def randn(seed, *shape):
+    return torch.randn(shape, generator=gen(seed), device="cuda")
+
+
+def operands(tokens, k, n, many, rank, dtype, seed=1, d_type=None, ranks=True, bare=True):
+    g = gen(seed + 100)
+    x = (randn(seed, tokens, k) * torch.exp(randn(seed + 1, tokens, 1))).to(dtype)
+    a, w = (randn(seed + 2, many, rank, k) * k ** -0.5).to(dtype), randn(seed + 3, many, n, rank).to(dtype)
+    index = torch.randint(-1 if bare else 0, many + (1 if bare else 0), (tokens,), generator=g, device="cuda").to(torch.int32)
+    scales = torch.exp(randn(seed + 4, many))
+    used = torch.randint(0, rank + 1, (many,), generator=g, device="cuda").to(torch.int32) if ranks else None
+    if ranks:                                                     # nothing beyond an adapter's rank is read
+        beyond = torch.arange(rank, device="cuda")[None, :] >= used[:, None]
+        a.masked_fill_(beyond[:, :, None], float("nan"))
+        w.masked_fill_(beyond[:, None, :], float("nan"))
+    c = (3 * randn(seed + 5, tokens, n)).to(d_type or dtype)
+    return x, a, w, index, c, scales, used
+
+
+def plain(x, a, w, index, c, scales, ranks):
+    """(the result, the sum of magnitudes, magnitudes of what stands beside one entry of L at the most) in 64 bits."""
+    tokens, n = len(x), w.shape[1]
+    d = torch.zeros(tokens, n, dtype=torch.float64, device="cuda") if c is None else c.double().clone()
+    size, beside = d.abs(), torch.zeros_like(d)
+    for i in range(len(a)):
+        rows = (index == i).nonzero()[:, 0]
+        r = a.shape[1] if ranks is None else int(ranks[i])
+        if not len(rows) or r == 0:
+            continue
+        s = 1.0 if scales is None else float(scales[i])
+        low, large = x[rows].double() @ a[i, :r].double().t() * s, x[rows].double().abs() @ a[i, :r].double().abs().t() * abs(s)
+        wt = w[i, :, :r].double().t()
+        d[rows] += low @ wt
+        size[rows] += large @ wt.abs()
+        beside[rows] = low.abs().amax(1, keepdim=True) * wt.abs().sum(0, keepdim=True)
+    return d, size, beside
+
+
+def workspace(tokens, rank, many):
+    return Workspace(b.workspace_bytes(b.OP_ADAPTER_ADD, tokens, rank, many, 1))
+
+
+def room(k, rank, want, size, beside, dtype, d_type):
+    """Products of 16-bit numbers are exact in 32 bits; sums of k and of 2 rank terms (aligned and cut, not rounded, is allowed for) with up to 40 pieces, two
+    roundings by the scale and back, the addition of C; L as two numbers: 2^-18 of it each (bf16), or half of fp16's smallest step, 2^-25, of a row whose largest
+    entry is in [1, 2); one rounding."""
+    split = 2.0 ** -18 * size if dtype == torch.bfloat16 else 2.0 ** -22 * size + 2.0 ** -25 * beside
+    return size * (k + 2 * rank + 48) * 2.0 ** -23 + split * 1.001 + STEP[d_type] * want.abs() * 1.001 + LEAST[d_type]
+
+
+def check(tokens, k, n, many, rank, dtype, d_type=None, add=True, seed=1, **how):
+    d_type = d_type or dtype
+    x, a, w, index, c, scales, used = operands(tokens, k, n, many, rank, dtype, seed, d_type, **how)
+    c = c if add else None
+    d = torch.full((tokens, n), float("nan"), device="cuda").to(d_type)
+    with workspace(tokens, rank, many) as ws:
+        ws.buf[4096:].fill_(0xff)
+        b.adapter_add(x, a, w, index, d, C=c, scales=scales, ranks=used)
+        b.device_status()
+    want, size, beside = plain(x, a, w, index, c, scales, used)
+    off, most = (d.double() - want).abs(), room(k, rank, want, size, beside, dtype, d_type)
+    assert bool((off <= most).all()), float((off / most).max())
+    bare = (index < 0) | (index >= many)
+    assert bool((d[bare] == (0 if c is None else c[bare])).all())
+    return d
+
+
+SIZES = [(1, 1, 1, 1, 1), (1, 4096, 512, 8, 16), (2, 33, 31, 3, 5), (3, 64, 64, 1, 8), (15, 1000, 130, 2, 16), (16, 128, 33, 1, 32), (17, 128, 257, 1, 17), (40, 511, 1000, 40, 64),
+         (64, 2048, 64, 5, 128), (256, 96, 200, 300, 33), (257, 96, 200, 300, 33), (300, 1024, 999, 1, 16), (700, 520, 264, 3, 24), (1000, 4096, 128, 7, 64), (515, 300, 600, 2, 128),
+         (3000, 64, 72, 200, 4), (129, 8, 2000, 1, 100), (1024, 1, 8, 5, 2), (20, 20000, 8, 2, 16), (400, 20000, 8, 2, 16)]
+
+
+@pytest.mark.parametrize("tokens,k,n,many,rank", SIZES)
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_adapters_against_64_bits(tokens, k, n, many, rank, dtype):
+    check(tokens, k, n, many, rank, dtype)
+
+
+@pytest.mark.parametrize("tokens", [5, 300])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("d_type", [torch.float32, torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("add", [True, False])
+def test_outputs_of_any_type_with_and_without_what_is_added(tokens, dtype, d_type, add):
+    for rank in (16, 48):
+        check(tokens, 200, 301, 3, rank, dtype, d_type, add)
+        check(tokens, 256, 320, 3, rank, dtype, d_type, add, ranks=False, bare=False)
+
+
+@pytest.mark.parametrize("tokens,rank", [(20, 16), (20, 40), (300, 16), (300, 40)])
+def test_in_place_rows_without_adapter_are_not_touched(tokens, rank):
+    x, a, w, index, c, scales, used = operands(tokens, 128, 260, 4, rank, torch.bfloat16, 11)
+    index[::3] = torch.tensor([-1, 4, 2 ** 31 - 1, -2 ** 31], dtype=torch.int32, device="cuda").repeat(tokens)[:len(index[::3])]
+    store = torch.cat([c, torch.full((5, 260), float("nan"), device="cuda").bfloat16()])          # rows behind the last token
+    before = store.clone()
+    apart = torch.empty_like(c)
+    with workspace(tokens, rank, 4):
+        b.adapter_add(x, a, w, index, apart, C=c, scales=scales, ranks=used)
+        b.adapter_add(x, a, w, index, store[:tokens], C=store[:tokens], scales=scales, ranks=used)
+    assert torch.equal(store[:tokens], apart)
+    assert torch.equal(store.view(torch.int16)[::3][:len(index[::3])], before.view(torch.int16)[::3][:len(index[::3])])
+    assert torch.equal(store.view(torch.int16)[tokens:], before.view(torch.int16)[tokens:])
+
+
+def test_all_tokens_without_adapter_or_with_the_last_one():
+    for tokens in (9, 500):
+        x, a, w, index, c, scales, _ = operands(tokens, 64, 128, 6, 8, torch.float16, 21, ranks=False)
+        for value in (-1, 5):
+            index.fill_(value)
+            d = torch.full_like(c, float("nan"))
+            with workspace(tokens, 8, 6):
+                b.adapter_add(x, a, w, index, d, C=c, scales=scales)
+            want, size, beside = plain(x, a, w, index, c, scales, None)
+            assert bool(((d.double() - want).abs() <= room(64, 8, want, size, beside, torch.float16, torch.float16)).all())
+
+
+@pytest.mark.parametrize("tokens", [30, 700])
+def test_a_token_by_itself_whatever_the_others_are(tokens):
+    x, a, w, index, c, scales, used = operands(tokens, 300, 200, 5, 24, torch.bfloat16, 31)
+    first, other = torch.empty_like(c), torch.empty_like(c)
+    order = torch.randperm(tokens, generator=gen(32), device="cuda")
+    with workspace(tokens, 24, 5):
+        b.adapter_add(x, a, w, index, first, C=c, scales=scales, ranks=used)
+        b.adapter_add(x[order], a, w, index[order], other, C=c[order], scales=scales, ranks=used)
+        assert torch.equal(first[order], other)
+        # NaN in other tokens and other adapters stays there
+        bad = index == int(index[0])
+        x2, a2 = x.clone(), a.clone()
+        x2[~bad] = float("nan")
+        a2[torch.arange(5, device="cuda") != int(index[0])] = float("inf")
+        b.adapter_add(x2, a2, w, index, other, C=c, scales=scales, ranks=used)
+        assert torch.equal(first[bad], other[bad])
+
+
+@pytest.mark.parametrize("tokens", [4, 300])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_values_near_the_ends_of_the_types(tokens, dtype):
+    k, n, rank = 64, 40, 16
+    big, small = (6e4, 6e-8) if dtype == torch.float16 else (1e18, 1e-18)
+    for factor in (big, small):
+        x, a, w, index, _, _, _ = operands(tokens, k, n, 2, rank, dtype, 41, ranks=False, bare=False)
+        # L far above and far below what 16 bits hold (fp16), brought back by the scales
+        x = (torch.sign(x.float()) * factor).to(dtype)
+        scales = torch.tensor([1 / factor, 0.5 / factor], device="cuda")
+        d = torch.empty(tokens, n, device="cuda")
+        with workspace(tokens, rank, 2):
+            b.adapter_add(x, a, w, index, d, scales=scales)
+            want, size, beside = plain(x, a, w, index, None, scales, None)
+            off, most = (d.double() - want).abs(), room(k, rank, want, size, beside, dtype, torch.float32)
+            assert bool((off <= most).all()), float((off / most).max())
+            b.adapter_add(x, a, w, index, d)                      # and not brought back: a 32-bit output holds it
+            want, size, beside = plain(x, a, w, index, None, None, None)
+            off, most = (d.double() - want).abs(), room(k, rank, want, size, beside, dtype, torch.float32)
+            assert bool((off <= most).all()), float((off / most).max())
+
+
+@pytest.mark.parametrize("tokens", [4, 300])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_infinities_and_nan(tokens, dtype):
+    x, a, w, index, c, scales, _ = operands(tokens, 64, 40, 2, 8, dtype, 51, ranks=False, bare=False)
+    x[1, 3], x[2, 5] = float("inf"), float("nan")
+    a[:, 0, 3] = 1.0
+    a[:, 1:, 3] = 0.0                                             # 0 x inf is NaN in the other entries of L
+    d = torch.empty_like(c)
+    with workspace(tokens, 8, 2):
+        b.adapter_add(x, a, w, index, d, C=c, scales=scales)
+        assert bool(torch.isnan(d[1:3]).all()) and bool(torch.isfinite(d[3:]).all()) and bool(torch.isfinite(d[0]).all())
+        a[:, 1:, 3] = 0.5                                         # every entry of L infinite: the sign of the sum, or NaN
+        w.copy_(w.float().abs() + 0.1)
+        b.adapter_add(x, a, w, index, d, C=c, scales=scales)
+    assert bool((d[1] == float("inf")).all()) and bool(torch.isnan(d[2]).all())
+
+
+@pytest.mark.parametrize("tokens", [30, 300])
+@pytest.mark.parametrize("dtype,rank", [(torch.bfloat16, 16), (torch.float16, 40)])
+def test_strided_unaligned_operands_and_nothing_beside_them(tokens, dtype, rank):
+    k, n, many = 120, 248, 3
+    x, a, w, index, c, scales, used = operands(tokens, k, n, many, rank, dtype, 61)
+    want = torch.empty_like(c)
+
+    def apart(t, skip, *pad):                                     # the same values in a larger store, `skip` entries past its start
+        store = torch.full((math.prod(s + p for s, p in zip(t.shape, pad)) + skip,), float("nan"), device="cuda").to(t.dtype)
+        view = store[skip:].view([s + p for s, p in zip(t.shape, pad)])[tuple(slice(0, s) for s in t.shape)]
+        view.copy_(t)
+        return view
+
+    with workspace(tokens, rank, many):
+        b.adapter_add(x, a, w, index, want, C=c, scales=scales, ranks=used)
+        for skip, pad in ((0, 8), (1, 0), (3, 5), (4, 4)):
+            store = torch.full((tokens + 2, n + 9), 7.0, device="cuda").to(dtype)
+            d = store[1:-1, skip:skip + n]
+            b.adapter_add(apart(x, skip, 1, pad), apart(a, skip, 1, 2, pad), apart(w, skip, 1, 3, pad), index, d, C=apart(c, skip, 2, pad), scales=scales, ranks=used)
+            assert torch.equal(d, want)
+            assert bool((store[0] == 7).all()) and bool((store[-1] == 7).all()) and bool((store[:, :skip] == 7).all()) and bool((store[:, skip + n:] == 7).all())
+        one = a[:1].expand(many, rank, k)                         # one A for all adapters
+        b.adapter_add(x, one.contiguous(), w, index, want, C=c, scales=scales, ranks=None)
+        b.adapter_add(x, one, w, index, d, C=c, scales=scales, ranks=None)
+        assert torch.equal(d.isnan(), want.isnan()) and torch.equal(d.nan_to_num(), want.nan_to_num())
+
+
+def test_nothing_to_add():
+    c = randn(71, 5, 9).bfloat16()
+    x = torch.ones(5, 4, dtype=torch.bfloat16, device="cuda")
+    for k, rank, many in ((0, 3, 2), (4, 0, 2), (4, 3, 0)):
+        a, w = torch.ones(many, rank, k, dtype=torch.bfloat16, device="cuda"), torch.ones(many, 9, rank, dtype=torch.bfloat16, device="cuda")
+        index = torch.zeros(5, dtype=torch.int32, device="cuda")
+        d = torch.full_like(c, float("nan"))
+        b.adapter_add(x[:, :k], a, w, index, d, C=c)
+        assert torch.equal(d, c)
+        b.adapter_add(x[:, :k], a, w, index, d)
+        assert bool((d == 0).all())
+    none = torch.empty(0, 4, dtype=torch.bfloat16, device="cuda")
+    a, w = torch.ones(2, 3, 4, dtype=torch.bfloat16, device="cuda"), torch.ones(2, 9, 3, dtype=torch.bfloat16, device="cuda")
+    b.adapter_add(none, a, w, index[:0], torch.empty(0, 9, device="cuda"))
+    b.adapter_add(x, a, w[:, :0], index, torch.empty(5, 0, device="cuda"))
+
+
+@pytest.mark.parametrize("tokens", [8, 300])
+def test_offsets_beyond_32_bits(tokens):
+    stride = 2 ** 31 + 64                                         # adapters 4 GB apart, in A and in B
+    store = torch.empty(2 * stride, dtype=torch.bfloat16, device="cuda")
+    x, a, w, index, c, scales, _ = operands(tokens, 64, 32, 2, 8, torch.bfloat16, 81, ranks=False)
+    far_a, far_w = torch.as_strided(store, (2, 8, 64), (stride, 64, 1)), torch.as_strided(store, (2, 32, 8), (stride, 8, 1), 1024)
+    far_a.copy_(a)
+    far_w.copy_(w)
+    d, want = torch.empty_like(c), torch.empty_like(c)
+    with workspace(tokens, 8, 2):
+        b.adapter_add(x, a, w, index, want, C=c, scales=scales)
+        b.adapter_add(x, far_a, far_w, index, d, C=c, scales=scales)
+    assert torch.equal(d, want)
+
+
+@pytest.mark.parametrize("tokens,rank", [(40, 16), (600, 64)])
+def test_another_stream_and_a_captured_graph(tokens, rank):
+    x, a, w, index, c, scales, used = operands(tokens, 256, 512, 6, rank, torch.bfloat16, 91)
+    d, want = torch.empty_like(c), torch.empty_like(c)
+    with workspace(tokens, rank, 6):
+        b.adapter_add(x, a, w, index, want, C=c, scales=scales, ranks=used)
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=side):
+            b.adapter_add(x, a, w, index, d, C=c, scales=scales, ranks=used)
+        d.zero_()
+        for _ in range(3):
+            graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(d, want)
+        index.copy_(index.flip(0))                                # other requests by the next replay
+        graph.replay()
+        b.adapter_add(x, a, w, index, want, C=c, scales=scales, ranks=used)
+        torch.cuda.synchronize()
+        assert torch.equal(d, want)
+        del graph

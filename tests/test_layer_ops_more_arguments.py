@@ -208,3 +208,71 @@ def test_clip_refuses_tensors_that_it_cannot_walk(calls):  # noqa: F811
         with pytest.raises(ValueError):
             b.clip_gradients([fine], 1.0, norm=norm)
     assert not calls
+
+
+# ------------------------------------------------------------------------------------------------------------------- adapters
+def _adapters(tokens=4, n=4, k=4, adapters=2, rank=4, X=one, type=b.BF16, ldx=4, A=one, lda=4, sa=16, B=one, ldb=4, sb=16, index=one, scales=null, ranks=null,
+              C=null, ldc=4, D=two, d_type=b.F32, ldd=4):
+    return b.lib().gemm2m_adapter_add(tokens, n, k, adapters, rank, X, type, ldx, A, lda, sa, B, ldb, sb, index, scales, ranks, C, ldc, D, d_type, ldd, null)
+
+
+@pytest.mark.parametrize("bad", [dict(tokens=-1), dict(n=-1), dict(k=-1), dict(tokens=2 ** 31), dict(adapters=-1), dict(adapters=16385), dict(rank=-1), dict(rank=129, ldb=129),
+                                 dict(type=b.F32), dict(type=b.E4M3), dict(d_type=b.E4M3), dict(ldx=3), dict(lda=3), dict(ldb=3), dict(ldd=3), dict(C=one, ldc=3),
+                                 dict(C=two, ldc=8), dict(sa=-1), dict(sb=-1), dict(X=null), dict(A=null), dict(B=null), dict(index=null), dict(D=null),
+                                 dict(X=257), dict(A=257), dict(B=257), dict(index=258), dict(scales=258), dict(ranks=258), dict(C=258), dict(D=4098), dict(D=4097, d_type=b.F16)])
+def test_adapters_refuse(bad):
+    assert not refused(_adapters())
+    assert refused(_adapters(**bad))
+
+
+def test_adapters_of_nothing_are_fine():
+    assert _adapters(tokens=0, X=null, index=null, D=null) == 0 and _adapters(n=0, B=null, D=null) == 0
+
+
+def test_adapter_workspace_sizes():
+    size = lambda *s: b.workspace_bytes(b.OP_ADAPTER_ADD, *s, 1)
+    for bad in ((-1, 4, 4), (4, -1, 4), (4, 129, 4), (4, 4, -1), (4, 4, 16385)):
+        assert size(*bad) == 0
+    for fine in ((0, 0, 0), (0, 16, 4), (1, 0, 4), (1, 16, 0), (1, 1, 1)):
+        assert 256 <= size(*fine) <= size(300, 64, 16)
+    assert size(100000, 64, 16) >= 100000 * (4 + 4 * 64)
+
+
+def adapter_operands(tokens=30, k=50, n=40, many=3, rank=8):
+    half = lambda *shape: Standin(torch.zeros(*shape, dtype=torch.bfloat16))
+    return dict(X=half(tokens, k), A=half(many, rank, k), B=half(many, n, rank), index=vector(tokens, torch.int32), D=dense(tokens, n), C=dense(tokens, n),
+                scales=vector(many), ranks=vector(many, torch.int32))
+
+
+def test_adapter_operands_lie_on_the_current_device_and_have_their_shapes_and_types(calls):  # noqa: F811
+    b.adapter_add(**adapter_operands())
+    assert len(calls) == 1
+    wrong = adapter_operands(31, 51, 41, 4, 9)
+    for operand in adapter_operands():
+        for elsewhere in (1, -1):
+            t = adapter_operands()
+            t[operand].index = elsewhere
+            with pytest.raises(ValueError):
+                b.adapter_add(**t)
+        with pytest.raises(ValueError):
+            b.adapter_add(**{**adapter_operands(), operand: wrong[operand]})
+        with pytest.raises(ValueError):
+            b.adapter_add(**{**adapter_operands(), operand: Standin(torch.zeros(adapter_operands()[operand].shape, dtype=torch.float64))})
+    for operand, bad in (("A", torch.zeros(3, 50, 8, dtype=torch.bfloat16).transpose(1, 2)), ("index", torch.zeros(60, dtype=torch.int32)[::2]),
+                         ("A", torch.zeros(3, 8, 50, dtype=torch.float16)), ("scales", torch.zeros(6)[::2])):
+        with pytest.raises(ValueError):
+            b.adapter_add(**{**adapter_operands(), operand: Standin(bad)})
+    assert len(calls) == 1
+
+
+def test_adapters_pass_their_strides_on(calls):  # noqa: F811
+    t = adapter_operands()
+    t["A"] = Standin(torch.zeros(3, 10, 64, dtype=torch.bfloat16)[:, :8, :50])
+    t["B"] = Standin(torch.zeros(1, 40, 8, dtype=torch.bfloat16).expand(3, 40, 8))
+    b.adapter_add(**t)
+    _, a = calls[-1]
+    assert a[:5] == (30, 40, 50, 3, 8) and a[9:11] == (64, 640) and a[12:14] == (8, 0)
+    for rank, many in ((1, 3), (8, 1), (1, 1), (0, 2), (3, 0)):
+        b.adapter_add(**adapter_operands(rank=rank, many=many))
+        _, a = calls[-1]
+        assert a[9] >= 50 and a[12] >= max(rank, 1) and a[10] >= 0 and a[13] >= 0
