@@ -11,32 +11,28 @@
 //
 // L is held in 32 bits, and goes into the second product as the sum of two 16-bit numbers (hi + lo, 2^-18 of L for bf16, 2^-22 of the largest entry of the row for fp16),
 // after a power of two per token that brings its largest entry near 1, so that no size of L overflows or underflows 16 bits.
-#include "layer_ops.cuh"
+#include "adapters.cuh"
 
 namespace gemm2m {
 
 namespace {
 
-constexpr int kFewTokens = 256;           // up to here blocks find their tile themselves; beyond, a kernel sorts the tokens first
-constexpr int kFewTile = 16, kManyTile = 128;
-constexpr int kFewWarps = 4, kManyWarps = 8;
-
-struct Tile { int32_t key, start, count, pad; };         // key = adapter, or `adapters`: tokens without one
-struct Layout { int64_t off_perm, off_tiles, off_count, off_low, total; int splits, padded; int64_t max_tiles; };
+constexpr int kFewWarps = 4;
 
 int64_t up(int64_t x, int64_t a) { return (x + a - 1) / a * a; }
 
-Layout layout_of(int64_t tokens, int rank, int adapters) {
-    Layout l;
+AdapterLayout layout_of(int64_t tokens, int rank, int adapters) {
+    AdapterLayout l;
     const bool few = tokens <= kFewTokens;
     const int64_t keys = adapters + 1, tile = few ? kFewTile : kManyTile;
     l.max_tiles = tokens / tile + (tokens < keys ? tokens : keys);
-    const int64_t want = l.max_tiles ? (2 * kSms + l.max_tiles - 1) / l.max_tiles : 1;
-    l.splits = (int)(want > 32 ? 32 : want);
+    // blocks for two rounds (few tokens: small ones) or for the two that an SM holds
+    const int64_t want = l.max_tiles == 0 ? 1 : few ? (2 * kSms + l.max_tiles - 1) / l.max_tiles : 2 * kSms / l.max_tiles, most = few ? 32 : 8;
+    l.splits = (int)(want > most ? most : want < 1 ? 1 : want);
     l.padded = rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128;
     l.off_perm = 0;
     l.off_tiles = up(4 * tokens, 256);
-    l.off_count = l.off_tiles + up((int64_t)sizeof(Tile) * l.max_tiles, 256);
+    l.off_count = l.off_tiles + up((int64_t)sizeof(AdapterTile) * l.max_tiles, 256);
     l.off_low = l.off_count + 256;
     l.total = l.off_low + up(4 * l.splits * tokens * l.padded, 256);
     return l;
@@ -48,12 +44,12 @@ __device__ __forceinline__ int key_of(const AdapterArgs& a, int64_t t) {
 }
 
 // Sorts the tokens by adapter (any order among the tokens of one: nothing depends on it) and cuts them into tiles; one block.
-__global__ void __launch_bounds__(1024) adapter_tiles_kernel(const AdapterArgs a, const Layout l) {
+__global__ void __launch_bounds__(1024) adapter_tiles_kernel(const AdapterArgs a, const AdapterLayout l) {
     extern __shared__ int32_t counts[];                  // [keys], then where each key's next token goes
     __shared__ int2 warps[32];
     const int keys = a.adapters + 1, lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     int32_t* perm = (int32_t*)(a.ws + l.off_perm);
-    Tile* tiles = (Tile*)(a.ws + l.off_tiles);
+    AdapterTile* tiles = (AdapterTile*)(a.ws + l.off_tiles);
     for (int i = threadIdx.x; i < keys; i += 1024) counts[i] = 0;
     __syncthreads();
     wait_for_prior_kernels();
@@ -105,18 +101,9 @@ __global__ void __launch_bounds__(1024) adapter_tiles_kernel(const AdapterArgs a
     }
 }
 
-// Tile blockIdx.x: its key and tokens.  FEW: every block works it out from the indexes (at most 256), else from the sorted list.
-// Returns the number of tokens, 0 where there is no such tile.
-template <bool FEW>
-__device__ __forceinline__ int find_tile(const AdapterArgs& a, const Layout& l, int32_t* tokens, int* key) {
-    if (!FEW) {
-        if ((int)blockIdx.x >= *(const int32_t*)(a.ws + l.off_count)) return 0;
-        const Tile t = ((const Tile*)(a.ws + l.off_tiles))[blockIdx.x];
-        for (int i = threadIdx.x; i < kManyTile; i += blockDim.x) tokens[i] = i < t.count ? ((const int32_t*)(a.ws + l.off_perm))[t.start + i] : -1;
-        __syncthreads();
-        *key = t.key;
-        return t.count;
-    }
+// Tile blockIdx.x: its key and tokens (-1 beyond its last), worked out by every block from the indexes.  Returns the number of tokens, 0 where there is
+// no such tile.
+__device__ __forceinline__ int find_tile(const AdapterArgs& a, int32_t* tokens, int* key) {
     constexpr int kThreads = kFewWarps * 32, kPer = kFewTokens / kThreads;
     __shared__ int32_t keys[kFewTokens], places[kFewTokens];
     __shared__ uint32_t firsts[kFewTokens / 32];
@@ -177,103 +164,62 @@ __device__ __forceinline__ uint4 row8(const T* row, int64_t at, int64_t end, boo
     return load8_part<T>(row + at, end - at).w[0];
 }
 
-// The rank in use of adapter `key`.
-__device__ __forceinline__ int rank_of(const AdapterArgs& a, int key) {
-    if (key >= a.adapters) return 0;
-    return a.ranks ? min(max(a.ranks[key], 0), a.rank) : a.rank;
-}
-
-// Pieces of L: block (tile, piece of k); MT x 16 tokens and all of the rank per warp, the warps beside each other along the tokens and then along k.
-template <typename T, int RT, int MT, bool FEW>
-__global__ void __launch_bounds__((FEW ? kFewWarps : kManyWarps) * 32) adapter_down_kernel(const AdapterArgs a, const Layout l, int splits, int vec) {
-    constexpr int kTile = FEW ? kFewTile : kManyTile, kWarps = FEW ? kFewWarps : kManyWarps;
-    constexpr int kAlongM = kTile / (16 * MT), kAlongK = kWarps / kAlongM, kPadded = 16 * RT;
-    extern __shared__ __align__(16) float pieces[];                    // [kAlongK][kTile][kPadded]
-    __shared__ int32_t tokens[kTile];
+// Pieces of L: block (tile, piece of k), the warps beside each other along k.
+template <typename T, int RT>
+__global__ void __launch_bounds__(kFewWarps * 32) adapter_down_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int vec) {
+    constexpr int kPadded = 16 * RT;
+    extern __shared__ __align__(16) float pieces[];      // [warp][token][kPadded]
+    __shared__ int32_t tokens[kFewTile];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int m0 = (warp % kAlongM) * 16 * MT, along = warp / kAlongM;
     wait_for_prior_kernels();
     int key;
-    const int count = find_tile<FEW>(a, l, tokens, &key);
+    const int count = find_tile(a, tokens, &key);
     if (count == 0) return;
     const int rank = rank_of(a, key);
     if (rank == 0) return;
     const T* A = (const T*)a.A + key * a.stride_a;
-    const T* X[2 * MT];
-    bool there[2 * MT];
+    const bool there0 = tokens[g] >= 0, there1 = tokens[g + 8] >= 0;
+    const T* X0 = (const T*)a.X + (there0 ? tokens[g] : 0) * a.ldx;
+    const T* X1 = (const T*)a.X + (there1 ? tokens[g + 8] : 0) * a.ldx;
+    float acc[2 * RT][4];
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
-        const int t = tokens[m0 + i * 8 + g];
-        there[i] = t >= 0;
-        X[i] = (const T*)a.X + (there[i] ? t : 0) * a.ldx;
-    }
-    float acc[MT][2 * RT][4];
+    for (int j = 0; j < 2 * RT; ++j)
 #pragma unroll
-    for (int i = 0; i < MT; ++i)
-#pragma unroll
-        for (int j = 0; j < 2 * RT; ++j)
-#pragma unroll
-            for (int c = 0; c < 4; ++c) acc[i][j][c] = 0.f;
+        for (int c = 0; c < 4; ++c) acc[j][c] = 0.f;
     // steps of 32 along k, dealt out to the pieces in runs and to the warps in turn
     const int64_t steps = (a.k + 31) / 32, per = (steps + splits - 1) / splits;
     const int64_t first = blockIdx.y * per, last = min(steps, first + per);
-    if (count > m0) {
 #pragma unroll 2
-        for (int64_t s = first + along; s < last; s += kAlongK) {
-            const int64_t at = s * 32 + q * 8;
-            uint4 x[2 * MT], w[2 * RT];
+    for (int64_t s = first + warp; s < last; s += kFewWarps) {
+        const int64_t at = s * 32 + q * 8;
+        uint4 w[2 * RT];
+        const uint4 x0 = there0 ? row8<T>(X0, at, a.k, vec) : make_uint4(0, 0, 0, 0), x1 = there1 ? row8<T>(X1, at, a.k, vec) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-            for (int i = 0; i < 2 * MT; ++i) x[i] = there[i] ? row8<T>(X[i], at, a.k, vec) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int j = 0; j < 2 * RT; ++j) w[j] = j * 8 + g < rank ? row8<T>(A + (j * 8 + g) * a.lda, at, a.k, vec) : make_uint4(0, 0, 0, 0);
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < 2 * RT; ++j) {
-                    mma<T>(acc[i][j], x[2 * i].x, x[2 * i + 1].x, x[2 * i].y, x[2 * i + 1].y, w[j].x, w[j].y);
-                    mma<T>(acc[i][j], x[2 * i].z, x[2 * i + 1].z, x[2 * i].w, x[2 * i + 1].w, w[j].z, w[j].w);
-                }
-        }
-    }
-    float* mine = pieces + (along * kTile + m0) * kPadded;
-#pragma unroll
-    for (int i = 0; i < MT; ++i)
+        for (int j = 0; j < 2 * RT; ++j) w[j] = j * 8 + g < rank ? row8<T>(A + (j * 8 + g) * a.lda, at, a.k, vec) : make_uint4(0, 0, 0, 0);
 #pragma unroll
         for (int j = 0; j < 2 * RT; ++j) {
-            *reinterpret_cast<float2*>(mine + (i * 16 + g) * kPadded + j * 8 + 2 * q) = make_float2(acc[i][j][0], acc[i][j][1]);
-            *reinterpret_cast<float2*>(mine + (i * 16 + g + 8) * kPadded + j * 8 + 2 * q) = make_float2(acc[i][j][2], acc[i][j][3]);
+            mma<T>(acc[j], x0.x, x1.x, x0.y, x1.y, w[j].x, w[j].y);
+            mma<T>(acc[j], x0.z, x1.z, x0.w, x1.w, w[j].z, w[j].w);
         }
+    }
+    float* mine = pieces + warp * kFewTile * kPadded;
+#pragma unroll
+    for (int j = 0; j < 2 * RT; ++j) {
+        *reinterpret_cast<float2*>(mine + g * kPadded + j * 8 + 2 * q) = make_float2(acc[j][0], acc[j][1]);
+        *reinterpret_cast<float2*>(mine + (g + 8) * kPadded + j * 8 + 2 * q) = make_float2(acc[j][2], acc[j][3]);
+    }
     __syncthreads();
     float* low = (float*)(a.ws + l.off_low) + blockIdx.y * a.tokens * kPadded;
-    for (int i = threadIdx.x; i < count * (kPadded / 4); i += kWarps * 32) {
+    for (int i = threadIdx.x; i < count * (kPadded / 4); i += kFewWarps * 32) {
         const int row = i / (kPadded / 4), c = i % (kPadded / 4) * 4;
         float4 sum = *reinterpret_cast<const float4*>(pieces + row * kPadded + c);
 #pragma unroll
-        for (int p = 1; p < kAlongK; ++p) {
-            const float4 v = *reinterpret_cast<const float4*>(pieces + (p * kTile + row) * kPadded + c);
+        for (int p = 1; p < kFewWarps; ++p) {
+            const float4 v = *reinterpret_cast<const float4*>(pieces + (p * kFewTile + row) * kPadded + c);
             sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
         }
         *reinterpret_cast<float4*>(low + tokens[row] * (int64_t)kPadded + c) = sum;
     }
-}
-
-template <typename T> __device__ __forceinline__ float largest() { return 3.3895314e38f; }
-template <> __device__ __forceinline__ float largest<__half>() { return 65504.f; }
-
-// v as hi + lo of 16 bits.  What is not finite stays in hi; what is too large (beside something that is not finite) saturates.
-template <typename T>
-__device__ __forceinline__ void split2(float v, T* hi, T* lo) {
-    const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
-    if (finite) v = fminf(fmaxf(v, -largest<T>()), largest<T>());
-    *hi = from_float<T>(v);
-    *lo = finite ? from_float<T>(v - to_float<T>(*hi)) : T(0.f);
-}
-
-// 2^-e for a row whose largest magnitude is in [2^e, 2^(e+1)), and 2^e, with e kept to [-126, 126]; 1 where that is not finite.
-__device__ __forceinline__ void row_power(float top, float* down, float* back) {
-    const int field = (int)(__float_as_uint(top) >> 23), e = field == 255 ? 0 : min(max(field - 127, -126), 126);
-    *down = __uint_as_float((uint32_t)(127 - e) << 23);
-    *back = __uint_as_float((uint32_t)(127 + e) << 23);
 }
 
 __device__ __forceinline__ void load8_of(const void* p, int type, int64_t at, int64_t valid, bool vec, float (&v)[8]) {
@@ -289,19 +235,17 @@ __device__ __forceinline__ void store8_of(void* p, int type, int64_t at, int64_t
     else store8_as<__nv_bfloat16>((__nv_bfloat16*)p + at, v, whole, valid);
 }
 
-// D = C + L B^T: block (tile, run of columns); MT x 16 tokens per warp, the warps beside each other along the tokens and then along the columns, 32 at a time.
-template <typename T, int RT, int MT, bool FEW>
-__global__ void __launch_bounds__((FEW ? kFewWarps : kManyWarps) * 32) adapter_up_kernel(const AdapterArgs a, const Layout l, int splits, int64_t run, int vec_b, int vec_d) {
-    constexpr int kTile = FEW ? kFewTile : kManyTile, kWarps = FEW ? kFewWarps : kManyWarps;
-    constexpr int kAlongM = kTile / (16 * MT), kAlongN = kWarps / kAlongM, kPadded = 16 * RT, kRow = kPadded + 4;
-    extern __shared__ __align__(16) float rows[];                    // [kTile][kRow]: L times s_a
-    __shared__ int32_t tokens[kTile];
-    __shared__ float backs[kTile];
+// D = C + L B^T: block (tile, run of columns), the warps beside each other along the columns, 32 at a time.
+template <typename T, int RT>
+__global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int64_t run, int vec_b, int vec_d) {
+    constexpr int kPadded = 16 * RT, kRow = kPadded + 4;
+    extern __shared__ __align__(16) float rows[];        // [kFewTile][kRow]: L times s_a
+    __shared__ int32_t tokens[kFewTile];
+    __shared__ float backs[kFewTile];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    const int m0 = (warp % kAlongM) * 16 * MT, along = warp / kAlongM;
     wait_for_prior_kernels();
     int key;
-    const int count = find_tile<FEW>(a, l, tokens, &key);
+    const int count = find_tile(a, tokens, &key);
     if (count == 0) return;
     const int rank = rank_of(a, key);
     if (rank == 0 && a.C == a.D) return;
@@ -309,7 +253,7 @@ __global__ void __launch_bounds__((FEW ? kFewWarps : kManyWarps) * 32) adapter_u
         // a warp per row: the pieces added up, times s_a, and the power of two of its largest entry
         const float scale = a.scales ? a.scales[key] : 1.f;
         const float* low = (const float*)(a.ws + l.off_low);
-        for (int r = warp; r < kTile; r += kWarps) {
+        for (int r = warp; r < kFewTile; r += kFewWarps) {
             float v[(kPadded + 31) / 32], top = 0.f;
 #pragma unroll
             for (int i = 0; i < (kPadded + 31) / 32; ++i) {
@@ -331,44 +275,39 @@ __global__ void __launch_bounds__((FEW ? kFewWarps : kManyWarps) * 32) adapter_u
         }
         __syncthreads();
     }
-    if (count <= m0) return;
     // operand A of the MMAs: lane (g, q) holds entries 4q, 4q+1 | 4q+2, 4q+3 of every 16 (RT = 1) or 8q .. 8q+7 of every 32
     constexpr int kStep = RT == 1 ? 4 : 8;
-    uint32_t hi[MT][RT][4], lo[MT][RT][4];
+    uint32_t hi[RT][4], lo[RT][4];
     if (rank > 0) {
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int s = 0; s < RT; ++s)
 #pragma unroll
-            for (int s = 0; s < RT; ++s)
-#pragma unroll
-                for (int h = 0; h < 4; ++h) {                // (row g + 8 (h & 1), pair h >> 1)
-                    const float* p = rows + (m0 + i * 16 + g + 8 * (h & 1)) * kRow + (RT == 1 ? 0 : (s >> 1) * 32) + q * kStep + (RT == 1 ? 0 : (s & 1) * 4) + (h >> 1) * 2;
-                    T x[2], y[2];
-                    split2<T>(p[0], &x[0], &y[0]);
-                    split2<T>(p[1], &x[1], &y[1]);
-                    hi[i][s][h] = *reinterpret_cast<const uint32_t*>(x);
-                    lo[i][s][h] = *reinterpret_cast<const uint32_t*>(y);
-                }
+            for (int h = 0; h < 4; ++h) {                    // (row g + 8 (h & 1), pair h >> 1)
+                const float* p = rows + (g + 8 * (h & 1)) * kRow + (RT == 1 ? 0 : (s >> 1) * 32) + q * kStep + (RT == 1 ? 0 : (s & 1) * 4) + (h >> 1) * 2;
+                T x[2], y[2];
+                split2<T>(p[0], &x[0], &y[0]);
+                split2<T>(p[1], &x[1], &y[1]);
+                hi[s][h] = *reinterpret_cast<const uint32_t*>(x);
+                lo[s][h] = *reinterpret_cast<const uint32_t*>(y);
+            }
     }
-    int64_t row[2 * MT];
-    float back[2 * MT];
-    bool there[2 * MT];
+    int64_t row[2];
+    float back[2];
+    bool there[2];
 #pragma unroll
-    for (int i = 0; i < 2 * MT; ++i) {
-        there[i] = m0 + i * 8 + g < count;
-        row[i] = there[i] ? tokens[m0 + i * 8 + g] : 0;
-        back[i] = rank > 0 ? backs[m0 + i * 8 + g] : 0.f;
+    for (int i = 0; i < 2; ++i) {
+        there[i] = i * 8 + g < count;
+        row[i] = there[i] ? tokens[i * 8 + g] : 0;
+        back[i] = rank > 0 ? backs[i * 8 + g] : 0.f;
     }
     const T* B = (const T*)a.B + (rank > 0 ? key : 0) * a.stride_b;
     const int64_t first = blockIdx.y * run, last = min(a.n, first + run);
-    for (int64_t n0 = first + along * 32; n0 < last; n0 += kAlongN * 32) {
-        float acc[MT][4][4];
+    for (int64_t n0 = first + warp * 32; n0 < last; n0 += kFewWarps * 32) {
+        float acc[4][4];
 #pragma unroll
-        for (int i = 0; i < MT; ++i)
+        for (int j = 0; j < 4; ++j)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int c = 0; c < 4; ++c) acc[i][j][c] = 0.f;
+            for (int c = 0; c < 4; ++c) acc[j][c] = 0.f;
         if (rank > 0) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -382,37 +321,31 @@ __global__ void __launch_bounds__((FEW ? kFewWarps : kManyWarps) * 32) adapter_u
                         const uint4 part = load8_part<T>(b + q * 4, in ? min(4, rank - q * 4) : 0).w[0];
                         w = make_uint2(part.x, part.y);
                     }
-#pragma unroll
-                    for (int i = 0; i < MT; ++i) {
-                        mma<T>(acc[i][j], hi[i][0][0], hi[i][0][1], hi[i][0][2], hi[i][0][3], w.x, w.y);
-                        mma<T>(acc[i][j], lo[i][0][0], lo[i][0][1], lo[i][0][2], lo[i][0][3], w.x, w.y);
-                    }
+                    mma<T>(acc[j], hi[0][0], hi[0][1], hi[0][2], hi[0][3], w.x, w.y);
+                    mma<T>(acc[j], lo[0][0], lo[0][1], lo[0][2], lo[0][3], w.x, w.y);
                 } else {
 #pragma unroll
                     for (int s = 0; s < RT; s += 2) {
                         const uint4 w = row8<T>(b, s * 16 + q * 8, in ? rank : 0, vec_b);
-#pragma unroll
-                        for (int i = 0; i < MT; ++i) {
-                            mma<T>(acc[i][j], hi[i][s][0], hi[i][s][1], hi[i][s][2], hi[i][s][3], w.x, w.y);
-                            mma<T>(acc[i][j], hi[i][s + 1][0], hi[i][s + 1][1], hi[i][s + 1][2], hi[i][s + 1][3], w.z, w.w);
-                            mma<T>(acc[i][j], lo[i][s][0], lo[i][s][1], lo[i][s][2], lo[i][s][3], w.x, w.y);
-                            mma<T>(acc[i][j], lo[i][s + 1][0], lo[i][s + 1][1], lo[i][s + 1][2], lo[i][s + 1][3], w.z, w.w);
-                        }
+                        mma<T>(acc[j], hi[s][0], hi[s][1], hi[s][2], hi[s][3], w.x, w.y);
+                        mma<T>(acc[j], hi[s + 1][0], hi[s + 1][1], hi[s + 1][2], hi[s + 1][3], w.z, w.w);
+                        mma<T>(acc[j], lo[s][0], lo[s][1], lo[s][2], lo[s][3], w.x, w.y);
+                        mma<T>(acc[j], lo[s + 1][0], lo[s + 1][1], lo[s + 1][2], lo[s + 1][3], w.z, w.w);
                     }
                 }
             }
         }
         const int64_t col = n0 + 8 * q, valid = a.n - col;
 #pragma unroll
-        for (int i = 0; i < 2 * MT; ++i) {
+        for (int i = 0; i < 2; ++i) {
             if (!there[i] || valid <= 0) continue;
             float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
             if (a.C) load8_of(a.C, a.d_type, row[i] * a.ldc + col, valid, vec_d, v);
             if (rank > 0) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    v[2 * j] += acc[i >> 1][j][2 * (i & 1)] * back[i];
-                    v[2 * j + 1] += acc[i >> 1][j][2 * (i & 1) + 1] * back[i];
+                    v[2 * j] += acc[j][2 * i] * back[i];
+                    v[2 * j + 1] += acc[j][2 * i + 1] * back[i];
                 }
             }
             store8_of(a.D, a.d_type, row[i] * a.ldd + col, valid, vec_d, v);
@@ -425,59 +358,36 @@ cudaError_t allow_smem(K kernel, size_t bytes) {
     return bytes > 48 * 1024 ? cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) : cudaSuccess;
 }
 
-template <typename T, int RT, bool FEW>
-cudaError_t launch_tiles(const AdapterArgs& a, const Layout& l, cudaStream_t st, int launches[2]) {
-    constexpr int kTile = FEW ? kFewTile : kManyTile, kWarps = FEW ? kFewWarps : kManyWarps;
-    constexpr int MT = FEW || RT > 4 ? 1 : 2;
-    constexpr int kAlongK = kWarps / (kTile / (16 * MT)), kAlongN = kAlongK;
-    if (!FEW) {
-        const size_t smem = 4 * (size_t)(a.adapters + 1);
-        cudaError_t err = allow_smem(adapter_tiles_kernel, smem);
-        if (err != cudaSuccess) return err;
-        err = launch_chained(adapter_tiles_kernel, dim3(1), dim3(1024), smem, st, a, l);
-        if (err != cudaSuccess) return err;
-        ++launches[0];
-    }
+template <typename T, int RT>
+cudaError_t launch_few(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st, int launches[2]) {
     auto even = [](const void* p, int64_t ld, int64_t stride, int64_t bytes) { return ((uintptr_t)p | (uintptr_t)(ld * 2) | (uintptr_t)(stride * 2)) % bytes == 0; };
-    const int64_t steps = (a.k + 31) / 32, most = (steps + 2 * kAlongK - 1) / (2 * kAlongK);      // at least two steps for every warp
+    const int64_t steps = (a.k + 31) / 32, most = (steps + 2 * kFewWarps - 1) / (2 * kFewWarps);      // at least two steps for every warp
     const int splits = (int)(l.splits < most ? l.splits : most);
     const int vec = even(a.X, a.ldx, 0, 16) && even(a.A, a.lda, a.stride_a, 16);
-    auto* down = adapter_down_kernel<T, RT, MT, FEW>;
-    size_t smem = 4 * (size_t)kAlongK * kTile * 16 * RT;
-    cudaError_t err = allow_smem(down, smem);
-    if (err != cudaSuccess) return err;
-    err = launch_chained(down, dim3((unsigned)l.max_tiles, (unsigned)splits), dim3(kWarps * 32), smem, st, a, l, splits, vec);
+    cudaError_t err = launch_chained(adapter_down_kernel<T, RT>, dim3((unsigned)l.max_tiles, (unsigned)splits), dim3(kFewWarps * 32), 4 * (size_t)kFewWarps * kFewTile * 16 * RT, st, a, l,
+                                     splits, vec);
     if (err != cudaSuccess) return err;
     ++launches[0];
     const size_t es = a.d_type == kF32 ? 4 : 2;
     const int vec_b = even(a.B, a.ldb, a.stride_b, RT == 1 ? 8 : 16);
     const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * es)) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * es)) % 16 == 0);
     // runs of columns: a few blocks for every SM, and at least two steps of 32 columns for every warp
-    const int64_t groups = (a.n + 32 * kAlongN - 1) / (32 * kAlongN), runs = (4 * kSms + l.max_tiles - 1) / l.max_tiles;
+    const int64_t groups = (a.n + 32 * kFewWarps - 1) / (32 * kFewWarps), runs = (4 * kSms + l.max_tiles - 1) / l.max_tiles;
     int64_t per = (groups + runs - 1) / runs;
     if (per < 2) per = 2;
-    const int64_t run = per * 32 * kAlongN;
-    auto* upk = adapter_up_kernel<T, RT, MT, FEW>;
-    smem = 4 * (size_t)kTile * (16 * RT + 4);
-    err = allow_smem(upk, smem);
-    if (err != cudaSuccess) return err;
-    err = launch_chained(upk, dim3((unsigned)l.max_tiles, (unsigned)((a.n + run - 1) / run)), dim3(kWarps * 32), smem, st, a, l, splits, run, vec_b, vec_d);
+    const int64_t run = per * 32 * kFewWarps;
+    err = launch_chained(adapter_up_kernel<T, RT>, dim3((unsigned)l.max_tiles, (unsigned)((a.n + run - 1) / run)), dim3(kFewWarps * 32), 4 * (size_t)kFewTile * (16 * RT + 4), st, a, l, splits,
+                         run, vec_b, vec_d);
     if (err == cudaSuccess) ++launches[1];
     return err;
 }
 
-template <typename T, int RT>
-cudaError_t launch_rank(const AdapterArgs& a, const Layout& l, cudaStream_t st, int launches[2]) {
-    return a.tokens <= kFewTokens ? launch_tiles<T, RT, true>(a, l, st, launches) : launch_tiles<T, RT, false>(a, l, st, launches);
-}
-
 template <typename T>
-cudaError_t launch_typed(const AdapterArgs& a, cudaStream_t st, int launches[2]) {
-    const Layout l = layout_of(a.tokens, a.rank, a.adapters);
-    if (l.padded == 16) return launch_rank<T, 1>(a, l, st, launches);
-    if (l.padded == 32) return launch_rank<T, 2>(a, l, st, launches);
-    if (l.padded == 64) return launch_rank<T, 4>(a, l, st, launches);
-    return launch_rank<T, 8>(a, l, st, launches);
+cudaError_t launch_typed(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st, int launches[2]) {
+    if (l.padded == 16) return launch_few<T, 1>(a, l, st, launches);
+    if (l.padded == 32) return launch_few<T, 2>(a, l, st, launches);
+    if (l.padded == 64) return launch_few<T, 4>(a, l, st, launches);
+    return launch_few<T, 8>(a, l, st, launches);
 }
 
 }  // namespace
@@ -485,7 +395,15 @@ cudaError_t launch_typed(const AdapterArgs& a, cudaStream_t st, int launches[2])
 int64_t adapter_bytes(int64_t tokens, int rank, int adapters) { return layout_of(tokens, rank, adapters).total; }
 
 cudaError_t launch_adapter_add(const AdapterArgs& a, cudaStream_t st, int launches[2]) {
-    return a.type == kF16 ? launch_typed<__half>(a, st, launches) : launch_typed<__nv_bfloat16>(a, st, launches);
+    const AdapterLayout l = layout_of(a.tokens, a.rank, a.adapters);
+    if (a.tokens <= kFewTokens) return a.type == kF16 ? launch_typed<__half>(a, l, st, launches) : launch_typed<__nv_bfloat16>(a, l, st, launches);
+    const size_t smem = 4 * (size_t)(a.adapters + 1);
+    cudaError_t err = allow_smem(adapter_tiles_kernel, smem);
+    if (err != cudaSuccess) return err;
+    err = launch_chained(adapter_tiles_kernel, dim3(1), dim3(1024), smem, st, a, l);
+    if (err != cudaSuccess) return err;
+    ++launches[0];
+    return launch_adapter_many(a, l, st, launches);
 }
 
 }  // namespace gemm2m

@@ -1,0 +1,45 @@
+// What the two forms of the low-rank updates share: few tokens (adapters.cu) and many (adapters_many.cu).
+#pragma once
+#include "layer_ops.cuh"
+
+namespace gemm2m {
+
+constexpr int kFewTokens = 256;           // up to here the first form, whose blocks find their tile themselves; beyond, a kernel sorts the tokens first
+constexpr int kFewTile = 16, kManyTile = 128;
+
+struct AdapterTile { int32_t key, start, count, pad; };      // key = adapter, or `adapters`: tokens without one; start: in the sorted list
+struct AdapterLayout {
+    int64_t off_perm, off_tiles, off_count, off_low, total;  // bytes: sorted tokens, tiles, their number, pieces of L
+    int splits, padded;                   // pieces of L at the most, and entries of a token in one
+    int64_t max_tiles;
+};
+cudaError_t launch_adapter_many(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st, int launches[2]);
+
+#ifdef __CUDACC__
+// The rank in use of adapter `key`.
+__device__ __forceinline__ int rank_of(const AdapterArgs& a, int key) {
+    if (key >= a.adapters) return 0;
+    return a.ranks ? min(max(a.ranks[key], 0), a.rank) : a.rank;
+}
+
+template <typename T> __device__ __forceinline__ float largest() { return 3.3895314e38f; }
+template <> __device__ __forceinline__ float largest<__half>() { return 65504.f; }
+
+// v as hi + lo of 16 bits.  What is not finite stays in hi; what is too large (beside something that is not finite) saturates.
+template <typename T>
+__device__ __forceinline__ void split2(float v, T* hi, T* lo) {
+    const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
+    if (finite) v = fminf(fmaxf(v, -largest<T>()), largest<T>());
+    *hi = from_float<T>(v);
+    *lo = finite ? from_float<T>(v - to_float<T>(*hi)) : T(0.f);
+}
+
+// 2^-e for a row whose largest magnitude is in [2^e, 2^(e+1)), and 2^e, with e kept to [-126, 126]; 1 where that is not finite.
+__device__ __forceinline__ void row_power(float top, float* down, float* back) {
+    const int field = (int)(__float_as_uint(top) >> 23), e = field == 255 ? 0 : min(max(field - 127, -126), 126);
+    *down = __uint_as_float((uint32_t)(127 - e) << 23);
+    *back = __uint_as_float((uint32_t)(127 + e) << 23);
+}
+#endif
+
+}  // namespace gemm2m

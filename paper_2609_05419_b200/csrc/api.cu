@@ -1168,7 +1168,7 @@ int gemm2m_adapter_add(int64_t tokens, int64_t n, int64_t k, int adapters, int r
     Phases ph;
     if (int s = begin_call(&ph)) return s;
     const AdapterArgs a = {tokens, n, k, adapters, rank, X, type, ldx, A, lda, stride_a, B, ldb, stride_b, index, scales, ranks, C, ldc, D, d_type, ldd,
-                           (char*)dev.ws + kLayerOpsOffset};
+                           (char*)dev.ws + kLayerOpsOffset, (int*)dev.ws};
     int launches[2] = {0, 0};
     CK(ph.begin(2, st));
     CK(launch_adapter_add(a, st, launches));

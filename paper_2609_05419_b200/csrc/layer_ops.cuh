@@ -108,6 +108,7 @@ struct AdapterArgs {
     const void* C; int64_t ldc;
     void* D; int d_type; int64_t ldd;
     char* ws;
+    int* dev_status;
 };
 int64_t adapter_bytes(int64_t tokens, int rank, int adapters);      // workspace
 cudaError_t launch_adapter_add(const AdapterArgs& a, cudaStream_t st, int launches[2]);
