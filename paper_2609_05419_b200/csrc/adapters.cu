@@ -54,18 +54,28 @@ __global__ void __launch_bounds__(1024) adapter_tiles_kernel(const AdapterArgs a
     __syncthreads();
     wait_for_prior_kernels();
     const int64_t rounds = (a.tokens + 1023) / 1024;
-    auto take = [&](int64_t t, int key, int* rank) {     // place of this lane's token among those counted so far
+    auto take = [&](bool there, int key) {               // place of this lane's token among those of its key taken so far
         const unsigned same = __match_any_sync(0xffffffffu, key);
         const int leader = __ffs(same) - 1;
         int base = 0;
-        if (lane == leader && t < a.tokens) base = atomicAdd(&counts[key], __popc(same));
-        *rank = __shfl_sync(0xffffffffu, base, leader) + __popc(same & ((1u << lane) - 1));
+        if (lane == leader && there) base = atomicAdd(&counts[key], __popc(same));
+        return __shfl_sync(0xffffffffu, base, leader) + __popc(same & ((1u << lane) - 1));
     };
-    for (int64_t r = 0; r < rounds; ++r) {
-        const int64_t t = r * 1024 + threadIdx.x;
-        int rank;
-        take(t, t < a.tokens ? key_of(a, t) : -1, &rank);
-    }
+    // eight rounds' indexes in flight together
+    auto each = [&](auto&& f) {
+        for (int64_t r0 = 0; r0 < rounds; r0 += 8) {
+            int key[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int64_t t = (r0 + i) * 1024 + threadIdx.x;
+                key[i] = t < a.tokens ? key_of(a, t) : -1;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (r0 + i < rounds) f((r0 + i) * 1024 + threadIdx.x, key[i]);
+        }
+    };
+    each([&](int64_t t, int key) { take(t < a.tokens, key); });
     __syncthreads();
     // exclusive sums over the keys of tokens and of tiles: a run of keys per thread
     const int per = (keys + 1023) / 1024, k0 = min(keys, (int)threadIdx.x * per), k1 = min(keys, k0 + per);
@@ -93,12 +103,10 @@ __global__ void __launch_bounds__(1024) adapter_tiles_kernel(const AdapterArgs a
         before.x += count;
     }
     __syncthreads();
-    for (int64_t r = 0; r < rounds; ++r) {
-        const int64_t t = r * 1024 + threadIdx.x;
-        int place;
-        take(t, t < a.tokens ? key_of(a, t) : -1, &place);
+    each([&](int64_t t, int key) {
+        const int place = take(t < a.tokens, key);
         if (t < a.tokens) perm[place] = (int32_t)t;
-    }
+    });
 }
 
 // Tile blockIdx.x: its key and tokens (-1 beyond its last), worked out by every block from the indexes.  Returns the number of tokens, 0 where there is

@@ -2,8 +2,9 @@
 //
 // L = X A_a^T: a block takes a tile and a piece of k, in steps of 64 entries (one 128-byte swizzle row): four MMAs of 128 x rank x 16 per step.  The tile's rows of X lie
 // anywhere, so they come by asynchronous 16-byte copies (8- and 4-byte ones where rows start there), three or four steps ahead.
-// D = C + L B_a^T: a block takes a tile and a run of columns, 128 at a time.  L, as hi + lo, stays in shared memory; the MMAs of one piece of columns run
-// while the one before is read back, turned in shared memory so that four lanes hold 32 columns of a row, added to what was fetched of C a piece earlier, and stored.
+// D = C + L B_a^T: a block takes a tile and pieces of 128 columns.  L, as hi + lo, stays in shared memory; the MMAs of one piece run while the one before is
+// read back, added to what was fetched of C a piece earlier, and stored.  The read-back hands a lane pairs of columns 8 apart; the rows of B
+// lie in shared memory in such an order that these are eight neighbouring columns of D.
 #include "adapters.cuh"
 #include "gemm_ptx.cuh"
 
@@ -62,6 +63,17 @@ __device__ __forceinline__ void copy8(uint32_t dst, const uint16_t* row, int64_t
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ void fence_async_proxy() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// 16 rows of 32 columns of an accumulator: lane (g, q) of a warp receives columns 8j + 2q, 8j + 2q + 1 of row g in v[4j], v[4j + 1] and of row g + 8 in v[4j + 2], v[4j + 3].
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t (&v)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+          "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+        : "r"(taddr)
+        : "memory");
+}
 
 // 16-byte piece `piece` of row `row` of an operand (8 pieces a row, 128-byte swizzle).
 __device__ __forceinline__ uint32_t swizzled(uint32_t base, int row, int piece) { return base + (uint32_t)(row * kRowBytes + ((piece ^ (row & 7)) << 4)); }
@@ -196,9 +208,9 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
 
 // T: type of B (and of L's two parts), DT: of C and D; KB blocks of 64 along the rank.
 template <typename T, typename DT, int KB>
-__global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int64_t run, int align, int vec_d, uint32_t idesc,
+__global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int align, int vec_d, uint32_t idesc,
                                                                                   int* dev_status) {
-    constexpr int kTmemCols = 256, E = 16 / (int)sizeof(DT), kTurnBytes = 4096;      // E entries of D per lane and access
+    constexpr int kTmemCols = 256, E = 16 / (int)sizeof(DT), kAccesses = 8 / E;      // eight columns of a row per lane, E in one access
     extern __shared__ unsigned char smem_raw[];
     __shared__ uint64_t bars[4];
     __shared__ float backs[kManyTile];
@@ -210,68 +222,79 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const DT* C = (const DT*)a.C;
     DT* D = (DT*)a.D;
-    const int64_t first = blockIdx.y * run, last = min(a.n, first + run);
+    // pieces of 128 columns, dealt out in turn: the blocks of a tile of tokens read and write neighbouring columns at about the same time
+    const int64_t all = (a.n + kManyTile - 1) / kManyTile, tiles = (all - blockIdx.y + gridDim.y - 1) / gridDim.y;
+    auto column0 = [&](int64_t t) { return (t * gridDim.y + blockIdx.y) * kManyTile; };
     if (rank == 0) {                                     // D = C, or zero
         if (a.C == a.D) return;
-        for (int r = warp; r < tile.count; r += kThreads / 32) {
-            const int64_t t = tokens[r];
-            for (int64_t c = first + lane * E; c < last; c += 32 * E) {
-                if (vec_d && c + E <= last) {
-                    *reinterpret_cast<uint4*>(D + t * a.ldd + c) = C ? *reinterpret_cast<const uint4*>(C + t * a.ldc + c) : make_uint4(0, 0, 0, 0);
+        for (int64_t t = 0; t < tiles; ++t)
+            for (int i = threadIdx.x; i < tile.count * (kManyTile / E); i += kThreads) {
+                const int64_t row = tokens[i / (kManyTile / E)], c = column0(t) + i % (kManyTile / E) * E;
+                if (vec_d && c + E <= a.n) {
+                    *reinterpret_cast<uint4*>(D + row * a.ldd + c) = C ? *reinterpret_cast<const uint4*>(C + row * a.ldc + c) : make_uint4(0, 0, 0, 0);
                 } else {
-                    for (int64_t i = c; i < min(last, c + E); ++i) D[t * a.ldd + i] = C ? C[t * a.ldc + i] : DT(0.f);
+                    for (int64_t j = c; j < min(a.n, c + E); ++j) D[row * a.ldd + j] = C ? C[row * a.ldc + j] : DT(0.f);
                 }
             }
-        }
         return;
     }
     Frame<2> frame;
     frame.open(bars, kTmemCols, dev_status);
     const uint32_t low_hi = (smem_u32(smem_raw) + 1023u) & ~1023u, low_lo = low_hi + KB * kOperandBytes, b_base = low_lo + KB * kOperandBytes;
-    const uint32_t turn = b_base + 2 * KB * kOperandBytes + (uint32_t)warp * kTurnBytes;
 
     const uint16_t* B = (const uint16_t*)a.B + tile.key * a.stride_b;
     const int ksteps = (rank + 15) / 16, pieces = 2 * ksteps;         // 16-byte pieces of a row of B that the MMAs read
     auto load_b = [&](int64_t t) {
         const uint32_t dst = b_base + (uint32_t)(t & 1) * (KB * kOperandBytes);
         for (int i = threadIdx.x; i < kManyTile * 8 * KB; i += kThreads) {
-            const int piece = i % (8 * KB), row = i / (8 * KB);
-            const int64_t col = first + t * kManyTile + row;
-            if (piece < pieces && col < last) copy8(swizzled(dst + (piece >> 3) * kOperandBytes, row, piece & 7), B + col * a.ldb, piece * 8, rank, align);
+            const int piece = i % (8 * KB), c = i / (8 * KB);
+            const int64_t col = column0(t) + c;
+            const int row = (c & 96) | (c & 6) << 2 | (c & 24) >> 2 | (c & 1);      // columns 8q + 2j + e of every 32 are rows 8j + 2q + e
+            if (piece < pieces && col < a.n) copy8(swizzled(dst + (piece >> 3) * kOperandBytes, row, piece & 7), B + col * a.ldb, piece * 8, rank, align);
         }
     };
-    const int64_t tiles = (last - first + kManyTile - 1) / kManyTile;
     load_b(0);
     copies_commit();
     {
-        // L: a warp per row adds the pieces up, times s_a, and brings the largest entry near 1
+        // L: a warp adds the pieces of 16 rows up, all their loads of a piece in flight together, times s_a, and brings each row's largest entry near 1
+        constexpr int kRows = kManyTile / (kThreads / 32);
         const float scale = a.scales ? a.scales[tile.key] : 1.f;
-        const float* low = (const float*)(a.ws + l.off_low);
-        for (int r = warp; r < kManyTile; r += kThreads / 32) {
-            float2 v[KB];
+        const int token = lane < kRows && warp * kRows + lane < tile.count ? tokens[warp * kRows + lane] : 0;
+        const float* low = (const float*)(a.ws + l.off_low) + lane * 2;
+        const float* p[kRows];
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) p[i] = low + (int64_t)__shfl_sync(0xffffffffu, token, i) * l.padded;
+        float2 v[KB][kRows];
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+#pragma unroll
+            for (int i = 0; i < kRows; ++i) v[b][i] = make_float2(0.f, 0.f);
+            if (b * 64 + lane * 2 < rank)
+                for (int s = 0; s < splits; ++s) {
+                    float2 w[kRows];
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) w[i] = *reinterpret_cast<const float2*>(p[i] + s * a.tokens * l.padded + b * 64);
+#pragma unroll
+                    for (int i = 0; i < kRows; ++i) v[b][i].x += w[i].x, v[b][i].y += w[i].y;
+                }
+        }
+#pragma unroll
+        for (int i = 0; i < kRows; ++i) {
+            const int r = warp * kRows + i;
             float top = 0.f;
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
                 const int c = b * 64 + lane * 2;
-                v[b] = make_float2(0.f, 0.f);
-                if (c < rank && r < tile.count) {
-                    const float* p = low + (int64_t)tokens[r] * l.padded + c;
-                    for (int s = 0; s < splits; ++s) {
-                        const float2 w = *reinterpret_cast<const float2*>(p + s * a.tokens * l.padded);
-                        v[b].x += w.x, v[b].y += w.y;
-                    }
-                    v[b].x *= scale;
-                    v[b].y = c + 1 < rank ? v[b].y * scale : 0.f;
-                }
-                top = fmaxf(top, fmaxf(fabsf(v[b].x), fabsf(v[b].y)));
+                v[b][i] = make_float2(c < rank ? v[b][i].x * scale : 0.f, c + 1 < rank ? v[b][i].y * scale : 0.f);
+                top = fmaxf(top, fmaxf(fabsf(v[b][i].x), fabsf(v[b][i].y)));
             }
             float down, back;
             row_power(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))), &down, &back);
 #pragma unroll
             for (int b = 0; b < KB; ++b) {
                 T hi[2], lo[2];
-                split2<T>(v[b].x * down, &hi[0], &lo[0]);
-                split2<T>(v[b].y * down, &hi[1], &lo[1]);
+                split2<T>(v[b][i].x * down, &hi[0], &lo[0]);
+                split2<T>(v[b][i].y * down, &hi[1], &lo[1]);
                 const uint32_t at = swizzled((uint32_t)(b * kOperandBytes), r, lane >> 2) + (lane & 3) * 4;
                 asm volatile("st.shared.u32 [%0], %1;" ::"r"(low_hi + at), "r"(*reinterpret_cast<const uint32_t*>(hi)) : "memory");
                 asm volatile("st.shared.u32 [%0], %1;" ::"r"(low_lo + at), "r"(*reinterpret_cast<const uint32_t*>(lo)) : "memory");
@@ -280,26 +303,46 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
         }
     }
 
-    // Read-back: this warp's 32 rows and 64 of a piece's 128 columns, 32 at a time; a lane ends with E neighbouring columns of 32 / E rows.
-    const int quarter = warp & 3, half = warp >> 2, across = lane % (32 / E), row_in = lane / (32 / E);
-    int64_t place_c[32 / E], place_d[32 / E];
-    bool there[32 / E];
+    // Read-back: this warp's 32 rows (two halves of 16) and 64 of a piece's 128 columns, 32 at a time.
+    const int quarter = warp & 3, half = warp >> 2, g = lane >> 2, q = lane & 3;
+    int64_t place_c[4], place_d[4];                      // rows g, g + 8 of either half
+    float back[4];
+    bool there[4];
 #pragma unroll
-    for (int i = 0; i < 32 / E; ++i) {
-        const int row = quarter * 32 + i * E + row_in;
+    for (int i = 0; i < 4; ++i) {
+        const int row = quarter * 32 + i * 8 + g;
         there[i] = row < tile.count;
         const int64_t t = there[i] ? tokens[row] : 0;
         place_c[i] = t * a.ldc;
         place_d[i] = t * a.ldd;
     }
-    uint4 in[2][32 / E];
-    auto column = [&](int64_t t, int p) { return first + t * kManyTile + half * 64 + p * 32 + across * E; };
-    auto fetch = [&](int64_t t, int p) {
-        const int64_t col = column(t, p);
-        if (C && vec_d && col + E <= last)
+    uint4 in[2][4][kAccesses];                           // what is to be added, a piece ahead
 #pragma unroll
-            for (int i = 0; i < 32 / E; ++i)
-                if (there[i]) in[p][i] = *reinterpret_cast<const uint4*>(C + place_c[i] + col);
+    for (int p = 0; p < 2; ++p)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int k = 0; k < kAccesses; ++k) in[p][i][k] = make_uint4(0, 0, 0, 0);
+    auto column = [&](int64_t t, int p) { return column0(t) + half * 64 + p * 32 + q * 8; };
+    auto fetch = [&](int64_t t, int p) {
+        if (!C) return;
+        const int64_t col = column(t, p);
+        if (vec_d && col + 8 <= a.n) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (there[i])
+#pragma unroll
+                    for (int k = 0; k < kAccesses; ++k) in[p][i][k] = reinterpret_cast<const uint4*>(C + place_c[i] + col)[k];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (there[i]) {
+                    DT* to = reinterpret_cast<DT*>(in[p][i]);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (col + j < a.n) to[j] = C[place_c[i] + col + j];
+                }
+        }
     };
     fetch(0, 0);
     fetch(0, 1);
@@ -331,40 +374,25 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
         copies_commit();
         if (t == 0 || !ok) continue;
         tcgen05_fence_after();
+        if (t == 1)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) back[i] = backs[quarter * 32 + i * 8 + g];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
-            uint32_t v[32];
-            tmem_ld32(frame.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((t - 1) & 1) * kManyTile + half * 64 + p * 32, v);
+            uint32_t v[2][16];
+            const uint32_t at = frame.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((t - 1) & 1) * kManyTile + half * 64 + p * 32;
+            tmem_ld_16x32(at, v[0]);
+            tmem_ld_16x32(at + (16u << 16), v[1]);
             tmem_ld_wait();
-            __syncwarp();                                // the columns before have been read
-#pragma unroll
-            for (int q = 0; q < 8; ++q)
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(swizzled(turn, lane, q)), "r"(v[4 * q]), "r"(v[4 * q + 1]), "r"(v[4 * q + 2]), "r"(v[4 * q + 3]) : "memory");
-            __syncwarp();
             const int64_t col = column(t - 1, p);
-            const bool whole = vec_d && col + E <= last;
+            const bool whole = vec_d && col + 8 <= a.n;
 #pragma unroll
-            for (int i = 0; i < 32 / E; ++i) {
-                const int r = i * E + row_in;
-                float x[E];
+            for (int i = 0; i < 4; ++i) {
+                const DT* add = reinterpret_cast<const DT*>(in[p][i]);
+                float x[8];
 #pragma unroll
-                for (int q = 0; q < E / 4; ++q)
-                    asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(x[4 * q]), "=f"(x[4 * q + 1]), "=f"(x[4 * q + 2]), "=f"(x[4 * q + 3])
-                                 : "r"(swizzled(turn, r, across * (E / 4) + q)) : "memory");
-                if (!there[i]) continue;
-                const float back = backs[quarter * 32 + r];
-                if (whole) {
-                    const DT* add = reinterpret_cast<const DT*>(&in[p][i]);
-                    uint4 out;
-                    DT* o = reinterpret_cast<DT*>(&out);
-#pragma unroll
-                    for (int j = 0; j < E; ++j) o[j] = from_float<DT>(C ? to_float<DT>(add[j]) + x[j] * back : x[j] * back);
-                    *reinterpret_cast<uint4*>(D + place_d[i] + col) = out;
-                } else {
-#pragma unroll
-                    for (int j = 0; j < E; ++j)
-                        if (col + j < last) D[place_d[i] + col + j] = from_float<DT>(C ? to_float<DT>(C[place_c[i] + col + j]) + x[j] * back : x[j] * back);
-                }
+                for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]), back[i], to_float<DT>(add[j]));      // (the product is exact)
+                if (there[i]) store8_as<DT>(D + place_d[i] + col, x, whole, a.n - col);
             }
             if (t < tiles) fetch(t, p);
         }
@@ -391,14 +419,14 @@ cudaError_t launch_down(const AdapterArgs& a, const AdapterLayout& l, int splits
 
 template <typename T, typename DT, int KB>
 cudaError_t launch_up(const AdapterArgs& a, const AdapterLayout& l, int splits, int* status, cudaStream_t st) {
-    constexpr size_t smem = (size_t)4 * KB * kOperandBytes + kThreads / 32 * 4096 + 1024;
+    constexpr size_t smem = (size_t)4 * KB * kOperandBytes + 1024;
     cudaError_t err = set_smem(adapter_up_many_kernel<T, DT, KB>, smem);
     if (err != cudaSuccess) return err;
     const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * sizeof(DT))) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * sizeof(DT))) % 16 == 0);
-    // one round of blocks, in runs of whole pieces of 128 columns
-    const int64_t pieces = (a.n + kManyTile - 1) / kManyTile, slots = (KB == 1 ? 2 : 1) * kSms / l.max_tiles, runs = slots > 1 ? slots : 1;
-    const int64_t run = (pieces + runs - 1) / runs * kManyTile;
-    return launch_chained(adapter_up_many_kernel<T, DT, KB>, dim3((unsigned)l.max_tiles, (unsigned)((a.n + run - 1) / run)), dim3(kThreads), smem, st, a, l, splits, run,
+    // one round of blocks; those of a tile of tokens share its pieces of 128 columns evenly
+    const int64_t pieces = (a.n + kManyTile - 1) / kManyTile, slots = (KB == 1 ? 2 : 1) * kSms / l.max_tiles, most = slots > 1 ? slots : 1;
+    const int64_t per = (pieces + most - 1) / most, blocks = (pieces + per - 1) / per;
+    return launch_chained(adapter_up_many_kernel<T, DT, KB>, dim3((unsigned)l.max_tiles, (unsigned)blocks), dim3(kThreads), smem, st, a, l, splits,
                           alignment(a.B, a.ldb, a.stride_b), vec_d, make_idesc(a.type, kManyTile), status);
 }
 
