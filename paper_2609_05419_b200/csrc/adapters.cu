@@ -26,15 +26,16 @@ AdapterLayout layout_of(int64_t tokens, int rank, int adapters) {
     const bool few = tokens <= kFewTokens;
     const int64_t keys = adapters + 1, tile = few ? kFewTile : kManyTile;
     l.max_tiles = tokens / tile + (tokens < keys ? tokens : keys);
-    // blocks for two rounds (few tokens: small ones) or for the two that an SM holds
+    // few tokens: blocks for two rounds; many: the two that an SM holds, in clusters of up to 8
     const int64_t want = l.max_tiles == 0 ? 1 : few ? (2 * kSms + l.max_tiles - 1) / l.max_tiles : 2 * kSms / l.max_tiles, most = few ? 32 : 8;
     l.splits = (int)(want > most ? most : want < 1 ? 1 : want);
     l.padded = rank <= 16 ? 16 : rank <= 32 ? 32 : rank <= 64 ? 64 : 128;
     l.off_perm = 0;
     l.off_tiles = up(4 * tokens, 256);
     l.off_count = l.off_tiles + up((int64_t)sizeof(AdapterTile) * l.max_tiles, 256);
-    l.off_low = l.off_count + 256;
-    l.total = l.off_low + up(4 * l.splits * tokens * l.padded, 256);
+    l.off_back = l.off_count + 256;
+    l.off_low = l.off_back + up(4 * tokens, 256);
+    l.total = l.off_low + up((few ? 4 * (int64_t)l.splits : 4) * tokens * l.padded, 256);      // few: pieces of L in 32 bits; many: L as two 16-bit numbers
     return l;
 }
 
@@ -77,29 +78,33 @@ __global__ void __launch_bounds__(1024) adapter_tiles_kernel(const AdapterArgs a
     };
     each([&](int64_t t, int key) { take(t < a.tokens, key); });
     __syncthreads();
-    // exclusive sums over the keys of tokens and of tiles: a run of keys per thread
+    // exclusive sums over the keys of tokens and of tiles: a run of keys per thread, then over the lanes, then over the warps
     const int per = (keys + 1023) / 1024, k0 = min(keys, (int)threadIdx.x * per), k1 = min(keys, k0 + per);
     int2 mine = make_int2(0, 0);
     for (int k = k0; k < k1; ++k) mine.x += counts[k], mine.y += (counts[k] + kManyTile - 1) / kManyTile;
-    int2 sum = mine;
+    auto scan = [&](int2 v) {
 #pragma unroll
-    for (int d = 1; d < 32; d <<= 1) {
-        const int x = __shfl_up_sync(0xffffffffu, sum.x, d), y = __shfl_up_sync(0xffffffffu, sum.y, d);
-        if (lane >= d) sum.x += x, sum.y += y;
-    }
+        for (int d = 1; d < 32; d <<= 1) {
+            const int x = __shfl_up_sync(0xffffffffu, v.x, d), y = __shfl_up_sync(0xffffffffu, v.y, d);
+            if (lane >= d) v.x += x, v.y += y;
+        }
+        return v;
+    };
+    const int2 sum = scan(mine);
     if (lane == 31) warps[warp] = sum;
     __syncthreads();
+    const int2 over = scan(warps[lane]);
     int2 before = make_int2(sum.x - mine.x, sum.y - mine.y);
-    int total = 0;
-    for (int w = 0; w < 32; ++w) {
-        if (w < warp) before.x += warps[w].x, before.y += warps[w].y;
-        total += warps[w].y;
-    }
-    if (threadIdx.x == 0) *(int32_t*)(a.ws + l.off_count) = total;
+    const int bx = __shfl_sync(0xffffffffu, over.x, max(warp - 1, 0)), by = __shfl_sync(0xffffffffu, over.y, max(warp - 1, 0));
+    const int total = __shfl_sync(0xffffffffu, over.y, 31);
+    if (warp > 0) before.x += bx, before.y += by;
+    for (int64_t i = total + threadIdx.x; i < l.max_tiles; i += 1024) tiles[i] = {a.adapters, 0, 0, 0};
     for (int k = k0; k < k1; ++k) {
-        const int count = counts[k];
+        const int count = counts[k], rank = count ? rank_of(a, k) : 0;
         counts[k] = before.x;
-        for (int i = 0; i < count; i += kManyTile) tiles[before.y++] = {k, before.x + i, min(kManyTile, count - i), 0};
+        // the last key's tiles, of tokens without adapter, have nothing to do in place
+        if (k == a.adapters) *(int32_t*)(a.ws + l.off_count) = a.C == a.D ? before.y : total;
+        for (int i = 0; i < count; i += kManyTile) tiles[before.y++] = {k, before.x + i, min(kManyTile, count - i), rank};
         before.x += count;
     }
     __syncthreads();

@@ -7,10 +7,10 @@ namespace gemm2m {
 constexpr int kFewTokens = 256;           // up to here the first form, whose blocks find their tile themselves; beyond, a kernel sorts the tokens first
 constexpr int kFewTile = 16, kManyTile = 128;
 
-struct AdapterTile { int32_t key, start, count, pad; };      // key = adapter, or `adapters`: tokens without one; start: in the sorted list
+struct AdapterTile { int32_t key, start, count, rank; };     // key = adapter, or `adapters`: tokens without one; start: in the sorted list; rank in use
 struct AdapterLayout {
-    int64_t off_perm, off_tiles, off_count, off_low, total;  // bytes: sorted tokens, tiles, their number, pieces of L
-    int splits, padded;                   // pieces of L at the most, and entries of a token in one
+    int64_t off_perm, off_tiles, off_count, off_back, off_low, total;      // bytes: sorted tokens, tiles, how many have something to do, powers of two of the rows of L, L
+    int splits, padded;                   // pieces of k at the most, and entries of a token in L
     int64_t max_tiles;
 };
 cudaError_t launch_adapter_many(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st, int launches[2]);

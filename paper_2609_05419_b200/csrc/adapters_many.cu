@@ -1,12 +1,15 @@
 // Low-rank updates of many adapters, many tokens: tiles of 128 tokens of one adapter on the tensor cores (tcgen05, one CTA per tile).
 //
-// L = X A_a^T: a block takes a tile and a piece of k, in steps of 64 entries (one 128-byte swizzle row): four MMAs of 128 x rank x 16 per step.  The tile's rows of X lie
-// anywhere, so they come by asynchronous 16-byte copies (8- and 4-byte ones where rows start there), three or four steps ahead.
-// D = C + L B_a^T: a block takes a tile and pieces of 128 columns.  L, as hi + lo, stays in shared memory; the MMAs of one piece run while the one before is
+// L = X A_a^T: a cluster takes a tile, each of its blocks a piece of k, in steps of 64 entries (one 128-byte swizzle row): four MMAs of 128 x rank x 16 per step.  The tile's
+// rows of X lie anywhere, so they come by asynchronous 16-byte copies (8- and 4-byte ones where rows start there), three or four steps ahead.  The blocks then add their
+// pieces up through one another's shared memory, each for a part of the rows, in the order of k.
+// D = C + L B_a^T: all tiles' pieces of 128 columns are cut into even runs, one per block, which goes through the (at most few) tiles of its run.  L, as hi + lo, stays in shared memory; the MMAs of one piece run while the one before is
 // read back, added to what was fetched of C a piece earlier, and stored.  The read-back hands a lane pairs of columns 8 apart; the rows of B
 // lie in shared memory in such an order that these are eight neighbouring columns of D.
 #include "adapters.cuh"
 #include "gemm_ptx.cuh"
+
+#include <type_traits>
 
 namespace gemm2m {
 
@@ -128,20 +131,27 @@ struct Frame {
     }
 };
 
-// RP: padded rank, S: stages.
-template <int RP, int S>
-__global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const AdapterArgs a, const AdapterLayout l, int64_t per, int align, uint32_t idesc, int* dev_status) {
-    constexpr int kStageBytes = kOperandBytes + RP * kRowBytes, kTmemCols = RP < 32 ? 32 : RP;
+__device__ __forceinline__ float2 ld_cluster_f32x2(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+
+// T: type of X, A and of L's two parts; RP: padded rank, S: stages; ALIGN: bytes that rows are aligned to, 16 or 0: to be seen at run time.
+template <typename T, int RP, int S, int ALIGN>
+__global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int64_t per, int run_align, uint32_t idesc) {
+    constexpr int kStageBytes = kOperandBytes + RP * kRowBytes, kTmemCols = RP < 32 ? 32 : RP, kPitch = RP * 4 + 16;
+    static_assert(kManyTile * kPitch <= S * kStageBytes, "a piece of L takes the place of the stages");
     extern __shared__ unsigned char smem_raw[];
     __shared__ uint64_t bars[S + 2];
+    const int align = ALIGN ? ALIGN : run_align;
+    const int part = blockIdx.x % (unsigned)splits;          // (also the block's rank in its cluster)
     wait_for_prior_kernels();
-    if ((int)blockIdx.x >= *(const int32_t*)(a.ws + l.off_count)) return;
-    const AdapterTile tile = ((const AdapterTile*)(a.ws + l.off_tiles))[blockIdx.x];
+    const AdapterTile tile = ((const AdapterTile*)(a.ws + l.off_tiles))[blockIdx.x / (unsigned)splits];
+    if (tile.rank == 0) return;                              // no such tile, or nothing to multiply: the same in all of the cluster
     const int32_t* tokens = (const int32_t*)(a.ws + l.off_perm) + tile.start;
-    const int rank = rank_of(a, tile.key);
-    if (rank == 0) return;
     Frame<S> frame;
-    frame.open(bars, kTmemCols, dev_status);
+    frame.open(bars, kTmemCols, a.dev_status);
     const uint32_t base = (smem_u32(smem_raw) + 1023u) & ~1023u;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
 
@@ -151,251 +161,275 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
 #pragma unroll
     for (int j = 0; j < 4; ++j) x[j] = (const uint16_t*)a.X + (row0 + 32 * j < tile.count ? tokens[row0 + 32 * j] : 0) * a.ldx;
     const uint16_t* A = (const uint16_t*)a.A + tile.key * a.stride_a + row0 * a.lda;
-    const int64_t total = (a.k + 63) / 64, first = blockIdx.y * per;
+    const int64_t total = (a.k + 63) / 64, first = part * per;
     const int steps = (int)(min(total, first + per) - first);
-    auto load = [&](int step) {
-        const uint32_t stage = base + (uint32_t)(step % S) * kStageBytes;
+    auto load = [&](int step, int slot) {
+        const uint32_t stage = base + (uint32_t)slot * kStageBytes;
         const int64_t at = (first + step) * 64 + piece * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j)
             if (row0 + 32 * j < tile.count) copy8(swizzled(stage, row0 + 32 * j, piece), x[j], at, a.k, align);
 #pragma unroll
         for (int j = 0; j < (RP + 31) / 32; ++j)
-            if (row0 + 32 * j < rank) copy8(swizzled(stage + kOperandBytes, row0 + 32 * j, piece), A + 32 * j * a.lda, at, a.k, align);
+            if (row0 + 32 * j < tile.rank) copy8(swizzled(stage + kOperandBytes, row0 + 32 * j, piece), A + 32 * j * a.lda, at, a.k, align);
     };
 #pragma unroll
     for (int i = 0; i < S - 1; ++i) {
-        if (i < steps) load(i);
+        if (i < steps) load(i, i);
         copies_commit();
     }
+    int slot = 0, last_slot = S - 1;                         // of this step, and of the one before, which is filled next
+    uint32_t phase = 0, last_phase = 1;
     for (int i = 0; i < steps; ++i) {
         copies_wait<S - 2>();
         fence_async_proxy();
         // the stage that is filled next was read by the MMAs of the step before
-        if (warp == 0 && i > 0) frame.wait_warp((i - 1) % S, (uint32_t)((i - 1) / S) & 1u, kDevTimeoutProducer);
+        if (warp == 0 && i > 0) frame.wait_warp(last_slot, last_phase, kDevTimeoutProducer);
         __syncthreads();
         if (*frame.abort_flag) break;
         if (warp == 0) {
             tcgen05_fence_after();
-            const uint32_t stage = base + (uint32_t)(i % S) * kStageBytes;
+            const uint32_t stage = base + (uint32_t)slot * kStageBytes;
             const uint64_t adesc = make_smem_desc(stage), bdesc = make_smem_desc(stage + kOperandBytes);
             if (elect_lane()) {
 #pragma unroll
                 for (int s = 0; s < 4; ++s) umma_f16(frame.tmem, adesc + (uint64_t)(s * 2), bdesc + (uint64_t)(s * 2), idesc, (uint32_t)((i | s) != 0));
-                umma_commit(frame.bars + 8 * (i % S));
+                umma_commit(frame.bars + 8 * (uint32_t)slot);
             }
             __syncwarp();
         }
-        if (i + S - 1 < steps) load(i + S - 1);
+        if (i + S - 1 < steps) load(i + S - 1, last_slot);
         copies_commit();
+        last_slot = slot;
+        last_phase = phase;
+        if (++slot == S) slot = 0, phase ^= 1u;
     }
     // (not the abort flag: a wait that is given up fails at once here too)
-    if (frame.wait_warp((steps - 1) % S, (uint32_t)((steps - 1) / S) & 1u, kDevTimeoutEpilogue)) {
+    if (frame.wait_warp(last_slot, last_phase, kDevTimeoutEpilogue)) {
         tcgen05_fence_after();
-        const int row = (warp & 3) * 32 + lane;
-        float* low = (float*)(a.ws + l.off_low) + (blockIdx.y * a.tokens + (row < tile.count ? tokens[row] : 0)) * RP;
+        // this block's piece of L takes the place of the stages
+        const uint32_t row = base + (uint32_t)((warp & 3) * 32 + lane) * kPitch;
         for (int c = (warp >> 2) * 16; c < RP; c += 32) {
             uint32_t v[16];
             tmem_ld16(frame.tmem + ((uint32_t)((warp & 3) * 32) << 16) + c, v);
             tmem_ld_wait();
-            if (row < tile.count)
 #pragma unroll
-                for (int j = 0; j < 16; j += 4) *reinterpret_cast<uint4*>(low + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            for (int j = 0; j < 16; j += 4)
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(row + (c + j) * 4), "r"(v[j]), "r"(v[j + 1]), "r"(v[j + 2]), "r"(v[j + 3]) : "memory");
         }
     }
     frame.close(kTmemCols);
+    cluster_sync_all();
+    // a warp per row: the pieces added up, times s_a, the largest entry brought near 1, as two 16-bit numbers
+    const float scale = a.scales ? a.scales[tile.key] : 1.f;
+    T* low = (T*)(a.ws + l.off_low) + (int64_t)tile.start * (2 * RP);
+    float* backs = (float*)(a.ws + l.off_back) + tile.start;
+    for (int r = part * (kThreads / 32) + warp; r < tile.count; r += splits * (kThreads / 32)) {
+        constexpr int kPairs = (RP + 63) / 64;
+        float2 v[kPairs];
+        float top = 0.f;
+#pragma unroll
+        for (int b = 0; b < kPairs; ++b) {
+            const int c = b * 64 + lane * 2;
+            float2 w[8];
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (p < splits && c < RP) w[p] = ld_cluster_f32x2(map_to_cta(base + (uint32_t)r * kPitch + c * 4, (uint32_t)p));
+            v[b] = make_float2(0.f, 0.f);
+#pragma unroll
+            for (int p = 0; p < 8; ++p)
+                if (p < splits && c < RP) v[b].x += w[p].x, v[b].y += w[p].y;
+            v[b] = make_float2(c < tile.rank ? v[b].x * scale : 0.f, c + 1 < tile.rank ? v[b].y * scale : 0.f);
+            top = fmaxf(top, fmaxf(fabsf(v[b].x), fabsf(v[b].y)));
+        }
+        float down, back;
+        row_power(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))), &down, &back);
+#pragma unroll
+        for (int b = 0; b < kPairs; ++b) {
+            const int c = b * 64 + lane * 2;
+            T hi[2], lo[2];
+            split2<T>(v[b].x * down, &hi[0], &lo[0]);
+            split2<T>(v[b].y * down, &hi[1], &lo[1]);
+            if (c < RP) {
+                *reinterpret_cast<uint32_t*>(low + r * (2 * RP) + c) = *reinterpret_cast<const uint32_t*>(hi);
+                *reinterpret_cast<uint32_t*>(low + r * (2 * RP) + RP + c) = *reinterpret_cast<const uint32_t*>(lo);
+            }
+        }
+        if (lane == 0) backs[r] = back;
+    }
+    cluster_sync_all();                                      // nobody's piece goes away while another block reads it
 }
 
-// T: type of B (and of L's two parts), DT: of C and D; KB blocks of 64 along the rank.
-template <typename T, typename DT, int KB>
-__global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int align, int vec_d, uint32_t idesc,
-                                                                                  int* dev_status) {
+// DT: type of C and D; KB: blocks of 64 along the rank.  (The operands' 16-bit type is the instruction descriptor's matter.)
+template <typename DT, int KB, int ALIGN>
+__global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_kernel(const AdapterArgs a, const AdapterLayout l, int run_align, int vec_d, uint32_t idesc) {
     constexpr int kTmemCols = 256, E = 16 / (int)sizeof(DT), kAccesses = 8 / E;      // eight columns of a row per lane, E in one access
     extern __shared__ unsigned char smem_raw[];
     __shared__ uint64_t bars[4];
-    __shared__ float backs[kManyTile];
+    const int align = ALIGN ? ALIGN : run_align;
     wait_for_prior_kernels();
-    if ((int)blockIdx.x >= *(const int32_t*)(a.ws + l.off_count)) return;
-    const AdapterTile tile = ((const AdapterTile*)(a.ws + l.off_tiles))[blockIdx.x];
-    const int32_t* tokens = (const int32_t*)(a.ws + l.off_perm) + tile.start;
-    const int rank = rank_of(a, tile.key);
+    const int64_t pieces = (a.n + kManyTile - 1) / kManyTile, all = *(const int32_t*)(a.ws + l.off_count) * pieces;
+    int64_t at = all * blockIdx.x / gridDim.x;
+    const int64_t end = all * (blockIdx.x + 1) / gridDim.x;
+    if (at == end) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const DT* C = (const DT*)a.C;
     DT* D = (DT*)a.D;
-    // pieces of 128 columns, dealt out in turn: the blocks of a tile of tokens read and write neighbouring columns at about the same time
-    const int64_t all = (a.n + kManyTile - 1) / kManyTile, tiles = (all - blockIdx.y + gridDim.y - 1) / gridDim.y;
-    auto column0 = [&](int64_t t) { return (t * gridDim.y + blockIdx.y) * kManyTile; };
-    if (rank == 0) {                                     // D = C, or zero
-        if (a.C == a.D) return;
-        for (int64_t t = 0; t < tiles; ++t)
-            for (int i = threadIdx.x; i < tile.count * (kManyTile / E); i += kThreads) {
-                const int64_t row = tokens[i / (kManyTile / E)], c = column0(t) + i % (kManyTile / E) * E;
-                if (vec_d && c + E <= a.n) {
-                    *reinterpret_cast<uint4*>(D + row * a.ldd + c) = C ? *reinterpret_cast<const uint4*>(C + row * a.ldc + c) : make_uint4(0, 0, 0, 0);
-                } else {
-                    for (int64_t j = c; j < min(a.n, c + E); ++j) D[row * a.ldd + j] = C ? C[row * a.ldc + j] : DT(0.f);
-                }
-            }
-        return;
-    }
     Frame<2> frame;
-    frame.open(bars, kTmemCols, dev_status);
+    frame.open(bars, kTmemCols, a.dev_status);
     const uint32_t low_hi = (smem_u32(smem_raw) + 1023u) & ~1023u, low_lo = low_hi + KB * kOperandBytes, b_base = low_lo + KB * kOperandBytes;
-
-    const uint16_t* B = (const uint16_t*)a.B + tile.key * a.stride_b;
-    const int ksteps = (rank + 15) / 16, pieces = 2 * ksteps;         // 16-byte pieces of a row of B that the MMAs read
-    auto load_b = [&](int64_t t) {
-        const uint32_t dst = b_base + (uint32_t)(t & 1) * (KB * kOperandBytes);
-        for (int i = threadIdx.x; i < kManyTile * 8 * KB; i += kThreads) {
-            const int piece = i % (8 * KB), c = i / (8 * KB);
-            const int64_t col = column0(t) + c;
-            const int row = (c & 96) | (c & 6) << 2 | (c & 24) >> 2 | (c & 1);      // columns 8q + 2j + e of every 32 are rows 8j + 2q + e
-            if (piece < pieces && col < a.n) copy8(swizzled(dst + (piece >> 3) * kOperandBytes, row, piece & 7), B + col * a.ldb, piece * 8, rank, align);
-        }
-    };
-    load_b(0);
-    copies_commit();
-    {
-        // L: a warp adds the pieces of 16 rows up, all their loads of a piece in flight together, times s_a, and brings each row's largest entry near 1
-        constexpr int kRows = kManyTile / (kThreads / 32);
-        const float scale = a.scales ? a.scales[tile.key] : 1.f;
-        const int token = lane < kRows && warp * kRows + lane < tile.count ? tokens[warp * kRows + lane] : 0;
-        const float* low = (const float*)(a.ws + l.off_low) + lane * 2;
-        const float* p[kRows];
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) p[i] = low + (int64_t)__shfl_sync(0xffffffffu, token, i) * l.padded;
-        float2 v[KB][kRows];
-#pragma unroll
-        for (int b = 0; b < KB; ++b) {
-#pragma unroll
-            for (int i = 0; i < kRows; ++i) v[b][i] = make_float2(0.f, 0.f);
-            if (b * 64 + lane * 2 < rank)
-                for (int s = 0; s < splits; ++s) {
-                    float2 w[kRows];
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) w[i] = *reinterpret_cast<const float2*>(p[i] + s * a.tokens * l.padded + b * 64);
-#pragma unroll
-                    for (int i = 0; i < kRows; ++i) v[b][i].x += w[i].x, v[b][i].y += w[i].y;
-                }
-        }
-#pragma unroll
-        for (int i = 0; i < kRows; ++i) {
-            const int r = warp * kRows + i;
-            float top = 0.f;
-#pragma unroll
-            for (int b = 0; b < KB; ++b) {
-                const int c = b * 64 + lane * 2;
-                v[b][i] = make_float2(c < rank ? v[b][i].x * scale : 0.f, c + 1 < rank ? v[b][i].y * scale : 0.f);
-                top = fmaxf(top, fmaxf(fabsf(v[b][i].x), fabsf(v[b][i].y)));
-            }
-            float down, back;
-            row_power(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))), &down, &back);
-#pragma unroll
-            for (int b = 0; b < KB; ++b) {
-                T hi[2], lo[2];
-                split2<T>(v[b][i].x * down, &hi[0], &lo[0]);
-                split2<T>(v[b][i].y * down, &hi[1], &lo[1]);
-                const uint32_t at = swizzled((uint32_t)(b * kOperandBytes), r, lane >> 2) + (lane & 3) * 4;
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(low_hi + at), "r"(*reinterpret_cast<const uint32_t*>(hi)) : "memory");
-                asm volatile("st.shared.u32 [%0], %1;" ::"r"(low_lo + at), "r"(*reinterpret_cast<const uint32_t*>(lo)) : "memory");
-            }
-            if (lane == 0) backs[r] = back;
-        }
-    }
-
-    // Read-back: this warp's 32 rows (two halves of 16) and 64 of a piece's 128 columns, 32 at a time.
+    // this thread copies piece `piece` (and `piece` + 8) of rows, or columns, c0, c0 + 32, ... of 128; columns 8q + 2j + e of every 32 are rows 8j + 2q + e of B's tile
+    const int piece = threadIdx.x & 7, c0 = threadIdx.x >> 3;
+    const uint32_t b_dst = swizzled(b_base, (c0 & 6) << 2 | (c0 & 24) >> 2 | (c0 & 1), piece);
     const int quarter = warp & 3, half = warp >> 2, g = lane >> 2, q = lane & 3;
-    int64_t place_c[4], place_d[4];                      // rows g, g + 8 of either half
-    float back[4];
-    bool there[4];
+
+    uint32_t it = 0;                                     // pieces so far: buffer it % 2, its use number it / 2
+    bool ok = true;
+    while (ok && at < end) {
+        const AdapterTile tile = ((const AdapterTile*)(a.ws + l.off_tiles))[at / pieces];
+        const int32_t* tokens = (const int32_t*)(a.ws + l.off_perm) + tile.start;
+        const int64_t piece0 = at % pieces;
+        const int here = (int)min(pieces - piece0, end - at);
+        at += here;
+        auto column0 = [&](int t) { return (piece0 + t) * kManyTile; };
+        if (tile.rank == 0) {                            // D = C, or zero
+            if (a.C == a.D) continue;
+            for (int t = 0; t < here; ++t)
+                for (int i = threadIdx.x; i < tile.count * (kManyTile / E); i += kThreads) {
+                    const int64_t row = tokens[i / (kManyTile / E)], c = column0(t) + i % (kManyTile / E) * E;
+                    if (vec_d && c + E <= a.n) {
+                        *reinterpret_cast<uint4*>(D + row * a.ldd + c) = C ? *reinterpret_cast<const uint4*>(C + row * a.ldc + c) : make_uint4(0, 0, 0, 0);
+                    } else {
+                        for (int64_t j = c; j < min(a.n, c + E); ++j) D[row * a.ldd + j] = C ? C[row * a.ldc + j] : DT(0.f);
+                    }
+                }
+            continue;
+        }
+        const int ksteps = (tile.rank + 15) / 16, width = 2 * ksteps;         // 16-byte pieces of a row that the MMAs read
+        const uint16_t* b_row = (const uint16_t*)a.B + tile.key * a.stride_b + c0 * a.ldb;
+        auto load_b = [&](int t) {
+            const uint32_t dst = b_dst + ((it + t) & 1) * (KB * kOperandBytes);
+            const int64_t col = column0(t);
+            const uint16_t* row = b_row + col * a.ldb;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = quarter * 32 + i * 8 + g;
-        there[i] = row < tile.count;
-        const int64_t t = there[i] ? tokens[row] : 0;
-        place_c[i] = t * a.ldc;
-        place_d[i] = t * a.ldd;
-    }
-    uint4 in[2][4][kAccesses];                           // what is to be added, a piece ahead
+            for (int k = 0; k < kManyTile / 32; ++k, row += 32 * a.ldb) {
+                if (col + c0 + 32 * k >= a.n) break;
 #pragma unroll
-    for (int p = 0; p < 2; ++p)
+                for (int b = 0; b < KB; ++b)
+                    if (b * 8 + piece < width) copy8(dst + b * kOperandBytes + k * 32 * kRowBytes, row, (b * 8 + piece) * 8, tile.rank, align);
+            }
+        };
+        // (the MMAs that read the last tile's L and B have been waited for by every thread, and all of them have passed its last barrier since)
+        load_b(0);
+        {
+            const uint16_t* low = (const uint16_t*)(a.ws + l.off_low) + (int64_t)tile.start * (2 * l.padded);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
+            for (int k = 0; k < kManyTile / 32; ++k) {
+                const int r = c0 + 32 * k;
+                if (r < tile.count)
 #pragma unroll
-            for (int k = 0; k < kAccesses; ++k) in[p][i][k] = make_uint4(0, 0, 0, 0);
-    auto column = [&](int64_t t, int p) { return column0(t) + half * 64 + p * 32 + q * 8; };
-    auto fetch = [&](int64_t t, int p) {
-        if (!C) return;
-        const int64_t col = column(t, p);
-        if (vec_d && col + 8 <= a.n) {
+                    for (int b = 0; b < KB; ++b)
+                        if (b * 8 + piece < width) {
+                            const uint32_t dst = swizzled(low_hi + b * kOperandBytes, r, piece);
+                            copy8(dst, low + r * (2 * l.padded), (b * 8 + piece) * 8, l.padded, 16);
+                            copy8(dst + KB * kOperandBytes, low + r * (2 * l.padded) + l.padded, (b * 8 + piece) * 8, l.padded, 16);
+                        }
+            }
+        }
+        copies_commit();
+
+        // Read-back: this warp's 32 rows (rows g, g + 8 of two halves of 16) and 64 of a piece's 128 columns, 32 at a time.
+        int64_t place_c[4], place_d[4];
+        float back[4];
+        bool there[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = quarter * 32 + i * 8 + g;
+            there[i] = row < tile.count;
+            const int64_t t = there[i] ? tokens[row] : 0;
+            back[i] = there[i] ? ((const float*)(a.ws + l.off_back))[tile.start + row] : 0.f;
+            place_c[i] = t * a.ldc;
+            place_d[i] = t * a.ldd;
+        }
+        uint4 in[2][4][kAccesses];                       // what is to be added, a piece ahead
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (there[i])
 #pragma unroll
-                    for (int k = 0; k < kAccesses; ++k) in[p][i][k] = reinterpret_cast<const uint4*>(C + place_c[i] + col)[k];
-        } else {
+                for (int k = 0; k < kAccesses; ++k) in[p][i][k] = make_uint4(0, 0, 0, 0);
+        auto column = [&](int t, int p) { return column0(t) + half * 64 + p * 32 + q * 8; };
+        auto fetch = [&](int t, int p) {
+            if (!C) return;
+            const int64_t col = column(t, p);
+            if (vec_d && col + 8 <= a.n) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (there[i]) {
+                for (int i = 0; i < 4; ++i)
+                    if (there[i])
+#pragma unroll
+                        for (int k = 0; k < kAccesses; ++k) in[p][i][k] = reinterpret_cast<const uint4*>(C + place_c[i] + col)[k];
+            } else {
+                // (no branches around the loads, each of which would be waited for at its branch's end: what lies beyond the row's end, or the tile's, reads something that exists)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
                     DT* to = reinterpret_cast<DT*>(in[p][i]);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (col + j < a.n) to[j] = C[place_c[i] + col + j];
+                    for (int j = 0; j < 8; ++j) to[j] = C[place_c[i] + min(col + j, a.n - 1)];
                 }
-        }
-    };
-    fetch(0, 0);
-    fetch(0, 1);
-    for (int64_t t = 0; t <= tiles; ++t) {
-        copies_wait<0>();
-        fence_async_proxy();
-        tcgen05_fence_before();
-        __syncthreads();                                 // B of this piece and L are there; the accumulator of the piece before the last has been read
-        if (*frame.abort_flag) break;
-        if (t < tiles && warp == 0) {
+            }
+        };
+        fetch(0, 0);
+        fetch(0, 1);
+        for (int t = 0; t <= here; ++t) {
+            copies_wait<0>();
+            fence_async_proxy();
+            tcgen05_fence_before();
+            __syncthreads();                             // B of this piece and L are there; the accumulator of the piece before the last has been read
+            if (*frame.abort_flag) { ok = false; break; }
+            const uint32_t buf = (it + t) & 1;
+            if (t < here && warp == 0) {
+                tcgen05_fence_after();
+                const uint32_t b = b_base + buf * (KB * kOperandBytes), d = frame.tmem + buf * kManyTile;
+                if (elect_lane()) {
+                    for (int s = 0; s < ksteps; ++s) {
+                        const uint32_t block = (uint32_t)(s >> 2) * kOperandBytes;
+                        const uint64_t in_row = (uint64_t)((s & 3) * 2);
+                        const uint64_t bdesc = make_smem_desc(b + block) + in_row;
+                        umma_f16(d, make_smem_desc(low_hi + block) + in_row, bdesc, idesc, (uint32_t)(s != 0));
+                        umma_f16(d, make_smem_desc(low_lo + block) + in_row, bdesc, idesc, 1u);
+                    }
+                    umma_commit(frame.bars + 8 * buf);
+                }
+                __syncwarp();
+            }
+            // (a wait that is given up, seconds after this barrier, is acted on by all threads behind the next one)
+            const bool done = t == 0 || frame.wait_warp((int)(buf ^ 1), ((it + t - 1) >> 1) & 1u, kDevTimeoutEpilogue);
+            // (every thread has seen the MMAs that read this buffer of B complete)
+            if (done && t + 1 < here) load_b(t + 1);
+            copies_commit();
+            if (t == 0 || !done) continue;
             tcgen05_fence_after();
-            const uint32_t b = b_base + (uint32_t)(t & 1) * (KB * kOperandBytes), d = frame.tmem + (uint32_t)(t & 1) * kManyTile;
-            if (elect_lane()) {
-                for (int s = 0; s < ksteps; ++s) {
-                    const uint32_t block = (uint32_t)(s >> 2) * kOperandBytes;
-                    const uint64_t in_row = (uint64_t)((s & 3) * 2);
-                    const uint64_t bdesc = make_smem_desc(b + block) + in_row;
-                    umma_f16(d, make_smem_desc(low_hi + block) + in_row, bdesc, idesc, (uint32_t)(s != 0));
-                    umma_f16(d, make_smem_desc(low_lo + block) + in_row, bdesc, idesc, 1u);
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                uint32_t v[2][16];
+                const uint32_t from = frame.tmem + ((uint32_t)(quarter * 32) << 16) + (buf ^ 1) * kManyTile + half * 64 + p * 32;
+                tmem_ld_16x32(from, v[0]);
+                tmem_ld_16x32(from + (16u << 16), v[1]);
+                tmem_ld_wait();
+                const int64_t col = column(t - 1, p);
+                const bool whole = vec_d && col + 8 <= a.n;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const DT* add = reinterpret_cast<const DT*>(in[p][i]);
+                    float x[8];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]), back[i], to_float<DT>(add[j]));      // (the product is exact)
+                    if (there[i]) store8_as<DT>(D + place_d[i] + col, x, whole, a.n - col);
                 }
-                umma_commit(frame.bars + 8 * (uint32_t)(t & 1));
+                if (t < here) fetch(t, p);
             }
-            __syncwarp();
         }
-        // (a wait that is given up, seconds after this barrier, is acted on by all threads behind the next one)
-        const bool ok = t == 0 || frame.wait_warp((int)((t - 1) & 1), (uint32_t)((t - 1) >> 1) & 1u, kDevTimeoutEpilogue);
-        // (every thread has seen the MMAs that read this buffer of B complete)
-        if (ok && t + 1 < tiles) load_b(t + 1);
-        copies_commit();
-        if (t == 0 || !ok) continue;
-        tcgen05_fence_after();
-        if (t == 1)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) back[i] = backs[quarter * 32 + i * 8 + g];
-#pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            uint32_t v[2][16];
-            const uint32_t at = frame.tmem + ((uint32_t)(quarter * 32) << 16) + (uint32_t)((t - 1) & 1) * kManyTile + half * 64 + p * 32;
-            tmem_ld_16x32(at, v[0]);
-            tmem_ld_16x32(at + (16u << 16), v[1]);
-            tmem_ld_wait();
-            const int64_t col = column(t - 1, p);
-            const bool whole = vec_d && col + 8 <= a.n;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const DT* add = reinterpret_cast<const DT*>(in[p][i]);
-                float x[8];
-#pragma unroll
-                for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]), back[i], to_float<DT>(add[j]));      // (the product is exact)
-                if (there[i]) store8_as<DT>(D + place_d[i] + col, x, whole, a.n - col);
-            }
-            if (t < tiles) fetch(t, p);
-        }
+        it += here;
     }
     frame.close(kTmemCols);
 }
@@ -409,51 +443,58 @@ int alignment(const void* p, int64_t ld, int64_t stride) {
     return all % 16 == 0 ? 16 : all % 8 == 0 ? 8 : all % 4 == 0 ? 4 : 2;
 }
 
-template <int RP, int S>
-cudaError_t launch_down(const AdapterArgs& a, const AdapterLayout& l, int splits, int64_t per, int align, int* status, cudaStream_t st) {
+template <typename T, int RP, int S, int ALIGN>
+cudaError_t launch_down_as(const AdapterArgs& a, const AdapterLayout& l, int splits, int64_t per, int align, cudaStream_t st) {
     constexpr size_t smem = (size_t)S * (kOperandBytes + RP * kRowBytes) + 1024;
-    cudaError_t err = set_smem(adapter_down_many_kernel<RP, S>, smem);
+    cudaError_t err = set_smem(adapter_down_many_kernel<T, RP, S, ALIGN>, smem);
     if (err != cudaSuccess) return err;
-    return launch_chained(adapter_down_many_kernel<RP, S>, dim3((unsigned)l.max_tiles, (unsigned)splits), dim3(kThreads), smem, st, a, l, per, align, make_idesc(a.type, RP), status);
+    return launch_chained_cluster(adapter_down_many_kernel<T, RP, S, ALIGN>, dim3((unsigned)(l.max_tiles * splits)), dim3(kThreads), smem, splits, st, a, l, splits, per, align,
+                                  make_idesc(a.type, RP));
 }
 
-template <typename T, typename DT, int KB>
-cudaError_t launch_up(const AdapterArgs& a, const AdapterLayout& l, int splits, int* status, cudaStream_t st) {
-    constexpr size_t smem = (size_t)4 * KB * kOperandBytes + 1024;
-    cudaError_t err = set_smem(adapter_up_many_kernel<T, DT, KB>, smem);
-    if (err != cudaSuccess) return err;
-    const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * sizeof(DT))) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * sizeof(DT))) % 16 == 0);
-    // one round of blocks; those of a tile of tokens share its pieces of 128 columns evenly
-    const int64_t pieces = (a.n + kManyTile - 1) / kManyTile, slots = (KB == 1 ? 2 : 1) * kSms / l.max_tiles, most = slots > 1 ? slots : 1;
-    const int64_t per = (pieces + most - 1) / most, blocks = (pieces + per - 1) / per;
-    return launch_chained(adapter_up_many_kernel<T, DT, KB>, dim3((unsigned)l.max_tiles, (unsigned)blocks), dim3(kThreads), smem, st, a, l, splits,
-                          alignment(a.B, a.ldb, a.stride_b), vec_d, make_idesc(a.type, kManyTile), status);
-}
-
-template <typename T, int KB>
-cudaError_t launch_up_typed(const AdapterArgs& a, const AdapterLayout& l, int splits, int* status, cudaStream_t st) {
-    if (a.d_type == kF32) return launch_up<T, float, KB>(a, l, splits, status, st);
-    if (a.d_type == kF16) return launch_up<T, __half, KB>(a, l, splits, status, st);
-    return launch_up<T, __nv_bfloat16, KB>(a, l, splits, status, st);
-}
-
-}  // namespace
-
-cudaError_t launch_adapter_many(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st, int launches[2]) {
-    int* status = a.dev_status;
+template <typename T>
+cudaError_t launch_down(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st) {
     const int64_t steps = (a.k + 63) / 64;
     int64_t per = (steps + l.splits - 1) / l.splits;
     if (per < 4) per = 4;                                // fewer do not fill the stages
     const int splits = (int)((steps + per - 1) / per);
     const int x_align = alignment(a.X, a.ldx, 0), a_align = alignment(a.A, a.lda, a.stride_a), align = x_align < a_align ? x_align : a_align;
-    cudaError_t err = l.padded == 16   ? launch_down<16, 5>(a, l, splits, per, align, status, st)
-                      : l.padded == 32 ? launch_down<32, 5>(a, l, splits, per, align, status, st)
-                      : l.padded == 64 ? launch_down<64, 4>(a, l, splits, per, align, status, st)
-                                       : launch_down<128, 3>(a, l, splits, per, align, status, st);
+    auto with = [&](auto rp, auto s) {
+        constexpr int RP = decltype(rp)::value, S = decltype(s)::value;
+        return align == 16 ? launch_down_as<T, RP, S, 16>(a, l, splits, per, align, st) : launch_down_as<T, RP, S, 0>(a, l, splits, per, align, st);
+    };
+    using std::integral_constant;
+    if (l.padded == 16) return with(integral_constant<int, 16>(), integral_constant<int, 5>());
+    if (l.padded == 32) return with(integral_constant<int, 32>(), integral_constant<int, 5>());
+    if (l.padded == 64) return with(integral_constant<int, 64>(), integral_constant<int, 4>());
+    return with(integral_constant<int, 128>(), integral_constant<int, 3>());
+}
+
+template <typename DT, int KB, int ALIGN>
+cudaError_t launch_up_as(const AdapterArgs& a, const AdapterLayout& l, int align, cudaStream_t st) {
+    constexpr size_t smem = (size_t)4 * KB * kOperandBytes + 1024;
+    cudaError_t err = set_smem(adapter_up_many_kernel<DT, KB, ALIGN>, smem);
+    if (err != cudaSuccess) return err;
+    const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * sizeof(DT))) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * sizeof(DT))) % 16 == 0);
+    // as many blocks as the GPU holds, or one for every piece that there can be
+    const int64_t pieces = l.max_tiles * ((a.n + kManyTile - 1) / kManyTile), slots = (KB == 1 ? 2 : 1) * kSms;
+    return launch_chained(adapter_up_many_kernel<DT, KB, ALIGN>, dim3((unsigned)(pieces < slots ? pieces : slots)), dim3(kThreads), smem, st, a, l, align, vec_d, make_idesc(a.type, kManyTile));
+}
+
+template <typename DT>
+cudaError_t launch_up(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st) {
+    const int align = alignment(a.B, a.ldb, a.stride_b);
+    if (l.padded <= 64) return align == 16 ? launch_up_as<DT, 1, 16>(a, l, align, st) : launch_up_as<DT, 1, 0>(a, l, align, st);
+    return align == 16 ? launch_up_as<DT, 2, 16>(a, l, align, st) : launch_up_as<DT, 2, 0>(a, l, align, st);
+}
+
+}  // namespace
+
+cudaError_t launch_adapter_many(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st, int launches[2]) {
+    cudaError_t err = a.type == kF16 ? launch_down<__half>(a, l, st) : launch_down<__nv_bfloat16>(a, l, st);
     if (err != cudaSuccess) return err;
     ++launches[0];
-    if (a.type == kF16) err = l.padded <= 64 ? launch_up_typed<__half, 1>(a, l, splits, status, st) : launch_up_typed<__half, 2>(a, l, splits, status, st);
-    else err = l.padded <= 64 ? launch_up_typed<__nv_bfloat16, 1>(a, l, splits, status, st) : launch_up_typed<__nv_bfloat16, 2>(a, l, splits, status, st);
+    err = a.d_type == kF32 ? launch_up<float>(a, l, st) : a.d_type == kF16 ? launch_up<__half>(a, l, st) : launch_up<__nv_bfloat16>(a, l, st);
     if (err == cudaSuccess) ++launches[1];
     return err;
 }

@@ -161,13 +161,27 @@ template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }
 template <> __device__ __forceinline__ __half from_float<__half>(float v) { return __float2half_rn(v); }
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float v) { return __float2bfloat16_rn(v); }
+// Two values rounded to a 16-bit type, the first in the low half (one instruction).
+template <typename T> __device__ __forceinline__ uint32_t pack_as(float a, float b);
+template <> __device__ __forceinline__ uint32_t pack_as<__half>(float a, float b) {
+    const __half2 h = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
+template <> __device__ __forceinline__ uint32_t pack_as<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 h = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&h);
+}
 // Eight values rounded to T; a whole aligned group, or the first `valid` entries one by one.
 template <typename T>
 __device__ __forceinline__ void store8_as(T* p, const float (&v)[8], bool whole, int64_t valid) {
     Raw8<T> r;
-    T* t = reinterpret_cast<T*>(&r);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) t[i] = from_float<T>(v[i]);
+    if constexpr (sizeof(T) == 2) {
+        r.w[0] = make_uint4(pack_as<T>(v[0], v[1]), pack_as<T>(v[2], v[3]), pack_as<T>(v[4], v[5]), pack_as<T>(v[6], v[7]));
+    } else {
+        r.w[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        r.w[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+    }
+    const T* t = reinterpret_cast<const T*>(&r);
     if (whole) {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) reinterpret_cast<uint4*>(p)[i] = r.w[i];
