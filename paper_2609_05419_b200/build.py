@@ -8,8 +8,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 SOURCES = ["api.cu", "tables.cu", "scan.cu", "residues.cu", "post.cu", "post_fp.cu", "post_herk.cu", "gemm_check.cu", "gemm_i8_2cta.cu", "static_scratch.cu",
-           "fp8_quantise.cu", "fp8_gemm.cu", "newton_schulz.cu", "rms_norm.cu", "clip_gradients.cu", "adapters.cu", "adapters_many.cu"]
-HEADERS = ["common.cuh", "layer_ops.cuh", "fp8_pack.cuh", "adapters.cuh", "pair_pipeline.cuh", "gemm_ptx.cuh", "prepost_common.cuh", "residues_common.cuh", "post_common.cuh", "post_mma.cuh", os.path.join("..", "..", "include", "gemm2m.h")]
+           "fp8_quantise.cu", "fp8_gemm.cu", "newton_schulz.cu", "rms_norm.cu", "rms_norm_turned.cu", "rms_norm_backward.cu", "clip_gradients.cu", "adapters.cu", "adapters_many.cu"]
+HEADERS = ["common.cuh", "layer_ops.cuh", "fp8_pack.cuh", "adapters.cuh", "rms_norm.cuh", "pair_pipeline.cuh", "gemm_ptx.cuh", "prepost_common.cuh", "residues_common.cuh", "post_common.cuh", "post_mma.cuh", os.path.join("..", "..", "include", "gemm2m.h")]
 LIB = os.path.join(HERE, "libgemm2m.so")
 
 

@@ -1,0 +1,177 @@
+// Gradients of the root-mean-square norm (rms_norm.cu): with n = H rstd and dN = dY W,
+// dX = rn(rstd (dN - n mean_j(dN n)) + dR), dW = (dW) + sum_i dY n.
+#include "rms_norm.cuh"
+
+namespace gemm2m {
+
+namespace {
+
+// Blocks of a kernel for so many threads that an SM is to hold.
+constexpr int backward_blocks(int threads) { return threads <= 320 ? 2 : 1; }
+
+// Groups of rows blockIdx, blockIdx + grid, ...; the sums of dW over them go to row blockIdx of `part`.
+template <typename T, int NV, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS, backward_blocks(THREADS)) rms_norm_backward_kernel(const RmsNormBackwardArgs a, int warps, float inv_cols, int w_vec) {
+    __shared__ float sums[2][THREADS / 32 * NV];
+    __shared__ __align__(16) float turns[VEC ? 1 : THREADS / 32][VEC ? 4 : kSegment];
+    extern __shared__ float columns[];                       // rows of a block beyond one: [rows - 1][cols], to add their sums up
+    const Position at(warps, a.cols);
+    const int lane = at.lane, row_in = at.row_in, warp_in_row = at.warp_in_row, rows_here = at.rows(), cols = at.cols, segments = at.segments;
+    float* turn = turns[VEC ? 0 : at.warp];
+    auto first_of = [&](int i) { return at.first(i); };
+    // Two places: weights, dY and n stay in registers; four: they are read from the first-level cache, and converted, a second time.  (Formed again for two places as
+    // well, with three blocks on an SM: 85 against 62 us, the registers do not suffice.)
+    constexpr bool kHold = NV == 2;
+    float acc[NV][8], w[kHold ? NV : 1][8];
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = 0.f;
+    wait_for_prior_kernels();
+    if constexpr (kHold) load_weights<NV>(a.W, a.w_type, w_vec, cols, first_of, w);
+    const int64_t stride = gridDim.x * (int64_t)rows_here;
+    float next_rstd = a.rstd[min(blockIdx.x * (int64_t)rows_here + row_in, a.rows - 1)];
+    int turn_of = 0;
+    for (int64_t first = blockIdx.x * (int64_t)rows_here; first < a.rows; first += stride, turn_of ^= 1) {
+        const bool write = first + row_in < a.rows;          // a row beyond the last does the last one's work again, for nothing
+        const int64_t row = min(first + row_in, a.rows - 1);
+        const float rstd = next_rstd;
+        next_rstd = a.rstd[min(row + stride, a.rows - 1)];
+        Place<T, VEC> g[NV], h[NV], r[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) g[i].load((const T*)a.dY + row * a.lddy, first_of(i), cols);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) h[i].load((const T*)a.H + row * a.ldh, first_of(i), cols);
+        if (a.dR)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) r[i].load((const T*)a.dR + row * a.lddr, first_of(i), cols);
+        float sum[NV], n[kHold ? NV : 1][8], dy[kHold ? NV : 1][8];
+        auto numbers = [&](int i) {
+            constexpr int kNone = kHold ? 0 : 1;
+            const int at_i = kNone ? 0 : i;
+            if constexpr (!kHold) load_weights<1>(a.W, a.w_type, w_vec, cols, [&](int) { return first_of(i); }, w);
+            g[i].get(dy[at_i], turn);
+            h[i].get(n[at_i], turn);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) n[at_i][j] *= rstd;
+        };
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at_i = kHold ? i : 0;
+            numbers(i);
+            float s = 0.f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float t = dy[at_i][j] * n[at_i][j];
+                acc[i][j] += write ? t : 0.f;
+                s += t * w[at_i][j];
+            }
+            sum[i] = at.there(i) ? s : 0.f;
+        }
+        // (two tables in turn: a warp may be a row ahead of one that still reads)
+        const float mean = row_sum<NV>(sum, sums[turn_of] + row_in * warps * NV, warp_in_row, warps, segments) * inv_cols;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int at_i = kHold ? i : 0;
+            float t[8], out[8];
+            if (!kHold) numbers(i);
+            if (a.dR) r[i].get(t, turn);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                out[j] = rstd * (dy[at_i][j] * w[at_i][j] - n[at_i][j] * mean);
+                if (a.dR) out[j] += t[j];
+            }
+            store_place<T, VEC>((T*)a.dX + row * a.lddx, first_of(i), cols, write, out, turn);
+        }
+    }
+    if (!a.dW) return;
+    // the rows of a block first, in their order
+    if (row_in > 0)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (first_of(i) + lane * 8 + j < cols) columns[(row_in - 1) * cols + first_of(i) + lane * 8 + j] = acc[i][j];
+    __syncthreads();
+    if (row_in > 0) return;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int col = first_of(i) + lane * 8 + j;
+            if (col >= cols) continue;
+            float v = acc[i][j];
+            for (int k = 1; k < rows_here; ++k) v += columns[(k - 1) * cols + col];
+            a.part[blockIdx.x * a.cols + col] = v;
+        }
+}
+
+// dW = (dW) + the sum of the `parts` rows of partial sums: 32 columns per block, 32 threads deep, in a fixed order.
+__global__ void __launch_bounds__(1024) rms_norm_dw_kernel(const float* __restrict__ part, int64_t parts, int64_t cols, float* dW, int add) {
+    __shared__ float sums[32][33];
+    const int64_t col = blockIdx.x * 32LL + threadIdx.x;
+    wait_for_prior_kernels();
+    float s = 0.f;
+    if (col < cols)
+        for (int64_t p = threadIdx.y; p < parts; p += 32) s += part[p * cols + col];
+    sums[threadIdx.y][threadIdx.x] = s;
+    __syncthreads();
+    float t = sums[threadIdx.x][threadIdx.y];
+#pragma unroll
+    for (int d = 16; d; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+    const int64_t out = blockIdx.x * 32LL + threadIdx.y;
+    if (threadIdx.x == 0 && out < cols) dW[out] = add ? dW[out] + t : t;
+}
+
+// Two segments per warp up to 8192 columns, four beyond.
+struct BackwardShape { int places, warps, threads, here, bound; int64_t blocks; };
+BackwardShape backward_shape(int64_t rows, int64_t cols) {
+    BackwardShape s;
+    s.places = cols <= 32 * kSegment ? 2 : 4;
+    s.warps = row_warps(cols, s.places);
+    s.threads = block_threads(s.warps);
+    s.here = s.threads / (32 * s.warps);
+    s.bound = s.places == 2 ? (s.threads <= 256 ? 256 : s.threads <= 320 ? 320 : 512) : s.threads <= 512 ? 512 : 1024;
+    const int64_t need = (rows + s.here - 1) / s.here, most = backward_blocks(s.bound) * (int64_t)kSms;
+    s.blocks = need < most ? need : most;
+    return s;
+}
+
+template <typename T, int NV, bool VEC, int THREADS>
+cudaError_t launch_rows(const RmsNormBackwardArgs& a, const BackwardShape& s, int w_vec, cudaStream_t st) {
+    const size_t smem = a.dW ? (size_t)(s.here - 1) * a.cols * 4 : 0;      // (at most 7 x 512 columns)
+    return launch_chained(rms_norm_backward_kernel<T, NV, VEC, THREADS>, dim3((unsigned)s.blocks), dim3(s.threads), smem, st, a, s.warps, 1.f / (float)a.cols, w_vec);
+}
+
+template <typename T, bool VEC>
+cudaError_t launch_shape(const RmsNormBackwardArgs& a, const BackwardShape& s, int w_vec, cudaStream_t st) {
+    if (s.places == 4) return s.bound == 512 ? launch_rows<T, 4, VEC, 512>(a, s, w_vec, st) : launch_rows<T, 4, VEC, 1024>(a, s, w_vec, st);
+    if (s.bound == 256) return launch_rows<T, 2, VEC, 256>(a, s, w_vec, st);
+    return s.bound == 320 ? launch_rows<T, 2, VEC, 320>(a, s, w_vec, st) : launch_rows<T, 2, VEC, 512>(a, s, w_vec, st);
+}
+
+template <typename T>
+cudaError_t launch_typed(const RmsNormBackwardArgs& a, cudaStream_t st, int* launches) {
+    const BackwardShape s = backward_shape(a.rows, a.cols);
+    const bool vec = aligned8<T>(a.dY, a.lddy) && aligned8<T>(a.H, a.ldh) && aligned8<T>(a.dX, a.lddx) && (!a.dR || aligned8<T>(a.dR, a.lddr)) && a.cols * sizeof(T) % 16 == 0;
+    const int w_vec = ((uintptr_t)a.W & 15) == 0 && a.cols % 8 == 0;
+    cudaError_t err = vec ? launch_shape<T, true>(a, s, w_vec, st) : launch_shape<T, false>(a, s, w_vec, st);
+    if (err != cudaSuccess) return err;
+    ++*launches;
+    if (!a.dW) return cudaSuccess;
+    err = launch_chained(rms_norm_dw_kernel, dim3((unsigned)((a.cols + 31) / 32)), dim3(32, 32), 0, st, (const float*)a.part, a.parts, a.cols, a.dW, a.add);
+    if (err == cudaSuccess) ++*launches;
+    return err;
+}
+
+}  // namespace
+
+int64_t rms_norm_backward_parts(int64_t rows, int64_t cols) { return backward_shape(rows, cols).blocks; }
+
+cudaError_t launch_rms_norm_backward(const RmsNormBackwardArgs& a, cudaStream_t st, int* launches) {
+    if (a.type == kF32) return launch_typed<float>(a, st, launches);
+    if (a.type == kF16) return launch_typed<__half>(a, st, launches);
+    return launch_typed<__nv_bfloat16>(a, st, launches);
+}
+
+}  // namespace gemm2m
