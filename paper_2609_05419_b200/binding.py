@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+from array import array as _array
 
 OP_GAUSSIAN_INT, OP_ZGEMM, OP_CGEMM, OP_ZHERK, OP_ZHER2K, OP_DSYRK, OP_DSYR2K, OP_DGEMM_OZAKI2 = 0, 1, 2, 3, 4, 5, 6, 7
 OP_ZGEMM_EISENSTEIN = 8
@@ -496,21 +497,26 @@ def newton_schulz(G, O, steps=5, coeffs=None, eps=1e-7, stream=None):
                                       _stream_of(stream, device)), "gemm2m_newton_schulz")
 
 
-def _like(t, name, shape, kind, device):
-    """(pointer, leading dimension) of a matrix that has to have this shape and type, (None, 0) for None."""
+def _like(t, name, like, shape, device):
+    """(pointer, leading dimension) of a matrix that has to have this shape and the type of `like`, (None, 0) for None."""
     if t is None:
         return None, 0
-    p, code, rows, cols, ld = _rowmajor(t, name, _FLOATS, device)
-    if (rows, cols) != shape or code != kind:
-        raise ValueError(f"{name}: shape or type mismatch")
-    return p, ld
+    if t.shape != shape or t.dtype is not like.dtype or t.get_device() != device:
+        raise ValueError(f"{name}: need a CUDA tensor of shape {tuple(shape)} and type {like.dtype} on the current device")
+    ld, step = t.stride()
+    rows, cols = shape
+    if step != 1 and cols > 1:
+        raise ValueError(f"{name}: need row-major storage (stride 1 along dim 1)")
+    if rows <= 1 or cols == 0:
+        ld = (max(cols, 1) + 15) // 16 * 16
+    return t.data_ptr(), ld
 
 
 def _vector(t, name, size, allowed, device):
     """(pointer, type code) of a contiguous vector, (None, F32) for None."""
     if t is None:
         return None, F32
-    if t.dim() != 1 or t.shape[0] != size or t.get_device() != device or (size > 1 and t.stride(0) != 1):
+    if t.shape != (size,) or t.get_device() != device or not t.is_contiguous():
         raise ValueError(f"{name}: need a contiguous CUDA tensor of {size} entries on the current device")
     return t.data_ptr(), _type_of(t, name, allowed)
 
@@ -532,10 +538,10 @@ def rms_norm(X, W=None, R=None, H=None, Y=None, Q=None, S=None, Qt=None, St=None
     transposed Qt with St (both as fp8_empty lays them out), rstd (float32, one per row)."""
     device = _launch_device(X, "X")
     px, tx, rows, cols, ldx = _rowmajor(X, "X", _FLOATS, device)
-    shape = (rows, cols)
-    pr, ldr = _like(R, "R", shape, tx, device)
-    ph, ldh = _like(H, "H", shape, tx, device)
-    py, ldy = _like(Y, "Y", shape, tx, device)
+    shape = X.shape
+    pr, ldr = _like(R, "R", X, shape, device)
+    ph, ldh = _like(H, "H", X, shape, device)
+    py, ldy = _like(Y, "Y", X, shape, device)
     pw, tw = _vector(W, "W", cols, _FLOATS, device)
     fmt, form = _fp8_form(Q, S, "Q, S", rows, cols, device)
     fmt_t, form_t = _fp8_form(Qt, St, "Qt, St", cols, rows, device)
@@ -551,40 +557,44 @@ def rms_norm_backward(dY, H, W, rstd, dX, dR=None, dW=None, add=False, stream=No
     H and rstd as rms_norm left them; W None: ones."""
     device = _launch_device(dY, "dY")
     pg, tg, rows, cols, ldg = _rowmajor(dY, "dY", _FLOATS, device)
-    shape = (rows, cols)
+    shape = dY.shape
     if H is None or dX is None or rstd is None:
         raise ValueError("need H, rstd and dX")
-    ph, ldh = _like(H, "H", shape, tg, device)
-    px, ldx = _like(dX, "dX", shape, tg, device)
-    pr, ldr = _like(dR, "dR", shape, tg, device)
+    ph, ldh = _like(H, "H", dY, shape, device)
+    px, ldx = _like(dX, "dX", dY, shape, device)
+    pr, ldr = _like(dR, "dR", dY, shape, device)
     pw, tw = _vector(W, "W", cols, _FLOATS, device)
     _check(lib().gemm2m_rms_norm_backward(rows, cols, pg, tg, ldg, ph, ldh, pw, tw, _vector(rstd, "rstd", rows, (F32,), device)[0], pr, ldr, px, ldx,
                                           _vector(dW, "dW", cols, (F32,), device)[0], 1 if add else 0, _stream_of(stream, device)), "gemm2m_rms_norm_backward")
 
 
-def _rows_of(t, name, device):
-    """(pointer, type code, rows, columns, leading dimension) of a float tensor of any shape: dense in any order of its axes, or 2-D with rows apart."""
-    if t.get_device() != device:
-        raise ValueError(f"{name}: need CUDA tensors on the current device")
-    code = _type_of(t, name, _FLOATS)
+def _rows_of(t, name):
+    """(rows, columns, leading dimension) of a tensor of any shape: dense in any order of its axes, or 2-D with rows apart."""
     if t.is_contiguous():
         size = t.numel()
-        return t.data_ptr(), code, 1, size, size
+        return 1, size, size
     shape, strides = t.shape, t.stride()
     if len(shape) == 2 and strides[1] == 1 and strides[0] >= shape[1]:
-        return t.data_ptr(), code, shape[0], shape[1], strides[0]
+        return shape[0], shape[1], strides[0]
     dense = 1
     for stride, size in sorted(zip(strides, shape)):
         if size > 1:
             if stride != dense:
                 raise ValueError(f"{name}: need tensors that are dense, or 2-D with contiguous rows")
             dense *= size
-    return t.data_ptr(), code, 1, dense, dense
+    return 1, dense, dense
+
+
+def _dtypes_of(tensors, name, device):
+    if any([t.get_device() != device for t in tensors]):
+        raise ValueError(f"{name}: need CUDA tensors on the current device")
+    return [t.dtype for t in tensors]
 
 
 def clip_gradients(grads, max_norm, out=None, norm=None, eps=1e-6, stream=None):
     """Common 2-norm of a list of tensors (float32 / float16 / bfloat16) into `norm` (float32, one entry), and the tensors times
-    min(1, max_norm / (norm + eps)), in place or into the list `out`.  max_norm = inf: the norm alone, unless there is an `out`."""
+    min(1, max_norm / (norm + eps)), in place or into the list `out` (of the same types, shapes and orders of axes, or contiguous both and as many entries).
+    max_norm = inf: the norm alone, unless there is an `out`."""
     grads = list(grads)
     count = len(grads)
     device = _current_device()
@@ -592,36 +602,57 @@ def clip_gradients(grads, max_norm, out=None, norm=None, eps=1e-6, stream=None):
         if norm.numel() != 1 or norm.get_device() != device:
             raise ValueError("norm: need a CUDA tensor of one entry on the current device")
         _type_of(norm, "norm", (F32,))
-    rows = [_rows_of(t, "grads", device) for t in grads]
-    array = lambda kind, values: (kind * max(count, 1))(*values)
-    i64 = ctypes.c_int64
-    p_out = ld_out = None
+    dtypes = _dtypes_of(grads, "grads", device)
+    if count:
+        _type_of(grads[0], "grads", _FLOATS)        # (fills the table of codes)
+    types = [_type_codes.get(d, -1) for d in dtypes]
+    if count and (min(types) < F32 or max(types) > BF16):
+        raise ValueError("grads: unsupported type")
+    contiguous = all([t.is_contiguous() for t in grads])
     if out is not None:
         out = list(out)
-        if len(out) != count:
-            raise ValueError("out: need as many tensors as grads")
-        outs = [_rows_of(t, "out", device) for t in out]
-        for i, (g, o) in enumerate(zip(grads, out)):
-            if g.shape != o.shape or rows[i][1] != outs[i][1]:
-                raise ValueError("out: shape or type mismatch")
-            if rows[i][2:] != outs[i][2:] or any(size > 1 and a != c for size, a, c in zip(g.shape, g.stride(), o.stride())):
+        if _dtypes_of(out, "out", device) != dtypes:
+            raise ValueError("out: need as many tensors as grads, of their types")
+        contiguous = contiguous and all([t.is_contiguous() for t in out])
+    # host arrays for the library: 64-bit numbers, one array for each argument
+    array = lambda values: _array("q", values)
+    address = lambda a: a.buffer_info()[0]
+    if contiguous:
+        rows, cols = array([1]) * count, array([t.numel() for t in grads])
+        if out is not None and array([t.numel() for t in out]) != cols:
+            raise ValueError("out: need the shapes of grads")
+        lds = ld_out = cols
+    else:
+        walks, walks_out = [], []
+        for g, o in zip(grads, grads if out is None else out):
+            if g.shape != o.shape:
+                raise ValueError("out: need the shapes of grads")
+            walk, walk_out = _rows_of(g, "grads"), _rows_of(o, "out")
+            if walk != walk_out or any(size > 1 and a != c for size, a, c in zip(g.shape, g.stride(), o.stride())):
                 # the same order of entries, with rows of their own distance
                 if g.dim() != 2 or any(t.shape[1] > 1 and t.stride(1) != 1 for t in (g, o)):
                     raise ValueError("out: need the order of the gradient's axes in memory")
                 m, n = g.shape
-                rows[i], outs[i] = ((*r[:2], m, n, t.stride(0) if m > 1 else n) for r, t in ((rows[i], g), (outs[i], o)))
-        p_out, ld_out = array(ctypes.c_void_p, [r[0] for r in outs]), array(i64, [r[4] for r in outs])
-    _check(lib().gemm2m_clip_gradients(count, array(ctypes.c_void_p, [r[0] for r in rows]), p_out, array(ctypes.c_int, [r[1] for r in rows]),
-                                       *(array(i64, [r[k] for r in rows]) for k in (2, 3, 4)), ld_out, max_norm, eps,
-                                       None if norm is None else norm.data_ptr(), _stream_of(stream, device)), "gemm2m_clip_gradients")
+                walk, walk_out = ((m, n, t.stride(0) if m > 1 else n) for t in (g, o))
+            walks.append(walk)
+            walks_out.append(walk_out)
+        rows, cols, lds = (array([w[k] for w in walks]) for k in range(3))
+        ld_out = array([w[2] for w in walks_out])
+    types = _array("i", types)
+    pointers = array([t.data_ptr() for t in grads])
+    p_out = None if out is None else array([t.data_ptr() for t in out])
+    _check(lib().gemm2m_clip_gradients(count, address(pointers), p_out and address(p_out), address(types), address(rows), address(cols), address(lds),
+                                       None if out is None else address(ld_out), max_norm, eps, None if norm is None else norm.data_ptr(), _stream_of(stream, device)),
+           "gemm2m_clip_gradients")
 
 
 def _stack(t, name, kind, device):
     """(pointer, matrices, rows, cols, leading dimension, stride) of a 3-D CUDA tensor of row-major matrices."""
-    if t.dim() != 3 or t.get_device() != device:
+    shape = t.shape
+    if len(shape) != 3 or t.get_device() != device:
         raise ValueError(f"{name}: need a 3-D CUDA tensor on the current device")
     _type_of(t, name, (kind,))
-    many, rows, cols = t.shape
+    many, rows, cols = shape
     stride, ld, step = t.stride()
     if cols > 1 and step != 1:
         raise ValueError(f"{name}: need row-major storage (stride 1 along the last dim)")
@@ -642,13 +673,13 @@ def adapter_add(X, A, B, index, D, C=None, scales=None, ranks=None, stream=None)
     pd, td, md, nd, ldd = _rowmajor(D, "D", _FLOATS, device)
     if k2 != k or many2 != many or rank2 != rank or (md, nd) != (tokens, n):
         raise ValueError("shape mismatch")
-    pc, ldc = _like(C, "C", (tokens, n), td, device)
+    pc, ldc = _like(C, "C", D, D.shape, device)
     pointers = []
     for t, name, size in ((index, "index", tokens), (ranks, "ranks", many)):
         if t is None and name == "ranks":
             pointers.append(None)
             continue
-        if t.dim() != 1 or t.shape[0] != size or t.dtype != torch.int32 or t.get_device() != device or (size > 1 and t.stride(0) != 1):
+        if t.shape != (size,) or t.dtype is not torch.int32 or t.get_device() != device or not t.is_contiguous():
             raise ValueError(f"{name}: need a contiguous int32 CUDA tensor of {size} entries on the current device")
         pointers.append(t.data_ptr())
     _check(lib().gemm2m_adapter_add(tokens, n, k, many, rank, px, tx, ldx, pa, lda, stride_a, pb, ldb, stride_b, pointers[0],

@@ -3,7 +3,7 @@
 // norm = sqrt(sum over all tensors and entries of g^2); factor = 1 where max_norm >= norm + eps, else max_norm / (norm + eps) (NaN for a NaN norm),
 // formed in 64 bits and rounded to 32; o = rn(g factor).
 //
-// Tensors are cut into chunks of 8192 entries, dealt out in turn to the blocks of one launch for up to 512 tensors, which it gets as a kernel parameter
+// Tensors are cut into chunks of 32 KB, dealt out in turn to the blocks of one launch for up to 512 tensors, which it gets as a kernel parameter
 // (nothing to copy first; captured by value).  First launch: every thread sums squares of 8 entries in 32 bits and these sums in 64 bits, every block
 // leaves one number.  Second launch: every block adds those up, in the same order, and scales its chunks, last chunk first: those are still
 // in the on-chip cache where all of them do not fit.
@@ -13,7 +13,7 @@ namespace gemm2m {
 
 namespace {
 
-constexpr int kChunk = 8192, kClipThreads = 256, kBlocks = 4 * kSms, kFew = 64, kMany = 512;
+constexpr int kChunkBytes = 32768, kClipThreads = 256, kBlocks = 4 * kSms, kFew = 64, kMany = 512;
 
 struct Entry {
     const void* g; void* o;
@@ -56,26 +56,27 @@ __device__ __forceinline__ double block_sum(double v, double* warps) {
 
 // The entry that chunk c belongs to.
 template <int N>
-__device__ __forceinline__ const Entry& entry_of(const Table<N>& t, uint32_t c) {
+__device__ __forceinline__ int entry_of(const Table<N>& t, uint32_t c) {
     int lo = 0, hi = t.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
         if (t.t[mid].first <= c) lo = mid;
         else hi = mid;
     }
-    return t.t[lo];
+    return lo;
 }
 
-// The four groups of eight entries of a chunk that a thread deals with.
-template <typename T, typename F>
-__device__ __forceinline__ void for_chunk(const Entry& e, uint32_t c, F&& f) {
+// The groups of eight entries of a chunk that a thread deals with.  `meanwhile` runs when the loads are on their way.
+template <typename T, typename M, typename F>
+__device__ __forceinline__ void for_chunk(const Entry& e, uint32_t c, M&& meanwhile, F&& f) {
+    constexpr int kChunk = kChunkBytes / (int)sizeof(T), kGroups = kChunk / (8 * kClipThreads);
     const int64_t base = (int64_t)(c - e.first) * kChunk;
     const T* g = (const T*)e.g;
-    constexpr int kGroups = kChunk / (8 * kClipThreads);
     if (e.vec && base + kChunk <= e.size) {
         Raw8<T> raw[kGroups];
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) raw[k] = load8_rw<T>(g + place(e, base + (k * kClipThreads + threadIdx.x) * 8, e.ldg));
+        meanwhile();
 #pragma unroll
         for (int k = 0; k < kGroups; ++k) {
             float v[8];
@@ -84,30 +85,34 @@ __device__ __forceinline__ void for_chunk(const Entry& e, uint32_t c, F&& f) {
         }
         return;
     }
-    // neighbouring threads take neighbouring entries
-#pragma unroll 1
+    meanwhile();
+    // neighbouring threads take neighbouring entries; (no branches around the loads: beyond the end they read the last entry)
+#pragma unroll 2
     for (int k = 0; k < kGroups; ++k) {
+        if (base + k * 8 * kClipThreads >= e.size) break;
         float v[8];
+        T t[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int64_t i = base + (k * 8 + j) * kClipThreads + threadIdx.x;
-            v[j] = i < e.size ? to_float<T>(g[place(e, i, e.ldg)]) : 0.f;
-        }
+        for (int j = 0; j < 8; ++j) t[j] = g[place(e, min(base + (k * 8 + j) * kClipThreads + threadIdx.x, e.size - 1), e.ldg)];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = base + (k * 8 + j) * kClipThreads + threadIdx.x < e.size ? to_float<T>(t[j]) : 0.f;
         f(v, base + k * 8 * kClipThreads + threadIdx.x, 0);
     }
 }
 
 template <int N>
-__global__ void __launch_bounds__(kClipThreads) squares_kernel(const __grid_constant__ Table<N> t, double* partials) {
+__global__ void __launch_bounds__(kClipThreads, 4) squares_kernel(const __grid_constant__ Table<N> t, double* partials) {
     __shared__ double warps[kClipThreads / 32];
     wait_for_prior_kernels();
     double sum = 0.0;
     auto add = [&](const float (&v)[8], int64_t, int) { sum += squares8(v); };
+    int at = entry_of(t, blockIdx.x);
     for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-        const Entry& e = entry_of(t, c);
-        if (e.type == kF32) for_chunk<float>(e, c, add);
-        else if (e.type == kF16) for_chunk<__half>(e, c, add);
-        else for_chunk<__nv_bfloat16>(e, c, add);
+        const Entry& e = t.t[at];
+        auto meanwhile = [&] { at = entry_of(t, c + gridDim.x); };
+        if (e.type == kF32) for_chunk<float>(e, c, meanwhile, add);
+        else if (e.type == kF16) for_chunk<__half>(e, c, meanwhile, add);
+        else for_chunk<__nv_bfloat16>(e, c, meanwhile, add);
     }
     sum = block_sum(sum, warps);
     if (threadIdx.x == 0) partials[blockIdx.x] = sum;
@@ -130,8 +135,9 @@ __global__ void __launch_bounds__(kClipThreads) fold_kernel(const double* partia
 }
 
 template <int N>
-__global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_constant__ Table<N> t, const double* partials, int64_t count, float max_norm, float eps, float* norm) {
+__global__ void __launch_bounds__(kClipThreads, 4) scale_kernel(const __grid_constant__ Table<N> t, const double* partials, int64_t count, float max_norm, float eps, float* norm) {
     __shared__ double warps[kClipThreads / 32];
+    int at = entry_of(t, t.chunks - 1 - blockIdx.x);
     wait_for_prior_kernels();
     const double size = sqrt(total_of(partials, count, warps));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)size;
@@ -139,20 +145,24 @@ __global__ void __launch_bounds__(kClipThreads) scale_kernel(const __grid_consta
     const float factor = (double)max_norm >= room ? 1.f : (float)((double)max_norm / room);      // (NaN: the second)
     for (uint32_t i = blockIdx.x; i < t.chunks; i += gridDim.x) {
         const uint32_t c = t.chunks - 1 - i;
-        const Entry& e = entry_of(t, c);
-        if (factor == 1.f && e.o == e.g) continue;
+        const Entry& e = t.t[at];
+        auto meanwhile = [&] { at = entry_of(t, c >= gridDim.x ? c - gridDim.x : 0); };
+        if (factor == 1.f && e.o == e.g) {
+            meanwhile();
+            continue;
+        }
         auto scale = [&](auto kind) {
             using T = decltype(kind);
-            for_chunk<T>(e, c, [&](const float (&v)[8], int64_t at, int whole) {
+            for_chunk<T>(e, c, meanwhile, [&](const float (&v)[8], int64_t from, int whole) {
                 float out[8];
 #pragma unroll
                 for (int j = 0; j < 8; ++j) out[j] = v[j] * factor;
                 if (whole) {
-                    store8_as<T>((T*)e.o + place(e, at, e.ldo), out, true, 8);
+                    store8_as<T>((T*)e.o + place(e, from, e.ldo), out, true, 8);
                 } else {
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
-                        if (at + j * kClipThreads < e.size) ((T*)e.o)[place(e, at + j * kClipThreads, e.ldo)] = from_float<T>(out[j]);
+                        if (from + j * kClipThreads < e.size) ((T*)e.o)[place(e, from + j * kClipThreads, e.ldo)] = from_float<T>(out[j]);
                 }
             });
         };
@@ -176,7 +186,7 @@ int64_t fill(Table<N>* t, const GradTensor* g, int64_t count) {
         const bool rows_vec = flat || (g[i].cols % 8 == 0 && g[i].ldg * es % 16 == 0 && g[i].ldo * es % 16 == 0);
         const bool vec = rows_vec && (((uintptr_t)g[i].g | (uintptr_t)g[i].o) & 15) == 0;
         t->t[t->count++] = {g[i].g, g[i].o, size, g[i].ldg, g[i].ldo, flat ? 0 : (int32_t)g[i].cols, t->chunks, g[i].type, vec ? 1 : 0};
-        t->chunks += (uint32_t)((size + kChunk - 1) / kChunk);
+        t->chunks += (uint32_t)((size * es + kChunkBytes - 1) / kChunkBytes);
     }
     return i;
 }

@@ -174,23 +174,39 @@ def test_clip_workspace_sizes():
     assert 256 <= size(0) <= size(1) <= size(1000) < 10 ** 6 and size(-1) == 0 and size(2 ** 20 + 1) == 0 and size(2 ** 20) > size(1000)
 
 
-def test_clip_passes_every_tensor_on(calls):  # noqa: F811
-    read = lambda p, n: [int(v or 0) for v in p[:n]]
+def test_clip_passes_every_tensor_on(calls, monkeypatch):  # noqa: F811
+    seen = []
+
+    def record(count, G, O, types, rows, cols, ldg, ldo, max_norm, eps, norm, stream):
+        many = lambda at, kind=ctypes.c_int64: at if at is None else list((kind * count).from_address(at))
+        seen.append((many(G), many(O), many(types, ctypes.c_int), many(rows), many(cols), many(ldg), many(ldo), max_norm, eps, norm))
+        return b.OK
+
+    monkeypatch.setattr(b, "lib", lambda: type("Recorder", (), {"gemm2m_clip_gradients": staticmethod(record)}))
     whole = torch.zeros(6, 40)
     grads = [dense(5, 7), Standin(torch.zeros(3, 4, dtype=torch.bfloat16)), Standin(whole[:, 8:20]), Standin(torch.zeros(8, 9).t()), Standin(torch.zeros(())),
              Standin(torch.zeros(2, 3, 4).permute(2, 0, 1))]
-    b.clip_gradients(grads, 2.0, norm=vector(1))
-    _, a = calls[-1]
-    assert a[0] == 6 and a[2] is None and a[7] is None and (a[8], a[9]) == (2.0, 1e-6)
-    assert read(a[1], 6) == [t.data_ptr() for t in grads] and read(a[3], 6) == [b.F32, b.BF16] + [b.F32] * 4
-    assert read(a[4], 6) == [1, 1, 6, 1, 1, 1] and read(a[5], 6) == [35, 12, 12, 72, 1, 24] and read(a[6], 6)[2] == 40
+    addresses = lambda tensors: [t.data_ptr() for t in tensors]
+    norm = vector(1)
+    b.clip_gradients(grads, 2.0, norm=norm)
+    g, o, types, rows, cols, ldg, ldo, *rest = seen[-1]
+    assert g == addresses(grads) and o is None and ldo is None and rest == [2.0, 1e-6, norm.data_ptr()]
+    assert types == [b.F32, b.BF16] + [b.F32] * 4 and rows == [1, 1, 6, 1, 1, 1] and cols == [35, 12, 12, 72, 1, 24] and ldg[2] == 40
     # into outputs whose rows are further apart, or closer together
     outs = [Standin(torch.zeros(5, 20)[:, :7]), dense(3, 4, torch.bfloat16), dense(6, 12), Standin(torch.zeros(8, 9).t()), Standin(torch.zeros(())),
             Standin(torch.zeros(2, 3, 4).permute(2, 0, 1))]
     b.clip_gradients(grads, 2.0, out=outs)
-    _, a = calls[-1]
-    assert read(a[4], 6) == [5, 1, 6, 1, 1, 1] and read(a[5], 6) == [7, 12, 12, 72, 1, 24]
-    assert read(a[6], 6)[0] == 7 and read(a[7], 6)[0] == 20 and read(a[6], 6)[2] == 40 and read(a[7], 6)[2] == 12
+    g, o, types, rows, cols, ldg, ldo, *rest = seen[-1]
+    assert o == addresses(outs) and rest == [2.0, 1e-6, None] and rows == [5, 1, 6, 1, 1, 1] and cols == [7, 12, 12, 72, 1, 24]
+    assert ldg[0] == 7 and ldo[0] == 20 and ldg[2] == 40 and ldo[2] == 12
+    # all of them contiguous
+    flat = [dense(5, 7), Standin(torch.zeros(3, 4, 2, dtype=torch.bfloat16)), Standin(torch.zeros(0, 3))]
+    for out in (None, [dense(5, 7), Standin(torch.zeros(3, 4, 2, dtype=torch.bfloat16)), Standin(torch.zeros(0, 3))]):
+        b.clip_gradients(iter(flat), 2.0, out=out)
+        g, o, types, rows, cols, ldg, ldo, *rest = seen[-1]
+        assert g == addresses(flat) and (o is None if out is None else o == addresses(out)) and types == [b.F32, b.BF16, b.F32] and rows == [1, 1, 1] and cols == [35, 24, 0]
+    b.clip_gradients([], 2.0)
+    assert seen[-1][0] == []
 
 
 def test_clip_refuses_tensors_that_it_cannot_walk(calls):  # noqa: F811
