@@ -5,8 +5,8 @@
 //
 // Tensors are cut into chunks of 32 KB, dealt out in turn to the blocks of one launch for up to 512 tensors, which it gets as a kernel parameter
 // (nothing to copy first; captured by value).  First launch: every thread sums squares of 8 entries in 32 bits and these sums in 64 bits, every block
-// leaves one number.  Second launch: every block adds those up, in the same order, and scales its chunks, last chunk first: those are still
-// in the on-chip cache where all of them do not fit.
+// leaves one number.  These are added up, in the same order, by every block of the second launch (few chunks) or by one block in between (many).  Second
+// launch: every block scales a chunk, last chunk first: those are still in the on-chip cache where all of them do not fit.
 #include "layer_ops.cuh"
 
 namespace gemm2m {
@@ -134,42 +134,36 @@ __global__ void __launch_bounds__(kClipThreads) fold_kernel(const double* partia
     if (norm) *norm = (float)sqrt(sum);
 }
 
+// A block per chunk, which it scales.  (705 million f32 entries: 6.4 TB/s; 5.6 with the chunks dealt out to four blocks on every SM.)
 template <int N>
 __global__ void __launch_bounds__(kClipThreads, 4) scale_kernel(const __grid_constant__ Table<N> t, const double* partials, int64_t count, float max_norm, float eps, float* norm) {
     __shared__ double warps[kClipThreads / 32];
-    int at = entry_of(t, t.chunks - 1 - blockIdx.x);
+    const uint32_t c = t.chunks - 1 - blockIdx.x;
+    const Entry& e = t.t[entry_of(t, c)];
     wait_for_prior_kernels();
-    const double size = sqrt(total_of(partials, count, warps));
+    const double size = sqrt(count == 1 ? *partials : total_of(partials, count, warps));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)size;
     const double room = size + (double)eps;
     const float factor = (double)max_norm >= room ? 1.f : (float)((double)max_norm / room);      // (NaN: the second)
-    for (uint32_t i = blockIdx.x; i < t.chunks; i += gridDim.x) {
-        const uint32_t c = t.chunks - 1 - i;
-        const Entry& e = t.t[at];
-        auto meanwhile = [&] { at = entry_of(t, c >= gridDim.x ? c - gridDim.x : 0); };
-        if (factor == 1.f && e.o == e.g) {
-            meanwhile();
-            continue;
-        }
-        auto scale = [&](auto kind) {
-            using T = decltype(kind);
-            for_chunk<T>(e, c, meanwhile, [&](const float (&v)[8], int64_t from, int whole) {
-                float out[8];
+    if (factor == 1.f && e.o == e.g) return;
+    auto scale = [&](auto kind) {
+        using T = decltype(kind);
+        for_chunk<T>(e, c, [] {}, [&](const float (&v)[8], int64_t from, int whole) {
+            float out[8];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) out[j] = v[j] * factor;
-                if (whole) {
-                    store8_as<T>((T*)e.o + place(e, from, e.ldo), out, true, 8);
-                } else {
+            for (int j = 0; j < 8; ++j) out[j] = v[j] * factor;
+            if (whole) {
+                store8_as<T>((T*)e.o + place(e, from, e.ldo), out, true, 8);
+            } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
-                        if (from + j * kClipThreads < e.size) ((T*)e.o)[place(e, from + j * kClipThreads, e.ldo)] = from_float<T>(out[j]);
-                }
-            });
-        };
-        if (e.type == kF32) scale(float());
-        else if (e.type == kF16) scale(__half());
-        else scale(__nv_bfloat16());
-    }
+                for (int j = 0; j < 8; ++j)
+                    if (from + j * kClipThreads < e.size) ((T*)e.o)[place(e, from + j * kClipThreads, e.ldo)] = from_float<T>(out[j]);
+            }
+        });
+    };
+    if (e.type == kF32) scale(float());
+    else if (e.type == kF16) scale(__half());
+    else scale(__nv_bfloat16());
 }
 
 // Up to N tensors as a kernel parameter; returns how many were taken.
@@ -209,8 +203,9 @@ cudaError_t launch_all(const GradTensor* g, int64_t count, bool scale, float max
         parts += blocks;
         ++launches[0];
     }
-    // with several tables, or no tensor to scale, one block adds the partial sums up
-    if (tables != 1 || !scale || parts == 0) {
+    // With few chunks every block of the second launch adds the partial sums up itself; with more of them than of partial sums, with several tables, or no tensor to
+    // scale, one block does.
+    if (tables != 1 || !scale || parts == 0 || t.chunks > (uint32_t)kBlocks) {
         cudaError_t err = launch_chained(fold_kernel, dim3(1), dim3(kClipThreads), 0, st, (const double*)part, parts, total, norm);
         if (err != cudaSuccess) return err;
         ++launches[0];
@@ -223,7 +218,7 @@ cudaError_t launch_all(const GradTensor* g, int64_t count, bool scale, float max
         if (tables != 1) i += fill(&t, g + i, count - i);
         else i = count;
         if (t.chunks == 0) continue;
-        cudaError_t err = launch_chained(scale_kernel<N>, dim3(blocks_for(t.chunks)), dim3(kClipThreads), 0, st, t, (const double*)part, parts, max_norm, eps, norm);
+        cudaError_t err = launch_chained(scale_kernel<N>, dim3(t.chunks), dim3(kClipThreads), 0, st, t, (const double*)part, parts, max_norm, eps, norm);
         if (err != cudaSuccess) return err;
         ++launches[1];
     }
