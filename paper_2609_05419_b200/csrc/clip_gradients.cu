@@ -3,7 +3,7 @@
 // norm = sqrt(sum over all tensors and entries of g^2); factor = 1 where max_norm >= norm + eps, else max_norm / (norm + eps) (NaN for a NaN norm),
 // formed in 64 bits and rounded to 32; o = rn(g factor).
 //
-// Tensors are cut into chunks of 32 KB, dealt out in turn to the blocks of one launch for up to 512 tensors, which it gets as a kernel parameter
+// Tensors are cut into chunks of 32 and 16 KB, dealt out in turn to the blocks of one launch for up to 512 tensors, which it gets as a kernel parameter
 // (nothing to copy first; captured by value).  First launch: every thread sums squares of 8 entries in 32 bits and these sums in 64 bits, every block
 // leaves one number.  These are added up, in the same order, by every block of the second launch (few chunks) or by one block in between (many).  Second
 // launch: every block scales a chunk, last chunk first: those are still in the on-chip cache where all of them do not fit.
@@ -13,16 +13,17 @@ namespace gemm2m {
 
 namespace {
 
-constexpr int kChunkBytes = 32768, kClipThreads = 256, kBlocks = 4 * kSms, kFew = 64, kMany = 512;
+constexpr int kReadBytes = 32768, kWriteBytes = 16384;      // chunks of the first and of the second launch
+constexpr int kClipThreads = 256, kBlocks = 4 * kSms, kFew = 64, kMany = 512;
 
 struct Entry {
     const void* g; void* o;
     int64_t size, ldg, ldo;
     int32_t cols;                         // of a row, 0 where all entries are contiguous
-    uint32_t first;                       // number of its first chunk
-    int32_t type, vec;                    // vec: groups of 8 entries are aligned, in g and in o
+    uint32_t first_read, first_write;     // numbers of its first chunks
+    int16_t type, vec;                    // vec: groups of 8 entries are aligned, in g and in o
 };
-template <int N> struct Table { Entry t[N]; int32_t count; uint32_t chunks; };
+template <int N> struct Table { Entry t[N]; int32_t count; uint32_t read, write; };      // numbers of chunks
 
 __device__ __forceinline__ int64_t place(const Entry& e, int64_t i, int64_t ld) {
     if (!e.cols) return i;
@@ -55,22 +56,22 @@ __device__ __forceinline__ double block_sum(double v, double* warps) {
 }
 
 // The entry that chunk c belongs to.
-template <int N>
+template <bool READ, int N>
 __device__ __forceinline__ int entry_of(const Table<N>& t, uint32_t c) {
     int lo = 0, hi = t.count;
     while (hi - lo > 1) {
         const int mid = (lo + hi) >> 1;
-        if (t.t[mid].first <= c) lo = mid;
+        if ((READ ? t.t[mid].first_read : t.t[mid].first_write) <= c) lo = mid;
         else hi = mid;
     }
     return lo;
 }
 
-// The groups of eight entries of a chunk that a thread deals with.  `meanwhile` runs when the loads are on their way.
-template <typename T, typename M, typename F>
+// The groups of eight entries of chunk c of a tensor that a thread deals with.  `meanwhile` runs when the loads are on their way.
+template <typename T, int BYTES, typename M, typename F>
 __device__ __forceinline__ void for_chunk(const Entry& e, uint32_t c, M&& meanwhile, F&& f) {
-    constexpr int kChunk = kChunkBytes / (int)sizeof(T), kGroups = kChunk / (8 * kClipThreads);
-    const int64_t base = (int64_t)(c - e.first) * kChunk;
+    constexpr int kChunk = BYTES / (int)sizeof(T), kGroups = kChunk / (8 * kClipThreads);
+    const int64_t base = (int64_t)c * kChunk;
     const T* g = (const T*)e.g;
     if (e.vec && base + kChunk <= e.size) {
         Raw8<T> raw[kGroups];
@@ -106,13 +107,13 @@ __global__ void __launch_bounds__(kClipThreads, 4) squares_kernel(const __grid_c
     wait_for_prior_kernels();
     double sum = 0.0;
     auto add = [&](const float (&v)[8], int64_t, int) { sum += squares8(v); };
-    int at = entry_of(t, blockIdx.x);
-    for (uint32_t c = blockIdx.x; c < t.chunks; c += gridDim.x) {
+    int at = entry_of<true>(t, blockIdx.x);
+    for (uint32_t c = blockIdx.x; c < t.read; c += gridDim.x) {
         const Entry& e = t.t[at];
-        auto meanwhile = [&] { at = entry_of(t, c + gridDim.x); };
-        if (e.type == kF32) for_chunk<float>(e, c, meanwhile, add);
-        else if (e.type == kF16) for_chunk<__half>(e, c, meanwhile, add);
-        else for_chunk<__nv_bfloat16>(e, c, meanwhile, add);
+        auto meanwhile = [&] { at = entry_of<true>(t, c + gridDim.x); };
+        if (e.type == kF32) for_chunk<float, kReadBytes>(e, c - e.first_read, meanwhile, add);
+        else if (e.type == kF16) for_chunk<__half, kReadBytes>(e, c - e.first_read, meanwhile, add);
+        else for_chunk<__nv_bfloat16, kReadBytes>(e, c - e.first_read, meanwhile, add);
     }
     sum = block_sum(sum, warps);
     if (threadIdx.x == 0) partials[blockIdx.x] = sum;
@@ -134,12 +135,13 @@ __global__ void __launch_bounds__(kClipThreads) fold_kernel(const double* partia
     if (norm) *norm = (float)sqrt(sum);
 }
 
-// A block per chunk, which it scales.  (705 million f32 entries: 6.4 TB/s; 5.6 with the chunks dealt out to four blocks on every SM.)
+// A block per chunk, which it scales.  (705 million f32 entries: 6.9 TB/s; 6.4 with chunks of 32 KB, 5.6 with these dealt out to four
+// blocks on every SM.)
 template <int N>
-__global__ void __launch_bounds__(kClipThreads, 4) scale_kernel(const __grid_constant__ Table<N> t, const double* partials, int64_t count, float max_norm, float eps, float* norm) {
+__global__ void __launch_bounds__(kClipThreads, 6) scale_kernel(const __grid_constant__ Table<N> t, const double* partials, int64_t count, float max_norm, float eps, float* norm) {
     __shared__ double warps[kClipThreads / 32];
-    const uint32_t c = t.chunks - 1 - blockIdx.x;
-    const Entry& e = t.t[entry_of(t, c)];
+    const uint32_t c = t.write - 1 - blockIdx.x;
+    const Entry& e = t.t[entry_of<false>(t, c)];
     wait_for_prior_kernels();
     const double size = sqrt(count == 1 ? *partials : total_of(partials, count, warps));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)size;
@@ -148,7 +150,7 @@ __global__ void __launch_bounds__(kClipThreads, 4) scale_kernel(const __grid_con
     if (factor == 1.f && e.o == e.g) return;
     auto scale = [&](auto kind) {
         using T = decltype(kind);
-        for_chunk<T>(e, c, [] {}, [&](const float (&v)[8], int64_t from, int whole) {
+        for_chunk<T, kWriteBytes>(e, c - e.first_write, [] {}, [&](const float (&v)[8], int64_t from, int whole) {
             float out[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) out[j] = v[j] * factor;
@@ -170,7 +172,7 @@ __global__ void __launch_bounds__(kClipThreads, 4) scale_kernel(const __grid_con
 template <int N>
 int64_t fill(Table<N>* t, const GradTensor* g, int64_t count) {
     t->count = 0;
-    t->chunks = 0;
+    t->read = t->write = 0;
     int64_t i = 0;
     for (; i < count && t->count < N; ++i) {
         const int64_t size = g[i].rows * g[i].cols;
@@ -179,8 +181,9 @@ int64_t fill(Table<N>* t, const GradTensor* g, int64_t count) {
         const bool flat = g[i].rows == 1 || (g[i].ldg == g[i].cols && g[i].ldo == g[i].cols);
         const bool rows_vec = flat || (g[i].cols % 8 == 0 && g[i].ldg * es % 16 == 0 && g[i].ldo * es % 16 == 0);
         const bool vec = rows_vec && (((uintptr_t)g[i].g | (uintptr_t)g[i].o) & 15) == 0;
-        t->t[t->count++] = {g[i].g, g[i].o, size, g[i].ldg, g[i].ldo, flat ? 0 : (int32_t)g[i].cols, t->chunks, g[i].type, vec ? 1 : 0};
-        t->chunks += (uint32_t)((size * es + kChunkBytes - 1) / kChunkBytes);
+        t->t[t->count++] = {g[i].g, g[i].o, size, g[i].ldg, g[i].ldo, flat ? 0 : (int32_t)g[i].cols, t->read, t->write, (int16_t)g[i].type, (int16_t)(vec ? 1 : 0)};
+        t->read += (uint32_t)((size * es + kReadBytes - 1) / kReadBytes);
+        t->write += (uint32_t)((size * es + kWriteBytes - 1) / kWriteBytes);
     }
     return i;
 }
@@ -196,8 +199,8 @@ cudaError_t launch_all(const GradTensor* g, int64_t count, bool scale, float max
     int tables = 0;
     for (int64_t i = 0; i < count; ++tables) {
         i += fill(&t, g + i, count - i);
-        if (t.chunks == 0) continue;
-        const int blocks = blocks_for(t.chunks);
+        if (t.read == 0) continue;
+        const int blocks = blocks_for(t.read);
         cudaError_t err = launch_chained(squares_kernel<N>, dim3(blocks), dim3(kClipThreads), 0, st, t, part + parts);
         if (err != cudaSuccess) return err;
         parts += blocks;
@@ -205,7 +208,7 @@ cudaError_t launch_all(const GradTensor* g, int64_t count, bool scale, float max
     }
     // With few chunks every block of the second launch adds the partial sums up itself; with more of them than of partial sums, with several tables, or no tensor to
     // scale, one block does.
-    if (tables != 1 || !scale || parts == 0 || t.chunks > (uint32_t)kBlocks) {
+    if (tables != 1 || !scale || parts == 0 || t.write > (uint32_t)kBlocks) {
         cudaError_t err = launch_chained(fold_kernel, dim3(1), dim3(kClipThreads), 0, st, (const double*)part, parts, total, norm);
         if (err != cudaSuccess) return err;
         ++launches[0];
@@ -217,8 +220,8 @@ cudaError_t launch_all(const GradTensor* g, int64_t count, bool scale, float max
     for (int64_t i = 0; i < count;) {
         if (tables != 1) i += fill(&t, g + i, count - i);
         else i = count;
-        if (t.chunks == 0) continue;
-        cudaError_t err = launch_chained(scale_kernel<N>, dim3(t.chunks), dim3(kClipThreads), 0, st, t, (const double*)part, parts, max_norm, eps, norm);
+        if (t.read == 0) continue;
+        cudaError_t err = launch_chained(scale_kernel<N>, dim3(t.write), dim3(kClipThreads), 0, st, t, (const double*)part, parts, max_norm, eps, norm);
         if (err != cudaSuccess) return err;
         ++launches[1];
     }
