@@ -420,10 +420,13 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
                 const bool whole = vec_d && col + 8 <= a.n;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const DT* add = reinterpret_cast<const DT*>(in[p][i]);
-                    float x[8];
+                    Raw8<DT> raw;
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]), back[i], to_float<DT>(add[j]));      // (the product is exact)
+                    for (int k = 0; k < kAccesses; ++k) raw.w[k] = in[p][i][k];
+                    float add[8], x[8];
+                    to_floats8<DT>(raw, add);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]), back[i], add[j]);      // (the product is exact)
                     if (there[i]) store8_as<DT>(D + place_d[i] + col, x, whole, a.n - col);
                 }
                 if (t < here) fetch(t, p);

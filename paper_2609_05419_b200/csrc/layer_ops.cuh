@@ -151,11 +151,33 @@ __device__ __forceinline__ Raw8<T> load8_part(const T* p, int64_t valid) {
     for (int i = 0; i < (int)sizeof(T) / 2; ++i) r.w[i] = reinterpret_cast<const uint4*>(t)[i];
     return r;
 }
+// Two 16-bit numbers of a word, the first in the low half.  (bf16: one shift and one mask; taken out of memory one by one they cost twice the instructions.)
+template <typename T> __device__ __forceinline__ void unpack_as(uint32_t w, float* a, float* b);
+template <> __device__ __forceinline__ void unpack_as<__nv_bfloat16>(uint32_t w, float* a, float* b) {
+    *a = __uint_as_float(w << 16);
+    *b = __uint_as_float(w & 0xffff0000u);
+}
+template <> __device__ __forceinline__ void unpack_as<__half>(uint32_t w, float* a, float* b) {
+    const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w));
+    *a = f.x;
+    *b = f.y;
+}
 template <typename T>
 __device__ __forceinline__ void to_floats8(const Raw8<T>& r, float (&v)[8]) {
-    const T* t = reinterpret_cast<const T*>(&r);
+    if constexpr (sizeof(T) == 2) {
+        unpack_as<T>(r.w[0].x, &v[0], &v[1]);
+        unpack_as<T>(r.w[0].y, &v[2], &v[3]);
+        unpack_as<T>(r.w[0].z, &v[4], &v[5]);
+        unpack_as<T>(r.w[0].w, &v[6], &v[7]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = to_float<T>(t[i]);
+        for (int i = 0; i < 2; ++i) {
+            v[4 * i] = __uint_as_float(r.w[i].x);
+            v[4 * i + 1] = __uint_as_float(r.w[i].y);
+            v[4 * i + 2] = __uint_as_float(r.w[i].z);
+            v[4 * i + 3] = __uint_as_float(r.w[i].w);
+        }
+    }
 }
 template <typename T> __device__ __forceinline__ T from_float(float v);
 template <> __device__ __forceinline__ float from_float<float>(float v) { return v; }

@@ -37,9 +37,7 @@ __global__ void __launch_bounds__(THREADS, THREADS != 256 ? 1 : VEC ? 4 : 2) rms
                 // rounded two at a time
 #pragma unroll
                 for (int j = 0; j < 8; j += 2) {
-                    const uint32_t w = pack_as<T>(h[i][j] + t[j], h[i][j + 1] + t[j + 1]);
-                    const T* two = reinterpret_cast<const T*>(&w);
-                    h[i][j] = to_float<T>(two[0]), h[i][j + 1] = to_float<T>(two[1]);
+                    unpack_as<T>(pack_as<T>(h[i][j] + t[j], h[i][j + 1] + t[j + 1]), &h[i][j], &h[i][j + 1]);
                 }
             } else {
 #pragma unroll

@@ -71,19 +71,25 @@ __global__ void __launch_bounds__(128, 4) rms_norm_turned_kernel(const RmsNormAr
     };
 #pragma unroll
     for (int i = 0; i < 8; ++i) rstd[i] = __ldg(a.rstd + min(row0 + i, a.rows - 1));
+    // (rows beyond the last: their entries are zero, and stay so)
+    if (row0 + 8 > a.rows)
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (row0 + i >= a.rows) rstd[i] = 0.f;
     read(a.H ? (const T*)a.H : (const T*)a.X, a.H ? a.ldh : a.ldx, std::false_type());
     if (a.R && !a.H) read((const T*)a.R, a.ldr, std::true_type());
     if (a.W) load8_any(a.W, a.w_type, col0, valid, w_vec && valid >= 8, w);
+    else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j] = 1.f;
     float top[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            y[i][j] = row0 + i >= a.rows ? 0.f : a.W ? y[i][j] * rstd[i] * w[j] : y[i][j] * rstd[i];
-            if (i == 7) top[j] = top3(top3(top3(y[0][j], y[1][j], y[2][j]), y[3][j], y[4][j]), top3(y[5][j], y[6][j], y[7][j]), 0.f);
-        }
+        for (int j = 0; j < 8; ++j) y[i][j] = y[i][j] * rstd[i] * w[j];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
+        top[j] = top3(top3(top3(y[0][j], y[1][j], y[2][j]), y[3][j], y[4][j]), top3(y[5][j], y[6][j], y[7][j]), 0.f);
         top[j] = top3(top[j], __shfl_xor_sync(0xffffffffu, top[j], 8), 0.f);
         top[j] = top3(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16), 0.f);
     }
