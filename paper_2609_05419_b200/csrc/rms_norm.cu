@@ -100,7 +100,7 @@ __global__ void __launch_bounds__(THREADS, THREADS != 256 ? 1 : VEC ? 4 : 2) rms
         for (int i = 0; i < NV; ++i) {
             const uint2 q = to_fp8<decltype(fmt)::value>(h[i], __shfl_sync(0xffffffffu, ratio, (lane & 16) + i * kLanes + 1));
             const int col = at.first(i) + lane * 8;
-            if (write && col + 8 <= cols) *reinterpret_cast<uint2*>(Q + col) = q;
+            if (write && col + 8 <= cols) __stcs(reinterpret_cast<uint2*>(Q + col), q);
             else if (write) store8(Q + col, q, cols - col);
         }
     };

@@ -48,7 +48,7 @@ template <typename T> struct Place<T, true> {
 #pragma unroll
         for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
             const bool in = col + i * kPer < cols;
-            const uint4 v = *reinterpret_cast<const uint4*>(row + (in ? col + i * kPer : 0));
+            const uint4 v = __ldcs(reinterpret_cast<const uint4*>(row + (in ? col + i * kPer : 0)));
             raw.w[i] = i == 0 || in ? v : make_uint4(0, 0, 0, 0);
         }
     }

@@ -13,7 +13,8 @@ __global__ void __launch_bounds__(128, 4) rms_norm_turned_kernel(const RmsNormAr
     __shared__ __align__(16) uint2 turned[64][16];
     __shared__ __align__(16) float turns[VEC ? 1 : 4][VEC ? 4 : kSegment];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t tile_r = blockIdx.x / (unsigned)col_tiles, tile_c = blockIdx.x - tile_r * col_tiles;
+    const unsigned tile = gridDim.x - 1 - blockIdx.x;
+    const int64_t tile_r = tile / (unsigned)col_tiles, tile_c = tile - tile_r * col_tiles;
     const int group = lane & 7;                          // columns 8 group .. of the tile
     const int rows8 = warp * 4 + (lane >> 3);            // rows 8 rows8 .. of the tile
     const int64_t row0 = tile_r * 128 + rows8 * 8, col0 = tile_c * 64 + group * 8;
