@@ -328,8 +328,8 @@ int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, c
 /* Low-rank updates of many requests' adapters beside a shared projection, row by row (token by token):
  *   D_t = C_t + s_a (X_t A_a^T) B_a^T,  a = index[t].
  * X: tokens x k; A_a (rank x k) and B_a (n x rank) of `adapters` (<= 16384) adapters, stride_a / stride_b elements apart; X, A, B of the same type F16 /
- * BF16.  rank <= 128; ranks (device, `adapters` entries, may be NULL): adapter a uses the first ranks[a] rows of A_a and columns of B_a, and nothing beyond them is
- * read.  index: device, one entry per token, in any order; a token whose entry is not in [0, adapters) has no adapter: D_t = C_t.  scales: device, one
+ * BF16.  rank <= 128; ranks (device, `adapters` entries, may be NULL): adapter a uses the first ranks[a] rows of A_a and columns of B_a, whatever lies beyond
+ * them.  index: device, one entry per token, in any order; a token whose entry is not in [0, adapters) has no adapter: D_t = C_t.  scales: device, one
  * per adapter, NULL for ones.  C and D: tokens x n of type d_type (F32 / F16 / BF16); C may be NULL (zero) or D itself (then ldc = ldd), not otherwise overlap D;
  * with C = D rows without an adapter are not touched.  Any alignment and stride.  k = 0 or rank = 0 adds nothing.
  * X A^T is summed and held in 32 bits (and multiplied by B as two 16-bit numbers, 2^-17 of its largest entry in a row), D is rounded once.  A token's

@@ -13,6 +13,8 @@
 // after a power of two per token that brings its largest entry near 1, so that no size of L overflows or underflows 16 bits.
 #include "adapters.cuh"
 
+#include <type_traits>
+
 namespace gemm2m {
 
 namespace {
@@ -118,7 +120,8 @@ __global__ void __launch_bounds__(1024) adapter_tiles_kernel(const AdapterArgs a
 // no such tile.
 __device__ __forceinline__ int find_tile(const AdapterArgs& a, int32_t* tokens, int* key) {
     constexpr int kThreads = kFewWarps * 32, kPer = kFewTokens / kThreads;
-    __shared__ int32_t keys[kFewTokens], places[kFewTokens];
+    __shared__ __align__(16) int32_t keys[kFewTokens];
+    __shared__ int32_t places[kFewTokens];
     __shared__ uint32_t firsts[kFewTokens / 32];
     const int count = (int)a.tokens;
 #pragma unroll
@@ -132,8 +135,15 @@ __device__ __forceinline__ int find_tile(const AdapterArgs& a, int32_t* tokens, 
     for (int i = 0; i < kPer; ++i) {
         const int t = i * kThreads + threadIdx.x;
         int place = 0;
-        if (t < count)
-            for (int u = 0; u < t; ++u) place += keys[u] == keys[t];
+        if (t < count) {
+            const int key = keys[t];
+#pragma unroll 4
+            for (int u = 0; u < t >> 2; ++u) {
+                const int4 four = reinterpret_cast<const int4*>(keys)[u];
+                place += (four.x == key) + (four.y == key) + (four.z == key) + (four.w == key);
+            }
+            for (int u = t & ~3; u < t; ++u) place += keys[u] == key;
+        }
         places[t] = place;
         const unsigned first = __ballot_sync(0xffffffffu, t < count && place % kFewTile == 0);
         if ((threadIdx.x & 31) == 0) firsts[t >> 5] = first;
@@ -170,11 +180,32 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
                      : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 
-// Eight entries of a row from entry `at` on; those at or beyond `end` are zero.
-template <typename T>
-__device__ __forceinline__ uint4 row8(const T* row, int64_t at, int64_t end, bool vec) {
-    if (vec && at + 8 <= end) return __ldg(reinterpret_cast<const uint4*>(row + at));
-    return load8_part<T>(row + at, end - at).w[0];
+// W neighbouring entries of a row (4 or 8, in the first words of the result) from entry `at` on; those at or beyond `end` are zero.  No branches, so that loads stay in
+// flight together: what is not wanted reads something that exists.  VEC: whole aligned groups that lie in the row's `stored` entries; `there`: whether the row is wanted.
+template <typename T, int W, bool VEC>
+__device__ __forceinline__ uint4 entries(const T* row, int64_t at, int64_t end, int64_t stored, bool there) {
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (VEC) {
+        const T* p = row + (at + W <= stored ? at : 0);
+        if (W == 4) {
+            const uint2 v = __ldg(reinterpret_cast<const uint2*>(p));
+            w[0] = v.x, w[1] = v.y;
+        } else {
+            const uint4 v = __ldg(reinterpret_cast<const uint4*>(p));
+            w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+        }
+    } else {
+        const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
+        uint16_t t[W];
+#pragma unroll
+        for (int i = 0; i < W; ++i) t[i] = p[min(at + i, stored - 1)];
+#pragma unroll
+        for (int i = 0; i < W; i += 2) w[i >> 1] = (uint32_t)t[i] | (uint32_t)t[i + 1] << 16;
+    }
+    const int valid = there ? (int)max((int64_t)0, min((int64_t)W, end - at)) : 0;
+#pragma unroll
+    for (int i = 0; i < W / 2; ++i) w[i] = valid >= 2 * i + 2 ? w[i] : valid == 2 * i + 1 ? w[i] & 0xffffu : 0u;
+    return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Pieces of L: block (tile, piece of k), the warps beside each other along k.
@@ -202,19 +233,24 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_down_kernel(const Adap
     // steps of 32 along k, dealt out to the pieces in runs and to the warps in turn
     const int64_t steps = (a.k + 31) / 32, per = (steps + splits - 1) / splits;
     const int64_t first = blockIdx.y * per, last = min(steps, first + per);
+    auto multiply = [&](auto whole) {
+        constexpr bool VEC = decltype(whole)::value;
 #pragma unroll 2
-    for (int64_t s = first + warp; s < last; s += kFewWarps) {
-        const int64_t at = s * 32 + q * 8;
-        uint4 w[2 * RT];
-        const uint4 x0 = there0 ? row8<T>(X0, at, a.k, vec) : make_uint4(0, 0, 0, 0), x1 = there1 ? row8<T>(X1, at, a.k, vec) : make_uint4(0, 0, 0, 0);
+        for (int64_t s = first + warp; s < last; s += kFewWarps) {
+            const int64_t at = s * 32 + q * 8;
+            uint4 w[2 * RT];
+            const uint4 x0 = entries<T, 8, VEC>(X0, at, a.k, a.k, there0), x1 = entries<T, 8, VEC>(X1, at, a.k, a.k, there1);
 #pragma unroll
-        for (int j = 0; j < 2 * RT; ++j) w[j] = j * 8 + g < rank ? row8<T>(A + (j * 8 + g) * a.lda, at, a.k, vec) : make_uint4(0, 0, 0, 0);
+            for (int j = 0; j < 2 * RT; ++j) w[j] = entries<T, 8, VEC>(A + min(j * 8 + g, rank - 1) * a.lda, at, a.k, a.k, j * 8 + g < rank);
 #pragma unroll
-        for (int j = 0; j < 2 * RT; ++j) {
-            mma<T>(acc[j], x0.x, x1.x, x0.y, x1.y, w[j].x, w[j].y);
-            mma<T>(acc[j], x0.z, x1.z, x0.w, x1.w, w[j].z, w[j].w);
+            for (int j = 0; j < 2 * RT; ++j) {
+                mma<T>(acc[j], x0.x, x1.x, x0.y, x1.y, w[j].x, w[j].y);
+                mma<T>(acc[j], x0.z, x1.z, x0.w, x1.w, w[j].z, w[j].w);
+            }
         }
-    }
+    };
+    if (vec) multiply(std::true_type());
+    else multiply(std::false_type());
     float* mine = pieces + warp * kFewTile * kPadded;
 #pragma unroll
     for (int j = 0; j < 2 * RT; ++j) {
@@ -235,11 +271,34 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_down_kernel(const Adap
     }
 }
 
-__device__ __forceinline__ void load8_of(const void* p, int type, int64_t at, int64_t valid, bool vec, float (&v)[8]) {
-    const bool whole = vec && valid >= 8;
-    if (type == kF32) to_floats8<float>(whole ? load8_rw<float>((const float*)p + at) : load8_part<float>((const float*)p + at, valid), v);
-    else if (type == kF16) to_floats8<__half>(whole ? load8_rw<__half>((const __half*)p + at) : load8_part<__half>((const __half*)p + at, valid), v);
-    else to_floats8<__nv_bfloat16>(whole ? load8_rw<__nv_bfloat16>((const __nv_bfloat16*)p + at) : load8_part<__nv_bfloat16>((const __nv_bfloat16*)p + at, valid), v);
+// Eight entries of a row of C as they are in memory, `bytes` each: loads only, and no branch that goes by the lane (vec: whole aligned groups; else entry by entry, those
+// beyond the row's end reading its last), so that they can be asked for ahead.  As numbers later, by floats_of.
+__device__ __forceinline__ void raw8_of(const char* row, int64_t col, int64_t n, int bytes, bool vec, uint4 (&r)[2]) {
+    const int64_t at = vec ? (col < n ? col : 0) : col;
+    if (bytes == 4) {
+        if (vec) {
+            r[0] = reinterpret_cast<const uint4*>(row + at * 4)[0];
+            r[1] = reinterpret_cast<const uint4*>(row + at * 4)[1];
+        } else {
+            uint32_t t[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) t[j] = reinterpret_cast<const uint32_t*>(row)[min(at + j, n - 1)];
+            r[0] = make_uint4(t[0], t[1], t[2], t[3]);
+            r[1] = make_uint4(t[4], t[5], t[6], t[7]);
+        }
+    } else if (vec) {
+        r[0] = *reinterpret_cast<const uint4*>(row + at * 2);
+    } else {
+        uint32_t t[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) t[j] = reinterpret_cast<const uint16_t*>(row)[min(at + j, n - 1)];
+        r[0] = make_uint4(t[0] | t[1] << 16, t[2] | t[3] << 16, t[4] | t[5] << 16, t[6] | t[7] << 16);
+    }
+}
+__device__ __forceinline__ void floats_of(const uint4 (&r)[2], int type, float (&v)[8]) {
+    if (type == kF32) to_floats8<float>({r[0], r[1]}, v);
+    else if (type == kF16) to_floats8<__half>({r[0]}, v);
+    else to_floats8<__nv_bfloat16>({r[0]}, v);
 }
 __device__ __forceinline__ void store8_of(void* p, int type, int64_t at, int64_t valid, bool vec, const float (&v)[8]) {
     const bool whole = vec && valid >= 8;
@@ -262,6 +321,41 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const Adapte
     if (count == 0) return;
     const int rank = rank_of(a, key);
     if (rank == 0 && a.C == a.D) return;
+    // What the first 32 columns need is asked for before L is added up, that of the next ones before these are worked on.
+    const T* B = (const T*)a.B + (rank > 0 ? key : 0) * a.stride_b;
+    const int64_t first = blockIdx.y * run, last = min(a.n, first + run);
+    constexpr int kWords = RT == 1 ? 1 : RT / 2;         // loads of a row of B per lane
+    uint4 b_ahead[4][kWords];
+    auto fetch_b = [&](int64_t n0) {
+        if (rank == 0) return;
+        auto fetch = [&](auto whole) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int64_t col = n0 + 8 * (g >> 1) + 2 * j + (g & 1);
+                const T* b = B + min(col, a.n - 1) * a.ldb;
+#pragma unroll
+                for (int s = 0; s < kWords; ++s) b_ahead[j][s] = entries<T, RT == 1 ? 4 : 8, decltype(whole)::value>(b, RT == 1 ? q * 4 : s * 32 + q * 8, rank, a.rank, true);
+            }
+        };
+        if (vec_b) fetch(std::true_type());
+        else fetch(std::false_type());
+    };
+    int64_t row[2];
+    bool there[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        there[i] = i * 8 + g < count;
+        row[i] = there[i] ? tokens[i * 8 + g] : 0;
+    }
+    const int es = a.d_type == kF32 ? 4 : 2;
+    uint4 c_ahead[2][2] = {};
+    auto fetch_c = [&](int64_t n0) {
+        if (a.C)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) raw8_of((const char*)a.C + row[i] * a.ldc * es, n0 + 8 * q, a.n, es, vec_d && a.n % 8 == 0, c_ahead[i]);
+    };
+    fetch_b(first + warp * 32);
+    fetch_c(first + warp * 32);
     if (rank > 0) {
         // a warp per row: the pieces added up, times s_a, and the power of two of its largest entry
         const float scale = a.scales ? a.scales[key] : 1.f;
@@ -273,7 +367,9 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const Adapte
                 const int c = i * 32 + lane;
                 v[i] = 0.f;
                 if (c < rank && r < count) {
-                    for (int p = 0; p < splits; ++p) v[i] += low[(p * a.tokens + tokens[r]) * kPadded + c];
+                    const float* piece = low + tokens[r] * (int64_t)kPadded + c;
+#pragma unroll 8
+                    for (int p = 0; p < splits; ++p) v[i] += piece[p * a.tokens * kPadded];
                     v[i] *= scale;
                 }
                 top = fmaxf(top, fabsf(v[i]));
@@ -304,65 +400,43 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const Adapte
                 lo[s][h] = *reinterpret_cast<const uint32_t*>(y);
             }
     }
-    int64_t row[2];
     float back[2];
-    bool there[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        there[i] = i * 8 + g < count;
-        row[i] = there[i] ? tokens[i * 8 + g] : 0;
-        back[i] = rank > 0 ? backs[i * 8 + g] : 0.f;
-    }
-    const T* B = (const T*)a.B + (rank > 0 ? key : 0) * a.stride_b;
-    const int64_t first = blockIdx.y * run, last = min(a.n, first + run);
+    for (int i = 0; i < 2; ++i) back[i] = rank > 0 ? backs[i * 8 + g] : 0.f;
     for (int64_t n0 = first + warp * 32; n0 < last; n0 += kFewWarps * 32) {
-        float acc[4][4];
+        float acc[4][4], v[2][8];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[j][c] = 0.f;
         if (rank > 0) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int64_t col = n0 + 8 * (g >> 1) + 2 * j + (g & 1);
-                const T* b = B + col * a.ldb;
-                const bool in = col < a.n;
-                if constexpr (RT == 1) {
-                    uint2 w;
-                    if (in && vec_b && q * 4 + 4 <= rank) w = __ldg(reinterpret_cast<const uint2*>(b + q * 4));
-                    else {
-                        const uint4 part = load8_part<T>(b + q * 4, in ? min(4, rank - q * 4) : 0).w[0];
-                        w = make_uint2(part.x, part.y);
-                    }
-                    mma<T>(acc[j], hi[0][0], hi[0][1], hi[0][2], hi[0][3], w.x, w.y);
-                    mma<T>(acc[j], lo[0][0], lo[0][1], lo[0][2], lo[0][3], w.x, w.y);
-                } else {
+            for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int s = 0; s < RT; s += 2) {
-                        const uint4 w = row8<T>(b, s * 16 + q * 8, in ? rank : 0, vec_b);
-                        mma<T>(acc[j], hi[s][0], hi[s][1], hi[s][2], hi[s][3], w.x, w.y);
-                        mma<T>(acc[j], hi[s + 1][0], hi[s + 1][1], hi[s + 1][2], hi[s + 1][3], w.z, w.w);
-                        mma<T>(acc[j], lo[s][0], lo[s][1], lo[s][2], lo[s][3], w.x, w.y);
-                        mma<T>(acc[j], lo[s + 1][0], lo[s + 1][1], lo[s + 1][2], lo[s + 1][3], w.z, w.w);
+                for (int s = 0; s < kWords; ++s) {
+                    const uint4 w = b_ahead[j][s];
+                    mma<T>(acc[j], hi[2 * s][0], hi[2 * s][1], hi[2 * s][2], hi[2 * s][3], w.x, w.y);
+                    mma<T>(acc[j], lo[2 * s][0], lo[2 * s][1], lo[2 * s][2], lo[2 * s][3], w.x, w.y);
+                    if constexpr (RT > 1) {
+                        mma<T>(acc[j], hi[2 * s + 1][0], hi[2 * s + 1][1], hi[2 * s + 1][2], hi[2 * s + 1][3], w.z, w.w);
+                        mma<T>(acc[j], lo[2 * s + 1][0], lo[2 * s + 1][1], lo[2 * s + 1][2], lo[2 * s + 1][3], w.z, w.w);
                     }
                 }
-            }
         }
-        const int64_t col = n0 + 8 * q, valid = a.n - col;
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-            if (!there[i] || valid <= 0) continue;
-            float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (a.C) load8_of(a.C, a.d_type, row[i] * a.ldc + col, valid, vec_d, v);
-            if (rank > 0) {
+            floats_of(c_ahead[i], a.d_type, v[i]);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    v[2 * j] += acc[j][2 * i] * back[i];
-                    v[2 * j + 1] += acc[j][2 * i + 1] * back[i];
-                }
-            }
-            store8_of(a.D, a.d_type, row[i] * a.ldd + col, valid, vec_d, v);
+            for (int j = 0; j < 8; ++j) v[i][j] = fmaf(acc[j >> 1][2 * i + (j & 1)], back[i], v[i][j]);      // (the product is exact)
         }
+        if (n0 + kFewWarps * 32 < last) {
+            fetch_b(n0 + kFewWarps * 32);
+            fetch_c(n0 + kFewWarps * 32);
+        }
+        const int64_t col = n0 + 8 * q;
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (there[i] && col < a.n) store8_of(a.D, a.d_type, row[i] * a.ldd + col, a.n - col, vec_d, v[i]);
     }
 }
 
@@ -376,13 +450,13 @@ cudaError_t launch_few(const AdapterArgs& a, const AdapterLayout& l, cudaStream_
     auto even = [](const void* p, int64_t ld, int64_t stride, int64_t bytes) { return ((uintptr_t)p | (uintptr_t)(ld * 2) | (uintptr_t)(stride * 2)) % bytes == 0; };
     const int64_t steps = (a.k + 31) / 32, most = (steps + 2 * kFewWarps - 1) / (2 * kFewWarps);      // at least two steps for every warp
     const int splits = (int)(l.splits < most ? l.splits : most);
-    const int vec = even(a.X, a.ldx, 0, 16) && even(a.A, a.lda, a.stride_a, 16);
+    const int vec = even(a.X, a.ldx, 0, 16) && even(a.A, a.lda, a.stride_a, 16) && a.k % 8 == 0;
     cudaError_t err = launch_chained(adapter_down_kernel<T, RT>, dim3((unsigned)l.max_tiles, (unsigned)splits), dim3(kFewWarps * 32), 4 * (size_t)kFewWarps * kFewTile * 16 * RT, st, a, l,
                                      splits, vec);
     if (err != cudaSuccess) return err;
     ++launches[0];
     const size_t es = a.d_type == kF32 ? 4 : 2;
-    const int vec_b = even(a.B, a.ldb, a.stride_b, RT == 1 ? 8 : 16);
+    const int vec_b = even(a.B, a.ldb, a.stride_b, RT == 1 ? 8 : 16) && a.rank % (RT == 1 ? 4 : 8) == 0;
     const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * es)) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * es)) % 16 == 0);
     // runs of columns: a few blocks for every SM, and at least two steps of 32 columns for every warp
     const int64_t groups = (a.n + 32 * kFewWarps - 1) / (32 * kFewWarps), runs = (4 * kSms + l.max_tiles - 1) / l.max_tiles;

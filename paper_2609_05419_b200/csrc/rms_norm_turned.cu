@@ -91,13 +91,18 @@ __global__ void __launch_bounds__(128, 4) rms_norm_turned_kernel(const RmsNormAr
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
         top[j] = top3(top3(top3(y[0][j], y[1][j], y[2][j]), y[3][j], y[4][j]), top3(y[5][j], y[6][j], y[7][j]), 0.f);
-        top[j] = top3(top[j], __shfl_xor_sync(0xffffffffu, top[j], 8), 0.f);
-        top[j] = top3(top[j], __shfl_xor_sync(0xffffffffu, top[j], 16), 0.f);
     }
-    if (lane < 8) {
-        *reinterpret_cast<float4*>(&warp_top[warp][group * 8]) = make_float4(top[0], top[1], top[2], top[3]);
-        *reinterpret_cast<float4*>(&warp_top[warp][group * 8 + 4]) = make_float4(top[4], top[5], top[6], top[7]);
+    // over the four lanes of a group of columns, which keep half of the columns after every exchange
+#pragma unroll
+    for (int d = 16, keep = 4; d >= 8; d >>= 1, keep >>= 1) {
+        const bool upper = (lane & d) != 0;
+#pragma unroll
+        for (int j = 0; j < keep; ++j) {
+            const float mine = upper ? top[j + keep] : top[j], theirs = upper ? top[j] : top[j + keep];
+            top[j] = top3(mine, __shfl_xor_sync(0xffffffffu, theirs, d), 0.f);
+        }
     }
+    *reinterpret_cast<float2*>(&warp_top[warp][group * 8 + (lane >> 4) * 4 + (lane >> 3 & 1) * 2]) = make_float2(top[0], top[1]);
     __syncthreads();
     // one thread per column forms the scale and leaves the inverse in row 0 of the table
     if (threadIdx.x < 64) {
