@@ -417,6 +417,8 @@ def _stream_of(stream, device):
 
 _FP8 = (E4M3, E5M2)
 _FLOATS = (F32, F16, BF16)
+_HALVES = (F16, BF16)
+_int32 = None
 _NO_FORM = (None, 0, None, 0)
 
 
@@ -646,12 +648,11 @@ def clip_gradients(grads, max_norm, out=None, norm=None, eps=1e-6, stream=None):
            "gemm2m_clip_gradients")
 
 
-def _stack(t, name, kind, device):
-    """(pointer, matrices, rows, cols, leading dimension, stride) of a 3-D CUDA tensor of row-major matrices."""
+def _stack(t, name, like, device):
+    """(pointer, matrices, rows, cols, leading dimension, stride) of a 3-D CUDA tensor of row-major matrices of the type of `like`."""
     shape = t.shape
-    if len(shape) != 3 or t.get_device() != device:
-        raise ValueError(f"{name}: need a 3-D CUDA tensor on the current device")
-    _type_of(t, name, (kind,))
+    if len(shape) != 3 or t.get_device() != device or t.dtype is not like.dtype:
+        raise ValueError(f"{name}: need a 3-D CUDA tensor of type {like.dtype} on the current device")
     many, rows, cols = shape
     stride, ld, step = t.stride()
     if cols > 1 and step != 1:
@@ -661,29 +662,33 @@ def _stack(t, name, kind, device):
     return t.data_ptr(), many, rows, cols, ld, stride if many > 1 else rows * max(cols, 1)
 
 
+def _indexes(t, name, size, device):
+    """Pointer of a contiguous vector of 32-bit whole numbers."""
+    global _int32
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
+    if t.shape != (size,) or t.dtype is not _int32 or t.get_device() != device or not t.is_contiguous():
+        raise ValueError(f"{name}: need a contiguous int32 CUDA tensor of {size} entries on the current device")
+    return t.data_ptr()
+
+
 def adapter_add(X, A, B, index, D, C=None, scales=None, ranks=None, stream=None):
     """D[t] = C[t] + scales[a] (X[t] A[a]^T) B[a]^T with a = index[t] (int32; no adapter where it is not an index of A): X tokens x k,
     A adapters x rank x k, B adapters x n x rank in float16 / bfloat16; D, C float32 / float16 / bfloat16 (C may be D, or None for zero).
     ranks (int32): how many rows of A[a] and columns of B[a] are in use."""
-    import torch
     device = _launch_device(X, "X")
-    px, tx, tokens, k, ldx = _rowmajor(X, "X", (F16, BF16), device)
-    pa, many, rank, k2, lda, stride_a = _stack(A, "A", tx, device)
-    pb, many2, n, rank2, ldb, stride_b = _stack(B, "B", tx, device)
+    px, tx, tokens, k, ldx = _rowmajor(X, "X", _HALVES, device)
+    pa, many, rank, k2, lda, stride_a = _stack(A, "A", X, device)
+    pb, many2, n, rank2, ldb, stride_b = _stack(B, "B", X, device)
     pd, td, md, nd, ldd = _rowmajor(D, "D", _FLOATS, device)
-    if k2 != k or many2 != many or rank2 != rank or (md, nd) != (tokens, n):
+    if k2 != k or many2 != many or rank2 != rank or md != tokens or nd != n:
         raise ValueError("shape mismatch")
     pc, ldc = _like(C, "C", D, D.shape, device)
-    pointers = []
-    for t, name, size in ((index, "index", tokens), (ranks, "ranks", many)):
-        if t is None and name == "ranks":
-            pointers.append(None)
-            continue
-        if t.shape != (size,) or t.dtype is not torch.int32 or t.get_device() != device or not t.is_contiguous():
-            raise ValueError(f"{name}: need a contiguous int32 CUDA tensor of {size} entries on the current device")
-        pointers.append(t.data_ptr())
-    _check(lib().gemm2m_adapter_add(tokens, n, k, many, rank, px, tx, ldx, pa, lda, stride_a, pb, ldb, stride_b, pointers[0],
-                                    _vector(scales, "scales", many, (F32,), device)[0], pointers[1], pc, ldc, pd, td, ldd, _stream_of(stream, device)),
+    pi = _indexes(index, "index", tokens, device)
+    pr = None if ranks is None else _indexes(ranks, "ranks", many, device)
+    _check(lib().gemm2m_adapter_add(tokens, n, k, many, rank, px, tx, ldx, pa, lda, stride_a, pb, ldb, stride_b, pi,
+                                    _vector(scales, "scales", many, (F32,), device)[0], pr, pc, ldc, pd, td, ldd, _stream_of(stream, device)),
            "gemm2m_adapter_add")
 
 
