@@ -260,9 +260,13 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
     cluster_sync_all();                                      // nobody's piece goes away while another block reads it
 }
 
-// DT: type of C and D; KB: blocks of 64 along the rank.  (The operands' 16-bit type is the instruction descriptor's matter.)
-template <typename DT, int KB, int ALIGN>
-__global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_kernel(const AdapterArgs a, const AdapterLayout l, int run_align, int vec_d, uint32_t idesc) {
+// DT: type of C and D; KB: blocks of 64 along the rank.  (The operands' 16-bit type is the instruction descriptor's matter.)  VEC: rows of C and D are whole 16-byte pieces;
+// otherwise a warp turns each 32 x 32 columns in shared memory and reads and writes row by row, a lane per column (a lane's own eight columns, entry by
+// entry, would be as many sectors per instruction as there are lanes: 1001 tokens, 1999 columns: 38 us in all, now 29).
+constexpr int up_blocks(int KB) { return KB == 1 ? 2 : 1; }       // on an SM
+constexpr int kTurnPitch = 36, kTurnBytes = 32 * kTurnPitch * 4;                     // of a warp
+template <typename DT, int KB, int ALIGN, bool VEC>
+__global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kernel(const AdapterArgs a, const AdapterLayout l, int run_align, uint32_t idesc) {
     constexpr int kTmemCols = 256, E = 16 / (int)sizeof(DT), kAccesses = 8 / E;      // eight columns of a row per lane, E in one access
     extern __shared__ unsigned char smem_raw[];
     __shared__ uint64_t bars[4];
@@ -282,6 +286,7 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
     const int piece = threadIdx.x & 7, c0 = threadIdx.x >> 3;
     const uint32_t b_dst = swizzled(b_base, (c0 & 6) << 2 | (c0 & 24) >> 2 | (c0 & 1), piece);
     const int quarter = warp & 3, half = warp >> 2, g = lane >> 2, q = lane & 3;
+    float* turn = reinterpret_cast<float*>(smem_raw + (low_hi - smem_u32(smem_raw)) + 4 * KB * kOperandBytes + warp * kTurnBytes);      // (not VEC)
 
     uint32_t it = 0;                                     // pieces so far: buffer it % 2, its use number it / 2
     bool ok = true;
@@ -297,8 +302,8 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
             for (int t = 0; t < here; ++t)
                 for (int i = threadIdx.x; i < tile.count * (kManyTile / E); i += kThreads) {
                     const int64_t row = tokens[i / (kManyTile / E)], c = column0(t) + i % (kManyTile / E) * E;
-                    if (vec_d && c + E <= a.n) {
-                        *reinterpret_cast<uint4*>(D + row * a.ldd + c) = C ? *reinterpret_cast<const uint4*>(C + row * a.ldc + c) : make_uint4(0, 0, 0, 0);
+                    if (VEC) {
+                        if (c < a.n) *reinterpret_cast<uint4*>(D + row * a.ldd + c) = C ? *reinterpret_cast<const uint4*>(C + row * a.ldc + c) : make_uint4(0, 0, 0, 0);
                     } else {
                         for (int64_t j = c; j < min(a.n, c + E); ++j) D[row * a.ldd + j] = C ? C[row * a.ldc + j] : DT(0.f);
                     }
@@ -339,47 +344,53 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
         copies_commit();
 
         // Read-back: this warp's 32 rows (rows g, g + 8 of two halves of 16) and 64 of a piece's 128 columns, 32 at a time.
-        int64_t place_c[4], place_d[4];
         float back[4];
-        bool there[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = quarter * 32 + i * 8 + g;
+            back[i] = row < tile.count ? ((const float*)(a.ws + l.off_back))[tile.start + row] : 0.f;
+        }
+        // VEC: rows 8i + g, eight columns; otherwise row `lane`'s token, which all lanes need
+        int64_t place_c[VEC ? 4 : 1], place_d[VEC ? 4 : 1];
+        bool there[VEC ? 4 : 1];
+#pragma unroll
+        for (int i = 0; i < (VEC ? 4 : 1); ++i) {
+            const int row = quarter * 32 + (VEC ? i * 8 + g : lane);
             there[i] = row < tile.count;
             const int64_t t = there[i] ? tokens[row] : 0;
-            back[i] = there[i] ? ((const float*)(a.ws + l.off_back))[tile.start + row] : 0.f;
-            place_c[i] = t * a.ldc;
-            place_d[i] = t * a.ldd;
+            place_c[i] = VEC ? t * a.ldc : t;
+            place_d[i] = VEC ? t * a.ldd : t;
         }
-        uint4 in[2][4][kAccesses];                       // what is to be added, a piece ahead
+        const int my_token = VEC ? 0 : (int)place_c[0], rows_here = min(32, tile.count - quarter * 32);
+        auto column = [&](int t, int p) { return column0(t) + half * 64 + p * 32 + (VEC ? q * 8 : lane); };
+        // What is to be added, a piece ahead.  (No branch that goes by the lane: what lies beyond the row's end, or the tile's, reads something that exists.)
+        uint4 in[2][VEC ? 4 : 1][kAccesses];
+        DT in_rows[VEC ? 1 : 32];                            // (one piece of 32 columns)
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (int p = 0; p < 2; ++p) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < (VEC ? 4 : 1); ++i)
 #pragma unroll
                 for (int k = 0; k < kAccesses; ++k) in[p][i][k] = make_uint4(0, 0, 0, 0);
-        auto column = [&](int t, int p) { return column0(t) + half * 64 + p * 32 + q * 8; };
+        }
+#pragma unroll
+        for (int i = 0; i < (VEC ? 1 : 32); ++i) in_rows[i] = from_float<DT>(0.f);
         auto fetch = [&](int t, int p) {
             if (!C) return;
             const int64_t col = column(t, p);
-            if (vec_d && col + 8 <= a.n) {
+            if constexpr (VEC) {
+                const int64_t at = col < a.n ? col : 0;
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (there[i])
 #pragma unroll
-                        for (int k = 0; k < kAccesses; ++k) in[p][i][k] = reinterpret_cast<const uint4*>(C + place_c[i] + col)[k];
+                    for (int k = 0; k < kAccesses; ++k) in[p][i][k] = reinterpret_cast<const uint4*>(C + place_c[i] + at)[k * E < a.n - at ? k : 0];
             } else {
-                // (no branches around the loads, each of which would be waited for at its branch's end: what lies beyond the row's end, or the tile's, reads something that exists)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    DT* to = reinterpret_cast<DT*>(in[p][i]);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) to[j] = C[place_c[i] + min(col + j, a.n - 1)];
-                }
+                for (int r = 0; r < 32; ++r) in_rows[r] = C[__shfl_sync(0xffffffffu, my_token, r) * a.ldc + min(col, a.n - 1)];
             }
         };
         fetch(0, 0);
-        fetch(0, 1);
+        if (VEC) fetch(0, 1);
         for (int t = 0; t <= here; ++t) {
             copies_wait<0>();
             fence_async_proxy();
@@ -417,19 +428,40 @@ __global__ void __launch_bounds__(kThreads, KB == 1 ? 2 : 1) adapter_up_many_ker
                 tmem_ld_16x32(from + (16u << 16), v[1]);
                 tmem_ld_wait();
                 const int64_t col = column(t - 1, p);
-                const bool whole = vec_d && col + 8 <= a.n;
+                if constexpr (VEC) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    Raw8<DT> raw;
+                    for (int i = 0; i < 4; ++i) {
+                        Raw8<DT> raw;
 #pragma unroll
-                    for (int k = 0; k < kAccesses; ++k) raw.w[k] = in[p][i][k];
-                    float add[8], x[8];
-                    to_floats8<DT>(raw, add);
+                        for (int k = 0; k < kAccesses; ++k) raw.w[k] = in[p][i][k];
+                        float add[8], x[8];
+                        to_floats8<DT>(raw, add);
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]), back[i], add[j]);      // (the product is exact)
-                    if (there[i]) store8_as<DT>(D + place_d[i] + col, x, whole, a.n - col);
+                        for (int j = 0; j < 8; ++j) x[j] = fmaf(__uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]), back[i], add[j]);      // (the product is exact)
+                        // (rows of E entries and multiples: a lane's eight columns are there as a whole, or their first half, or not at all)
+                        if (there[i] && col + 8 <= a.n) store8_as<DT>(D + place_d[i] + col, x, true, 8);
+                        else if (there[i]) store8_as<DT>(D + place_d[i] + col, x, false, a.n - col);
+                    }
+                } else {
+                    __syncwarp();                            // the columns before have been read
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float x[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]) * back[i];
+                        float4* to = reinterpret_cast<float4*>(turn + (i * 8 + g) * kTurnPitch + q * 8);
+                        to[0] = make_float4(x[0], x[1], x[2], x[3]);
+                        to[1] = make_float4(x[4], x[5], x[6], x[7]);
+                    }
+                    __syncwarp();
+#pragma unroll
+                    for (int r = 0; r < 32; ++r) {
+                        const DT out = from_float<DT>(to_float<DT>(in_rows[r]) + turn[r * kTurnPitch + lane]);
+                        const int64_t place = __shfl_sync(0xffffffffu, my_token, r) * a.ldd + col;
+                        if (r < rows_here && col < a.n) D[place] = out;
+                    }
                 }
-                if (t < here) fetch(t, p);
+                if (VEC ? t < here : t < here || p == 0) fetch(VEC || p == 1 ? t : t - 1, VEC ? p : p ^ 1);
             }
         }
         it += here;
@@ -473,22 +505,28 @@ cudaError_t launch_down(const AdapterArgs& a, const AdapterLayout& l, cudaStream
     return with(integral_constant<int, 128>(), integral_constant<int, 3>());
 }
 
-template <typename DT, int KB, int ALIGN>
+template <typename DT, int KB, int ALIGN, bool VEC>
 cudaError_t launch_up_as(const AdapterArgs& a, const AdapterLayout& l, int align, cudaStream_t st) {
-    constexpr size_t smem = (size_t)4 * KB * kOperandBytes + 1024;
-    cudaError_t err = set_smem(adapter_up_many_kernel<DT, KB, ALIGN>, smem);
+    constexpr size_t smem = (size_t)4 * KB * kOperandBytes + (VEC ? 0 : kThreads / 32 * kTurnBytes) + 1024;
+    cudaError_t err = set_smem(adapter_up_many_kernel<DT, KB, ALIGN, VEC>, smem);
     if (err != cudaSuccess) return err;
-    const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * sizeof(DT))) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * sizeof(DT))) % 16 == 0);
     // as many blocks as the GPU holds, or one for every piece that there can be
-    const int64_t pieces = l.max_tiles * ((a.n + kManyTile - 1) / kManyTile), slots = (KB == 1 ? 2 : 1) * kSms;
-    return launch_chained(adapter_up_many_kernel<DT, KB, ALIGN>, dim3((unsigned)(pieces < slots ? pieces : slots)), dim3(kThreads), smem, st, a, l, align, vec_d, make_idesc(a.type, kManyTile));
+    const int64_t pieces = l.max_tiles * ((a.n + kManyTile - 1) / kManyTile), slots = up_blocks(KB) * kSms;
+    return launch_chained(adapter_up_many_kernel<DT, KB, ALIGN, VEC>, dim3((unsigned)(pieces < slots ? pieces : slots)), dim3(kThreads), smem, st, a, l, align,
+                          make_idesc(a.type, kManyTile));
+}
+
+template <typename DT, int KB>
+cudaError_t launch_up_shape(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st) {
+    const int align = alignment(a.B, a.ldb, a.stride_b);
+    const bool vec = ((uintptr_t)a.D | (uintptr_t)(a.ldd * sizeof(DT)) | (uintptr_t)(a.n * sizeof(DT))) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * sizeof(DT))) % 16 == 0);
+    if (!vec) return launch_up_as<DT, KB, 0, false>(a, l, align, st);
+    return align == 16 ? launch_up_as<DT, KB, 16, true>(a, l, align, st) : launch_up_as<DT, KB, 0, true>(a, l, align, st);
 }
 
 template <typename DT>
 cudaError_t launch_up(const AdapterArgs& a, const AdapterLayout& l, cudaStream_t st) {
-    const int align = alignment(a.B, a.ldb, a.stride_b);
-    if (l.padded <= 64) return align == 16 ? launch_up_as<DT, 1, 16>(a, l, align, st) : launch_up_as<DT, 1, 0>(a, l, align, st);
-    return align == 16 ? launch_up_as<DT, 2, 16>(a, l, align, st) : launch_up_as<DT, 2, 0>(a, l, align, st);
+    return l.padded <= 64 ? launch_up_shape<DT, 1>(a, l, st) : launch_up_shape<DT, 2>(a, l, st);
 }
 
 }  // namespace
