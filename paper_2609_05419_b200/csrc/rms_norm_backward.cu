@@ -19,9 +19,10 @@ __global__ void __launch_bounds__(THREADS, backward_blocks(THREADS)) rms_norm_ba
     const int lane = at.lane, row_in = at.row_in, warp_in_row = at.warp_in_row, rows_here = at.rows(), cols = at.cols, segments = at.segments;
     float* turn = turns[VEC ? 0 : at.warp];
     auto first_of = [&](int i) { return at.first(i); };
-    // Two places: weights, dY and n stay in registers; four: they are read from the first-level cache, and converted, a second time.  (Formed again for two places as
-    // well, with three blocks on an SM: 85 against 62 us, the registers do not suffice.)
-    constexpr bool kHold = NV == 2;
+    // Two places: the weights stay in registers, and dY and n, too; four: they are read from the first-level cache, and formed, again.  Two places of aligned 16-bit numbers: dY and n
+    // are held as they came from memory and formed again behind the sum, and what that saves holds the next row, which is on its way meanwhile (8192 x 4096: 51 us; without it 60;
+    // with three blocks on an SM instead, whose registers do not suffice, 85).
+    constexpr bool kHold = NV == 2, kAhead = NV == 2 && VEC && sizeof(T) == 2, kKeep = NV == 2 && !kAhead;
     float acc[NV][8], w[kHold ? NV : 1][8];
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -30,55 +31,72 @@ __global__ void __launch_bounds__(THREADS, backward_blocks(THREADS)) rms_norm_ba
     wait_for_prior_kernels();
     if constexpr (kHold) load_weights<NV>(a.W, a.w_type, w_vec, cols, first_of, w);
     const int64_t stride = gridDim.x * (int64_t)rows_here;
-    float next_rstd = a.rstd[min(blockIdx.x * (int64_t)rows_here + row_in, a.rows - 1)];
+    struct Row { Place<T, VEC> g[NV], h[NV], r[NV]; float rstd; };
+    auto fetch = [&](Row& o, int64_t row) {
+        row = min(row, a.rows - 1);
+        o.rstd = a.rstd[row];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) o.g[i].load((const T*)a.dY + row * a.lddy, first_of(i), cols);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) o.h[i].load((const T*)a.H + row * a.ldh, first_of(i), cols);
+        if (a.dR)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) o.r[i].load((const T*)a.dR + row * a.lddr, first_of(i), cols);
+    };
+    Row o, ahead;
+    if (kAhead) fetch(ahead, blockIdx.x * (int64_t)rows_here + row_in);
     int turn_of = 0;
     for (int64_t first = blockIdx.x * (int64_t)rows_here; first < a.rows; first += stride, turn_of ^= 1) {
         const bool write = first + row_in < a.rows;          // a row beyond the last does the last one's work again, for nothing
         const int64_t row = min(first + row_in, a.rows - 1);
-        const float rstd = next_rstd;
-        next_rstd = a.rstd[min(row + stride, a.rows - 1)];
-        Place<T, VEC> g[NV], h[NV], r[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) g[i].load((const T*)a.dY + row * a.lddy, first_of(i), cols);
-#pragma unroll
-        for (int i = 0; i < NV; ++i) h[i].load((const T*)a.H + row * a.ldh, first_of(i), cols);
-        if (a.dR)
-#pragma unroll
-            for (int i = 0; i < NV; ++i) r[i].load((const T*)a.dR + row * a.lddr, first_of(i), cols);
-        float sum[NV], n[kHold ? NV : 1][8], dy[kHold ? NV : 1][8];
-        auto numbers = [&](int i) {
-            constexpr int kNone = kHold ? 0 : 1;
-            const int at_i = kNone ? 0 : i;
+        if (kAhead) {
+            o = ahead;
+            if (first + stride < a.rows) fetch(ahead, first + stride + row_in);
+        } else {
+            fetch(o, row);
+        }
+        auto numbers = [&](int i, float (&dy)[8], float (&n)[8]) {
             if constexpr (!kHold) load_weights<1>(a.W, a.w_type, w_vec, cols, [&](int) { return first_of(i); }, w);
-            g[i].get(dy[at_i], turn);
-            h[i].get(n[at_i], turn);
+            o.g[i].get(dy, turn);
+            o.h[i].get(n, turn);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) n[at_i][j] *= rstd;
+            for (int j = 0; j < 8; ++j) n[j] *= o.rstd;
         };
+        float sum[NV], all_dy[kKeep ? NV : 1][8], all_n[kKeep ? NV : 1][8];
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at_i = kHold ? i : 0;
-            numbers(i);
-            float s = 0.f;
+            const int of_w = kHold ? i : 0;
+            float new_dy[8], new_n[8], s = 0.f;
+            float (&dy)[8] = kKeep ? all_dy[kKeep ? i : 0] : new_dy, (&n)[8] = kKeep ? all_n[kKeep ? i : 0] : new_n;
+            numbers(i, dy, n);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float t = dy[at_i][j] * n[at_i][j];
+                const float t = dy[j] * n[j];
                 acc[i][j] += write ? t : 0.f;
-                s += t * w[at_i][j];
+                s += t * w[of_w][j];
             }
             sum[i] = at.there(i) ? s : 0.f;
         }
         // (two tables in turn: a warp may be a row ahead of one that still reads)
         const float mean = row_sum<NV>(sum, sums[turn_of] + row_in * warps * NV, warp_in_row, warps, segments) * inv_cols;
+        if constexpr (kAhead) {
+            // (the compiler would rather keep the numbers than form them again)
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                asm volatile("" : "+r"(o.g[i].raw.w[0].x), "+r"(o.g[i].raw.w[0].y), "+r"(o.g[i].raw.w[0].z), "+r"(o.g[i].raw.w[0].w));
+                asm volatile("" : "+r"(o.h[i].raw.w[0].x), "+r"(o.h[i].raw.w[0].y), "+r"(o.h[i].raw.w[0].z), "+r"(o.h[i].raw.w[0].w));
+            }
+        }
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int at_i = kHold ? i : 0;
-            float t[8], out[8];
-            if (!kHold) numbers(i);
-            if (a.dR) r[i].get(t, turn);
+            const int of_w = kHold ? i : 0;
+            float new_dy[8], new_n[8], t[8], out[8];
+            float (&dy)[8] = kKeep ? all_dy[kKeep ? i : 0] : new_dy, (&n)[8] = kKeep ? all_n[kKeep ? i : 0] : new_n;
+            if (!kKeep) numbers(i, dy, n);
+            if (a.dR) o.r[i].get(t, turn);
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                out[j] = rstd * (dy[at_i][j] * w[at_i][j] - n[at_i][j] * mean);
+                out[j] = o.rstd * (dy[j] * w[of_w][j] - n[j] * mean);
                 if (a.dR) out[j] += t[j];
             }
             store_place<T, VEC>((T*)a.dX + row * a.lddx, first_of(i), cols, write, out, turn);
