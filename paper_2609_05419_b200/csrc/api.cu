@@ -1089,7 +1089,7 @@ int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int typ
     Phases ph;
     if (int s = begin_call(&ph)) return s;
     const RmsNormBackwardArgs a = {rows, cols, dY, type, lddy, H, ldh, W, w_type, rstd, dR, lddr, dX, lddx, dW, add,
-                                   dW ? (float*)((char*)D().ws + kLayerOpsOffset) : nullptr, rms_norm_backward_parts(rows, cols)};
+                                   dW ? (float*)((char*)D().ws + kLayerOpsOffset) : nullptr};
     CK(ph.begin(2, st));
     CK(launch_rms_norm_backward(a, st, &g.launches[2]));
     CK(ph.end(st));

@@ -80,9 +80,9 @@ struct RmsNormBackwardArgs {
     const void* dR; int64_t lddr;
     void* dX; int64_t lddx;
     float* dW; int add;
-    float* part; int64_t parts;                              // workspace: partial sums of dW
+    float* part;                                             // workspace: partial sums of dW
 };
-int64_t rms_norm_backward_parts(int64_t rows, int64_t cols);      // rows of partial sums of dW
+int64_t rms_norm_backward_parts(int64_t rows, int64_t cols);      // rows of partial sums of dW at the most
 cudaError_t launch_rms_norm_backward(const RmsNormBackwardArgs& a, cudaStream_t st, int* launches);
 
 // Common 2-norm of many tensors, and the tensors scaled down where it is above a limit (clip_gradients.cu).

@@ -11,7 +11,7 @@ namespace {
 
 // One row for every `warps` warps of a block.
 template <typename T, int NV, bool VEC, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS != 256 ? 1 : VEC ? 4 : 2) rms_norm_rows_kernel(const RmsNormArgs a, int warps, float inv_cols, int w_vec) {
+__global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 512) / THREADS) rms_norm_rows_kernel(const RmsNormArgs a, int warps, float inv_cols, int w_vec) {
     __shared__ float sums[THREADS / 32 * NV];
     __shared__ __align__(16) float turns[VEC ? 1 : THREADS / 32][VEC ? 4 : kSegment];
     const Position at(warps, a.cols);

@@ -185,13 +185,13 @@ __device__ __forceinline__ uint2 to_fp8(const float (&y)[8], float inv) {
     return make_uint2(pack4<FMT>(y[0] * inv, y[1] * inv, y[2] * inv, y[3] * inv), pack4<FMT>(y[4] * inv, y[5] * inv, y[6] * inv, y[7] * inv));
 }
 
-// Where a warp stands: `warps` warps to a row, several rows to a block.
+// Where a warp stands: `warps` warps to a row, several rows to a block; columns [begin, cols) of it.
 struct Position {
-    int lane, warp, row_in, warp_in_row, warps, cols, segments;
-    __device__ __forceinline__ Position(int warps_, int64_t cols_)
-        : lane(threadIdx.x & 31), warp(threadIdx.x >> 5), row_in(warp / warps_), warp_in_row(warp - row_in * warps_), warps(warps_), cols((int)cols_),
-          segments((cols + kSegment - 1) / kSegment) {}
-    __device__ __forceinline__ int first(int i) const { return (i * warps + warp_in_row) * kSegment; }       // first column of the warp's i-th place
+    int lane, warp, row_in, warp_in_row, warps, begin, cols, segments;
+    __device__ __forceinline__ Position(int warps_, int64_t cols_, int begin_ = 0)
+        : lane(threadIdx.x & 31), warp(threadIdx.x >> 5), row_in(warp / warps_), warp_in_row(warp - row_in * warps_), warps(warps_), begin(begin_), cols((int)cols_),
+          segments((cols - begin + kSegment - 1) / kSegment) {}
+    __device__ __forceinline__ int first(int i) const { return begin + (i * warps + warp_in_row) * kSegment; }       // first column of the warp's i-th place
     // whether any of this thread's entries of its i-th place are in the row (their sums and maxima count)
     __device__ __forceinline__ bool there(int i) const { return first(i) + lane * 8 < cols; }
     __device__ __forceinline__ int rows() const { return (int)(blockDim.x / (32u * warps)); }

@@ -234,6 +234,12 @@ def test_gradients_against_64_bits(rows, cols, dtype, residual):
     check_backward(rows, cols, dtype, residual, True)
 
 
+@pytest.mark.parametrize("rows,cols", [(300, 8200), (333, 12289), (150, 24584), (111, 24833), (80, 32767)])      # rows shared by two to four blocks, several to a block
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_gradients_of_many_long_rows(rows, cols, dtype):
+    check_backward(rows, cols, dtype, True, True, add=True)
+
+
 @pytest.mark.parametrize("w_type", [torch.float32, torch.float16, torch.bfloat16, None])
 def test_gradients_with_weights_of_any_type_added_and_the_same_every_time(w_type):
     first = check_backward(300, 1000, torch.bfloat16, True, w_type is not None, w_type, add=True)
