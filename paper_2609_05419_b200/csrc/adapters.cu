@@ -181,9 +181,9 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
 }
 
 // W neighbouring entries of a row (4 or 8, in the first words of the result) from entry `at` on; those at or beyond `end` are zero.  No branches, so that loads stay in
-// flight together: what is not wanted reads something that exists.  VEC: whole aligned groups that lie in the row's `stored` entries; `there`: whether the row is wanted.
-template <typename T, int W, bool VEC>
-__device__ __forceinline__ uint4 entries(const T* row, int64_t at, int64_t end, int64_t stored, bool there) {
+// flight together: what is not wanted reads something that exists.  VEC: whole aligned groups that lie in the row's `stored` entries.
+template <typename T, int W, bool VEC, typename I>
+__device__ __forceinline__ uint4 entries(const T* row, I at, I end, I stored) {
     uint32_t w[4] = {0, 0, 0, 0};
     if (VEC) {
         const T* p = row + (at + W <= stored ? at : 0);
@@ -198,11 +198,12 @@ __device__ __forceinline__ uint4 entries(const T* row, int64_t at, int64_t end, 
         const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
         uint16_t t[W];
 #pragma unroll
-        for (int i = 0; i < W; ++i) t[i] = p[min(at + i, stored - 1)];
+        for (int i = 0; i < W; ++i) t[i] = p[min(at + (I)i, stored - 1)];
 #pragma unroll
         for (int i = 0; i < W; i += 2) w[i >> 1] = (uint32_t)t[i] | (uint32_t)t[i + 1] << 16;
     }
-    const int valid = there ? (int)max((int64_t)0, min((int64_t)W, end - at)) : 0;
+    const I left = end - at;
+    const int valid = left < 0 ? 0 : left > W ? W : (int)left;
 #pragma unroll
     for (int i = 0; i < W / 2; ++i) w[i] = valid >= 2 * i + 2 ? w[i] : valid == 2 * i + 1 ? w[i] & 0xffffu : 0u;
     return make_uint4(w[0], w[1], w[2], w[3]);
@@ -216,15 +217,15 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_down_kernel(const Adap
     __shared__ int32_t tokens[kFewTile];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
     wait_for_prior_kernels();
+    let_next_kernel_start();                             // (whatever came before has ended here: the second kernel may read all but L)
     int key;
     const int count = find_tile(a, tokens, &key);
     if (count == 0) return;
     const int rank = rank_of(a, key);
     if (rank == 0) return;
     const T* A = (const T*)a.A + key * a.stride_a;
-    const bool there0 = tokens[g] >= 0, there1 = tokens[g + 8] >= 0;
-    const T* X0 = (const T*)a.X + (there0 ? tokens[g] : 0) * a.ldx;
-    const T* X1 = (const T*)a.X + (there1 ? tokens[g + 8] : 0) * a.ldx;
+    const T* X0 = (const T*)a.X + max(tokens[g], 0) * a.ldx;
+    const T* X1 = (const T*)a.X + max(tokens[g + 8], 0) * a.ldx;
     float acc[2 * RT][4];
 #pragma unroll
     for (int j = 0; j < 2 * RT; ++j)
@@ -233,21 +234,28 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_down_kernel(const Adap
     // steps of 32 along k, dealt out to the pieces in runs and to the warps in turn
     const int64_t steps = (a.k + 31) / 32, per = (steps + splits - 1) / splits;
     const int64_t first = blockIdx.y * per, last = min(steps, first + per);
+    // (What rows beyond the tile's tokens and columns beyond the rank sum up is not looked at: they read what exists.)
     auto multiply = [&](auto whole) {
         constexpr bool VEC = decltype(whole)::value;
-#pragma unroll 2
-        for (int64_t s = first + warp; s < last; s += kFewWarps) {
+        auto step = [&](int64_t s, auto inside) {            // inside: all 32 entries are in the rows
+            constexpr bool IN = decltype(inside)::value;
             const int64_t at = s * 32 + q * 8;
+            auto load = [&](const T* row) { return IN ? __ldg(reinterpret_cast<const uint4*>(row + at)) : entries<T, 8, VEC>(row, at, a.k, a.k); };
             uint4 w[2 * RT];
-            const uint4 x0 = entries<T, 8, VEC>(X0, at, a.k, a.k, there0), x1 = entries<T, 8, VEC>(X1, at, a.k, a.k, there1);
+            const uint4 x0 = load(X0), x1 = load(X1);
 #pragma unroll
-            for (int j = 0; j < 2 * RT; ++j) w[j] = entries<T, 8, VEC>(A + min(j * 8 + g, rank - 1) * a.lda, at, a.k, a.k, j * 8 + g < rank);
+            for (int j = 0; j < 2 * RT; ++j) w[j] = load(A + min(j * 8 + g, rank - 1) * a.lda);
 #pragma unroll
             for (int j = 0; j < 2 * RT; ++j) {
                 mma<T>(acc[j], x0.x, x1.x, x0.y, x1.y, w[j].x, w[j].y);
                 mma<T>(acc[j], x0.z, x1.z, x0.w, x1.w, w[j].z, w[j].w);
             }
-        }
+        };
+        int64_t s = first + warp;
+        if (VEC)
+#pragma unroll 2
+            for (; s < last && s * 32 + 32 <= a.k; s += kFewWarps) step(s, std::true_type());
+        for (; s < last; s += kFewWarps) step(s, std::false_type());
     };
     if (vec) multiply(std::true_type());
     else multiply(std::false_type());
@@ -307,24 +315,30 @@ __device__ __forceinline__ void store8_of(void* p, int type, int64_t at, int64_t
     else store8_as<__nv_bfloat16>((__nv_bfloat16*)p + at, v, whole, valid);
 }
 
+// Blocks of the second kernel on an SM, by its registers.
+__host__ __device__ constexpr int up_blocks(int RT) { return RT == 1 ? 4 : RT == 8 ? 2 : 3; }
+
 // D = C + L B^T: block (tile, run of columns), the warps beside each other along the columns, 32 at a time.
 template <typename T, int RT>
-__global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int64_t run, int vec_b, int vec_d) {
+__global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int64_t run, int vec_b, int vec_d) {
     constexpr int kPadded = 16 * RT, kRow = kPadded + 4;
     extern __shared__ __align__(16) float rows[];        // [kFewTile][kRow]: L times s_a
     __shared__ int32_t tokens[kFewTile];
     __shared__ float backs[kFewTile];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
-    wait_for_prior_kernels();
     int key;
     const int count = find_tile(a, tokens, &key);
-    if (count == 0) return;
-    const int rank = rank_of(a, key);
-    if (rank == 0 && a.C == a.D) return;
-    // What the first 32 columns need is asked for before L is added up, that of the next ones before these are worked on.
+    const int rank = count > 0 ? rank_of(a, key) : 0;
+    if (count == 0 || (rank == 0 && a.C == a.D)) {
+        wait_for_prior_kernels();                            // (a kernel that ends lets the next one go on: no block may leave before the first kernel has ended)
+        return;
+    }
+    // What the first 32 columns need is asked for while the first kernel is at work (1 token, rank 16: 6.0 us in all, 8.4 without that), that of the next ones before these are
+    // worked on.
     const T* B = (const T*)a.B + (rank > 0 ? key : 0) * a.stride_b;
     const int64_t first = blockIdx.y * run, last = min(a.n, first + run);
     constexpr int kWords = RT == 1 ? 1 : RT / 2;         // loads of a row of B per lane
+    constexpr int kStride = kFewWarps * 32;
     uint4 b_ahead[4][kWords];
     auto fetch_b = [&](int64_t n0) {
         if (rank == 0) return;
@@ -334,10 +348,22 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const Adapte
                 const int64_t col = n0 + 8 * (g >> 1) + 2 * j + (g & 1);
                 const T* b = B + min(col, a.n - 1) * a.ldb;
 #pragma unroll
-                for (int s = 0; s < kWords; ++s) b_ahead[j][s] = entries<T, RT == 1 ? 4 : 8, decltype(whole)::value>(b, RT == 1 ? q * 4 : s * 32 + q * 8, rank, a.rank, true);
+                for (int s = 0; s < kWords; ++s) b_ahead[j][s] = entries<T, RT == 1 ? 4 : 8, decltype(whole)::value>(b, RT == 1 ? q * 4 : s * 32 + q * 8, rank, (int)a.rank);
             }
         };
-        if (vec_b) fetch(std::true_type());
+        if (vec_b && rank == kPadded) {                      // (nothing to leave out)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const T* b = B + min(n0 + 8 * (g >> 1) + 2 * j + (g & 1), a.n - 1) * a.ldb;
+                if constexpr (RT == 1) {
+                    const uint2 v = __ldg(reinterpret_cast<const uint2*>(b + q * 4));
+                    b_ahead[j][0] = make_uint4(v.x, v.y, 0, 0);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < kWords; ++s) b_ahead[j][s] = __ldg(reinterpret_cast<const uint4*>(b + s * 32 + q * 8));
+                }
+            }
+        } else if (vec_b) fetch(std::true_type());
         else fetch(std::false_type());
     };
     int64_t row[2];
@@ -356,6 +382,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const Adapte
     };
     fetch_b(first + warp * 32);
     fetch_c(first + warp * 32);
+    wait_for_prior_kernels();
     if (rank > 0) {
         // a warp per row: the pieces added up, times s_a, and the power of two of its largest entry
         const float scale = a.scales ? a.scales[key] : 1.f;
@@ -403,7 +430,7 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const Adapte
     float back[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) back[i] = rank > 0 ? backs[i * 8 + g] : 0.f;
-    for (int64_t n0 = first + warp * 32; n0 < last; n0 += kFewWarps * 32) {
+    for (int64_t n0 = first + warp * 32; n0 < last; n0 += kStride) {
         float acc[4][4], v[2][8];
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -429,9 +456,9 @@ __global__ void __launch_bounds__(kFewWarps * 32) adapter_up_kernel(const Adapte
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = fmaf(acc[j >> 1][2 * i + (j & 1)], back[i], v[i][j]);      // (the product is exact)
         }
-        if (n0 + kFewWarps * 32 < last) {
-            fetch_b(n0 + kFewWarps * 32);
-            fetch_c(n0 + kFewWarps * 32);
+        if (n0 + kStride < last) {
+            fetch_b(n0 + kStride);
+            fetch_c(n0 + kStride);
         }
         const int64_t col = n0 + 8 * q;
 #pragma unroll
@@ -458,8 +485,9 @@ cudaError_t launch_few(const AdapterArgs& a, const AdapterLayout& l, cudaStream_
     const size_t es = a.d_type == kF32 ? 4 : 2;
     const int vec_b = even(a.B, a.ldb, a.stride_b, RT == 1 ? 8 : 16) && a.rank % (RT == 1 ? 4 : 8) == 0;
     const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * es)) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * es)) % 16 == 0);
-    // runs of columns: a few blocks for every SM, and at least two steps of 32 columns for every warp
-    const int64_t groups = (a.n + 32 * kFewWarps - 1) / (32 * kFewWarps), runs = (4 * kSms + l.max_tiles - 1) / l.max_tiles;
+    // runs of columns: as many as the SMs take at once, since a block's way to its first columns is long (48 tokens to 16384 columns: 13.8 us; with half as many blocks 17, and
+    // loads two steps ahead in these gain nothing), and at least two steps of 32 columns for every warp
+    const int64_t groups = (a.n + 32 * kFewWarps - 1) / (32 * kFewWarps), runs = (up_blocks(RT) * kSms + l.max_tiles - 1) / l.max_tiles;
     int64_t per = (groups + runs - 1) / runs;
     if (per < 2) per = 2;
     const int64_t run = per * 32 * kFewWarps;

@@ -131,7 +131,9 @@ bool chained_launch_enabled();
 #ifdef __CUDACC__
 __device__ __forceinline__ void wait_for_prior_kernels() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
 // (Releasing the next kernel early, with griddepcontrol.launch_dependents at the top of each kernel, measured slower than the
-// implicit release at block exit: 42 against 39 us per call at 512^3, 97 against 95 us at 1024^3.)
+// implicit release at block exit: 42 against 39 us per call at 512^3, 97 against 95 us at 1024^3.  It pays where the next kernel has work of its own before it needs this one's
+// results; called behind wait_for_prior_kernels(), it leaves the next kernel free to read what was there before this one, too.  That kernel's blocks all wait before they end.)
+__device__ __forceinline__ void let_next_kernel_start() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
 template <typename... P, typename... A>
 inline cudaError_t launch_chained(void (*kernel)(P...), dim3 grid, dim3 block, size_t smem, cudaStream_t st, A&&... args) {
     cudaLaunchConfig_t c = {};
