@@ -1,6 +1,7 @@
 // Operators of a layer's training step next to the products of common.cuh: quantisation to 8-bit floating point with block
-// scales (fp8_quantise.cu), the product of two such matrices (fp8_gemm.cu) and Newton-Schulz orthogonalisation
-// (newton_schulz.cu).  Matrices are row-major here: rows contiguous, leading dimension = elements between rows.
+// scales (fp8_quantise.cu), the product of two such matrices (fp8_gemm.cu), Newton-Schulz orthogonalisation
+// (newton_schulz.cu), the root-mean-square norm and its gradients (rms_norm*.cu), clipping of gradients (clip_gradients.cu) and low-rank
+// updates of many adapters (adapters*.cu).  Matrices are row-major here: rows contiguous, leading dimension = elements between rows.
 #pragma once
 #include "common.cuh"
 
