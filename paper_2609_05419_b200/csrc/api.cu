@@ -1050,7 +1050,7 @@ int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t
     if ((Q || Qt) && fmt != GEMM2M_E4M3 && fmt != GEMM2M_E5M2) return GEMM2M_ERR_ARG;
     if (!fp8_form_ok(Q, ldq, S, lds, cols, rows) || !fp8_form_ok(Qt, ldqt, St, ldst, rows, cols)) return GEMM2M_ERR_ARG;
     if (rows == 0 || cols == 0) return GEMM2M_OK;
-    if (!X || (!H && !Y && !Q && !Qt && !rstd) || ((rows + 127) / 128) * ((cols + 127) / 128) > INT32_MAX) return GEMM2M_ERR_ARG;
+    if (!X || (!H && !Y && !Q && !Qt && !rstd) || ((rows + 127) / 128) * ((cols + 63) / 64) > INT32_MAX) return GEMM2M_ERR_ARG;
     if (int s = check_device()) return s;
     if (Qt && !rstd) {
         if (!D().ws || D().ws_bytes < rms_norm_bytes(rows)) return GEMM2M_ERR_WORKSPACE;
