@@ -53,7 +53,7 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 5
     if (a.H)
 #pragma unroll
         for (int i = 0; i < NV; ++i) store_place<T, VEC>((T*)a.H + row * a.ldh, at.first(i), cols, write, h[i], turn);
-    const float rstd = rsqrtf(row_sum<NV>(sum, sums + at.row_in * warps * NV, at.warp_in_row, warps, at.segments) * inv_cols + a.eps);
+    const float rstd = __frsqrt_rn(row_sum<NV>(sum, sums + at.row_in * warps * NV, at.warp_in_row, warps, at.segments) * inv_cols + a.eps);
     if (a.rstd && write && at.warp_in_row == 0 && lane == 0) a.rstd[row] = rstd;
     if (!a.Y && !a.Q) return;
     float top[NV];
