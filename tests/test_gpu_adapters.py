@@ -273,3 +273,49 @@ def test_another_stream_and_a_captured_graph(tokens, rank):
         torch.cuda.synchronize()
         assert torch.equal(d, want)
         del graph
+
+
+@pytest.mark.parametrize("tokens,rank", [(1, 16), (48, 16), (200, 64), (300, 24)])
+def test_calls_that_follow_what_they_read(tokens, rank):
+    """Every call reads what was written just before it: rows, what is added, indexes, ranks, the adapters themselves."""
+    size, many, calls = 512, 6, 12
+    x, a, w, _, c, scales, _ = operands(tokens, size, size, many, rank, torch.bfloat16, 61, ranks=False)
+    w = w * 0.2
+    indexes = [torch.randint(-1, many, (tokens,), generator=gen(70 + i), device="cuda").to(torch.int32) for i in range(calls)]
+    ranks = [torch.randint(0, rank + 1, (many,), generator=gen(90 + i), device="cuda").to(torch.int32) for i in range(calls)]
+    rows, added, out, index, used, a_now, w_now = x.clone(), c.clone(), torch.empty_like(c), indexes[0].clone(), ranks[0].clone(), a.clone(), w.clone()
+
+    def chain(pause):
+        rows.copy_(x)
+        added.copy_(c)
+        for i in range(calls):
+            index.copy_(indexes[i])
+            used.copy_(ranks[i])
+            torch.mul(a, 1 - 2 * (i & 1), out=a_now)
+            torch.mul(w, 1 - (i & 2), out=w_now)
+            pause()
+            b.adapter_add(rows, a_now, w_now, index, out, C=added, scales=scales, ranks=used)
+            pause()
+            b.adapter_add(out, a_now, w_now, index, rows, C=out, scales=scales)      # reads what the call before wrote
+            pause()
+            b.adapter_add(rows, a_now, w_now, index, rows if i & 1 else added, C=rows if i & 1 else None)
+            pause()
+            torch.tanh(rows, out=rows)
+            torch.tanh(added, out=added)
+
+    with workspace(tokens, rank, many):
+        chain(torch.cuda.synchronize)
+        want = [t.clone() for t in (rows, added, out)]
+        assert all(bool(torch.isfinite(t).all()) for t in want)
+        for _ in range(5):
+            chain(lambda: None)
+        assert all(torch.equal(t, v) for t, v in zip((rows, added, out), want))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            chain(lambda: None)
+        for _ in range(5):
+            out.zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(t, v) for t, v in zip((rows, added, out), want))
+        b.device_status()
