@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
 
 // DT: type of C and D; KB: blocks of 64 along the rank.  (The operands' 16-bit type is the instruction descriptor's matter.)  VEC: rows of C and D are whole 16-byte pieces;
 // otherwise a warp turns each 32 x 32 columns in shared memory and reads and writes row by row, a lane per column (a lane's own eight columns, entry by
-// entry, would be as many sectors per instruction as there are lanes: 1001 tokens, 1999 columns: 38 us in all, now 29).
+// entry, would be as many sectors per instruction as there are lanes: 1001 tokens, 1999 columns: 38 us in all, 29 so).
 constexpr int up_blocks(int KB) { return KB == 1 ? 2 : 1; }       // on an SM
 constexpr int kTurnPitch = 36, kTurnBytes = 32 * kTurnPitch * 4;                     // of a warp
 template <typename DT, int KB, int ALIGN, bool VEC>
@@ -301,15 +301,24 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
         auto column0 = [&](int t) { return (piece0 + t) * kManyTile; };
         if (tile.rank == 0) {                            // D = C, or zero
             if (a.C == a.D) continue;
-            for (int t = 0; t < here; ++t)
-                for (int i = threadIdx.x; i < tile.count * (kManyTile / E); i += kThreads) {
-                    const int64_t row = tokens[i / (kManyTile / E)], c = column0(t) + i % (kManyTile / E) * E;
-                    if (VEC) {
-                        if (c < a.n) *reinterpret_cast<uint4*>(D + row * a.ldd + c) = C ? *reinterpret_cast<const uint4*>(C + row * a.ldc + c) : make_uint4(0, 0, 0, 0);
-                    } else {
-                        for (int64_t j = c; j < min(a.n, c + E); ++j) D[row * a.ldd + j] = C ? C[row * a.ldc + j] : DT(0.f);
-                    }
+            // eight pieces of a row, or entries, in flight per thread (1001 tokens, a sixth without adapter, 1999 columns: 25.4 us in all, 28.9
+            // with one at a time)
+            using Unit = std::conditional_t<VEC, uint4, DT>;
+            constexpr int kPer = VEC ? kManyTile / E : kManyTile, kBatch = 8;
+            for (int t = 0; t < here; ++t) {
+                const int64_t col = column0(t) + threadIdx.x % kPer * (VEC ? E : 1), from = min(col, a.n - (VEC ? E : 1));
+                for (int r0 = threadIdx.x / kPer; r0 < tile.count; r0 += kBatch * (kThreads / kPer)) {
+                    int64_t row[kBatch];
+                    Unit v[kBatch];
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) row[u] = tokens[min(r0 + u * (kThreads / kPer), tile.count - 1)];
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u) v[u] = C ? *reinterpret_cast<const Unit*>(C + row[u] * a.ldc + from) : Unit();
+#pragma unroll
+                    for (int u = 0; u < kBatch; ++u)
+                        if (r0 + u * (kThreads / kPer) < tile.count && col < a.n) *reinterpret_cast<Unit*>(D + row[u] * a.ldd + col) = v[u];
                 }
+            }
             continue;
         }
         const int ksteps = (tile.rank + 15) / 16, width = 2 * ksteps;         // 16-byte pieces of a row that the MMAs read
@@ -352,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
             const int row = quarter * 32 + i * 8 + g;
             back[i] = row < tile.count ? ((const float*)(a.ws + l.off_back))[tile.start + row] : 0.f;
         }
-        // VEC: rows 8i + g, eight columns; otherwise row `lane`'s token, which all lanes need
+        // VEC: rows 8i + g, eight columns; otherwise row `lane`, for all lanes
         int64_t place_c[VEC ? 4 : 1], place_d[VEC ? 4 : 1];
         bool there[VEC ? 4 : 1];
 #pragma unroll
@@ -360,10 +369,10 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
             const int row = quarter * 32 + (VEC ? i * 8 + g : lane);
             there[i] = row < tile.count;
             const int64_t t = there[i] ? tokens[row] : 0;
-            place_c[i] = VEC ? t * a.ldc : t;
-            place_d[i] = VEC ? t * a.ldd : t;
+            place_c[i] = t * a.ldc;
+            place_d[i] = t * a.ldd;
         }
-        const int my_token = VEC ? 0 : (int)place_c[0], rows_here = min(32, tile.count - quarter * 32);
+        const int rows_here = min(32, tile.count - quarter * 32);
         auto column = [&](int t, int p) { return column0(t) + half * 64 + p * 32 + (VEC ? q * 8 : lane); };
         // What is to be added, a piece ahead.  (No branch that goes by the lane: what lies beyond the row's end, or the tile's, reads something that exists.)
         uint4 in[2][VEC ? 4 : 1][kAccesses];
@@ -387,8 +396,9 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
 #pragma unroll
                     for (int k = 0; k < kAccesses; ++k) in[p][i][k] = reinterpret_cast<const uint4*>(C + place_c[i] + at)[k * E < a.n - at ? k : 0];
             } else {
+                const DT* C_col = C + min(col, a.n - 1);
 #pragma unroll
-                for (int r = 0; r < 32; ++r) in_rows[r] = C[__shfl_sync(0xffffffffu, my_token, r) * a.ldc + min(col, a.n - 1)];
+                for (int r = 0; r < 32; ++r) in_rows[r] = C_col[__shfl_sync(0xffffffffu, place_c[0], r)];
             }
         };
         fetch(0, 0);
@@ -456,11 +466,13 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
                         to[1] = make_float4(x[4], x[5], x[6], x[7]);
                     }
                     __syncwarp();
+                    DT* D_col = D + col;
+                    const int rows_stored = col < a.n ? rows_here : 0;
 #pragma unroll
                     for (int r = 0; r < 32; ++r) {
                         const DT out = from_float<DT>(to_float<DT>(in_rows[r]) + turn[r * kTurnPitch + lane]);
-                        const int64_t place = __shfl_sync(0xffffffffu, my_token, r) * a.ldd + col;
-                        if (r < rows_here && col < a.n) D[place] = out;
+                        DT* place = D_col + __shfl_sync(0xffffffffu, place_d[0], r);
+                        if (r < rows_stored) *place = out;
                     }
                 }
                 if (VEC ? t < here : t < here || p == 0) fetch(VEC || p == 1 ? t : t - 1, VEC ? p : p ^ 1);
