@@ -12,7 +12,7 @@ namespace {
 // One row for every `warps` warps of a block, held in registers: read once, all outputs from there.  Bound by memory (8192 x 4096 bf16 with residual, H and 8-bit rows: 44 us,
 // 5.3 TB/s; blocks of one wave each, whose loads, sums and stores overlap with the other blocks' of the SM).
 template <typename T, int NV, bool VEC, int THREADS>
-__global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 512) / THREADS) rms_norm_rows_kernel(const RmsNormArgs a, int warps, float inv_cols, int w_vec) {
+__global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 512) / THREADS) rms_norm_rows_kernel(const RmsNormArgs a, int warps, Two inv_cols, int w_vec) {
     __shared__ float sums[THREADS / 32 * NV];
     __shared__ __align__(16) float turns[VEC ? 1 : THREADS / 32][VEC ? 4 : kSegment];
     const Position at(warps, a.cols);
@@ -53,8 +53,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 5
     if (a.H)
 #pragma unroll
         for (int i = 0; i < NV; ++i) store_place<T, VEC>((T*)a.H + row * a.ldh, at.first(i), cols, write, h[i], turn);
-    // (rounded correctly: 0.7 us of 8192 x 4096)
-    const float rstd = __frsqrt_rn(row_sum<NV>(sum, sums + at.row_in * warps * NV, at.warp_in_row, warps, at.segments) * inv_cols + a.eps);
+    float* segments = sums + at.row_in * warps * NV;
+    segment_sums<NV>(sum, segments, at.warp_in_row, warps, at.segments);
+    const float rstd = inverse_root(over_segments(segments, at.segments), inv_cols, a.eps);
     if (a.rstd && write && at.warp_in_row == 0 && lane == 0) a.rstd[row] = rstd;
     if (!a.Y && !a.Q) return;
     float top[NV];
@@ -113,7 +114,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 5
 template <typename T, int NV, bool VEC, int THREADS>
 cudaError_t launch_rows(const RmsNormArgs& a, int warps, int threads, int w_vec, cudaStream_t st) {
     const int here = threads / (32 * warps);
-    return launch_chained(rms_norm_rows_kernel<T, NV, VEC, THREADS>, dim3((unsigned)((a.rows + here - 1) / here)), dim3(threads), 0, st, a, warps, 1.f / (float)a.cols, w_vec);
+    const double inv_cols = 1.0 / (double)a.cols;
+    const Two inv = {(float)inv_cols, (float)(inv_cols - (float)inv_cols)};
+    return launch_chained(rms_norm_rows_kernel<T, NV, VEC, THREADS>, dim3((unsigned)((a.rows + here - 1) / here)), dim3(threads), 0, st, a, warps, inv, w_vec);
 }
 
 template <typename T, bool VEC>

@@ -157,19 +157,61 @@ __device__ __forceinline__ float over_warp(float (&v)[NV], F&& f) {
     return v[0];
 }
 
-// Sum over a row of each thread's sums of its places.  `segments`: one number per 256 columns of this row, in shared memory; every thread of the block takes part.
+// Sums over the segments of each thread's sums of its places.  `segments`: one number per 256 columns of this row, in shared memory; every thread of the block takes part.
 template <int NV>
-__device__ __forceinline__ float row_sum(float (&places)[NV], float* segments, int warp_in_row, int warps, int count) {
+__device__ __forceinline__ void segment_sums(float (&places)[NV], float* segments, int warp_in_row, int warps, int count) {
     const int lane = threadIdx.x & 31;
     const float mine = over_warp<NV>(places, [](float x, float y) { return x + y; });
     constexpr int kShift = NV == 4 ? 3 : NV == 2 ? 4 : 5;
     const int segment = (lane >> kShift) * warps + warp_in_row;
     if ((lane & ((1 << kShift) - 1)) == 0 && segment < count) segments[segment] = mine;
     __syncthreads();
+}
+// Sum over a row, in the order of the columns.
+template <int NV>
+__device__ __forceinline__ float row_sum(float (&places)[NV], float* segments, int warp_in_row, int warps, int count) {
+    segment_sums<NV>(places, segments, warp_in_row, warps, count);
     float sum = 0.f;
 #pragma unroll 4
     for (int i = 0; i < count; ++i) sum += segments[i];
     return sum;
+}
+// A number as the sum of two of 32 bits, the second what the first's rounding left.
+struct Two { float hi, lo; };
+__device__ __forceinline__ Two two_sum(float a, float b) {
+    const float s = a + b, part = s - a;
+    return {s, (a - (s - part)) + (b - part)};
+}
+// The segments' sums added up as such pairs over the lanes of a warp, in every lane: of the roundings on the way to a sum of squares those of the last few additions would be left
+// over, the ones before average out (8192 x 4096 bf16: error of rstd 3.0e-8, its own rounding 2.6e-8; 4.5e-8 with these additions in 32 bits.  In 32 bits 8192 x 512 takes 8.0 us, so
+// 8.6, rows of 1024 columns and more as much; added up in 64 bits 8192 x 4096 takes 51 us, so 44).
+__device__ __forceinline__ Two over_segments(const float* segments, int count) {
+    const int over = count <= 4 ? 1 : 2 << (31 - __clz((count - 1) >> 2));      // lanes that share the work, a power of two; up to four numbers each
+    const int first = threadIdx.x & (over - 1);
+    float x[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) x[k] = first + k * over < count ? segments[first + k * over] : 0.f;
+    Two sum = two_sum(x[0], x[1]);
+#pragma unroll
+    for (int k = 2; k < 4; ++k) {
+        const Two t = two_sum(sum.hi, x[k]);
+        sum = {t.hi, sum.lo + t.lo};
+    }
+    for (int d = over >> 1; d; d >>= 1) {
+        const Two other = {__shfl_xor_sync(0xffffffffu, sum.hi, d), __shfl_xor_sync(0xffffffffu, sum.lo, d)}, t = two_sum(sum.hi, other.hi);
+        sum = {t.hi, t.lo + (sum.lo + other.lo)};
+    }
+    return sum;
+}
+// 1 / sqrt(sum / cols + eps), off by little more than half a step (inv_cols: 1 / cols as a pair): the root of the leading number, brought nearer by a Newton step whose residual takes in
+// what the pairs hold.
+__device__ __forceinline__ float inverse_root(Two sum, Two inv_cols, float eps) {
+    const float mean = __fmul_rn(sum.hi, inv_cols.hi);
+    const Two m = two_sum(mean, eps);
+    const float rest = m.lo + fmaf(sum.lo, inv_cols.hi, fmaf(sum.hi, inv_cols.lo, fmaf(sum.hi, inv_cols.hi, -mean)));
+    const float r = rsqrtf(m.hi), t = __fmul_rn(m.hi, r);
+    const float residual = fmaf(-rest * r, r, fmaf(-fmaf(m.hi, r, -t), r, fmaf(-t, r, 1.f)));
+    return r > 0.f && r < INFINITY ? fmaf(0.5f * r, residual, r) : r;        // (m = 0, infinite or NaN: nothing to improve)
 }
 
 // The largest magnitude of three; NaN if there is one among them.

@@ -17,7 +17,7 @@ constexpr int backward_blocks(int threads) { return threads <= 320 ? 2 : 1; }
 // has `slice` segments of it; they hand each other their sums (2048 x 16384: 78 us, and 51 for as many
 // bytes in 8192 x 4096; in one block with four segments per warp, or in twice the threads, 112).
 template <typename T, bool VEC, bool SPLIT, int THREADS>
-__global__ void __launch_bounds__(THREADS, backward_blocks(THREADS)) rms_norm_backward_kernel(const RmsNormBackwardArgs a, int warps, int slice, float inv_cols, int w_vec) {
+__global__ void __launch_bounds__(THREADS, backward_blocks(THREADS)) rms_norm_backward_kernel(const RmsNormBackwardArgs a, int warps, int slice, double inv_cols, int w_vec) {
     __shared__ float sums[2][THREADS / 32 * NV];
     __shared__ float slices[2][8];
     __shared__ __align__(16) float turns[VEC ? 1 : THREADS / 32][VEC ? 4 : kSegment];
@@ -94,7 +94,7 @@ __global__ void __launch_bounds__(THREADS, backward_blocks(THREADS)) rms_norm_ba
             total = 0.f;
             for (int i = 0; i < shares; ++i) total += slices[turn_of][i];
         }
-        const float mean = total * inv_cols;
+        const float mean = (float)((double)total * inv_cols);
         if constexpr (kAhead) {
             // (the compiler would rather keep the numbers than form them again)
 #pragma unroll
@@ -177,7 +177,7 @@ template <typename T, bool VEC, bool SPLIT, int THREADS>
 cudaError_t launch_rows(const RmsNormBackwardArgs& a, const BackwardShape& s, int w_vec, cudaStream_t st) {
     const size_t smem = a.dW ? (size_t)(s.here - 1) * a.cols * 4 : 0;      // (at most 7 x 512 columns)
     const dim3 grid((unsigned)(s.blocks * s.shares)), block(s.threads);
-    const float inv_cols = 1.f / (float)a.cols;
+    const double inv_cols = 1.0 / (double)a.cols;
     if (SPLIT) return launch_chained_cluster(rms_norm_backward_kernel<T, VEC, SPLIT, THREADS>, grid, block, smem, s.shares, st, a, s.warps, s.slice, inv_cols, w_vec);
     return launch_chained(rms_norm_backward_kernel<T, VEC, SPLIT, THREADS>, grid, block, smem, st, a, s.warps, s.slice, inv_cols, w_vec);
 }
