@@ -309,7 +309,7 @@ int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t
  *   dX = rstd (dY W - n mean_j(dY W n)) + dR,   dW = sum_i dY n, or dW + that sum where `add` is not 0.
  * dX is the gradient of X and of R alike; dR (may be NULL) is the gradient that reached H along the residual path.  dY, H, dR, dX: same type, dX may be
  * any of the others, entry on entry.  dW (32 bits, may be NULL) is summed in 32 bits and a fixed order.
- * Workspace: GEMM2M_OP_RMS_NORM_BACKWARD with (rows, cols), needed for dW. */
+ * Workspace: GEMM2M_OP_RMS_NORM_BACKWARD with (rows, cols), needed for dW; it suffices for fewer rows and columns too. */
 int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int type, int64_t lddy, const void* H, int64_t ldh, const void* W, int w_type,
                              const float* rstd, const void* dR, int64_t lddr, void* dX, int64_t lddx, float* dW, int add, void* stream);
 
@@ -334,7 +334,7 @@ int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, c
  * with C = D rows without an adapter are not touched.  Any alignment and stride.  k = 0 or rank = 0 adds nothing.
  * X A^T is summed and held in 32 bits (and multiplied by B as two 16-bit numbers, 2^-17 of its largest entry in a row), D is rounded once.  A token's
  * result does not depend on the other tokens, beyond their number.
- * Workspace: GEMM2M_OP_ADAPTER_ADD with (tokens, rank, adapters). */
+ * Workspace: GEMM2M_OP_ADAPTER_ADD with (tokens, rank, adapters); it suffices for fewer of each too. */
 int gemm2m_adapter_add(int64_t tokens, int64_t n, int64_t k, int adapters, int rank, const void* X, int type, int64_t ldx, const void* A, int64_t lda,
                        int64_t stride_a, const void* B, int64_t ldb, int64_t stride_b, const int32_t* index, const float* scales, const int32_t* ranks,
                        const void* C, int64_t ldc, void* D, int d_type, int64_t ldd, void* stream);

@@ -38,7 +38,14 @@ AdapterLayout layout_of(int64_t tokens, int rank, int adapters) {
     l.off_count = l.off_tiles + up((int64_t)sizeof(AdapterTile) * l.max_tiles, 256);
     l.off_back = l.off_count + 256;
     l.off_low = l.off_back + up(4 * tokens, 256);
-    l.total = l.off_low + up((few ? 4 * (int64_t)l.splits : 4) * tokens * l.padded, 256);      // few: pieces of L in 32 bits; many: L as two 16-bit numbers
+    l.total = l.off_low + up(4 * tokens * l.padded, 256);      // L as two 16-bit numbers
+    if (few) {                                                 // nothing but the pieces of L in 32 bits
+        l.off_low = 0;
+        // up to splits x tokens rows of them: fewer than 32 x tokens, and than 2 kSms x 16 + tokens, since there are more than tokens / 16 tiles.  The bound, unlike what is used,
+        // never falls as a size grows.
+        const int64_t rows = 32 * tokens < 2 * kSms * kFewTile + tokens ? 32 * tokens : 2 * kSms * kFewTile + tokens;
+        l.total = up(4 * rows * l.padded, 256);
+    }
     return l;
 }
 
@@ -508,7 +515,11 @@ cudaError_t launch_typed(const AdapterArgs& a, const AdapterLayout& l, cudaStrea
 
 }  // namespace
 
-int64_t adapter_bytes(int64_t tokens, int rank, int adapters) { return layout_of(tokens, rank, adapters).total; }
+// What the call needs, and any with fewer tokens, adapters or ranks.
+int64_t adapter_bytes(int64_t tokens, int rank, int adapters) {
+    const int64_t mine = layout_of(tokens, rank, adapters).total, few = tokens > kFewTokens ? layout_of(kFewTokens, rank, adapters).total : 0;
+    return mine > few ? mine : few;
+}
 
 cudaError_t launch_adapter_add(const AdapterArgs& a, cudaStream_t st, int launches[2]) {
     const AdapterLayout l = layout_of(a.tokens, a.rank, a.adapters);

@@ -202,7 +202,7 @@ bool newton_schulz_sizes_ok(int64_t batch, int64_t m, int64_t n) {
 bool norm_sizes_ok(int64_t rows, int64_t cols) { return rows >= 0 && rows <= kMaxCoord && cols >= 0 && cols <= kMaxNormCols; }
 size_t rms_norm_bytes(int64_t rows) { return (size_t)(kLayerOpsOffset + round_up(4 * rows, 256)); }      // rstd, where the caller does not keep it
 size_t rms_norm_backward_bytes(int64_t rows, int64_t cols) {
-    return (size_t)(kLayerOpsOffset + (rows && cols ? round_up(4 * cols * rms_norm_backward_parts(rows, cols), 256) : 0));
+    return (size_t)(kLayerOpsOffset + (rows && cols ? round_up(4 * rms_norm_backward_partials(rows, cols), 256) : 0));
 }
 bool float_type(int type) { return type >= GEMM2M_F32 && type <= GEMM2M_BF16; }
 // An address that entries of `size` bytes can have (or none): a misplaced one would be a fault on the device.

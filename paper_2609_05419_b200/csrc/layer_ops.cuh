@@ -83,7 +83,7 @@ struct RmsNormBackwardArgs {
     float* dW; int add;
     float* part;                                             // workspace: partial sums of dW
 };
-int64_t rms_norm_backward_parts(int64_t rows, int64_t cols);      // rows of partial sums of dW at the most
+int64_t rms_norm_backward_partials(int64_t rows, int64_t cols);      // partial sums of dW of a call of these sizes, or smaller ones, at the most
 cudaError_t launch_rms_norm_backward(const RmsNormBackwardArgs& a, cudaStream_t st, int* launches);
 
 // Common 2-norm of many tensors, and the tensors scaled down where it is above a limit (clip_gradients.cu).
@@ -111,7 +111,7 @@ struct AdapterArgs {
     char* ws;
     int* dev_status;
 };
-int64_t adapter_bytes(int64_t tokens, int rank, int adapters);      // workspace
+int64_t adapter_bytes(int64_t tokens, int rank, int adapters);      // workspace of a call of these sizes, or smaller ones
 cudaError_t launch_adapter_add(const AdapterArgs& a, cudaStream_t st, int launches[2]);
 
 #ifdef __CUDACC__

@@ -205,7 +205,13 @@ cudaError_t launch_typed(const RmsNormBackwardArgs& a, cudaStream_t st, int* lau
 
 }  // namespace
 
-int64_t rms_norm_backward_parts(int64_t rows, int64_t cols) { return backward_shape(rows, cols).blocks; }
+// Up to the width at which an SM still holds two blocks, what is used grows with both sizes.  Wider rows have fewer blocks; there a bound that does not fall stands in for it: a part for
+// each row, and as many entries as at that width (8192 columns in 148 blocks, or up to 4096 times the blocks of a cluster in 259 / that many clusters, are fewer).
+int64_t rms_norm_backward_partials(int64_t rows, int64_t cols) {
+    constexpr int64_t kTwoBlocks = 320 / 32 * NV * kSegment, kMost = kTwoBlocks * backward_blocks(320) * kSms;
+    if (cols <= kTwoBlocks) return backward_shape(rows, cols).blocks * cols;
+    return rows < kMost / cols ? rows * cols : kMost;
+}
 
 cudaError_t launch_rms_norm_backward(const RmsNormBackwardArgs& a, cudaStream_t st, int* launches) {
     if (a.type == kF32) return launch_typed<float>(a, st, launches);
