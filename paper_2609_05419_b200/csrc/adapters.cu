@@ -11,7 +11,7 @@
 // 13 MB; rank 128: 44 us, 2.9 TB/s.)  Above, one block sorts the tokens first (6 us for 8192), for tiles of 128 (adapters_many.cu).
 //
 // L is held in 32 bits, and goes into the second product as the sum of two 16-bit numbers (hi + lo, 2^-18 of L for bf16, 2^-22 of the largest entry of the row for fp16),
-// after a power of two per token that brings its largest entry near 1, so that no size of L overflows or underflows 16 bits.
+// after a power of two per token that keeps its largest entry well inside the range, so that no size of L overflows or underflows 16 bits.
 #include "adapters.cuh"
 
 #include <type_traits>
@@ -411,7 +411,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kern
             }
             const uint32_t all = __reduce_max_sync(0xffffffffu, __float_as_uint(top));
             float down, back;
-            row_power(__uint_as_float(all), &down, &back);
+            row_power<T>(__uint_as_float(all), &down, &back);
 #pragma unroll
             for (int i = 0; i < (kPadded + 31) / 32; ++i)
                 if (i * 32 + lane < kPadded) rows[r * kRow + i * 32 + lane] = v[i] * down;

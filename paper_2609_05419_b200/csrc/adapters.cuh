@@ -34,11 +34,15 @@ __device__ __forceinline__ void split2(float v, T* hi, T* lo) {
     *lo = finite ? from_float<T>(v - to_float<T>(*hi)) : T(0.f);
 }
 
-// 2^-e for a row whose largest magnitude is in [2^e, 2^(e+1)), and 2^e, with e kept to [-126, 126]; 1 where that is not finite.
+// 2^-s for a row whose largest magnitude is in [2^e, 2^(e+1)), and 2^s; 1 where that is not finite.  fp16: s = e - 14, near the top of its range, so that entries far below the largest keep
+// their bits too.  bf16, whose range is that of 32 bits: s = 0 from 2^-60 to 2^60, so that the products with B leave the range only where the results do (with the largest entry brought
+// to 1, a B of 1e38 would overflow beside an L of 1e-20); beyond, s brings the largest entry back to that range.
+template <typename T>
 __device__ __forceinline__ void row_power(float top, float* down, float* back) {
-    const int field = (int)(__float_as_uint(top) >> 23), e = field == 255 ? 0 : min(max(field - 127, -126), 126);
-    *down = __uint_as_float((uint32_t)(127 - e) << 23);
-    *back = __uint_as_float((uint32_t)(127 + e) << 23);
+    const int field = (int)(__float_as_uint(top) >> 23), e = field - 127;
+    const int s = field == 255 ? 0 : __is_same(T, __half) ? max(e - 14, -126) : e - min(max(e, -60), 60);
+    *down = __uint_as_float((uint32_t)(127 - s) << 23);
+    *back = __uint_as_float((uint32_t)(127 + s) << 23);
 }
 #endif
 

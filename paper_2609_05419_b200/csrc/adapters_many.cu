@@ -222,7 +222,7 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
     }
     frame.close(kTmemCols);
     cluster_sync_all();
-    // a warp per row: the pieces added up, times s_a, the largest entry brought near 1, as two 16-bit numbers
+    // a warp per row: the pieces added up, times s_a, the largest entry brought well inside the range, as two 16-bit numbers
     const float scale = a.scales ? a.scales[tile.key] : 1.f;
     T* low = (T*)(a.ws + l.off_low) + (int64_t)tile.start * (2 * RP);
     float* backs = (float*)(a.ws + l.off_back) + tile.start;
@@ -245,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
             top = fmaxf(top, fmaxf(fabsf(v[b].x), fabsf(v[b].y)));
         }
         float down, back;
-        row_power(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))), &down, &back);
+        row_power<T>(__uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(top))), &down, &back);
 #pragma unroll
         for (int b = 0; b < kPairs; ++b) {
             const int c = b * 64 + lane * 2;
