@@ -332,8 +332,8 @@ int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, c
  * them.  index: device, one entry per token, in any order; a token whose entry is not in [0, adapters) has no adapter: D_t = C_t.  scales: device, one
  * per adapter, NULL for ones.  C and D: tokens x n of type d_type (F32 / F16 / BF16); C may be NULL (zero) or D itself (then ldc = ldd), not otherwise overlap D;
  * with C = D rows without an adapter are not touched.  Any alignment and stride.  k = 0 or rank = 0 adds nothing.
- * X A^T is summed and held in 32 bits (and multiplied by B as two 16-bit numbers, 2^-17 of its largest entry in a row), D is rounded once.  A token's
- * result does not depend on the other tokens, beyond their number.
+ * X A^T is summed and held in 32 bits (and for a 16-bit D multiplied by B as two 16-bit numbers, which are off by 2^-17 of it for bf16, 2^-22 for fp16), D is
+ * rounded once.  A token's result does not depend on the other tokens, beyond their number.
  * Workspace: GEMM2M_OP_ADAPTER_ADD with (tokens, rank, adapters); it suffices for fewer of each too. */
 int gemm2m_adapter_add(int64_t tokens, int64_t n, int64_t k, int adapters, int rank, const void* X, int type, int64_t ldx, const void* A, int64_t lda,
                        int64_t stride_a, const void* B, int64_t ldb, int64_t stride_b, const int32_t* index, const float* scales, const int32_t* ranks,

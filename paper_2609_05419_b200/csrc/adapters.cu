@@ -10,8 +10,9 @@
 // of D is free too: four MMAs take columns such that a lane ends with eight neighbouring ones.  (48 tokens, 24 adapters of rank 16, 4096 to 16384 columns: 13.8 us in a graph,
 // 13 MB; rank 128: 44 us, 2.9 TB/s.)  Above, one block sorts the tokens first (6 us for 8192), for tiles of 128 (adapters_many.cu).
 //
-// L is held in 32 bits, and goes into the second product as the sum of two 16-bit numbers (hi + lo, 2^-18 of L for bf16, 2^-22 of the largest entry of the row for fp16),
-// after a power of two per token that keeps its largest entry well inside the range, so that no size of L overflows or underflows 16 bits.
+// L is held in 32 bits, and goes into the second product as the sum of 16-bit numbers, after a power of two per token that keeps its largest entry well inside the range, so that
+// no size of L overflows or underflows 16 bits: three for a 32-bit D, which hold all of L's bits (40 tokens, rank 16: error 1.1e-7, with two of bf16 2.5e-6; 48 tokens to
+// 16384 columns 13.2 us, with two 12.8; of rank 64 22.5 and 19.5), two for a 16-bit D, whose own rounding hides what is left (2^-17 of L for bf16, 2^-22 for fp16).
 #include "adapters.cuh"
 
 #include <type_traits>
@@ -38,7 +39,7 @@ AdapterLayout layout_of(int64_t tokens, int rank, int adapters) {
     l.off_count = l.off_tiles + up((int64_t)sizeof(AdapterTile) * l.max_tiles, 256);
     l.off_back = l.off_count + 256;
     l.off_low = l.off_back + up(4 * tokens, 256);
-    l.total = l.off_low + up(4 * tokens * l.padded, 256);      // L as two 16-bit numbers
+    l.total = l.off_low + up(2 * kParts * tokens * l.padded, 256);      // L as three 16-bit numbers
     if (few) {                                                 // nothing but the pieces of L in 32 bits
         l.off_low = 0;
         // up to splits x tokens rows of them: fewer than 32 x tokens, and than 2 kSms x 16 + tokens, since there are more than tokens / 16 tiles.  The bound, unlike what is used,
@@ -327,7 +328,7 @@ __device__ __forceinline__ void store8_of(void* p, int type, int64_t at, int64_t
 __host__ __device__ constexpr int up_blocks(int RT) { return RT == 1 ? 4 : RT == 8 ? 2 : 3; }
 
 // D = C + L B^T: block (tile, run of columns), the warps beside each other along the columns, 32 at a time.
-template <typename T, int RT>
+template <typename T, int RT, int PARTS>
 __global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kernel(const AdapterArgs a, const AdapterLayout l, int splits, int64_t run, int vec_b, int vec_d) {
     constexpr int kPadded = 16 * RT, kRow = kPadded + 4;
     extern __shared__ __align__(16) float rows[];        // [kFewTile][kRow]: L times s_a
@@ -394,7 +395,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kern
     if (rank > 0) {
         // a warp per row: the pieces added up, times s_a, and the power of two of its largest entry
         const float scale = a.scales ? a.scales[key] : 1.f;
-        const float* low = (const float*)(a.ws + l.off_low);
+        const float* sums = (const float*)(a.ws + l.off_low);
         for (int r = warp; r < kFewTile; r += kFewWarps) {
             float v[(kPadded + 31) / 32], top = 0.f;
 #pragma unroll
@@ -402,7 +403,7 @@ __global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kern
                 const int c = i * 32 + lane;
                 v[i] = 0.f;
                 if (c < rank && r < count) {
-                    const float* piece = low + tokens[r] * (int64_t)kPadded + c;
+                    const float* piece = sums + tokens[r] * (int64_t)kPadded + c;
 #pragma unroll 8
                     for (int p = 0; p < splits; ++p) v[i] += piece[p * a.tokens * kPadded];
                     v[i] *= scale;
@@ -421,18 +422,21 @@ __global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kern
     }
     // operand A of the MMAs: lane (g, q) holds entries 4q, 4q+1 | 4q+2, 4q+3 of every 16 (RT = 1) or 8q .. 8q+7 of every 32
     constexpr int kStep = RT == 1 ? 4 : 8;
-    uint32_t hi[RT][4], lo[RT][4];
+    uint32_t low[PARTS][RT][4];
     if (rank > 0) {
 #pragma unroll
         for (int s = 0; s < RT; ++s)
 #pragma unroll
             for (int h = 0; h < 4; ++h) {                    // (row g + 8 (h & 1), pair h >> 1)
                 const float* p = rows + (g + 8 * (h & 1)) * kRow + (RT == 1 ? 0 : (s >> 1) * 32) + q * kStep + (RT == 1 ? 0 : (s & 1) * 4) + (h >> 1) * 2;
-                T x[2], y[2];
-                split2<T>(p[0], &x[0], &y[0]);
-                split2<T>(p[1], &x[1], &y[1]);
-                hi[s][h] = *reinterpret_cast<const uint32_t*>(x);
-                lo[s][h] = *reinterpret_cast<const uint32_t*>(y);
+                T x[PARTS], y[PARTS];
+                split<PARTS>(p[0], x);
+                split<PARTS>(p[1], y);
+#pragma unroll
+                for (int i = 0; i < PARTS; ++i) {
+                    const T pair[2] = {x[i], y[i]};
+                    low[i][s][h] = *reinterpret_cast<const uint32_t*>(pair);
+                }
             }
     }
     float back[2];
@@ -445,18 +449,17 @@ __global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kern
 #pragma unroll
             for (int c = 0; c < 4; ++c) acc[j][c] = 0.f;
         if (rank > 0) {
+            // (the last part first: every addition is cut to 32 bits, and those that come before the first part are small)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int i = PARTS - 1; i >= 0; --i)
 #pragma unroll
-                for (int s = 0; s < kWords; ++s) {
-                    const uint4 w = b_ahead[j][s];
-                    mma<T>(acc[j], hi[2 * s][0], hi[2 * s][1], hi[2 * s][2], hi[2 * s][3], w.x, w.y);
-                    mma<T>(acc[j], lo[2 * s][0], lo[2 * s][1], lo[2 * s][2], lo[2 * s][3], w.x, w.y);
-                    if constexpr (RT > 1) {
-                        mma<T>(acc[j], hi[2 * s + 1][0], hi[2 * s + 1][1], hi[2 * s + 1][2], hi[2 * s + 1][3], w.z, w.w);
-                        mma<T>(acc[j], lo[2 * s + 1][0], lo[2 * s + 1][1], lo[2 * s + 1][2], lo[2 * s + 1][3], w.z, w.w);
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int s = 0; s < kWords; ++s) {
+                        const uint4 w = b_ahead[j][s];
+                        mma<T>(acc[j], low[i][2 * s][0], low[i][2 * s][1], low[i][2 * s][2], low[i][2 * s][3], w.x, w.y);
+                        if constexpr (RT > 1) mma<T>(acc[j], low[i][2 * s + 1][0], low[i][2 * s + 1][1], low[i][2 * s + 1][2], low[i][2 * s + 1][3], w.z, w.w);
                     }
-                }
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
@@ -499,8 +502,10 @@ cudaError_t launch_few(const AdapterArgs& a, const AdapterLayout& l, cudaStream_
     int64_t per = (groups + runs - 1) / runs;
     if (per < 2) per = 2;
     const int64_t run = per * 32 * kFewWarps;
-    err = launch_chained(adapter_up_kernel<T, RT>, dim3((unsigned)l.max_tiles, (unsigned)((a.n + run - 1) / run)), dim3(kFewWarps * 32), 4 * (size_t)kFewTile * (16 * RT + 4), st, a, l, splits,
-                         run, vec_b, vec_d);
+    const dim3 grid((unsigned)l.max_tiles, (unsigned)((a.n + run - 1) / run)), block(kFewWarps * 32);
+    const size_t smem = 4 * (size_t)kFewTile * (16 * RT + 4);
+    err = a.d_type == kF32 ? launch_chained(adapter_up_kernel<T, RT, 3>, grid, block, smem, st, a, l, splits, run, vec_b, vec_d)
+                           : launch_chained(adapter_up_kernel<T, RT, 2>, grid, block, smem, st, a, l, splits, run, vec_b, vec_d);
     if (err == cudaSuccess) ++launches[1];
     return err;
 }

@@ -6,6 +6,7 @@ namespace gemm2m {
 
 constexpr int kFewTokens = 256;           // up to here the first form, whose blocks find their tile themselves; beyond, a kernel sorts the tokens first
 constexpr int kFewTile = 16, kManyTile = 128;
+constexpr int kParts = 3;                 // 16-bit numbers that hold a 32-bit one
 
 struct AdapterTile { int32_t key, start, count, rank; };     // key = adapter, or `adapters`: tokens without one; start: in the sorted list; rank in use
 struct AdapterLayout {
@@ -25,13 +26,18 @@ __device__ __forceinline__ int rank_of(const AdapterArgs& a, int key) {
 template <typename T> __device__ __forceinline__ float largest() { return 3.3895314e38f; }
 template <> __device__ __forceinline__ float largest<__half>() { return 65504.f; }
 
-// v as hi + lo of 16 bits.  What is not finite stays in hi; what is too large (beside something that is not finite) saturates.
-template <typename T>
-__device__ __forceinline__ void split2(float v, T* hi, T* lo) {
+// v as the sum of 16-bit numbers, each what the ones before left: three hold all bits of a 32-bit number (8 each for bf16, 11 for fp16), two 2^-17 of it (bf16) or 2^-22 (fp16).  What is
+// not finite stays in the first; what is too large (beside something that is not finite) saturates.
+template <int PARTS, typename T>
+__device__ __forceinline__ void split(float v, T (&part)[PARTS]) {
     const bool finite = (__float_as_uint(v) & 0x7f800000u) != 0x7f800000u;
     if (finite) v = fminf(fmaxf(v, -largest<T>()), largest<T>());
-    *hi = from_float<T>(v);
-    *lo = finite ? from_float<T>(v - to_float<T>(*hi)) : T(0.f);
+    part[0] = from_float<T>(v);
+#pragma unroll
+    for (int p = 1; p < PARTS; ++p) {
+        v = finite ? v - to_float<T>(part[p - 1]) : 0.f;
+        part[p] = from_float<T>(v);
+    }
 }
 
 // 2^-s for a row whose largest magnitude is in [2^e, 2^(e+1)), and 2^s; 1 where that is not finite.  fp16: s = e - 14, near the top of its range, so that entries far below the largest keep

@@ -3,7 +3,7 @@
 // L = X A_a^T: a cluster takes a tile, each of its blocks a piece of k, in steps of 64 entries (one 128-byte swizzle row): four MMAs of 128 x rank x 16 per step.  The tile's
 // rows of X lie anywhere, so they come by asynchronous 16-byte copies (8- and 4-byte ones where rows start there), three or four steps ahead.  The blocks then add their
 // pieces up through one another's shared memory, each for a part of the rows, in the order of k.
-// D = C + L B_a^T: all tiles' pieces of 128 columns are cut into even runs, one per block, which goes through the (at most few) tiles of its run.  L, as hi + lo, stays in shared memory; the MMAs of one piece run while the one before is
+// D = C + L B_a^T: all tiles' pieces of 128 columns are cut into even runs, one per block, which goes through the (at most few) tiles of its run.  L, as two or three 16-bit numbers, stays in shared memory; the MMAs of one piece run while the one before is
 // read back, added to what was fetched of C a piece earlier, and stored.  The read-back hands a lane pairs of columns 8 apart; the rows of B
 // lie in shared memory in such an order that these are eight neighbouring columns of D.
 // Both are bound by memory and the hand-overs between copies, MMAs and read-back (8192 tokens, 8192 to 8192 columns, 8 adapters of rank 64, bf16: 31 us, X at 4.4 TB/s, and
@@ -222,9 +222,9 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
     }
     frame.close(kTmemCols);
     cluster_sync_all();
-    // a warp per row: the pieces added up, times s_a, the largest entry brought well inside the range, as two 16-bit numbers
+    // a warp per row: the pieces added up, times s_a, the largest entry brought well inside the range, as three 16-bit numbers
     const float scale = a.scales ? a.scales[tile.key] : 1.f;
-    T* low = (T*)(a.ws + l.off_low) + (int64_t)tile.start * (2 * RP);
+    T* low = (T*)(a.ws + l.off_low) + (int64_t)tile.start * (kParts * RP);
     float* backs = (float*)(a.ws + l.off_back) + tile.start;
     for (int r = part * (kThreads / 32) + warp; r < tile.count; r += splits * (kThreads / 32)) {
         constexpr int kPairs = (RP + 63) / 64;
@@ -249,13 +249,15 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
 #pragma unroll
         for (int b = 0; b < kPairs; ++b) {
             const int c = b * 64 + lane * 2;
-            T hi[2], lo[2];
-            split2<T>(v[b].x * down, &hi[0], &lo[0]);
-            split2<T>(v[b].y * down, &hi[1], &lo[1]);
-            if (c < RP) {
-                *reinterpret_cast<uint32_t*>(low + r * (2 * RP) + c) = *reinterpret_cast<const uint32_t*>(hi);
-                *reinterpret_cast<uint32_t*>(low + r * (2 * RP) + RP + c) = *reinterpret_cast<const uint32_t*>(lo);
-            }
+            T x[kParts], y[kParts];
+            split<kParts>(v[b].x * down, x);
+            split<kParts>(v[b].y * down, y);
+            if (c < RP)
+#pragma unroll
+                for (int i = 0; i < kParts; ++i) {
+                    const T pair[2] = {x[i], y[i]};
+                    *reinterpret_cast<uint32_t*>(low + (r * kParts + i) * RP + c) = *reinterpret_cast<const uint32_t*>(pair);
+                }
         }
         if (lane == 0) backs[r] = back;
     }
@@ -263,12 +265,15 @@ __global__ void __launch_bounds__(kThreads, 2) adapter_down_many_kernel(const Ad
 }
 
 // DT: type of C and D; KB: blocks of 64 along the rank.  (The operands' 16-bit type is the instruction descriptor's matter.)  VEC: rows of C and D are whole 16-byte pieces;
-// otherwise a warp turns each 32 x 32 columns in shared memory and reads and writes row by row, a lane per column (a lane's own eight columns, entry by
+// otherwise a warp turns each 16 rows x 32 columns in shared memory and reads and writes row by row, a lane per column (a lane's own eight columns, entry by
 // entry, would be as many sectors per instruction as there are lanes: 1001 tokens, 1999 columns: 38 us in all, 29 so).
 constexpr int up_blocks(int KB) { return KB == 1 ? 2 : 1; }       // on an SM
-constexpr int kTurnPitch = 36, kTurnBytes = 32 * kTurnPitch * 4;                     // of a warp
+// Parts of L that the product takes: a 16-bit D's rounding hides the third.
+template <typename DT> __host__ __device__ constexpr int parts_of() { return sizeof(DT) == 4 ? kParts : 2; }
+constexpr int kTurnRows = 16, kTurnPitch = 36, kTurnBytes = kTurnRows * kTurnPitch * 4;      // of a warp: half of its rows at a time
 template <typename DT, int KB, int ALIGN, bool VEC>
 __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kernel(const AdapterArgs a, const AdapterLayout l, int run_align, uint32_t idesc) {
+    constexpr int PARTS = parts_of<DT>();
     constexpr int kTmemCols = 256, E = 16 / (int)sizeof(DT), kAccesses = 8 / E;      // eight columns of a row per lane, E in one access
     extern __shared__ unsigned char smem_raw[];
     __shared__ uint64_t bars[4];
@@ -283,12 +288,12 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
     DT* D = (DT*)a.D;
     Frame<2> frame;
     frame.open(bars, kTmemCols, a.dev_status);
-    const uint32_t low_hi = (smem_u32(smem_raw) + 1023u) & ~1023u, low_lo = low_hi + KB * kOperandBytes, b_base = low_lo + KB * kOperandBytes;
+    const uint32_t low_base = (smem_u32(smem_raw) + 1023u) & ~1023u, b_base = low_base + PARTS * KB * kOperandBytes;
     // this thread copies piece `piece` (and `piece` + 8) of rows, or columns, c0, c0 + 32, ... of 128; columns 8q + 2j + e of every 32 are rows 8j + 2q + e of B's tile
     const int piece = threadIdx.x & 7, c0 = threadIdx.x >> 3;
     const uint32_t b_dst = swizzled(b_base, (c0 & 6) << 2 | (c0 & 24) >> 2 | (c0 & 1), piece);
     const int quarter = warp & 3, half = warp >> 2, g = lane >> 2, q = lane & 3;
-    float* turn = reinterpret_cast<float*>(smem_raw + (low_hi - smem_u32(smem_raw)) + 4 * KB * kOperandBytes + warp * kTurnBytes);      // (not VEC)
+    float* turn = reinterpret_cast<float*>(smem_raw + (low_base - smem_u32(smem_raw)) + (PARTS + 2) * KB * kOperandBytes + warp * kTurnBytes);      // (not VEC)
 
     uint32_t it = 0;                                     // pieces so far: buffer it % 2, its use number it / 2
     bool ok = true;
@@ -338,7 +343,7 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
         // (the MMAs that read the last tile's L and B have been waited for by every thread, and all of them have passed its last barrier since)
         load_b(0);
         {
-            const uint16_t* low = (const uint16_t*)(a.ws + l.off_low) + (int64_t)tile.start * (2 * l.padded);
+            const uint16_t* low = (const uint16_t*)(a.ws + l.off_low) + (int64_t)tile.start * (kParts * l.padded);
 #pragma unroll
             for (int k = 0; k < kManyTile / 32; ++k) {
                 const int r = c0 + 32 * k;
@@ -346,9 +351,9 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
 #pragma unroll
                     for (int b = 0; b < KB; ++b)
                         if (b * 8 + piece < width) {
-                            const uint32_t dst = swizzled(low_hi + b * kOperandBytes, r, piece);
-                            copy8(dst, low + r * (2 * l.padded), (b * 8 + piece) * 8, l.padded, 16);
-                            copy8(dst + KB * kOperandBytes, low + r * (2 * l.padded) + l.padded, (b * 8 + piece) * 8, l.padded, 16);
+                            const uint32_t dst = swizzled(low_base + b * kOperandBytes, r, piece);
+#pragma unroll
+                            for (int i = 0; i < PARTS; ++i) copy8(dst + i * KB * kOperandBytes, low + (r * kParts + i) * l.padded, (b * 8 + piece) * 8, l.padded, 16);
                         }
             }
         }
@@ -414,13 +419,15 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
                 tcgen05_fence_after();
                 const uint32_t b = b_base + buf * (KB * kOperandBytes), d = frame.tmem + buf * kManyTile;
                 if (elect_lane()) {
-                    for (int s = 0; s < ksteps; ++s) {
-                        const uint32_t block = (uint32_t)(s >> 2) * kOperandBytes;
-                        const uint64_t in_row = (uint64_t)((s & 3) * 2);
-                        const uint64_t bdesc = make_smem_desc(b + block) + in_row;
-                        umma_f16(d, make_smem_desc(low_hi + block) + in_row, bdesc, idesc, (uint32_t)(s != 0));
-                        umma_f16(d, make_smem_desc(low_lo + block) + in_row, bdesc, idesc, 1u);
-                    }
+                    // (the last part first: every addition is cut to 32 bits, and those that come before the first part are small)
+#pragma unroll
+                    for (int i = PARTS - 1; i >= 0; --i)
+                        for (int s = 0; s < ksteps; ++s) {
+                            const uint32_t block = (uint32_t)(s >> 2) * kOperandBytes;
+                            const uint64_t in_row = (uint64_t)((s & 3) * 2);
+                            umma_f16(d, make_smem_desc(low_base + i * KB * kOperandBytes + block) + in_row, make_smem_desc(b + block) + in_row, idesc,
+                                     (uint32_t)(s != 0 || i != PARTS - 1));
+                        }
                     umma_commit(frame.bars + 8 * buf);
                 }
                 __syncwarp();
@@ -455,24 +462,27 @@ __global__ void __launch_bounds__(kThreads, up_blocks(KB)) adapter_up_many_kerne
                         else if (there[i]) store8_as<DT>(D + place_d[i] + col, x, false, a.n - col);
                     }
                 } else {
-                    __syncwarp();                            // the columns before have been read
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        float x[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]) * back[i];
-                        float4* to = reinterpret_cast<float4*>(turn + (i * 8 + g) * kTurnPitch + q * 8);
-                        to[0] = make_float4(x[0], x[1], x[2], x[3]);
-                        to[1] = make_float4(x[4], x[5], x[6], x[7]);
-                    }
-                    __syncwarp();
                     DT* D_col = D + col;
                     const int rows_stored = col < a.n ? rows_here : 0;
 #pragma unroll
-                    for (int r = 0; r < 32; ++r) {
-                        const DT out = from_float<DT>(to_float<DT>(in_rows[r]) + turn[r * kTurnPitch + lane]);
-                        DT* place = D_col + __shfl_sync(0xffffffffu, place_d[0], r);
-                        if (r < rows_stored) *place = out;
+                    for (int r0 = 0; r0 < 32; r0 += kTurnRows) {
+                        __syncwarp();                        // the rows and columns before have been read
+#pragma unroll
+                        for (int i = r0 / 8; i < (r0 + kTurnRows) / 8; ++i) {
+                            float x[8];
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) x[j] = __uint_as_float(v[i >> 1][(j >> 1) * 4 + (i & 1) * 2 + (j & 1)]) * back[i];
+                            float4* to = reinterpret_cast<float4*>(turn + (i * 8 + g - r0) * kTurnPitch + q * 8);
+                            to[0] = make_float4(x[0], x[1], x[2], x[3]);
+                            to[1] = make_float4(x[4], x[5], x[6], x[7]);
+                        }
+                        __syncwarp();
+#pragma unroll
+                        for (int r = r0; r < r0 + kTurnRows; ++r) {
+                            const DT out = from_float<DT>(to_float<DT>(in_rows[r]) + turn[(r - r0) * kTurnPitch + lane]);
+                            DT* place = D_col + __shfl_sync(0xffffffffu, place_d[0], r);
+                            if (r < rows_stored) *place = out;
+                        }
                     }
                 }
                 if (VEC ? t < here : t < here || p == 0) fetch(VEC || p == 1 ? t : t - 1, VEC ? p : p ^ 1);
@@ -521,7 +531,8 @@ cudaError_t launch_down(const AdapterArgs& a, const AdapterLayout& l, cudaStream
 
 template <typename DT, int KB, int ALIGN, bool VEC>
 cudaError_t launch_up_as(const AdapterArgs& a, const AdapterLayout& l, int align, cudaStream_t st) {
-    constexpr size_t smem = (size_t)4 * KB * kOperandBytes + (VEC ? 0 : kThreads / 32 * kTurnBytes) + 1024;
+    constexpr size_t smem = (size_t)(parts_of<DT>() + 2) * KB * kOperandBytes + (VEC ? 0 : kThreads / 32 * kTurnBytes) + 1024;
+    static_assert(up_blocks(KB) * (smem + 1024) <= 228 * 1024, "the blocks that the grid counts on fit an SM");
     cudaError_t err = set_smem(adapter_up_many_kernel<DT, KB, ALIGN, VEC>, smem);
     if (err != cudaSuccess) return err;
     // as many blocks as the GPU holds, or one for every piece that there can be

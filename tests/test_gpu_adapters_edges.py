@@ -22,3 +22,70 @@ def test_small_numbers_times_large_ones(tokens, rank, x_size, a_size, w_size):
     want, size, beside = plain(x, a, w, index, None, None, None)
     off, most = (d.double() - want).abs(), room(64, rank, want, size, beside, torch.bfloat16, torch.float32)
     assert bool((off <= most).all()), float((off / most).max())
+
+
+def exact_room(k, rank, want, size):
+    """Without any allowance for parts of L: products of 16-bit numbers are exact; sums of k and of 3 rank terms with up to 40 pieces, of which random roundings leave
+    the root; the scale, the power of two, C, and D's own rounding."""
+    return size * (k + 3 * rank + 48) ** 0.5 * 2.0 ** -23 + 2.0 ** -23 * want.abs()
+
+
+@pytest.mark.parametrize("tokens,k,n,many,rank", [(1, 64, 40, 1, 1), (40, 256, 320, 3, 16), (40, 100, 33, 3, 30), (200, 64, 256, 2, 64), (256, 96, 90, 5, 128),
+                                                  (600, 256, 320, 3, 16), (300, 100, 333, 3, 30), (700, 64, 256, 2, 64), (513, 96, 130, 5, 128), (300, 64, 129, 2, 65)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_outputs_of_32_bits_are_those_of_32_bit_sums(tokens, k, n, many, rank, dtype):
+    x, a, w, index, c, scales, _ = operands(tokens, k, n, many, rank, dtype, 21, torch.float32, ranks=False, bare=False)
+    d = torch.empty(tokens, n, device="cuda")
+    with workspace(tokens, rank, many) as ws:
+        ws.buf[4096:].fill_(0xff)
+        for add in (None, c):
+            b.adapter_add(x, a, w, index, d, C=add, scales=scales)
+            b.device_status()
+            want, size, _ = plain(x, a, w, index, add, scales, None)
+            off, most = (d.double() - want).abs(), exact_room(k, rank, want, size)
+            # In the mean the error is that of sums in 32 bits, relative to their partial sums, whose size is the root of the sum of the terms' squares.  (Not of the result: with one
+            # token and rank 1 all entries share the error of one sum L, and |L| may be an eighth of the root of 64 terms' squares.)  The tensor cores add 16 products at once and cut the
+            # sum, by up to 2^-23 of it and half of that in the mean, always towards zero, so that cuts add up: k / 16 for L, rank / 16 for the update, 2^-24 each; the parts beside the
+            # first are below 2^-8 of it and their cuts of no account; four roundings behind.
+            squares = torch.zeros_like(want) if add is None else add.double().square()
+            for i in range(many):
+                rows = (index == i).nonzero()[:, 0]
+                squares[rows] += float(scales[i]) ** 2 * (x[rows].double().square() @ a[i].double().square().t()) @ w[i].double().square().t()
+            terms = torch.maximum(want.abs(), squares.sqrt())
+            assert float(torch.linalg.vector_norm(off) / torch.linalg.vector_norm(terms)) <= (4 + (k + rank) / 16) * 2.0 ** -24
+            assert bool((off <= most).all()), float((off / most).max())
+
+
+@pytest.mark.parametrize("tokens", [30, 300])
+def test_outputs_of_32_bits_cancel_what_was_there(tokens):
+    """C holds the update with the opposite sign: what is left is the rounding of 32 bits, not of the parts that the product took."""
+    x, a, w, index, _, scales, _ = operands(tokens, 128, 70, 2, 8, torch.bfloat16, 31, ranks=False, bare=False)
+    update, size, _ = plain(x, a, w, index, None, scales, None)
+    d = torch.empty(tokens, 70, device="cuda")
+    with workspace(tokens, 8, 2):
+        b.adapter_add(x, a, w, index, d, C=-update.float(), scales=scales)
+    assert bool((d.abs().double() <= exact_room(128, 8, update, size)).all())
+
+
+@pytest.mark.parametrize("tokens,k,n,many,rank", [(1, 500, 40, 1, 2), (40, 256, 320, 3, 16), (37, 1000, 33, 3, 30), (200, 256, 256, 2, 64), (256, 600, 90, 5, 128),
+                                                  (600, 256, 320, 3, 16), (300, 1000, 333, 3, 30), (700, 256, 256, 2, 64), (513, 400, 130, 5, 128)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_whole_numbers_are_exact(tokens, k, n, many, rank, dtype):
+    """Every sum is a whole number below 2^24 and needs more bits than two 16-bit numbers hold (16 and 22): nothing may be rounded anywhere.  Two entries of B per column are not
+    zero.  |L| is below 6 x 127^2 / 3 sqrt(1000) < 2^20 (bf16) or 6 x 2047 x 511 / 3 sqrt(k) with k <= 16 entries < 2^23."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(tokens)
+    whole = lambda most, *shape: torch.randint(-most, most + 1, shape, generator=g, device="cuda").float()
+    x, a = (whole(127, tokens, k), whole(127, many, rank, k)) if dtype == torch.bfloat16 else (whole(2047, tokens, k), whole(511, many, rank, k))
+    if dtype == torch.float16:
+        a[:, :, 16:] = 0
+    w = torch.zeros(many, n, rank, device="cuda")
+    for _ in range(2):
+        w.scatter_(2, torch.randint(0, rank, (many, n, 1), generator=g, device="cuda"), whole(1, many, n, 1))
+    x, a, w = x.to(dtype), a.to(dtype), w.to(dtype)
+    index = torch.randint(0, many, (tokens,), generator=g, device="cuda").to(torch.int32)
+    c, d = whole(1000, tokens, n), torch.empty(tokens, n, device="cuda")
+    with workspace(tokens, rank, many):
+        b.adapter_add(x, a, w, index, d, C=c)
+    want = plain(x, a, w, index, c, None, None)[0]
+    assert float(want.abs().max()) < 2 ** 24 and bool((d.double() == want).all())
