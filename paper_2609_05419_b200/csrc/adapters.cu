@@ -317,6 +317,21 @@ __device__ __forceinline__ void floats_of(const uint4 (&r)[2], int type, float (
     else if (type == kF16) to_floats8<__half>({r[0]}, v);
     else to_floats8<__nv_bfloat16>({r[0]}, v);
 }
+// Eight entries as raw8_of read them back to memory, the first `valid` of them.
+__device__ __forceinline__ void store8_raw(char* p, int bytes, int64_t valid, bool vec, const uint4 (&r)[2]) {
+    if (vec && valid >= 8) {
+        reinterpret_cast<uint4*>(p)[0] = r[0];
+        if (bytes == 4) reinterpret_cast<uint4*>(p)[1] = r[1];
+        return;
+    }
+    const uint32_t w[8] = {r[0].x, r[0].y, r[0].z, r[0].w, r[1].x, r[1].y, r[1].z, r[1].w};
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+        if (j < valid) {
+            if (bytes == 4) reinterpret_cast<uint32_t*>(p)[j] = w[j];
+            else reinterpret_cast<uint16_t*>(p)[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+        }
+}
 __device__ __forceinline__ void store8_of(void* p, int type, int64_t at, int64_t valid, bool vec, const float (&v)[8]) {
     const bool whole = vec && valid >= 8;
     if (type == kF32) store8_as<float>((float*)p + at, v, whole, valid);
@@ -442,6 +457,25 @@ __global__ void __launch_bounds__(kFewWarps * 32, up_blocks(RT)) adapter_up_kern
     float back[2];
 #pragma unroll
     for (int i = 0; i < 2; ++i) back[i] = rank > 0 ? backs[i * 8 + g] : 0.f;
+    if (rank == 0) {                                         // D = C, bit for bit, or zero (a branch for this in the loop below costs all other tiles 3 %)
+        constexpr int kSteps = 2;
+        for (int64_t n0 = first + warp * 32; n0 < last; n0 += kSteps * kStride) {
+            uint4 c[kSteps][2][2] = {};
+            if (a.C)
+#pragma unroll
+                for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) raw8_of((const char*)a.C + row[i] * a.ldc * es, n0 + s * kStride + 8 * q, a.n, es, vec_d && a.n % 8 == 0, c[s][i]);
+#pragma unroll
+            for (int s = 0; s < kSteps; ++s)
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int64_t col = n0 + s * kStride + 8 * q;
+                    if (there[i] && n0 + s * kStride < last && col < a.n) store8_raw((char*)a.D + (row[i] * a.ldd + col) * es, es, a.n - col, vec_d, c[s][i]);
+                }
+        }
+        return;
+    }
     for (int64_t n0 = first + warp * 32; n0 < last; n0 += kStride) {
         float acc[4][4], v[2][8];
 #pragma unroll

@@ -89,3 +89,26 @@ def test_whole_numbers_are_exact(tokens, k, n, many, rank, dtype):
         b.adapter_add(x, a, w, index, d, C=c)
     want = plain(x, a, w, index, c, None, None)[0]
     assert float(want.abs().max()) < 2 ** 24 and bool((d.double() == want).all())
+
+
+@pytest.mark.parametrize("tokens", [1, 9, 256, 257])
+@pytest.mark.parametrize("n,skip", [(40, 0), (41, 0), (300, 0), (64, 1)])
+@pytest.mark.parametrize("d_type", [torch.float32, torch.float16, torch.bfloat16])
+def test_rows_without_an_adapter_are_those_of_c_bit_for_bit(tokens, n, skip, d_type):
+    """Negative zeros, NaN with payloads and subnormals among them; no adapter, or one of rank 0."""
+    x, a, w, index, c, _, _ = operands(tokens, 64, n, 3, 20, torch.bfloat16, 41, d_type, ranks=False)
+    index[::2] = -1
+    used = torch.tensor([20, 0, 7], dtype=torch.int32, device="cuda")
+    whole = torch.int32 if d_type == torch.float32 else torch.int16
+    odd = {torch.float32: [-2 ** 31, 0x7f812345, -0x3fedcb, 1, -2 ** 31 + 1], torch.float16: [-2 ** 15, 0x7d23, -0x2ed, 1, -2 ** 15 + 1],
+           torch.bfloat16: [-2 ** 15, 0x7fa3, -0x5d, 1, -2 ** 15 + 1]}[d_type]
+    c.view(whole)[:, :len(odd) * 7:7] = torch.tensor(odd, dtype=whole, device="cuda")[:c[:, :len(odd) * 7:7].shape[1]]
+    store = torch.full((tokens, n + 9), 3.0, device="cuda").to(d_type)
+    d = store[:, skip:skip + n]
+    with workspace(tokens, 20, 3):
+        b.adapter_add(x, a, w, index, d, C=c, ranks=used)
+        bare = (index < 0) | (index == 1)
+        assert torch.equal(d[bare].view(whole), c[bare].view(whole))
+        b.adapter_add(x, a, w, index, d, ranks=used)
+        assert bool((d[bare].view(whole) == 0).all())
+    assert bool((store[:, :skip] == 3).all()) and bool((store[:, skip + n:] == 3).all())
