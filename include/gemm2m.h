@@ -297,8 +297,9 @@ int gemm2m_newton_schulz(int64_t batch, int64_t m, int64_t n, const void* G, int
  *   H = X + R rounded to its type (R NULL: H = X);  rstd_i = 1 / sqrt(mean_j H_ij^2 + eps);  N_ij = H_ij rstd_i W_j, held in 32 bits.
  * Outputs, each may be NULL, at least one is not: H, Y = N rounded, rstd (rows), and N quantised exactly as gemm2m_fp8_quantise does it with
  * block_rows = 1 (fmt E4M3 / E5M2): Q, S with blocks along the rows, Qt, St with blocks along the columns.  H may be X or R, entry on entry; no
- * other output may overlap an input.  The norm reads H as stored.  A row whose sum of squares leaves the 32-bit range gives zeros (NaN where
- * H is infinite); a NaN makes its row NaN, and the scales of the blocks that it is in.
+ * other output may overlap an input.  The norm reads H as stored.  Squares and their sum may leave the 32-bit range (they
+ * are then formed of H times a power of two), rstd and N are 32-bit numbers: a row whose root mean square, with eps, is below 2^-128 (zeros with eps = 0) gives Inf or NaN.  A row
+ * with an infinite entry gives rstd = 0, zeros, and NaN where H is infinite; a NaN makes its row NaN, and the scales of the blocks that it is in.
  * Workspace: GEMM2M_OP_RMS_NORM with (rows, cols), needed for Qt where rstd is NULL. */
 int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t ldx, const void* R, int64_t ldr, const void* W, int w_type, float eps,
                     void* H, int64_t ldh, void* Y, int64_t ldy, int fmt, void* Q, int64_t ldq, float* S, int64_t lds, void* Qt, int64_t ldqt,

@@ -157,20 +157,21 @@ __device__ __forceinline__ float over_warp(float (&v)[NV], F&& f) {
     return v[0];
 }
 
-// Sums over the segments of each thread's sums of its places.  `segments`: one number per 256 columns of this row, in shared memory; every thread of the block takes part.
+// Sums over the segments of each thread's sums of its places: a lane has that of one of them.  `segments`: one number per 256 columns of this row, in shared memory, to be read behind a barrier.
 template <int NV>
-__device__ __forceinline__ void segment_sums(float (&places)[NV], float* segments, int warp_in_row, int warps, int count) {
+__device__ __forceinline__ float segment_sums(float (&places)[NV], float* segments, int warp_in_row, int warps, int count) {
     const int lane = threadIdx.x & 31;
     const float mine = over_warp<NV>(places, [](float x, float y) { return x + y; });
     constexpr int kShift = NV == 4 ? 3 : NV == 2 ? 4 : 5;
     const int segment = (lane >> kShift) * warps + warp_in_row;
     if ((lane & ((1 << kShift) - 1)) == 0 && segment < count) segments[segment] = mine;
-    __syncthreads();
+    return mine;
 }
-// Sum over a row, in the order of the columns.
+// Sum over a row, in the order of the columns; every thread of the block takes part.
 template <int NV>
 __device__ __forceinline__ float row_sum(float (&places)[NV], float* segments, int warp_in_row, int warps, int count) {
     segment_sums<NV>(places, segments, warp_in_row, warps, count);
+    __syncthreads();
     float sum = 0.f;
 #pragma unroll 4
     for (int i = 0; i < count; ++i) sum += segments[i];

@@ -6,7 +6,7 @@ from paper_2609_05419_b200 import binding as b
 
 pytestmark = pytest.mark.gpu
 
-from test_gpu_rms_norm import plain, stream  # noqa: E402
+from test_gpu_rms_norm import gen, plain, stream  # noqa: E402
 
 
 @pytest.mark.parametrize("rows,cols", [(4000, 4096), (4000, 1999), (200, 4000), (3000, 8000)])
@@ -28,3 +28,56 @@ def test_gradient_of_a_constant_row_along_itself_is_zero(cols, dtype):
     dx = torch.full_like(one, float("nan"))
     b.rms_norm_backward(one, one, None, torch.ones(3, device="cuda"), dx)      # 1 - 1 x mean of ones
     assert bool((dx == 0).all())
+
+
+@pytest.mark.parametrize("rows,cols", [(5, 3), (5, 300), (4, 4096), (300, 700), (600, 1000), (9, 8200), (3, 20001)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("residual,keep", [(False, False), (True, False), (True, True)])
+def test_squares_beyond_the_32_bit_range(rows, cols, dtype, residual, keep):
+    """Rows of sizes from 1e-37 to 1e37 beside one another, without an epsilon: their norm is of size 1."""
+    size = 10.0 ** torch.linspace(-37, 37, rows, device="cuda", dtype=torch.float64)[torch.randperm(rows, generator=gen(5), device="cuda")]
+    draw = lambda seed: (torch.randn(rows, cols, generator=gen(seed), device="cuda").clamp(-5, 5).double() * size[:, None]).to(dtype)
+    x, r = draw(7), draw(8) if residual else None
+    w = 1 + 0.3 * torch.randn(cols, generator=gen(9), device="cuda")
+    h, y, rstd = torch.empty_like(x), torch.empty_like(x), torch.empty(rows, device="cuda")
+    qt, st = b.fp8_empty(cols, rows)
+    b.rms_norm(x, w, R=r, H=h if keep else None, Y=y, rstd=rstd, Qt=qt, St=st, eps=0.0)
+    stored, want, n = plain(x, r, w, 0.0)
+    assert not keep or torch.equal(h, stored)
+    # 1.5 roundings of rstd, two of N, one of Y; H itself is of 24 bits or 8 down to 2^-126, N of size 1 and its entries not below 2^-100
+    assert bool(((rstd.double() - want) / want).abs().max() <= 3 * 2.0 ** -24)
+    step = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}[dtype]
+    assert bool(((y.double() - n).abs() <= (5 * 2.0 ** -24 + step * 1.001) * n.abs() + 2.0 ** -126).all())
+    assert bool(torch.isfinite(st).all())
+
+
+def test_squares_beyond_the_range_in_place_and_the_same_for_any_alignment():
+    rows, cols = 20, 1000
+    x = torch.randn(rows, cols, generator=gen(11), device="cuda") * 10.0 ** torch.linspace(-36, 36, rows, device="cuda", dtype=torch.float64)[:, None].float()
+    r = 0.5 * x.flip(1)
+    want, rstd = torch.empty_like(x), torch.empty(rows, device="cuda")
+    b.rms_norm(x, R=r, Y=want, rstd=rstd, eps=0.0)
+    for skip in (0, 1):
+        store = torch.zeros(rows * cols + 1, device="cuda")
+        h = store[skip:skip + rows * cols].view(rows, cols)
+        h.copy_(x)
+        y, got = torch.empty_like(x), torch.empty(rows, device="cuda")
+        b.rms_norm(h, R=r, H=h, Y=y, rstd=got, eps=0.0)
+        assert torch.equal(h, x + r) and torch.equal(got, rstd) and torch.equal(y, want)
+    many = torch.empty(400 * rows, device="cuda")
+    b.rms_norm(x.repeat(400, 1), R=r.repeat(400, 1), rstd=many, eps=0.0)
+    assert torch.equal(many.view(400, rows), rstd.expand(400, rows))
+
+
+@pytest.mark.parametrize("cols", [512, 4096, 32768])
+def test_a_sum_that_overflows_although_no_part_of_it_does(cols):
+    """Every segment of 256 columns sums to less than 2^128, the row does not."""
+    x = torch.full((3, cols), 2.0 ** 59.7, device="cuda")
+    x[1] = 1.0
+    rstd = torch.empty(3, device="cuda")
+    b.rms_norm(x, rstd=rstd, eps=0.0)
+    assert bool(((rstd.double() - 1 / x[:, 0].double()).abs() <= 2.0 ** -23 / x[:, 0].double()).all())
+    alone = torch.empty(1, device="cuda")
+    for row in range(3):
+        b.rms_norm(x[row:row + 1], rstd=alone, eps=0.0)
+        assert torch.equal(alone[0], rstd[row])
