@@ -228,9 +228,10 @@ bool adapter_sizes_ok(int64_t tokens, int64_t rank, int64_t adapters) {
 // Memory that a tensor spans, to find outputs that overlap something else.
 struct Span { uintptr_t begin, end; int64_t row, width; bool written; };      // bytes; row = distance of rows, width = of entries in a row
 bool spans_meet(const Span& a, const Span& b) {          // a.begin <= b.begin < a.end
-    if (a.row != b.row || a.row == a.width || b.row == b.width) return true;
-    const int64_t at = (int64_t)(b.begin - a.begin) % a.row;       // views of one matrix side by side: where b's rows begin between a's
-    return at < a.width || at + b.width > a.row;
+    // a without gaps; or rows of different distances, which are not looked at one by one (b may be a single row, or without gaps)
+    if (a.row == a.width || (b.row != a.row && b.row != b.width)) return true;
+    const int64_t at = (int64_t)(b.begin - a.begin) % a.row, width = b.row == a.row ? b.width : (int64_t)(b.end - b.begin);
+    return at < a.width || at + width > a.row;           // views of one matrix side by side: where b's rows begin between a's
 }
 bool gradients_apart(const std::vector<GradTensor>& t) {
     std::vector<Span> spans;
