@@ -297,7 +297,7 @@ int gemm2m_newton_schulz(int64_t batch, int64_t m, int64_t n, const void* G, int
  *   H = X + R rounded to its type (R NULL: H = X);  rstd_i = 1 / sqrt(mean_j H_ij^2 + eps);  N_ij = H_ij rstd_i W_j, held in 32 bits.
  * Outputs, each may be NULL, at least one is not: H, Y = N rounded, rstd (rows), and N quantised exactly as gemm2m_fp8_quantise does it with
  * block_rows = 1 (fmt E4M3 / E5M2): Q, S with blocks along the rows, Qt, St with blocks along the columns.  H may be X or R, entry on entry; no
- * other output may overlap an input.  The norm reads H as stored.  Squares and their sum may leave the 32-bit range (they
+ * other output may overlap an input, nor another output (such calls are refused).  The norm reads H as stored.  Squares and their sum may leave the 32-bit range (they
  * are then formed of H times a power of two), rstd and N are 32-bit numbers: a row whose root mean square, with eps, is below 2^-128 (zeros with eps = 0) gives Inf or NaN.  A row
  * with an infinite entry gives rstd = 0, zeros, and NaN where H is infinite; a NaN makes its row NaN, and the scales of the blocks that it is in.
  * Workspace: GEMM2M_OP_RMS_NORM with (rows, cols), needed for Qt where rstd is NULL. */
@@ -309,7 +309,7 @@ int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t
  * forward pass left them: with n = H rstd,
  *   dX = rstd (dY W - n mean_j(dY W n)) + dR,   dW = sum_i dY n, or dW + that sum where `add` is not 0.
  * dX is the gradient of X and of R alike; dR (may be NULL) is the gradient that reached H along the residual path.  dY, H, dR, dX: same type, dX may be
- * any of the others, entry on entry.  dW (32 bits, may be NULL) is summed in 32 bits and a fixed order.
+ * any of the others, entry on entry, and no output may overlap anything else (such calls are refused).  dW (32 bits, may be NULL) is summed in 32 bits and a fixed order.
  * Workspace: GEMM2M_OP_RMS_NORM_BACKWARD with (rows, cols), needed for dW; it suffices for fewer rows and columns too. */
 int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int type, int64_t lddy, const void* H, int64_t ldh, const void* W, int w_type,
                              const float* rstd, const void* dR, int64_t lddr, void* dX, int64_t lddx, float* dW, int add, void* stream);
@@ -331,8 +331,8 @@ int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, c
  * X: tokens x k; A_a (rank x k) and B_a (n x rank) of `adapters` (<= 16384) adapters, stride_a / stride_b elements apart; X, A, B of the same type F16 /
  * BF16.  rank <= 128; ranks (device, `adapters` entries, may be NULL): adapter a uses the first ranks[a] rows of A_a and columns of B_a, whatever lies beyond
  * them.  index: device, one entry per token, in any order; a token whose entry is not in [0, adapters) has no adapter: D_t = C_t.  scales: device, one
- * per adapter, NULL for ones.  C and D: tokens x n of type d_type (F32 / F16 / BF16); C may be NULL (zero) or D itself (then ldc = ldd), not otherwise overlap D;
- * with C = D rows without an adapter are not touched.  Any alignment and stride.  k = 0 or rank = 0 adds nothing.
+ * per adapter, NULL for ones.  C and D: tokens x n of type d_type (F32 / F16 / BF16); C may be NULL (zero) or D itself (then ldc = ldd); D may overlap X,
+ * but not otherwise C, nor B, index, scales or ranks (such calls are refused); with C = D rows without an adapter are not touched.  Any alignment and stride.  k = 0 or rank = 0 adds nothing.
  * X A^T is summed and held in 32 bits (and for a 16-bit D multiplied by B as two 16-bit numbers, which are off by 2^-17 of it for bf16, 2^-22 for fp16), D is
  * rounded once.  A token's result does not depend on the other tokens, beyond their number.
  * Workspace: GEMM2M_OP_ADAPTER_ADD with (tokens, rank, adapters); it suffices for fewer of each too. */

@@ -226,7 +226,16 @@ bool adapter_sizes_ok(int64_t tokens, int64_t rank, int64_t adapters) {
 }
 
 // Memory that a tensor spans, to find outputs that overlap something else.
-struct Span { uintptr_t begin, end; int64_t row, width; bool written; };      // bytes; row = distance of rows, width = of entries in a row
+struct Span {
+    uintptr_t begin, end; int64_t row, width; bool written;      // bytes; row = distance of rows, width = of entries in a row
+    int kind = 0;                                                // not 0: may lie where another of this kind does, entry on entry
+};
+Span span_of(const void* p, int64_t rows, int64_t ld, int64_t cols, int64_t size, bool written, int kind = 0) {
+    if (!p || rows == 0 || cols == 0) return {0, 0, 0, 0, false};
+    if (rows == 1) ld = cols;
+    const uintptr_t begin = (uintptr_t)p;
+    return {begin, begin + (uintptr_t)(((rows - 1) * ld + cols) * size), ld * size, cols * size, written, kind};
+}
 bool spans_meet(const Span& a, const Span& b) {          // a.begin <= b.begin < a.end
     // a without gaps; or rows of different distances, which are not looked at one by one (b may be a single row, or without gaps)
     if (a.row == a.width || (b.row != a.row && b.row != b.width)) return true;
@@ -239,12 +248,8 @@ bool gradients_apart(const std::vector<GradTensor>& t) {
     for (const GradTensor& x : t) {
         if (x.rows * x.cols == 0) continue;
         const int64_t es = x.type == GEMM2M_F32 ? 4 : 2;
-        auto span = [&](const void* p, int64_t ld, bool written) {
-            const uintptr_t begin = (uintptr_t)p;
-            spans.push_back({begin, begin + (uintptr_t)(((x.rows - 1) * ld + x.cols) * es), ld * es, x.cols * es, written});
-        };
-        span(x.o, x.ldo, true);
-        if (x.o != x.g) span(x.g, x.ldg, false);
+        spans.push_back(span_of(x.o, x.rows, x.ldo, x.cols, es, true));
+        if (x.o != x.g) spans.push_back(span_of(x.g, x.rows, x.ldg, x.cols, es, false));
     }
     std::sort(spans.begin(), spans.end(), [](const Span& a, const Span& b) { return a.begin < b.begin; });
     std::vector<const Span*> open;                       // spans that have not ended yet
@@ -258,6 +263,19 @@ bool gradients_apart(const std::vector<GradTensor>& t) {
         open.resize(kept);
         open.push_back(&s);
     }
+    return true;
+}
+
+// The same for the few operands of one call.
+template <size_t N>
+bool operands_apart(const Span (&spans)[N]) {
+    for (size_t i = 0; i < N; ++i)
+        for (size_t j = i + 1; j < N; ++j) {
+            const Span &a = spans[i].begin <= spans[j].begin ? spans[i] : spans[j], &b = &a == &spans[i] ? spans[j] : spans[i];
+            if (!(a.written || b.written) || b.begin >= a.end || b.end == b.begin) continue;
+            if (a.kind && a.kind == b.kind && a.begin == b.begin && a.row == b.row && a.width == b.width) continue;
+            if (spans_meet(a, b)) return false;
+        }
     return true;
 }
 
@@ -1052,6 +1070,11 @@ int gemm2m_rms_norm(int64_t rows, int64_t cols, const void* X, int type, int64_t
     if (!fp8_form_ok(Q, ldq, S, lds, cols, rows) || !fp8_form_ok(Qt, ldqt, St, ldst, rows, cols)) return GEMM2M_ERR_ARG;
     if (rows == 0 || cols == 0) return GEMM2M_OK;
     if (!X || (!H && !Y && !Q && !Qt && !rstd) || ((rows + 127) / 128) * ((cols + 63) / 64) > INT32_MAX) return GEMM2M_ERR_ARG;
+    const int64_t es = (int64_t)float_size(type), row_blocks = (rows + 127) / 128, col_blocks = (cols + 127) / 128;
+    const Span spans[] = {span_of(X, rows, ldx, cols, es, false, 1), span_of(R, rows, ldr, cols, es, false, 1), span_of(W, 1, cols, cols, (int64_t)float_size(w_type), false),
+                          span_of(H, rows, ldh, cols, es, true, 1), span_of(Y, rows, ldy, cols, es, true), span_of(Q, rows, ldq, cols, 1, true), span_of(S, col_blocks, lds, rows, 4, true),
+                          span_of(Qt, cols, ldqt, rows, 1, true), span_of(St, row_blocks, ldst, cols, 4, true), span_of(rstd, 1, rows, rows, 4, true)};
+    if (!operands_apart(spans)) return GEMM2M_ERR_ARG;
     if (int s = check_device()) return s;
     if (Qt && !rstd) {
         if (!D().ws || D().ws_bytes < rms_norm_bytes(rows)) return GEMM2M_ERR_WORKSPACE;
@@ -1079,6 +1102,11 @@ int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int typ
     if (!in_place_ok(dX, lddx, dY, lddy) || !in_place_ok(dX, lddx, H, ldh) || !in_place_ok(dX, lddx, dR, lddr)) return GEMM2M_ERR_ARG;
     if (cols == 0 || (rows == 0 && (!dW || add))) return GEMM2M_OK;
     if (rows && (!dY || !H || !rstd || !dX)) return GEMM2M_ERR_ARG;
+    const int64_t es = (int64_t)float_size(type);
+    const Span spans[] = {span_of(dY, rows, lddy, cols, es, false, 1), span_of(H, rows, ldh, cols, es, false, 1), span_of(W, 1, cols, cols, (int64_t)float_size(w_type), false),
+                          span_of(rstd, 1, rows, rows, 4, false), span_of(dR, rows, lddr, cols, es, false, 1), span_of(dX, rows, lddx, cols, es, true, 1),
+                          span_of(dW, 1, cols, cols, 4, true)};
+    if (!operands_apart(spans)) return GEMM2M_ERR_ARG;
     if (int s = check_device()) return s;
     cudaStream_t st = (cudaStream_t)stream;
     if (rows == 0) {                     // a sum over no rows
@@ -1155,6 +1183,12 @@ int gemm2m_adapter_add(int64_t tokens, int64_t n, int64_t k, int adapters, int r
     if (tokens == 0 || n == 0) return GEMM2M_OK;
     const bool nothing = k == 0 || rank == 0 || adapters == 0;
     if (!D || (!nothing && (!X || !A || !B || !index))) return GEMM2M_ERR_ARG;
+    // what is read while D is written (X and A have been read by then); of B, a matrix of each adapter
+    const int64_t out = (int64_t)float_size(d_type), b_matrix = (n - 1) * ldb + rank, many = nothing ? 0 : adapters, listed = nothing ? 0 : tokens;
+    const Span spans[] = {span_of(C, tokens, ldc, n, out, false, 1), span_of(D, tokens, ldd, n, out, true, 1), span_of(index, 1, listed, listed, 4, false),
+                          span_of(scales, 1, many, many, 4, false), span_of(ranks, 1, many, many, 4, false),
+                          many > 1 && stride_b > b_matrix ? span_of(B, many, stride_b, b_matrix, 2, false) : span_of(B, 1, 0, many ? (many - 1) * stride_b + b_matrix : 0, 2, false)};
+    if (!operands_apart(spans)) return GEMM2M_ERR_ARG;
     if (int s = check_device()) return s;
     cudaStream_t st = (cudaStream_t)stream;
     const size_t es = float_size(d_type);
