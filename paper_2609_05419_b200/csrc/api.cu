@@ -242,9 +242,10 @@ bool spans_meet(const Span& a, const Span& b) {          // a.begin <= b.begin <
     const int64_t at = (int64_t)(b.begin - a.begin) % a.row, width = b.row == a.row ? b.width : (int64_t)(b.end - b.begin);
     return at < a.width || at + width > a.row;           // views of one matrix side by side: where b's rows begin between a's
 }
-bool gradients_apart(const std::vector<GradTensor>& t) {
+bool gradients_apart(const std::vector<GradTensor>& t, const float* norm) {
     std::vector<Span> spans;
-    spans.reserve(2 * t.size());
+    spans.reserve(2 * t.size() + 1);
+    if (norm) spans.push_back(span_of(norm, 1, 1, 1, 4, true));
     for (const GradTensor& x : t) {
         if (x.rows * x.cols == 0) continue;
         const int64_t es = x.type == GEMM2M_F32 ? 4 : 2;
@@ -1151,7 +1152,7 @@ int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, c
             in_place = in_place && x.o == x.g;
         }
         const bool scale = !(in_place && std::isinf(max_norm));      // nothing is ever scaled: the norm alone
-        if (scale && !gradients_apart(t)) return GEMM2M_ERR_ARG;
+        if (scale && !gradients_apart(t, norm)) return GEMM2M_ERR_ARG;
         if (int s = check_device()) return s;
         if (!D().ws || D().ws_bytes < clip_bytes(count)) return GEMM2M_ERR_WORKSPACE;
         cudaStream_t st = (cudaStream_t)stream;

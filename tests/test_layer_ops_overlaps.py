@@ -95,3 +95,13 @@ def test_adapters_take_operands_side_by_side():
                                  dict(B=at(8)), dict(C=at(10)), dict(k=0, D=at(1)), dict(B=at(END - 30), adapters=1)])
 def test_adapters_refuse_outputs_that_overlap(bad):
     assert refused(adapters(**bad))
+
+
+def test_clip_refuses_a_norm_inside_a_gradient_or_an_output():
+    # one gradient of 5 rows of 8 columns 20 apart at 4096, its output contiguous at 8192
+    one = [_tensor(G=4096, O=8192, rows=5, cols=8, ldg=20, ldo=8)]
+    for inside in (4096, 4096 + 4 * 27, 4096 + 4 * 87, 8192, 8192 + 4 * 39):
+        assert refused(_clip(one, norm=inside)), inside
+    for beside in (4096 - 4, 4096 + 4 * 8, 4096 + 4 * 39, 4096 + 4 * 88, 8192 - 4, 8192 + 4 * 40):
+        assert not refused(_clip(one, norm=beside)), beside
+    assert refused(_clip(one, norm=4096, in_place=True)) and not refused(_clip(one, norm=4096 + 32, in_place=True))
