@@ -249,7 +249,6 @@ inline int row_warps(int64_t cols, int places) { return (int)((cols + kSegment *
 // Threads of a block: rows side by side up to 256 threads.
 inline int block_threads(int warps) { return warps >= 8 ? warps * 32 : 8 / warps * warps * 32; }
 
-
 cudaError_t launch_rms_norm_turned(const RmsNormArgs& a, bool vec, int w_vec, cudaStream_t st);      // Qt, St from H (or X + R) and rstd
 
 }  // namespace gemm2m

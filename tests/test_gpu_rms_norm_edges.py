@@ -6,7 +6,7 @@ from paper_2609_05419_b200 import binding as b
 
 pytestmark = pytest.mark.gpu
 
-from test_gpu_rms_norm import gen, plain, stream  # noqa: E402
+from test_gpu_rms_norm import LEAST, NORM, RSTD, STEP, check_backward, check_form, gen, outputs, plain, randn, stream  # noqa: E402
 
 
 @pytest.mark.parametrize("rows,cols", [(4000, 4096), (4000, 1999), (200, 4000), (3000, 8000)])
@@ -81,3 +81,28 @@ def test_a_sum_that_overflows_although_no_part_of_it_does(cols):
     for row in range(3):
         b.rms_norm(x[row:row + 1], rstd=alone, eps=0.0)
         assert torch.equal(alone[0], rstd[row])
+
+
+# Widths at which the kernels change: two blocks on an SM up to 5120 columns, one (of 512 threads) up to 8192, clusters beyond
+@pytest.mark.parametrize("rows,cols", [(3, 5121), (400, 5376), (333, 6001), (300, 6144), (149, 7160), (301, 8191), (400, 8192), (150, 8193), (700, 4609), (297, 5120)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32, torch.float16])
+def test_gradients_at_the_widths_where_kernels_change(rows, cols, dtype):
+    check_backward(rows, cols, dtype, True, True, add=True, seed=201)
+    check_backward(rows, cols, dtype, False, False, seed=211)
+
+
+@pytest.mark.parametrize("rows,cols", [(297, 2049), (300, 3080), (513, 4096), (298, 5376), (301, 6001), (400, 7168), (297, 8192), (299, 8200), (600, 1025), (2000, 257)])
+@pytest.mark.parametrize("dtype,fmt", [(torch.bfloat16, b.E4M3), (torch.float32, b.E5M2)])
+def test_norm_of_many_rows_of_any_width(rows, cols, dtype, fmt):
+    x, r, w = stream(rows, cols, dtype, 221), stream(rows, cols, dtype, 225), 1 + 0.3 * randn(229, cols)
+    out = outputs(rows, cols, dtype, fmt)
+    b.rms_norm(x, w, R=r, eps=1e-5, **out)
+    h, rstd, n = plain(x, r, w, 1e-5)
+    assert torch.equal(out["H"], h)
+    assert bool(((out["rstd"].double() - rstd).abs() <= RSTD * rstd).all())
+    assert bool(((out["Y"].double() - n).abs() <= (STEP[dtype] * (1 + NORM) + NORM) * n.abs() + LEAST[dtype]).all())
+    check_form(out["Q"], out["S"], n, fmt)
+    check_form(out["Qt"], out["St"], n.t(), fmt)
+    few = torch.empty(8, device="cuda")
+    b.rms_norm(x[:8], w, R=r[:8], rstd=few, eps=1e-5)                          # few rows: other warps to a row, the same numbers
+    assert torch.equal(few, out["rstd"][:8])
