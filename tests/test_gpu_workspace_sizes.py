@@ -14,7 +14,7 @@ class Guarded:
 
     def __init__(self, size):
         self.size, self.store = size, torch.full((size + (1 << 16),), 0xa5, dtype=torch.uint8, device="cuda")
-        self.store[:4096] = 0
+        self.store[:min(size, 4096)] = 0
 
     def __enter__(self):
         b.set_workspace(self.store[:self.size])
