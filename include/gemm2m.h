@@ -321,7 +321,8 @@ int gemm2m_rms_norm_backward(int64_t rows, int64_t cols, const void* dY, int typ
  * Host arrays of `count` entries each: device pointers G_i and O_i, types, rows, columns and leading dimensions (row-major; rows = 1 for any contiguous tensor;
  * empty tensors may have null pointers).  O = NULL, or O_i = G_i with the same leading dimension: in place; otherwise no output may overlap another output or
  * an input (views of one matrix side by side do not).  In place nothing is written where the factor is 1.  norm: device pointer to one float (Inf
- * where the norm is above the 32-bit range; the factor is formed from 64 bits) that lies in no gradient and no output, may be NULL.  max_norm may be infinite: with every tensor in place, the norm alone is formed.  The order of the sums goes by the tensors' sizes alone.
+ * where the norm is above the 32-bit range; the factor is formed from 64 bits) that lies in no gradient and no output, may be NULL.  max_norm may be infinite: with every tensor in place, the norm alone is formed.  The order of the sums goes by the
+ * tensors' sizes, types and alignment (to 16 bytes) alone.
  * Workspace: GEMM2M_OP_CLIP_GRADIENTS with m = count. */
 int gemm2m_clip_gradients(int64_t count, const void* const* G, void* const* O, const int* types, const int64_t* rows, const int64_t* cols, const int64_t* ldg,
                           const int64_t* ldo, float max_norm, float eps, float* norm, void* stream);

@@ -7,7 +7,7 @@
 // Up to 256 tokens (here) the tiles are of 16 tokens and every block finds its own from the indexes.  Both products are bound by the adapters' bytes and by the way of a block
 // to its first ones, so they run as warp-level m16n8k16 MMAs whose operands go from global memory straight to registers: the order of the inner dimension is free, so a lane
 // takes eight neighbouring entries of a row in one load and hands them to two MMAs, and the same lane's entries of the other operand meet them there.  The order of the columns
-// of D is free too: four MMAs take columns such that a lane ends with eight neighbouring ones.  (48 tokens, 24 adapters of rank 16, 4096 to 16384 columns: 13.8 us in a graph,
+// of D is free too: four MMAs take columns such that a lane ends with eight neighbouring ones.  (48 tokens, 24 adapters of rank 16, 4096 to 16384 columns: 13.9 us in a graph,
 // 13 MB; rank 128: 44 us, 2.9 TB/s.)  Above, one block sorts the tokens first (6 us for 8192), for tiles of 128 (adapters_many.cu).
 //
 // L is held in 32 bits, and goes into the second product as the sum of 16-bit numbers, after a power of two per token that keeps its largest entry well inside the range, so that
@@ -530,7 +530,7 @@ cudaError_t launch_few(const AdapterArgs& a, const AdapterLayout& l, cudaStream_
     const size_t es = a.d_type == kF32 ? 4 : 2;
     const int vec_b = even(a.B, a.ldb, a.stride_b, RT == 1 ? 8 : 16) && a.rank % (RT == 1 ? 4 : 8) == 0;
     const int vec_d = ((uintptr_t)a.D | (uintptr_t)(a.ldd * es)) % 16 == 0 && (!a.C || ((uintptr_t)a.C | (uintptr_t)(a.ldc * es)) % 16 == 0);
-    // runs of columns: as many as the SMs take at once, since a block's way to its first columns is long (48 tokens to 16384 columns: 13.8 us; with half as many blocks 17, and
+    // runs of columns: as many as the SMs take at once, since a block's way to its first columns is long (48 tokens to 16384 columns: 13.9 us; with half as many blocks 17, and
     // loads two steps ahead in these gain nothing), and at least two steps of 32 columns for every warp
     const int64_t groups = (a.n + 32 * kFewWarps - 1) / (32 * kFewWarps), runs = (up_blocks(RT) * kSms + l.max_tiles - 1) / l.max_tiles;
     int64_t per = (groups + runs - 1) / runs;

@@ -101,8 +101,9 @@ __device__ __forceinline__ void for_chunk(const Entry& e, uint32_t c, M&& meanwh
     }
 }
 
-// Chunks dealt out to four blocks on every SM, a partial sum each.  Bound by memory (705 million f32 entries: 7.3 TB/s, some of them still in the on-chip cache; 54 million in bf16,
-// 108 MB: 26 us from a cold start).
+// Chunks dealt out to four blocks on every SM, a partial sum each.  Bound by memory (705 million f32 entries: 389 us, 7.25 TB/s, some of them still in the on-chip cache; 54 million in bf16,
+// 108 MB: 26 us from a cold start.  Rows apart cost a division per group of eight entries, or per entry where they are not aligned: 1.6 GB of f32 as 24 views 236 us, 225 as 8 whole matrices; of 3999
+// columns on odd boundaries 919).
 template <int N>
 __global__ void __launch_bounds__(kClipThreads, 4) squares_kernel(const __grid_constant__ Table<N> t, double* partials) {
     __shared__ double warps[kClipThreads / 32];
@@ -152,8 +153,8 @@ __device__ __noinline__ void scale_far(const Entry& e, uint32_t c, double factor
     else as(__nv_bfloat16());
 }
 
-// A block per chunk, which it scales.  (705 million f32 entries: 6.9 TB/s; 6.4 with chunks of 32 KB, 5.6 with these dealt out to four
-// blocks on every SM.)
+// A block per chunk, which it scales.  (705 million f32 entries: 826 us, 6.8 TB/s; when that was 6.9, 6.4 with chunks of 32 KB and 5.6 with these
+// dealt out to four blocks on every SM.  As views of columns on odd boundaries, entry by entry, 2.1 TB/s.)
 template <int N>
 __global__ void __launch_bounds__(kClipThreads, 6) scale_kernel(const __grid_constant__ Table<N> t, const double* partials, int64_t count, float max_norm, float eps, float* norm) {
     __shared__ double warps[kClipThreads / 32];

@@ -9,8 +9,8 @@ namespace gemm2m {
 
 namespace {
 
-// One row for every `warps` warps of a block, held in registers: read once, all outputs from there.  Bound by memory (8192 x 4096 bf16 with residual, H and 8-bit rows: 44 us,
-// 5.3 TB/s; blocks of one wave each, whose loads, sums and stores overlap with the other blocks' of the SM).
+// One row for every `warps` warps of a block, held in registers: read once, all outputs from there.  Bound by memory (8192 x 4096 bf16 with residual, H and 8-bit rows: 45 us,
+// 5.2 TB/s; blocks of one wave each, whose loads, sums and stores overlap with the other blocks' of the SM).
 template <typename T, int NV, bool VEC, int THREADS>
 __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 512) / THREADS) rms_norm_rows_kernel(const RmsNormArgs a, int warps, Two inv_cols, int w_vec) {
     __shared__ float sums[THREADS / 32 * NV];

@@ -185,7 +185,7 @@ __device__ __forceinline__ Two two_sum(float a, float b) {
 }
 // The segments' sums added up as such pairs over the lanes of a warp, in every lane: of the roundings on the way to a sum of squares those of the last few additions would be left
 // over, the ones before average out (8192 x 4096 bf16: error of rstd 3.0e-8, its own rounding 2.6e-8; 4.5e-8 with these additions in 32 bits.  In 32 bits 8192 x 512 takes 8.0 us, so
-// 8.6, rows of 1024 columns and more as much; added up in 64 bits 8192 x 4096 takes 51 us, so 44).
+// 8.6, rows of 1024 columns and more as much; added up in 64 bits 8192 x 4096 takes 6.7 us more).
 __device__ __forceinline__ Two over_segments(const float* segments, int count) {
     const int over = count <= 4 ? 1 : 2 << (31 - __clz((count - 1) >> 2));      // lanes that share the work, a power of two; up to four numbers each
     const int first = threadIdx.x & (over - 1);

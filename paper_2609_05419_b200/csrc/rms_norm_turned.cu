@@ -7,7 +7,7 @@ namespace {
 
 // Qt, St from H (or X + R) and rstd: one block of 128 threads per tile of 128 rows x 64 columns, thread = 8 x 8 entries, otherwise as in the quantiser.  (Half a
 // tile of the quantiser's: with four blocks on an SM their loads, arithmetic and stores overlap better than with two.)  It waits for its loads
-// (8192 x 4096 bf16: 24 us; 67 of the 134 MB of H are still in the on-chip cache, since the tiles go from the last rows to the first).
+// (8192 x 4096 bf16: 25 us; 67 of the 134 MB of H are still in the on-chip cache, since the tiles go from the last rows to the first).
 template <typename T, int FMT, bool VEC>
 __global__ void __launch_bounds__(128, 4) rms_norm_turned_kernel(const RmsNormArgs a, int col_tiles, int w_vec) {
     __shared__ uint32_t warp_top[4][64];
