@@ -112,3 +112,27 @@ def test_rows_without_an_adapter_are_those_of_c_bit_for_bit(tokens, n, skip, d_t
         b.adapter_add(x, a, w, index, d, ranks=used)
         assert bool((d[bare].view(whole) == 0).all())
     assert bool((store[:, :skip] == 3).all()) and bool((store[:, skip + n:] == 3).all())
+
+
+@pytest.mark.parametrize("tokens,k,rank", [(300, 32768, 16), (300, 32768, 60), (300, 32768, 128), (4096, 8192, 16), (2000, 16384, 32), (257, 32001, 9)])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_sums_over_long_rows_of_positive_products(tokens, k, rank, dtype):
+    """Sums in which every cut goes the same way.  B is the unit matrix, so D is X A^T.  Up to eight blocks share k, and of a block's steps of 64 entries an accumulator has eight or, where there is not
+    room for so many of the padded rank in 256 columns, an even share; a step is four additions, each cut by up to 2^-23 of the partial sum (fp16, whose products are longer than
+    bf16's, by up to four times that), which is half of the accumulator's in the mean; then roundings to the nearest."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rank)
+    draw = lambda *shape: torch.randn(shape, generator=g, device="cuda").abs()
+    x, a = draw(tokens, k).to(dtype), (draw(1, rank, k) / 16).to(dtype)
+    w = torch.eye(rank, device="cuda").to(dtype)[None].contiguous()
+    d = torch.empty(tokens, rank, device="cuda")
+    with workspace(tokens, rank, 1):
+        b.adapter_add(x, a, w, torch.zeros(tokens, dtype=torch.int32, device="cuda"), d)
+        b.device_status()
+    want = x.double() @ a[0].double().t()
+    padded = 16 if rank <= 16 else 32 if rank <= 32 else 64 if rank <= 64 else 128
+    tiles = tokens // 128 + 2
+    blocks = max(1, min(8, 296 // tiles))
+    steps = -(-(-(-k // 64)) // blocks)
+    cuts = 4 * max(8, -(-steps // (256 // padded)))
+    assert bool(((d.double() - want).abs() <= (cuts / 2 * (1 if dtype == torch.bfloat16 else 4) + 8) * 2.0 ** -23 * want).all())
