@@ -58,11 +58,13 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 5
     // The barrier tells all threads of the block whether squares of any of its rows may leave the range in which 32 bits hold them and their sum (of up to 128 segments).  (8192 x 4096:
     // 44.9 us, 44.0 without this; with sums in 64 bits instead 50, in a function of their own 60.)
     const bool some = __syncthreads_or(!(mine < 0x1p120f) || (a.eps < 0x1p-99f && mine < 0x1p-80f));
-    float rstd = inverse_root(over_segments(segments, at.segments), inv_cols, a.eps);
+    Two total = over_segments(segments, at.segments);
+    float power = 1.f;
     if (some) {
         // Once more, of H 2^-72 where the sum is infinite (some entry is above 2^56), of H 2^75 where mean + eps is below 2^-99 (none is above 2^-41, and squares below 2^-126 have lost bits);
         // other rows get the number that they had.
-        const float about = fmaf(over_segments(segments, at.segments).hi, inv_cols.hi, a.eps), power = !(about < INFINITY) ? 0x1p-72f : about < 0x1p-99f ? 0x1p75f : 1.f;
+        const float about = fmaf(total.hi, inv_cols.hi, a.eps);
+        power = !(about < INFINITY) ? 0x1p-72f : about < 0x1p-99f ? 0x1p75f : 1.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             float s = 0.f;
@@ -73,8 +75,9 @@ __global__ void __launch_bounds__(THREADS, THREADS == 1024 ? 1 : (VEC ? 1024 : 5
         __syncthreads();
         segment_sums<NV>(sum, segments, at.warp_in_row, warps, at.segments);
         __syncthreads();
-        rstd = inverse_root(over_segments(segments, at.segments), inv_cols, a.eps * power * power) * power;
+        total = over_segments(segments, at.segments);
     }
+    const float rstd = inverse_root(total, inv_cols, a.eps * power * power) * power;
     if (a.rstd && write && at.warp_in_row == 0 && lane == 0) a.rstd[row] = rstd;
     if (!a.Y && !a.Q) return;
     float top[NV];
